@@ -70,6 +70,8 @@ extern "C" {
                               * unit's outputs are NaN from then on and its M and mu are unspecified */
 #define SUBGEN_ST_RANGE 2    /* non-finite input, or |x| > 32768 */
 #define SUBGEN_ST_TIMEOUT 4  /* a bounded wait inside a kernel ran out (not expected; the state is unusable) */
+#define SUBGEN_ST_PAGE 8     /* paged calls: a page outside the pool, a length beyond its page table, or offsets that
+                              * decrease or pass the number of rows */
 
 typedef struct subgen subgen_t;
 typedef struct subgen_exact subgen_exact_t;
@@ -333,6 +335,96 @@ int subgen_exact_export_tokens(subgen_exact_t* h, int seq, int kvhead, int* n_ou
 #define SUBGEN_NOALLOC_SCRATCH_BYTES (4u << 20)
 int subgen_exact_attention_noalloc(const void* q, const void* K, const void* V, void* out, int B, int H, int Hkv,
                                    int d, int n, int dtype, void* stream);
+
+/* ---- norms and position rotation of queries and keys ------------------------------------------ */
+
+/* The streams above take queries and keys as the attention formula uses them. Most models norm every head and rotate
+ * it by its position first; these two steps run in one pass over the fused projection's output, into the layout that
+ * subgen_step, subgen_prefill or an exact cache takes.
+ *   y = rot(position, w * x / sqrt(mean(x^2) + eps))
+ * per head, the norm only where w is given; rot turns the pair (a, b) of coordinates (i, i + r/2), or (2i, 2i + 1) if
+ * interleaved, i < r/2, by the angle position * f_i: (a cos - b sin, b cos + a sin). Coordinates from r on pass.
+ * Arithmetic in fp32, one rounding at the end; angles are exact to 2^-33 of a turn for any 31-bit position. */
+typedef struct subgen_rope {
+    const uint64_t* words;  /* device, [rotary_dim / 2], from subgen_rope_words; NULL: no rotation */
+    int rotary_dim;         /* r: a multiple of 16, at most d */
+    int interleaved;        /* 0: pairs (i, i + r/2), 1: pairs (2i, 2i + 1) */
+} subgen_rope;
+
+/* words[i] = the turns per position, f[i] / (2 pi), modulo 1, in units of 2^-64. Host arrays. f: radians per
+ * position, e.g. base^(-2i/r); finite. */
+int subgen_rope_words(const double* f, int count, uint64_t* words);
+
+/* Heads of a token are rows of d elements with unit stride; rows and the pointer are aligned to 16 bytes. */
+typedef struct subgen_heads {
+    void* p;               /* device */
+    int64_t token_stride;  /* elements from one token to the next */
+    int64_t head_stride;   /* elements from one head to the next */
+} subgen_heads;
+
+/* q, q_out: n tokens of H heads; k, k_out: of Hkv heads. An output may be its input (same strides), otherwise they must
+ * not overlap. positions: device [n], any 32-bit value (needed if there is a rotation). wq, wk: device [d] of the
+ * dtype, or NULL for no norm. q or k may be NULL (or have p = NULL): then only the other is done. */
+int subgen_qk_norm_rope(const subgen_heads* q, const subgen_heads* k, const subgen_heads* q_out, const subgen_heads* k_out,
+                        int n, int H, int Hkv, int d, int dtype, const int* positions, const subgen_rope* rope,
+                        const void* wq, const void* wk, float eps, void* stream);
+
+/* ---- paged exact cache ------------------------------------------------------------------------- */
+
+/* A pool of pages that any number of sequences share, owned by the caller, and what a call has to know about them. All
+ * pointers are device pointers; the functions below keep nothing between calls, so lengths and tables may change on
+ * the device (also inside a captured graph). Indices are checked on the device: a page outside [0, pages) or a length
+ * beyond its table is neither read nor written, sets SUBGEN_ST_PAGE in *status and makes the outputs that needed it
+ * NaN. */
+typedef struct subgen_pages {
+    void *K, *V;            /* element (page, head, row, x) of each at page * page_stride + head * head_stride + row * row_stride + x */
+    int64_t page_stride, head_stride, row_stride;   /* elements; multiples of 16 bytes */
+    int pages;              /* in the pool */
+    int page;               /* tokens per page: 16, 32, 64, ... 1024 (a power of two) */
+    int Hkv, d, dtype;      /* d: 64 or 128 */
+    int* status;            /* sticky SUBGEN_ST_* bits, or NULL */
+} subgen_pages;
+
+/* B sequences. Rows cu_q[b] .. cu_q[b+1] - 1 of a call's q, k, v and out are the new tokens of sequence b, the last of
+ * its lengths[b] own tokens; own token j lies in page table[b][j / page], row j % page. Rows from cu_q[B] on belong to
+ * nobody: they are neither read nor written. Sequences cu_group[g] .. cu_group[g+1] - 1 share prefix g: prefix_len[g]
+ * tokens (any number) in the pages prefix_table[g], which come before their own tokens. groups = 0: no prefixes.
+ * B + groups <= 2048. */
+typedef struct subgen_batch {
+    int B;
+    const int* cu_q;        /* [B + 1], non-decreasing from >= 0 to <= the rows of the call */
+    const int* lengths;     /* [B] own tokens, the new ones among them */
+    const int* table;       /* [B, table_stride] */
+    int table_stride;       /* pages a row of the table holds */
+    int groups;
+    const int* cu_group;    /* [groups + 1], from 0 to B */
+    const int* prefix_len;  /* [groups] */
+    const int* prefix_table;/* [groups, prefix_stride] */
+    int prefix_stride;
+} subgen_batch;
+
+/* Writes the n new tokens' keys, normed (if wk) and rotated (if rope), and their values into the pages of their
+ * sequences, and the queries, normed (if wq) and rotated, to q_out, which may be q (q, q_out may be NULL: keys and values
+ * only). positions: device [n], or NULL: a token's position is its place in its sequence, prefix included. Two rows must
+ * not have the same slot. Tokens whose own index is negative (more new tokens than the length says) are not written and
+ * set SUBGEN_ST_PAGE. Asynchronous on `stream`, one kernel. */
+int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* k, const subgen_heads* v,
+                        const subgen_heads* q, const subgen_heads* q_out, int n, int H, const int* positions,
+                        const subgen_rope* rope, const void* wq, const void* wk, float eps, void* stream);
+
+/* out = softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for each of the n new tokens' H query heads (head h reads KV
+ * head h / (H / Hkv); H / Hkv in {1, 2, 4, 8}), the new tokens' keys and values being in the cache already. A token sees
+ * its group's whole prefix and, of its own sequence, the tokens up to itself (causal = 1) or all of them (causal = 0).
+ * A row that sees nothing (an empty sequence, or one of more new tokens than its length says) is 0. The prefix is read
+ * once per group, whatever the number of its sequences. scale > 0. Stored keys and values that some row sees must be
+ * finite; what lies behind a sequence's length in its last page may be anything.
+ * Scores, maxima, sums and numerators are fp32; on bf16 caches the softmax weights are rounded to bf16 for the product
+ * with V. The result does not depend on how blocks are scheduled.
+ * workspace: device, subgen_paged_workspace_bytes(), 256-byte aligned, used by this call only until it has run (two calls
+ * that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */
+size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H);
+int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* q, const subgen_heads* out,
+                        int n, int H, float scale, int causal, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

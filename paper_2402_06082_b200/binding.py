@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsubgen.so")
 
 DTYPE_FP32, DTYPE_BF16 = 0, 1
-ST_CAPACITY, ST_RANGE = 1, 2
+ST_CAPACITY, ST_RANGE, ST_TIMEOUT, ST_PAGE = 1, 2, 4, 8
 STEP_MODES = {"auto": 0, "fused": 1, "split": 2}
 
 EXPORTS = [
@@ -28,6 +28,7 @@ EXPORTS = [
     "subgen_exact_append", "subgen_exact_append_varlen", "subgen_exact_step", "subgen_exact_bytes",
     "subgen_exact_launch_count", "subgen_exact_attention_noalloc",
     "subgen_exact_kcenter_compress", "subgen_exact_kcenter_counters", "subgen_exact_export_tokens",
+    "subgen_rope_words", "subgen_qk_norm_rope", "subgen_paged_append", "subgen_paged_workspace_bytes", "subgen_paged_attend",
 ]
 
 
@@ -50,6 +51,26 @@ class Stats(C.Structure):
     _fields_ = [(k, C.c_uint64) for k in ("units", "clusters", "singleton_clusters", "m_filled", "window_rows",
                                            "tokens", "prefill_pairs", "insert_bytes", "query_bytes", "cluster_bytes", "value_bytes",
                                            "distinct_sample_rows")]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("words", C.c_void_p), ("rotary_dim", C.c_int), ("interleaved", C.c_int)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("row_stride", C.c_int64), ("pages", C.c_int), ("page", C.c_int), ("Hkv", C.c_int), ("d", C.c_int),
+                ("dtype", C.c_int), ("status", C.c_void_p)]
+
+
+class BatchDesc(C.Structure):
+    _fields_ = [("B", C.c_int), ("cu_q", C.c_void_p), ("lengths", C.c_void_p), ("table", C.c_void_p),
+                ("table_stride", C.c_int), ("groups", C.c_int), ("cu_group", C.c_void_p), ("prefix_len", C.c_void_p),
+                ("prefix_table", C.c_void_p), ("prefix_stride", C.c_int)]
 
 
 _lib = None
@@ -107,6 +128,13 @@ def load():
     L.subgen_exact_kcenter_counters.argtypes = [vp, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
     L.subgen_exact_export_tokens.argtypes = [vp, C.c_int, C.c_int, ip, ip]
     L.subgen_exact_attention_noalloc.argtypes = [vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp]
+    hp, rp, pp, bp = C.POINTER(Heads), C.POINTER(RopeDesc), C.POINTER(PagesDesc), C.POINTER(BatchDesc)
+    L.subgen_rope_words.argtypes = [C.POINTER(C.c_double), C.c_int, C.POINTER(C.c_uint64)]
+    L.subgen_qk_norm_rope.argtypes = [hp, hp, hp, hp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp, rp, vp, vp, C.c_float, vp]
+    L.subgen_paged_append.argtypes = [pp, bp, hp, hp, hp, hp, C.c_int, C.c_int, vp, rp, vp, vp, C.c_float, vp]
+    L.subgen_paged_workspace_bytes.argtypes = [pp, bp, C.c_int, C.c_int]
+    L.subgen_paged_workspace_bytes.restype = C.c_size_t
+    L.subgen_paged_attend.argtypes = [pp, bp, hp, hp, C.c_int, C.c_int, C.c_float, C.c_int, vp, C.c_size_t, vp]
     _lib = L
     return L
 
@@ -390,3 +418,188 @@ def exact_attention_noalloc(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, o
         _dev(q, dt, (B, H, d), "q"), _dev(K, dt, (B, Hkv, n, d), "K"), _dev(V, dt, (B, Hkv, n, d), "V"),
         _dev(out, dt, (B, H, d), "out"), B, H, Hkv, d, n, _dtype_code(dt), st.cuda_stream))
     return out
+
+
+# ---- norms, rotation and the paged exact cache --------------------------------------------------
+#
+# These calls run on the current stream of their tensors' device and keep nothing between calls: outputs and scratch
+# come from torch's allocator, call by call, so captured graphs and calls on several streams do not share any.
+
+def _raw_stream(index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _heads(x: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, n: int, heads: int, d: int) -> Heads:
+    if x.dtype is not dtype or x.device != device or x.shape != (n, heads, d) or (x.stride(2) != 1 and d > 1):
+        raise ValueError("%s must be a %s tensor of shape %s on %s with unit stride along the last axis (got %s %s on %s)" %
+                         (name, dtype, (n, heads, d), device, x.dtype, tuple(x.shape), x.device))
+    return Heads(x.data_ptr(), x.stride(0), x.stride(1))
+
+
+def _ints(x: Optional[torch.Tensor], name: str, device: torch.device, shape) -> Optional[int]:
+    if x is None:
+        return None
+    if x.dtype is not torch.int32 or x.device != device or x.shape != shape or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s on %s (got %s %s on %s)" %
+                         (name, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
+    return x.data_ptr()
+
+
+def _weight(x: Optional[torch.Tensor], name: str, dtype: torch.dtype, device: torch.device, d: int) -> Optional[int]:
+    if x is None:
+        return None
+    if x.dtype is not dtype or x.device != device or x.shape != (d,) or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape (%d,) on %s" % (name, dtype, d, device))
+    return x.data_ptr()
+
+
+def _cuda(x: torch.Tensor, name: str) -> torch.device:
+    if not x.is_cuda:
+        raise ValueError("%s must be a CUDA tensor: this library has no CPU path" % name)
+    return x.device
+
+
+class Rope:
+    """Position rotation of the first `rotary_dim` of d coordinates: pairs (i, i + r/2), or (2i, 2i + 1) if interleaved.
+
+    Pair i turns by base^(-2i/r) radians per position, or by inv_freq[i] where r/2 values are given (scaled variants).
+    """
+
+    def __init__(self, d: int, base: float = 10000.0, rotary_dim: Optional[int] = None, interleaved: bool = False,
+                 inv_freq: Optional[Sequence[float]] = None, device="cuda"):
+        r = int(d if rotary_dim is None else rotary_dim)
+        if r <= 0 or r > d or r % 16:
+            raise ValueError("rotary_dim must be a multiple of 16 and at most d")
+        f = [float(base) ** (-2.0 * i / r) for i in range(r // 2)] if inv_freq is None else [float(x) for x in inv_freq]
+        if len(f) != r // 2:
+            raise ValueError("inv_freq must hold rotary_dim / 2 values")
+        words = np.zeros(r // 2, np.uint64)
+        _check(load().subgen_rope_words((C.c_double * (r // 2))(*f), r // 2, words.ctypes.data_as(C.POINTER(C.c_uint64))))
+        self.d, self.rotary_dim, self.interleaved = int(d), r, bool(interleaved)
+        self.words = torch.from_numpy(words.view(np.int64)).to(device)
+        self.device = self.words.device
+        self._desc = RopeDesc(self.words.data_ptr(), r, int(self.interleaved))
+
+    def _for(self, d: int, device: torch.device):
+        if self.device != device or self.d != d:
+            raise ValueError("rope was made for d = %d on %s" % (self.d, self.device))
+        return C.byref(self._desc)
+
+
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                 rope: Optional[Rope] = None, *, wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
+                 eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """RMS norm of every head (where a weight is given), then the rotation by `positions` (int32 [n]); see subgen_qk_norm_rope.
+
+    q [n, H, d], k [n, Hkv, d]: views with unit stride along d (slices of a fused projection). Returns (q_out, k_out), None for
+    what was not given; an output may be its input.
+    """
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("q and k must not both be None")
+    dev, dt, (n, _, d) = _cuda(x, "q" if q is not None else "k"), x.dtype, x.shape
+    code = _dtype_code(dt)
+    qd = kd = qo = ko = None
+    H = Hkv = 1
+    if q is not None:
+        H = q.shape[1]
+        q_out = torch.empty((n, H, d), dtype=dt, device=dev) if q_out is None else q_out
+        qd, qo = _heads(q, "q", dt, dev, n, H, d), _heads(q_out, "q_out", dt, dev, n, H, d)
+    if k is not None:
+        Hkv = k.shape[1]
+        k_out = torch.empty((n, Hkv, d), dtype=dt, device=dev) if k_out is None else k_out
+        kd, ko = _heads(k, "k", dt, dev, n, Hkv, d), _heads(k_out, "k_out", dt, dev, n, Hkv, d)
+    with torch.cuda.device(dev):
+        _check(load().subgen_qk_norm_rope(qd, kd, qo, ko, n, H, Hkv, d, code, _ints(positions, "positions", dev, (n,)),
+                                          rope._for(d, dev) if rope is not None else None, _weight(wq, "wq", dt, dev, d),
+                                          _weight(wk, "wk", dt, dev, d), eps, _raw_stream(dev.index)))
+    return q_out if q is not None else None, k_out if k is not None else None
+
+
+class PagedBatch:
+    """The sequences of a call on a PagedCache (see subgen_batch): int32 CUDA tensors, kept and read by every call.
+
+    cu_q [B + 1]: rows cu_q[b] .. cu_q[b + 1] of q, k, v are the new tokens of sequence b, the last of its lengths[b] own
+    tokens; table [B, m]: the pages of each. cu_group [g + 1], prefix_len [g], prefix_table [g, m']: sequences cu_group[i] ..
+    cu_group[i + 1] share the prefix_len[i] tokens in prefix_table[i]. Contents may change between calls (and replays).
+    """
+
+    def __init__(self, cu_q: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, cu_group: Optional[torch.Tensor] = None,
+                 prefix_len: Optional[torch.Tensor] = None, prefix_table: Optional[torch.Tensor] = None):
+        dev = self.device = _cuda(lengths, "lengths")
+        B = self.B = int(lengths.shape[0])
+        given = [x is not None for x in (cu_group, prefix_len, prefix_table)]
+        if any(given) != all(given):
+            raise ValueError("cu_group, prefix_len and prefix_table come together")
+        g = int(prefix_len.shape[0]) if all(given) else 0
+        if table.dim() != 2 or (g and prefix_table.dim() != 2):
+            raise ValueError("page tables are two-dimensional")
+        self.tensors = (cu_q, lengths, table, cu_group, prefix_len, prefix_table)
+        self._desc = BatchDesc(B, _ints(cu_q, "cu_q", dev, (B + 1,)), _ints(lengths, "lengths", dev, (B,)),
+                               _ints(table, "table", dev, (B, table.shape[1])), table.shape[1], g)
+        if g:
+            self._desc.cu_group = _ints(cu_group, "cu_group", dev, (g + 1,))
+            self._desc.prefix_len = _ints(prefix_len, "prefix_len", dev, (g,))
+            self._desc.prefix_table = _ints(prefix_table, "prefix_table", dev, (g, prefix_table.shape[1]))
+            self._desc.prefix_stride = prefix_table.shape[1]
+
+
+class PagedCache:
+    """An exact cache in pages: K, V [pages, Hkv, page, d], owned by the caller (any strides with unit stride along d, the
+    same for both, so that [pages, page, Hkv, d] pools and halves of one tensor serve as well). See subgen_pages."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor):
+        dev = self.device = _cuda(K, "K")
+        if K.dim() != 4 or K.stride(3) != 1 or V.shape != K.shape or V.stride() != K.stride() or V.dtype is not K.dtype or V.device != dev:
+            raise ValueError("K and V must be [pages, Hkv, page, d] tensors of one type, device and layout, unit stride along d")
+        self._L = load()
+        self.K, self.V, self.dtype = K, V, K.dtype
+        self.pages, self.Hkv, self.page, self.d = K.shape
+        self._status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self._desc = PagesDesc(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), self.pages, self.page, self.Hkv,
+                               self.d, _dtype_code(K.dtype), self._status.data_ptr())
+
+    def append(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, *, rope: Optional[Rope] = None,
+               positions: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               q: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
+        """Write the new tokens k, v [n, Hkv, d] into their pages, k normed (if wk) and rotated (if rope) on the way; q [n, H, d]
+        goes the same way into q_out, which is returned (None without q). One kernel; see subgen_paged_append."""
+        dev, dt, n, H = self.device, self.dtype, k.shape[0], 1
+        kd, vd = _heads(k, "k", dt, dev, n, self.Hkv, self.d), _heads(v, "v", dt, dev, n, self.Hkv, self.d)
+        qd = qo = None
+        if q is not None:
+            H = q.shape[1]
+            q_out = torch.empty((n, H, self.d), dtype=dt, device=dev) if q_out is None else q_out
+            qd, qo = _heads(q, "q", dt, dev, n, H, self.d), _heads(q_out, "q_out", dt, dev, n, H, self.d)
+        if batch.device != dev:
+            raise ValueError("the batch is on %s, the cache on %s" % (batch.device, dev))
+        with torch.cuda.device(dev):
+            _check(self._L.subgen_paged_append(self._desc, batch._desc, kd, vd, qd, qo, n, H, _ints(positions, "positions", dev, (n,)),
+                                               rope._for(self.d, dev) if rope is not None else None,
+                                               _weight(wq, "wq", dt, dev, self.d), _weight(wk, "wk", dt, dev, self.d), eps,
+                                               _raw_stream(dev.index)))
+        return q_out if q is not None else None
+
+    def attend(self, batch: PagedBatch, q: torch.Tensor, scale: float = 1.0, causal: bool = True, out: Optional[torch.Tensor] = None):
+        """softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for q [n, H, d], whose keys are in the cache already; the prefix is
+        read once per group. Rows of `out` behind the last sequence are not written. See subgen_paged_attend."""
+        dev, dt, d = self.device, self.dtype, self.d
+        n, H = q.shape[0], q.shape[1]
+        qd = _heads(q, "q", dt, dev, n, H, d)
+        out = torch.empty((n, H, d), dtype=dt, device=dev) if out is None else out
+        od = _heads(out, "out", dt, dev, n, H, d)
+        if batch.device != dev:
+            raise ValueError("the batch is on %s, the cache on %s" % (batch.device, dev))
+        size = self._L.subgen_paged_workspace_bytes(self._desc, batch._desc, n, H)
+        if size == 0:
+            raise SubgenError(self._L.subgen_last_error().decode())
+        with torch.cuda.device(dev):
+            ws = torch.empty(size, dtype=torch.uint8, device=dev)     # torch aligns allocations to 512 bytes
+            _check(self._L.subgen_paged_attend(self._desc, batch._desc, qd, od, n, H, scale, int(causal), ws.data_ptr(), size,
+                                               _raw_stream(dev.index)))
+        return out
+
+    def status(self) -> int:
+        """Waits for the device's work, returns the status bits that calls on this cache have set (0: none)."""
+        torch.cuda.synchronize(self.device)
+        return int(self._status.item())

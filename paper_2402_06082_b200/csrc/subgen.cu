@@ -38,6 +38,13 @@ int fail(int code, const char* fmt, ...) {
     return code;
 }
 
+}  // namespace
+
+// The thread's error text, for the library's other source file.
+__attribute__((visibility("hidden"))) int sgk_set_error(int code, const char* text) { return fail(code, "%s", text); }
+
+namespace {
+
 #define CUDA_TRY(expr)                                                                      \
     do {                                                                                    \
         cudaError_t err__ = (expr);                                                         \

@@ -1,0 +1,276 @@
+// Host side of the head norms with rotation and of the paged exact cache (see include/subgen.h).
+#include "../../include/subgen.h"
+
+#include <cuda.h>
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+#include <string.h>
+
+#include "subgen_paged.cuh"
+#include "subgen_paged_simt.cuh"
+
+using namespace sgk;
+
+int sgk_set_error(int code, const char* text);
+
+namespace {
+
+int fail(int code, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return sgk_set_error(code, buf);
+}
+
+#define CUDA_TRY(expr)                                                                      \
+    do {                                                                                    \
+        cudaError_t err__ = (expr);                                                         \
+        if (err__ != cudaSuccess) return fail(SUBGEN_ECUDA, "%s: %s", #expr, cudaGetErrorString(err__)); \
+    } while (0)
+
+constexpr int kSMs = 148;
+constexpr int kMaxDevices = 64;
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+size_t elem(int dtype) { return dtype == SUBGEN_DTYPE_FP32 ? 4 : 2; }
+bool odd_stride(int64_t s, int dtype) { return (s * (int64_t)elem(dtype)) % 16 != 0; }
+
+int check_heads(const char* fn, const char* name, const subgen_heads* x, int dtype) {
+    if (!x || !x->p) return fail(SUBGEN_EINVAL, "%s: %s must not be NULL", fn, name);
+    if (misaligned(x->p) || odd_stride(x->token_stride, dtype) || odd_stride(x->head_stride, dtype))
+        return fail(SUBGEN_EINVAL, "%s: %s: pointer and strides must be multiples of 16 bytes", fn, name);
+    return SUBGEN_OK;
+}
+
+int check_shape(const char* fn, int n, int H, int Hkv, int d, int dtype) {
+    if (dtype != SUBGEN_DTYPE_FP32 && dtype != SUBGEN_DTYPE_BF16) return fail(SUBGEN_EINVAL, "%s: unknown dtype", fn);
+    if (d != 64 && d != 128) return fail(SUBGEN_EINVAL, "%s: d must be 64 or 128", fn);
+    if (n < 0 || H <= 0 || Hkv <= 0) return fail(SUBGEN_EINVAL, "%s: n must be >= 0, the numbers of heads positive", fn);
+    if ((long long)n * (H + 2LL * Hkv) > 0x1fffffffLL) return fail(SUBGEN_EINVAL, "%s: too many rows in one call", fn);
+    return SUBGEN_OK;
+}
+
+int check_rope(const char* fn, const subgen_rope* r, int d) {
+    if (!r || !r->words) return SUBGEN_OK;
+    if (r->rotary_dim <= 0 || r->rotary_dim > d || r->rotary_dim % 16)
+        return fail(SUBGEN_EINVAL, "%s: rotary_dim must be a multiple of 16 and at most d", fn);
+    return SUBGEN_OK;
+}
+
+int check_norm(const char* fn, const void* wq, const void* wk, float eps) {
+    if (misaligned(wq) || misaligned(wk)) return fail(SUBGEN_EINVAL, "%s: norm weights must be 16-byte aligned", fn);
+    if ((wq || wk) && !(eps >= 0.f && isfinite(eps))) return fail(SUBGEN_EINVAL, "%s: eps must be finite and >= 0", fn);
+    return SUBGEN_OK;
+}
+
+int check_cache(const char* fn, const subgen_pages* c, const subgen_batch* b, PagedView* v) {
+    if (!c || !b) return fail(SUBGEN_EINVAL, "%s: cache and batch must not be NULL", fn);
+    if (!c->K || !c->V) return fail(SUBGEN_EINVAL, "%s: K and V must not be NULL", fn);
+    if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)))
+        return fail(SUBGEN_EINVAL, "%s: page must be a power of two, 16 to 1024", fn);
+    if (c->pages <= 0) return fail(SUBGEN_EINVAL, "%s: pages must be positive", fn);
+    if (c->page_stride <= 0 || c->head_stride <= 0 || c->row_stride < c->d)
+        return fail(SUBGEN_EINVAL, "%s: the strides of the pool must be positive, row_stride at least d", fn);
+    if (misaligned(c->K) || misaligned(c->V) || odd_stride(c->page_stride, c->dtype) || odd_stride(c->head_stride, c->dtype) ||
+        odd_stride(c->row_stride, c->dtype))
+        return fail(SUBGEN_EINVAL, "%s: the pool's pointers and strides must be multiples of 16 bytes", fn);
+    if (b->B < 0 || b->groups < 0 || (long long)b->B + b->groups > kPlanMax)
+        return fail(SUBGEN_EINVAL, "%s: B and groups must be >= 0, together at most %d", fn, kPlanMax);
+    if (b->B && (!b->cu_q || !b->lengths || !b->table || b->table_stride <= 0))
+        return fail(SUBGEN_EINVAL, "%s: cu_q, lengths and table must not be NULL, table_stride must be positive", fn);
+    if (b->groups && (!b->cu_group || !b->prefix_len || !b->prefix_table || b->prefix_stride <= 0))
+        return fail(SUBGEN_EINVAL, "%s: cu_group, prefix_len and prefix_table must not be NULL, prefix_stride must be positive", fn);
+    if ((long long)b->table_stride * c->page > 0x7fffffffLL || (b->groups && (long long)b->prefix_stride * c->page > 0x7fffffffLL))
+        return fail(SUBGEN_EINVAL, "%s: a page table must hold fewer than 2^31 tokens", fn);
+    int shift = 0;
+    while ((1 << shift) < c->page) ++shift;
+    *v = PagedView{(char*)c->K, (char*)c->V, c->page_stride, c->head_stride, c->row_stride, c->pages, shift, c->Hkv,
+                   b->B, b->groups, b->cu_q, b->lengths, b->table, b->cu_group, b->prefix_len, b->prefix_table,
+                   b->table_stride, b->prefix_stride, c->status};
+    return SUBGEN_OK;
+}
+
+HeadsView view(const subgen_heads* x) { return x && x->p ? HeadsView{x->p, x->token_stride, x->head_stride} : HeadsView{nullptr, 0, 0}; }
+
+// ---- norms, rotation, append ----
+template <typename T, int D, bool PAGED>
+void launch_norm_rope(NormRope a, const PagedView& P, cudaStream_t st) {
+    constexpr int RPW = 32 / (D / (16 / (int)sizeof(T)) / 2);
+    const int heads = a.H + (PAGED ? 2 : 1) * a.Hkv, groups = (heads + RPW - 1) / RPW;
+    // enough warps to fill the SMs (16 a SM); beyond that a token stays with one warp
+    const int want = (kSMs * 16 + a.n - 1) / a.n;
+    a.parts = want < 1 ? 1 : want > groups ? groups : want;
+    const long long warps = (long long)a.n * a.parts;
+    norm_rope_kernel<T, D, PAGED><<<(unsigned)((warps + kNrThreads / 32 - 1) / (kNrThreads / 32)), kNrThreads, 0, st>>>(a, P);
+}
+
+template <bool PAGED>
+int norm_rope(const NormRope& a, const PagedView& P, int d, int dtype, cudaStream_t st) {
+    const bool f32 = dtype == SUBGEN_DTYPE_FP32;
+    if (d == 64) f32 ? launch_norm_rope<float, 64, PAGED>(a, P, st) : launch_norm_rope<__nv_bfloat16, 64, PAGED>(a, P, st);
+    else f32 ? launch_norm_rope<float, 128, PAGED>(a, P, st) : launch_norm_rope<__nv_bfloat16, 128, PAGED>(a, P, st);
+    CUDA_TRY(cudaGetLastError());
+    return SUBGEN_OK;
+}
+
+// ---- attention ----
+size_t plan_bytes(int E) { return ((size_t)12 * (E + 1) + 15) & ~(size_t)15; }
+
+long long slot_count(const PagedView& P, int n, int H) {
+    // every row once per entry it belongs to, twice where two halves of a block share its tiles, and a row unit of up
+    // to 256 rows for every block that shares a unit with the block before it
+    return (long long)n * H * 2 * (P.groups ? 2 : 1) + 256LL * kSMs * 2;
+}
+
+template <typename K>
+int opt_in(K kern, size_t smem, bool* done) {
+    int dev = -1;
+    CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices) return fail(SUBGEN_EINVAL, "device index %d not supported", dev);
+    if (!done[dev]) {
+        CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        done[dev] = true;
+    }
+    return SUBGEN_OK;
+}
+
+template <typename T, int D, int RU, int KT, bool DUAL>
+int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t st) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    // a block per row unit of a sequence and KV head, as far as the grid goes
+    const long long units = ((long long)P.B + (long long)a.n * a.G / RU) * P.Hkv;
+    cfg.gridDim = dim3((unsigned)(units < kSMs * 8 ? units : kSMs * 8));
+    cfg.blockDim = dim3(kMergeThreads);
+    cfg.dynamicSmemBytes = plan_bytes(P.B + P.groups) + (size_t)4 * (P.B + 1);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_merge_kernel<T, D, RU, KT, DUAL>, P, a, blocks));
+    return SUBGEN_OK;
+}
+
+template <typename T, int D, int RU, int NT>
+int attend_simt(const PagedView& P, const Attend& a, cudaStream_t st) {
+    auto kern = paged_attend_simt_kernel<T, D, RU, NT>;
+    static bool done[kMaxDevices];
+    constexpr size_t tile = (sizeof(SimtSmem<D, RU>) + 15) & ~(size_t)15;
+    const int rc = opt_in(kern, tile + plan_bytes(kPlanMax), done);
+    if (rc) return rc;
+    const int blocks = kSMs * 2;
+    kern<<<blocks, NT, tile + plan_bytes(P.B + P.groups), st>>>(P, a);
+    CUDA_TRY(cudaGetLastError());
+    return launch_merge<T, D, RU, kSimtKT, false>(P, a, blocks, st);
+}
+
+template <typename T, int D>
+int attend_simt_rows(const PagedView& P, const Attend& a, cudaStream_t st) {
+    // 16-row units while a sequence has up to 16 rows on average, else 64
+    if ((long long)a.n * a.G <= 16LL * P.B) return attend_simt<T, D, 16, 128>(P, a, st);
+    return attend_simt<T, D, 64, 256>(P, a, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int subgen_rope_words(const double* f, int count, uint64_t* words) {
+    if (!f || !words || count < 0) return fail(SUBGEN_EINVAL, "subgen_rope_words: invalid argument");
+    for (int i = 0; i < count; ++i) {
+        if (!isfinite(f[i])) return fail(SUBGEN_EINVAL, "subgen_rope_words: f[%d] is not finite", i);
+        const long double turns = (long double)f[i] / 6.283185307179586476925286766559005768L;
+        const long double frac = turns - floorl(turns);                       // [0, 1)
+        const long double w = roundl(frac * 18446744073709551616.0L);
+        words[i] = w >= 18446744073709551616.0L ? 0 : (uint64_t)w;
+    }
+    return SUBGEN_OK;
+}
+
+int subgen_qk_norm_rope(const subgen_heads* q, const subgen_heads* k, const subgen_heads* q_out, const subgen_heads* k_out,
+                        int n, int H, int Hkv, int d, int dtype, const int* positions, const subgen_rope* rope,
+                        const void* wq, const void* wk, float eps, void* stream) {
+    const char* fn = "subgen_qk_norm_rope";
+    const bool has_q = q && q->p, has_k = k && k->p;
+    int rc = check_shape(fn, n, has_q || !has_k ? H : 1, has_k || !has_q ? Hkv : 1, d, dtype);
+    if (!rc) rc = check_rope(fn, rope, d);
+    if (!rc) rc = check_norm(fn, wq, wk, eps);
+    if (rc || n == 0) return rc;
+    if (!has_q && !has_k) rc = fail(SUBGEN_EINVAL, "%s: q and k must not both be NULL", fn);
+    if (!rc && has_q) { rc = check_heads(fn, "q", q, dtype); if (!rc) rc = check_heads(fn, "q_out", q_out, dtype); }
+    if (!rc && has_k) { rc = check_heads(fn, "k", k, dtype); if (!rc) rc = check_heads(fn, "k_out", k_out, dtype); }
+    const bool turn = rope && rope->words;
+    if (!rc && turn && !positions) rc = fail(SUBGEN_EINVAL, "%s: a rotation needs positions", fn);
+    if (rc) return rc;
+    NormRope a = {view(q), view(k), HeadsView{nullptr, 0, 0}, view(q_out), view(k_out), n, has_q ? H : 0, has_k ? Hkv : 0, 1, positions,
+                  turn ? (const unsigned long long*)rope->words : nullptr, turn ? rope->rotary_dim : 0, turn ? rope->interleaved : 0,
+                  wq, wk, eps};
+    PagedView none;
+    memset(&none, 0, sizeof none);
+    return norm_rope<false>(a, none, d, dtype, (cudaStream_t)stream);
+}
+
+int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* k, const subgen_heads* v,
+                        const subgen_heads* q, const subgen_heads* q_out, int n, int H, const int* positions,
+                        const subgen_rope* rope, const void* wq, const void* wk, float eps, void* stream) {
+    const char* fn = "subgen_paged_append";
+    PagedView P;
+    if (!cache || !batch) return fail(SUBGEN_EINVAL, "%s: cache and batch must not be NULL", fn);
+    const bool has_q = q && q->p;
+    int rc = check_shape(fn, n, has_q ? H : 1, cache->Hkv, cache->d, cache->dtype);
+    if (!rc) rc = check_cache(fn, cache, batch, &P);
+    if (!rc) rc = check_rope(fn, rope, cache->d);
+    if (!rc) rc = check_norm(fn, wq, wk, eps);
+    if (rc || n == 0 || batch->B == 0) return rc;
+    rc = check_heads(fn, "k", k, cache->dtype);
+    if (!rc) rc = check_heads(fn, "v", v, cache->dtype);
+    if (!rc && has_q) { rc = check_heads(fn, "q", q, cache->dtype); if (!rc) rc = check_heads(fn, "q_out", q_out, cache->dtype); }
+    if (rc) return rc;
+    const bool turn = rope && rope->words;
+    NormRope a = {view(q), view(k), view(v), view(q_out), HeadsView{nullptr, 0, 0}, n, has_q ? H : 0, cache->Hkv, 1, positions,
+                  turn ? (const unsigned long long*)rope->words : nullptr, turn ? rope->rotary_dim : 0, turn ? rope->interleaved : 0,
+                  wq, wk, eps};
+    return norm_rope<true>(a, P, cache->d, cache->dtype, (cudaStream_t)stream);
+}
+
+size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H) {
+    const char* fn = "subgen_paged_workspace_bytes";
+    PagedView P;
+    if (!cache || !batch) { fail(SUBGEN_EINVAL, "%s: cache and batch must not be NULL", fn); return 0; }
+    if (check_shape(fn, n, H, cache->Hkv, cache->d, cache->dtype) || check_cache(fn, cache, batch, &P)) return 0;
+    return (size_t)slot_count(P, n, H) * (cache->d * sizeof(float) + sizeof(float2));
+}
+
+int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* q, const subgen_heads* out,
+                        int n, int H, float scale, int causal, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "subgen_paged_attend";
+    PagedView P;
+    if (!cache || !batch) return fail(SUBGEN_EINVAL, "%s: cache and batch must not be NULL", fn);
+    int rc = check_shape(fn, n, H, cache->Hkv, cache->d, cache->dtype);
+    if (!rc) rc = check_cache(fn, cache, batch, &P);
+    if (rc) return rc;
+    const int G = H / cache->Hkv, d = cache->d;
+    if (H % cache->Hkv || (G != 1 && G != 2 && G != 4 && G != 8)) return fail(SUBGEN_EINVAL, "%s: H / Hkv must be 1, 2, 4 or 8", fn);
+    if (!(scale > 0.f) || !isfinite(scale)) return fail(SUBGEN_EINVAL, "%s: scale must be positive and finite", fn);
+    if (n == 0 || batch->B == 0) return SUBGEN_OK;
+    rc = check_heads(fn, "q", q, cache->dtype);
+    if (!rc) rc = check_heads(fn, "out", out, cache->dtype);
+    if (rc) return rc;
+    const long long slots = slot_count(P, n, H);
+    const size_t need = (size_t)slots * (d * sizeof(float) + sizeof(float2));
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
+        return fail(SUBGEN_ENOMEM, "%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, need);
+    Attend a = {view(q), view(out), n, H, G, causal != 0, scale * 1.4426950408889634f, (float*)workspace,
+                (float2*)((float*)workspace + slots * d), slots};
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool f32 = cache->dtype == SUBGEN_DTYPE_FP32;
+    if (d == 64) return f32 ? attend_simt_rows<float, 64>(P, a, st) : attend_simt_rows<__nv_bfloat16, 64>(P, a, st);
+    return f32 ? attend_simt_rows<float, 128>(P, a, st) : attend_simt_rows<__nv_bfloat16, 128>(P, a, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,191 @@
+// Attention over a paged cache in fp32 arithmetic throughout: the path of fp32 caches.
+//
+// One block takes a run of key tiles of one row unit (see Plan): RU query rows against KT = 64 tokens at a time, both
+// products on the fp32 pipes from shared memory, the running maximum and sum of the softmax in registers. A thread
+// holds RPT rows x 4 scores of a tile and RPT rows x D / 16 columns of the numerator; the 16 threads of a row are
+// half a warp, so row reductions are four shuffles.
+// Two sizes: RU = 16 for single tokens and drafts, where the cache is read once and 16 rows of arithmetic per byte
+// stay below what the memory takes; RU = 64 for many rows, where each value read from shared memory serves four rows.
+#pragma once
+#include "subgen_paged.cuh"
+
+namespace sgk {
+
+constexpr int kSimtKT = 64;
+
+template <int D, int RU>
+struct SimtSmem {
+    float Q[RU][D];
+    float K[kSimtKT][D + 4];                          // + 4: sixteen threads read sixteen rows at once
+    float V[kSimtKT][D];
+    float P[RU][kSimtKT];
+    int bad, flag;
+};
+
+template <typename T, int D, int RU, int NT>
+__global__ void __launch_bounds__(NT) paged_attend_simt_kernel(PagedView P, Attend a) {
+    constexpr int KT = kSimtKT, TY = NT / 16, RPT = RU / TY, VE = 16 / sizeof(T), LPR = D / VE;
+    static_assert(RPT * TY == RU, "rows divide");
+    extern __shared__ __align__(16) unsigned char dyn[];
+    SimtSmem<D, RU>& sm = *reinterpret_cast<SimtSmem<D, RU>*>(dyn);
+    Plan<RU, KT, false> plan(P, a);
+    plan.build(dyn + ((sizeof(SimtSmem<D, RU>) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
+    pdl_trigger();
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    long long x = (long long)blockIdx.x * plan.chunk;
+    const long long x1 = min(plan.total, x + plan.chunk);
+    while (x < x1) {
+        const Seg g = plan.next(x, x1, blockIdx.x);
+        if (g.tile0 >= g.tile1) continue;
+        const int row0 = g.ru * RU;
+        __syncthreads();
+        if (tid == 0) sm.bad = g.e.bad;
+        for (int p = tid; p < RU * LPR; p += NT) {
+            const int r = p / LPR, piece = p % LPR;
+            float f[VE];
+#pragma unroll
+            for (int e = 0; e < VE; ++e) f[e] = 0.f;
+            if (r < g.rows) {
+                const int row = row0 + r, tok = g.e.tok0 + row / a.G, h = g.head * a.G + row % a.G;
+                Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>((const T*)a.q.p + tok * a.q.ts + h * a.q.hs) + piece), f);
+            }
+#pragma unroll
+            for (int e = 0; e < VE; ++e) sm.Q[r][piece * VE + e] = f[e];
+        }
+        float m[RPT], l[RPT], acc[RPT][D / 16];
+        int own[RPT];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            m[i] = -INFINITY;
+            l[i] = 0.f;
+            own[i] = plan.own_limit(g.e, row0 + ty * RPT + i);
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) acc[i][j] = 0.f;
+        }
+        for (int t = g.tile0; t < g.tile1; ++t) {
+            const bool pre = t < g.kp;
+            const int base = (pre ? t : t - g.kp) * KT, limit = pre ? g.e.P : g.e.S;
+            const int* tab = pre ? g.e.ptab : g.e.stab;
+            __syncthreads();
+            for (int p = tid; p < KT * LPR; p += NT) {
+                const int j = p / LPR, piece = p % LPR, pos = base + j;
+                uint4 kr = make_uint4(0, 0, 0, 0), vr = kr;
+                if (pos < limit) {
+                    const int id = __ldg(tab + (pos >> P.page_shift));
+                    if (id >= 0 && id < P.pages) {
+                        const long long off = id * P.ps + g.head * P.hs + (pos & ((1 << P.page_shift) - 1)) * P.ts;
+                        kr = __ldg(reinterpret_cast<const uint4*>((const T*)P.K + off) + piece);
+                        vr = __ldg(reinterpret_cast<const uint4*>((const T*)P.V + off) + piece);
+                    } else {
+                        sm.bad = 1;
+                    }
+                }
+                float f[VE];
+                Elem<T>::unpack(kr, f);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) sm.K[j][piece * VE + e] = f[e];
+                Elem<T>::unpack(vr, f);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) sm.V[j][piece * VE + e] = f[e];
+            }
+            __syncthreads();
+            float s[RPT][4];
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+#pragma unroll 4
+            for (int e = 0; e < D; e += 4) {
+                float4 kv[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(&sm.K[tx + 16 * j][e]);
+#pragma unroll
+                for (int i = 0; i < RPT; ++i) {
+                    const float4 qv = *reinterpret_cast<const float4*>(&sm.Q[ty * RPT + i][e]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        s[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, s[i][j]))));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) {
+                const int lim = (pre ? limit : own[i]) - base;
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[i][j] = tx + 16 * j < lim ? s[i][j] * a.c : -INFINITY;
+                    top = fmaxf(top, s[i][j]);
+                }
+#pragma unroll
+                for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                const float mn = fmaxf(m[i], top), b = mn == -INFINITY ? 0.f : mn;
+                const float al = exp2f(m[i] - b);
+                m[i] = mn;
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p = exp2f(s[i][j] - b);
+                    sum += p;
+                    sm.P[ty * RPT + i][tx + 16 * j] = p;
+                }
+                l[i] = l[i] * al + sum;                              // this thread's share; the 16 are added at the end
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) acc[i][j] *= al;
+            }
+            __syncwarp();                                            // a row's scores come from and go to one half-warp
+#pragma unroll 4
+            for (int j = 0; j < KT; j += 4) {
+                float4 p[RPT];
+#pragma unroll
+                for (int i = 0; i < RPT; ++i) p[i] = *reinterpret_cast<const float4*>(&sm.P[ty * RPT + i][j]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                    for (int b = 0; b < D / 64; ++b) {
+                        const float4 v = *reinterpret_cast<const float4*>(&sm.V[j + q][b * 64 + tx * 4]);
+#pragma unroll
+                        for (int i = 0; i < RPT; ++i) {
+                            const float w = q == 0 ? p[i].x : q == 1 ? p[i].y : q == 2 ? p[i].z : p[i].w;
+                            acc[i][b * 4 + 0] = fmaf(w, v.x, acc[i][b * 4 + 0]);
+                            acc[i][b * 4 + 1] = fmaf(w, v.y, acc[i][b * 4 + 1]);
+                            acc[i][b * 4 + 2] = fmaf(w, v.z, acc[i][b * 4 + 2]);
+                            acc[i][b * 4 + 3] = fmaf(w, v.w, acc[i][b * 4 + 3]);
+                        }
+                    }
+                }
+            }
+        }
+        const bool bad = sm.bad != 0;                                // last written before the last tile's barrier
+        if (bad && tid == 0) paged_status(P, kStPage);
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
+            const int r = ty * RPT + i;
+            if (r >= g.rows) continue;
+            if (bad) l[i] = NAN;
+            float* y;
+            float f = 1.f;
+            if (g.direct) {
+                f = l[i] == 0.f ? 0.f : 1.f / l[i];
+                y = nullptr;
+            } else {
+                y = a.part + (g.slot + r) * D;
+                if (tx == 0) a.stat[g.slot + r] = make_float2(m[i], l[i]);
+            }
+            const int row = row0 + r;
+            T* o = (T*)a.o.p + (g.e.tok0 + row / a.G) * a.o.ts + (g.head * a.G + row % a.G) * a.o.hs;
+#pragma unroll
+            for (int b = 0; b < D / 64; ++b) {
+                const float4 v = make_float4(acc[i][b * 4] * f, acc[i][b * 4 + 1] * f, acc[i][b * 4 + 2] * f, acc[i][b * 4 + 3] * f);
+                if (y) *reinterpret_cast<float4*>(y + b * 64 + tx * 4) = v;
+                else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(o + b * 64 + tx * 4) = v;
+                else {
+                    __nv_bfloat162* ob = reinterpret_cast<__nv_bfloat162*>(o + b * 64 + tx * 4);
+                    ob[0] = __floats2bfloat162_rn(v.x, v.y);
+                    ob[1] = __floats2bfloat162_rn(v.z, v.w);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace sgk
