@@ -9,6 +9,7 @@
 
 #include "subgen_paged.cuh"
 #include "subgen_paged_simt.cuh"
+#include "subgen_paged_tc.cuh"
 
 using namespace sgk;
 
@@ -38,9 +39,12 @@ bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 size_t elem(int dtype) { return dtype == SUBGEN_DTYPE_FP32 ? 4 : 2; }
 bool odd_stride(int64_t s, int dtype) { return (s * (int64_t)elem(dtype)) % 16 != 0; }
 
-int check_heads(const char* fn, const char* name, const subgen_heads* x, int dtype) {
+// Also makes the kernel's view of it; the stride of an axis of one is not looked at.
+int check_heads(const char* fn, const char* name, const subgen_heads* x, int n, int heads, int d, int dtype, HeadsView* v) {
     if (!x || !x->p) return fail(SUBGEN_EINVAL, "%s: %s must not be NULL", fn, name);
-    if (misaligned(x->p) || odd_stride(x->token_stride, dtype) || odd_stride(x->head_stride, dtype))
+    *v = HeadsView{x->p, n == 1 ? (int64_t)heads * d : x->token_stride, heads == 1 ? d : x->head_stride};
+    if (v->ts <= 0 || v->hs <= 0) return fail(SUBGEN_EINVAL, "%s: %s: strides must be positive", fn, name);
+    if (misaligned(x->p) || odd_stride(v->ts, dtype) || odd_stride(v->hs, dtype))
         return fail(SUBGEN_EINVAL, "%s: %s: pointer and strides must be multiples of 16 bytes", fn, name);
     return SUBGEN_OK;
 }
@@ -92,8 +96,6 @@ int check_cache(const char* fn, const subgen_pages* c, const subgen_batch* b, Pa
                    b->table_stride, b->prefix_stride, c->status};
     return SUBGEN_OK;
 }
-
-HeadsView view(const subgen_heads* x) { return x && x->p ? HeadsView{x->p, x->token_stride, x->head_stride} : HeadsView{nullptr, 0, 0}; }
 
 // ---- norms, rotation, append ----
 template <typename T, int D, bool PAGED>
@@ -176,6 +178,61 @@ int attend_simt_rows(const PagedView& P, const Attend& a, cudaStream_t st) {
     return attend_simt<T, D, 64, 256>(P, a, st);
 }
 
+// ---- attention, bf16: tensor maps over the pool and the queries ----
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return (EncodeTiled)p;
+    }();
+    return f;
+}
+
+// extents and strides from the second axis on; the innermost is d, boxes are 64 columns (128 bytes) wide
+int make_map(CUtensorMap* m, void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+    const EncodeTiled f = encode_tiled();
+    if (!f) return fail(SUBGEN_ECUDA, "cuTensorMapEncodeTiled is not available");
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    const CUresult r = f(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, p, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(SUBGEN_ECUDA, "cuTensorMapEncodeTiled failed (%d): strides of 2^40 bytes or more?", (int)r);
+    return SUBGEN_OK;
+}
+
+template <int D>
+int attend_tc(const PagedView& P, const Attend& a, cudaStream_t st) {
+    auto kern = paged_attend_tc_kernel<D>;
+    static bool done[kMaxDevices];
+    constexpr size_t fixed = 1024 + ((sizeof(PtSmem<D>) + 15) & ~(size_t)15);
+    int rc = opt_in(kern, fixed + plan_bytes(kPlanMax), done);
+    if (rc) return rc;
+    CUtensorMap mq, mk, mv;
+    {
+        const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.H, (cuuint64_t)a.n};
+        const cuuint64_t strides[2] = {(cuuint64_t)a.q.hs * 2, (cuuint64_t)a.q.ts * 2};
+        const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)(128 / a.G)};
+        rc = make_map(&mq, a.q.p, 3, dims, strides, box);
+    }
+    const int page = 1 << P.page_shift;
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)page, (cuuint64_t)P.Hkv, (cuuint64_t)P.pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)P.ts * 2, (cuuint64_t)P.hs * 2, (cuuint64_t)P.ps * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(page < 128 ? page : 128), 1, 1};
+    if (!rc) rc = make_map(&mk, P.K, 4, dims, strides, box);
+    if (!rc) rc = make_map(&mv, P.V, 4, dims, strides, box);
+    if (rc) return rc;
+    kern<<<kSMs, kPtThreads, fixed + plan_bytes(P.B + P.groups), st>>>(P, a, mq, mk, mv);
+    CUDA_TRY(cudaGetLastError());
+    return launch_merge<__nv_bfloat16, D, kPtRU, kPtKT, true>(P, a, kSMs, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -202,12 +259,15 @@ int subgen_qk_norm_rope(const subgen_heads* q, const subgen_heads* k, const subg
     if (!rc) rc = check_norm(fn, wq, wk, eps);
     if (rc || n == 0) return rc;
     if (!has_q && !has_k) rc = fail(SUBGEN_EINVAL, "%s: q and k must not both be NULL", fn);
-    if (!rc && has_q) { rc = check_heads(fn, "q", q, dtype); if (!rc) rc = check_heads(fn, "q_out", q_out, dtype); }
-    if (!rc && has_k) { rc = check_heads(fn, "k", k, dtype); if (!rc) rc = check_heads(fn, "k_out", k_out, dtype); }
+    HeadsView vq = {nullptr, 0, 0}, vk = vq, vqo = vq, vko = vq;
+    if (!rc && has_q) rc = check_heads(fn, "q", q, n, H, d, dtype, &vq);
+    if (!rc && has_q) rc = check_heads(fn, "q_out", q_out, n, H, d, dtype, &vqo);
+    if (!rc && has_k) rc = check_heads(fn, "k", k, n, Hkv, d, dtype, &vk);
+    if (!rc && has_k) rc = check_heads(fn, "k_out", k_out, n, Hkv, d, dtype, &vko);
     const bool turn = rope && rope->words;
     if (!rc && turn && !positions) rc = fail(SUBGEN_EINVAL, "%s: a rotation needs positions", fn);
     if (rc) return rc;
-    NormRope a = {view(q), view(k), HeadsView{nullptr, 0, 0}, view(q_out), view(k_out), n, has_q ? H : 0, has_k ? Hkv : 0, 1, positions,
+    NormRope a = {vq, vk, HeadsView{nullptr, 0, 0}, vqo, vko, n, has_q ? H : 0, has_k ? Hkv : 0, 1, positions,
                   turn ? (const unsigned long long*)rope->words : nullptr, turn ? rope->rotary_dim : 0, turn ? rope->interleaved : 0,
                   wq, wk, eps};
     PagedView none;
@@ -227,12 +287,14 @@ int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, co
     if (!rc) rc = check_rope(fn, rope, cache->d);
     if (!rc) rc = check_norm(fn, wq, wk, eps);
     if (rc || n == 0 || batch->B == 0) return rc;
-    rc = check_heads(fn, "k", k, cache->dtype);
-    if (!rc) rc = check_heads(fn, "v", v, cache->dtype);
-    if (!rc && has_q) { rc = check_heads(fn, "q", q, cache->dtype); if (!rc) rc = check_heads(fn, "q_out", q_out, cache->dtype); }
+    HeadsView vk, vv, vq = {nullptr, 0, 0}, vqo = vq;
+    rc = check_heads(fn, "k", k, n, cache->Hkv, cache->d, cache->dtype, &vk);
+    if (!rc) rc = check_heads(fn, "v", v, n, cache->Hkv, cache->d, cache->dtype, &vv);
+    if (!rc && has_q) rc = check_heads(fn, "q", q, n, H, cache->d, cache->dtype, &vq);
+    if (!rc && has_q) rc = check_heads(fn, "q_out", q_out, n, H, cache->d, cache->dtype, &vqo);
     if (rc) return rc;
     const bool turn = rope && rope->words;
-    NormRope a = {view(q), view(k), view(v), view(q_out), HeadsView{nullptr, 0, 0}, n, has_q ? H : 0, cache->Hkv, 1, positions,
+    NormRope a = {vq, vk, vv, vqo, HeadsView{nullptr, 0, 0}, n, has_q ? H : 0, cache->Hkv, 1, positions,
                   turn ? (const unsigned long long*)rope->words : nullptr, turn ? rope->rotary_dim : 0, turn ? rope->interleaved : 0,
                   wq, wk, eps};
     return norm_rope<true>(a, P, cache->d, cache->dtype, (cudaStream_t)stream);
@@ -258,19 +320,19 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
     if (H % cache->Hkv || (G != 1 && G != 2 && G != 4 && G != 8)) return fail(SUBGEN_EINVAL, "%s: H / Hkv must be 1, 2, 4 or 8", fn);
     if (!(scale > 0.f) || !isfinite(scale)) return fail(SUBGEN_EINVAL, "%s: scale must be positive and finite", fn);
     if (n == 0 || batch->B == 0) return SUBGEN_OK;
-    rc = check_heads(fn, "q", q, cache->dtype);
-    if (!rc) rc = check_heads(fn, "out", out, cache->dtype);
+    HeadsView vq, vo;
+    rc = check_heads(fn, "q", q, n, H, d, cache->dtype, &vq);
+    if (!rc) rc = check_heads(fn, "out", out, n, H, d, cache->dtype, &vo);
     if (rc) return rc;
     const long long slots = slot_count(P, n, H);
     const size_t need = (size_t)slots * (d * sizeof(float) + sizeof(float2));
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
         return fail(SUBGEN_ENOMEM, "%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, need);
-    Attend a = {view(q), view(out), n, H, G, causal != 0, scale * 1.4426950408889634f, (float*)workspace,
+    Attend a = {vq, vo, n, H, G, causal != 0, scale * 1.4426950408889634f, (float*)workspace,
                 (float2*)((float*)workspace + slots * d), slots};
     cudaStream_t st = (cudaStream_t)stream;
-    const bool f32 = cache->dtype == SUBGEN_DTYPE_FP32;
-    if (d == 64) return f32 ? attend_simt_rows<float, 64>(P, a, st) : attend_simt_rows<__nv_bfloat16, 64>(P, a, st);
-    return f32 ? attend_simt_rows<float, 128>(P, a, st) : attend_simt_rows<__nv_bfloat16, 128>(P, a, st);
+    if (cache->dtype == SUBGEN_DTYPE_BF16) return d == 64 ? attend_tc<64>(P, a, st) : attend_tc<128>(P, a, st);
+    return d == 64 ? attend_simt_rows<float, 64>(P, a, st) : attend_simt_rows<float, 128>(P, a, st);
 }
 
 }  // extern "C"
