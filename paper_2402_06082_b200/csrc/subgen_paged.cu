@@ -119,7 +119,7 @@ int norm_rope(const NormRope& a, const PagedView& P, int d, int dtype, cudaStrea
 }
 
 // ---- attention ----
-size_t plan_bytes(int E) { return ((size_t)12 * (E + 1) + 15) & ~(size_t)15; }
+size_t plan_bytes(int E) { return ((size_t)8 * (E + 1) + 15) & ~(size_t)15; }
 
 long long slot_count(const PagedView& P, int n, int H) {
     // every row once per entry it belongs to, twice where two halves of a block share its tiles, and a row unit of up
@@ -139,12 +139,12 @@ int opt_in(K kern, size_t smem, bool* done) {
     return SUBGEN_OK;
 }
 
-template <typename T, int D, int RU, int KT, bool DUAL>
+template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
 int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     // a block per row unit of a sequence and KV head, as far as the grid goes
-    const long long units = ((long long)P.B + (long long)a.n * a.G / RU) * P.Hkv;
+    const long long units = ((long long)P.B + ((long long)a.n << a.g_shift) / RU) * P.Hkv;
     cfg.gridDim = dim3((unsigned)(units < kSMs * 8 ? units : kSMs * 8));
     cfg.blockDim = dim3(kMergeThreads);
     cfg.dynamicSmemBytes = plan_bytes(P.B + P.groups) + (size_t)4 * (P.B + 1);
@@ -154,7 +154,7 @@ int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t s
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_merge_kernel<T, D, RU, KT, DUAL>, P, a, blocks));
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_merge_kernel<T, D, RU, KT, DUAL, LEAD>, P, a, blocks));
     return SUBGEN_OK;
 }
 
@@ -168,13 +168,13 @@ int attend_simt(const PagedView& P, const Attend& a, cudaStream_t st) {
     const int blocks = kSMs * 2;
     kern<<<blocks, NT, tile + plan_bytes(P.B + P.groups), st>>>(P, a);
     CUDA_TRY(cudaGetLastError());
-    return launch_merge<T, D, RU, kSimtKT, false>(P, a, blocks, st);
+    return launch_merge<T, D, RU, kSimtKT, false, kSimtLead>(P, a, blocks, st);
 }
 
 template <typename T, int D>
 int attend_simt_rows(const PagedView& P, const Attend& a, cudaStream_t st) {
     // 16-row units while a sequence has up to 16 rows on average, else 64
-    if ((long long)a.n * a.G <= 16LL * P.B) return attend_simt<T, D, 16, 128>(P, a, st);
+    if (((long long)a.n << a.g_shift) <= 16LL * P.B) return attend_simt<T, D, 16, 128>(P, a, st);
     return attend_simt<T, D, 64, 256>(P, a, st);
 }
 
@@ -218,7 +218,7 @@ int attend_tc(const PagedView& P, const Attend& a, cudaStream_t st) {
     {
         const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.H, (cuuint64_t)a.n};
         const cuuint64_t strides[2] = {(cuuint64_t)a.q.hs * 2, (cuuint64_t)a.q.ts * 2};
-        const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)(128 / a.G)};
+        const cuuint32_t box[3] = {64, 1u << a.g_shift, 32u >> a.g_shift};       // 32 rows
         rc = make_map(&mq, a.q.p, 3, dims, strides, box);
     }
     const int page = 1 << P.page_shift;
@@ -230,7 +230,7 @@ int attend_tc(const PagedView& P, const Attend& a, cudaStream_t st) {
     if (rc) return rc;
     kern<<<kSMs, kPtThreads, fixed + plan_bytes(P.B + P.groups), st>>>(P, a, mq, mk, mv);
     CUDA_TRY(cudaGetLastError());
-    return launch_merge<__nv_bfloat16, D, kPtRU, kPtKT, true>(P, a, kSMs, st);
+    return launch_merge<__nv_bfloat16, D, kPtRU, kPtKT, true, kPtLead>(P, a, kSMs, st);
 }
 
 }  // namespace
@@ -325,11 +325,13 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
     if (!rc) rc = check_heads(fn, "out", out, n, H, d, cache->dtype, &vo);
     if (rc) return rc;
     const long long slots = slot_count(P, n, H);
+    if (slots > 0x7fffffffLL) return fail(SUBGEN_EINVAL, "%s: too many rows in one call", fn);
     const size_t need = (size_t)slots * (d * sizeof(float) + sizeof(float2));
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
         return fail(SUBGEN_ENOMEM, "%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, need);
-    Attend a = {vq, vo, n, H, G, causal != 0, scale * 1.4426950408889634f, (float*)workspace,
-                (float2*)((float*)workspace + slots * d), slots};
+    const int g_shift = G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : 3;
+    Attend a = {vq, vo, n, H, g_shift, causal != 0, scale * 1.4426950408889634f, (float*)workspace,
+                (float2*)((float*)workspace + slots * d)};
     cudaStream_t st = (cudaStream_t)stream;
     if (cache->dtype == SUBGEN_DTYPE_BF16) return d == 64 ? attend_tc<64>(P, a, st) : attend_tc<128>(P, a, st);
     return d == 64 ? attend_simt_rows<float, 64>(P, a, st) : attend_simt_rows<float, 128>(P, a, st);

@@ -190,13 +190,15 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRope a, Paged
 // groups first (their prefix against the rows of all their sequences at once: the prefix is read once per group),
 // then sequences (own tokens against the sequence's rows). An entry's rows (tokens x G heads, in packed order, so a
 // group's rows are one range of tokens) are cut into row units of RU rows, each unit's keys into tiles of KT tokens.
-// A unit's tiles carry weight 2 when both halves of its rows are in use. All weights of all heads lie on one line;
-// block c takes [c * chunk, (c+1) * chunk) of it, so every block has the same work whatever the lengths are, and a
-// unit that several blocks share leaves one partial result (numerator, largest score, sum) per block.
+// A unit with tiles has weight LEAD (what starting and ending a run costs, in tiles) plus 1 for each tile, or 2 where
+// both halves of its rows are in use. All weights of all heads lie on one line; block c takes [c * chunk, (c+1) * chunk)
+// of it, so every block has the same work whatever the lengths are, and a unit that several blocks share leaves one
+// partial result (numerator, largest score, sum) per block.
 // A group folds its prefix into the sequences' entries (own tiles follow the prefix's tiles there) when that costs no
 // tensor work: one sequence in it, or at least RU / 2 rows per sequence, so that the row units are full without
 // packing several sequences into one; that spares the rows' second partial.
-constexpr int kPlanMax = 2048;                        // groups + sequences of one call
+constexpr int kPlanMax = 1024;                        // groups + sequences of one call
+constexpr long long kPlanWeight = 1 << 30;            // longest line; some 10^13 (query row, key) pairs
 
 struct Entry {
     int tok0, rows;                                   // first token; rows = tokens * G
@@ -208,73 +210,39 @@ struct Seg {                                          // a run of tiles of one r
     Entry e;
     int entry, head, ru, rows, tile0, tile1, tiles, kp;   // rows of the unit; kp: tiles of the prefix
     bool direct;                                      // the unit's whole result: goes to `out` as it is
-    long long slot;                                   // row of the partials otherwise
+    int slot;                                         // row of the partials otherwise
 };
 
 struct Attend {
     HeadsView q, o;
-    int n, H, G, causal;
+    int n, H, g_shift, causal;                        // H / Hkv = 1 << g_shift
     float c;                                          // scale * log2(e)
     float* part;                                      // [slots][D] numerators
     float2* stat;                                     // [slots] largest score * c, sum
-    long long slots;
 };
 
-template <int RU, int KT, bool DUAL>
+template <int RU, int KT, bool DUAL, int LEAD>
 struct Plan {
     const PagedView& P;
     const Attend& a;
-    const long long* tscan;                           // [E+1] weights before each entry, per head
+    const int* tscan;                                 // [E+1] weights before each entry, per head
     const int* sscan;                                 // [E+1] partial slots before each entry, per head
-    int E, nblk;
-    long long head_w, total, chunk;
+    int E;
+    int head_w, total, chunk;
     bool broken;                                      // cu_q or cu_group is not what it has to be: nothing is computed
 
     __device__ Plan(const PagedView& P_, const Attend& a_) : P(P_), a(a_) {}
 
-    __device__ __forceinline__ bool folds(int g, int* b0, int* t0, int* t1) const {
-        *b0 = __ldg(P.cu_group + g);
-        const int b1 = __ldg(P.cu_group + g + 1);
-        *t0 = __ldg(P.cu_q + *b0);
+    __device__ __forceinline__ bool folds(int g, int* t0, int* t1) const {
+        const int b0 = __ldg(P.cu_group + g), b1 = __ldg(P.cu_group + g + 1);
+        *t0 = __ldg(P.cu_q + b0);
         *t1 = __ldg(P.cu_q + b1);
-        return b1 - *b0 <= 1 || (long long)(*t1 - *t0) * a.G >= (long long)(b1 - *b0) * (RU / 2);
+        return b1 - b0 <= 1 || ((long long)(*t1 - *t0) << a.g_shift) >= (long long)(b1 - b0) * (RU / 2);
     }
     __device__ __forceinline__ int clipped(int len, int stride, int* bad) const {
         const long long cap = (long long)stride << P.page_shift;
         if (len < 0 || len > cap) { *bad = 1; return len < 0 ? 0 : (int)cap; }
         return len;
-    }
-    __device__ Entry entry(int i) const {
-        Entry e;
-        e.bad = 0;
-        e.ptab = e.stab = nullptr;
-        if (i < P.groups) {
-            int b0, t0, t1;
-            const bool f = folds(i, &b0, &t0, &t1);
-            e.tok0 = t0;
-            e.nq = t1 - t0;
-            e.rows = f ? 0 : e.nq * a.G;
-            e.P = clipped(__ldg(P.prefix_len + i), P.prefix_stride, &e.bad);
-            e.S = 0;
-            e.ptab = P.prefix_table + (long long)i * P.prefix_stride;
-            return e;
-        }
-        const int b = i - P.groups;
-        e.tok0 = __ldg(P.cu_q + b);
-        e.nq = __ldg(P.cu_q + b + 1) - e.tok0;
-        e.rows = e.nq * a.G;
-        e.P = 0;
-        e.S = clipped(__ldg(P.lengths + b), P.table_stride, &e.bad);
-        e.stab = P.table + (long long)b * P.table_stride;
-        if (P.groups) {
-            const int g = group_of(b);
-            int b0, t0, t1;
-            if (folds(g, &b0, &t0, &t1)) {
-                e.P = clipped(__ldg(P.prefix_len + g), P.prefix_stride, &e.bad);
-                e.ptab = P.prefix_table + (long long)g * P.prefix_stride;
-            }
-        }
-        return e;
     }
     __device__ __forceinline__ int group_of(int b) const {
         int lo = 0, hi = P.groups - 1;
@@ -284,10 +252,42 @@ struct Plan {
         }
         return lo;
     }
+    __device__ __forceinline__ Entry entry(int i) const {
+        Entry e;
+        e.bad = 0;
+        e.ptab = e.stab = nullptr;
+        if (i < P.groups) {
+            int t0, t1;
+            const bool f = folds(i, &t0, &t1);
+            e.tok0 = t0;
+            e.nq = t1 - t0;
+            e.rows = f ? 0 : e.nq << a.g_shift;
+            e.P = clipped(__ldg(P.prefix_len + i), P.prefix_stride, &e.bad);
+            e.S = 0;
+            e.ptab = P.prefix_table + (long long)i * P.prefix_stride;
+            return e;
+        }
+        const int b = i - P.groups;
+        e.tok0 = __ldg(P.cu_q + b);
+        e.nq = __ldg(P.cu_q + b + 1) - e.tok0;
+        e.rows = e.nq << a.g_shift;
+        e.P = 0;
+        e.S = clipped(__ldg(P.lengths + b), P.table_stride, &e.bad);
+        e.stab = P.table + (long long)b * P.table_stride;
+        if (P.groups) {
+            const int g = group_of(b);
+            int t0, t1;
+            if (folds(g, &t0, &t1)) {
+                e.P = clipped(__ldg(P.prefix_len + g), P.prefix_stride, &e.bad);
+                e.ptab = P.prefix_table + (long long)g * P.prefix_stride;
+            }
+        }
+        return e;
+    }
     // own tokens that row r of an entry sees
     __device__ __forceinline__ int own_limit(const Entry& e, int r) const {
         if (!a.causal) return e.S;
-        const int lim = e.S - e.nq + 1 + r / a.G;
+        const int lim = e.S - e.nq + 1 + (r >> a.g_shift);
         return lim < 0 ? 0 : lim > e.S ? e.S : lim;
     }
     __device__ __forceinline__ int unit_rows(const Entry& e, int ru) const { return min(RU, e.rows - ru * RU); }
@@ -296,14 +296,16 @@ struct Plan {
         const int last = min(e.rows, (ru + 1) * RU) - 1;
         return prefix_tiles(e) + (own_limit(e, last) + KT - 1) / KT;
     }
-    __device__ static __forceinline__ int weight(int rows) { return DUAL && rows > RU / 2 ? 2 : 1; }
+    __device__ static __forceinline__ int shift(int rows) { return DUAL && rows > RU / 2 ? 1 : 0; }     // a tile weighs 1 << shift
+    __device__ __forceinline__ int unit_weight(int tiles, int rows) const { return tiles ? LEAD + (tiles << shift(rows)) : 0; }
+    // tiles of a unit before position p of its weight
+    __device__ static __forceinline__ int tile_at(int p, int sh) { return p <= LEAD ? 0 : (p - LEAD + sh) >> sh; }
 
-    // All threads of the block. sm: 12 bytes for each of E + 1, 8-byte aligned; flag: one int of shared memory.
-    __device__ void build(void* sm, int* flag, int nblk_) {
+    // All threads of the block. sm: 8 bytes for each of E + 1; flag: one int of shared memory.
+    __device__ void build(void* sm, int* flag, int nblk) {
         E = P.groups + P.B;
-        nblk = nblk_;
-        long long* t = (long long*)sm;
-        int* s = (int*)(t + E + 1);
+        int* t = (int*)sm;
+        int* s = t + E + 1;
         if (threadIdx.x == 0) *flag = 0;
         __syncthreads();
         bool bad = false;
@@ -319,23 +321,22 @@ struct Plan {
         }
         if (bad) *flag = 1;
         __syncthreads();
-        broken = *flag != 0;
-        if (!broken) {
+        if (*flag == 0) {
             for (int i = threadIdx.x; i < E; i += blockDim.x) {
                 const Entry e = entry(i);
                 long long w = 0;
                 int sl = 0;
                 for (int ru = 0; ru * RU < e.rows; ++ru) {
                     const int rows = unit_rows(e, ru);
-                    w += (long long)unit_tiles(e, ru) * weight(rows);
+                    w += unit_weight(unit_tiles(e, ru), rows);
                     sl = ru * RU + (DUAL && rows <= RU / 2 ? 2 * rows : rows);
                 }
-                t[i + 1] = w;
+                t[i + 1] = (int)(w > kPlanWeight ? kPlanWeight : w);
                 s[i + 1] = sl;
             }
         }
         __syncthreads();
-        if (threadIdx.x < 32 && !broken) {
+        if (threadIdx.x < 32 && *flag == 0) {
             long long at = 0;
             int as = 0;
             for (int i0 = 0; i0 < E; i0 += 32) {
@@ -348,38 +349,35 @@ struct Plan {
                     const int yo = __shfl_up_sync(0xffffffffu, y, off);
                     if ((int)threadIdx.x >= off) { x += xo; y += yo; }
                 }
-                if (i < E) { t[i + 1] = at + x; s[i + 1] = as + y; }
+                if (i < E) { t[i + 1] = (int)(at + x); s[i + 1] = as + y; }
                 at += __shfl_sync(0xffffffffu, x, 31);
                 as += __shfl_sync(0xffffffffu, y, 31);
             }
-            if (threadIdx.x == 0) { t[0] = 0; s[0] = 0; }
+            if (threadIdx.x == 0) {
+                t[0] = s[0] = 0;
+                if (at * P.Hkv > kPlanWeight) *flag = 1;
+            }
         }
         __syncthreads();
+        broken = *flag != 0;
         tscan = t;
         sscan = s;
         head_w = broken ? 0 : t[E];
         total = head_w * P.Hkv;
         chunk = total ? (total + nblk - 1) / nblk : 1;
     }
-    // first position of the line that belongs to row unit ru of entry i, head h
-    __device__ long long unit_start(const Entry& e, int i, int ru, int h) const {
-        long long x = h * head_w + tscan[i];
-        for (int k = 0; k < ru; ++k) x += (long long)unit_tiles(e, k) * weight(RU);
-        return x;
+    __device__ __forceinline__ int slot_of(int i, int ru, int h, int blk) const {
+        return h * sscan[E] + sscan[i] + ru * RU + blk * RU;
     }
-    __device__ __forceinline__ long long slot_of(int i, int ru, int h, int blk) const {
-        return (long long)h * sscan[E] + sscan[i] + (long long)ru * RU + (long long)blk * RU;
-    }
-    __device__ __forceinline__ bool is_direct(const Entry& e, int i, int rows, int tiles, int tile0, int tile1) const {
-        if (tile0 != 0 || tile1 != tiles || i < P.groups) return false;
-        if (P.groups && !e.ptab) return false;                       // the prefix's partials come from the group's entry
+    __device__ __forceinline__ bool is_direct(const Entry& e, int i, int rows, int tiles) const {
+        if (i < P.groups || (P.groups && !e.ptab)) return false;     // partials of the group's entry join in
         return !DUAL || rows > RU / 2 || tiles == 1;
     }
     // The run of tiles that starts at x (< x1 <= total) on the line; moves x behind it. May be empty (tile0 == tile1).
-    __device__ Seg next(long long& x, long long x1, int blk) const {
+    __device__ Seg next(int& x, int x1, int blk) const {
         Seg g;
-        g.head = (int)(x / head_w);
-        long long r = x - (long long)g.head * head_w;
+        g.head = x / head_w;
+        int r = x - g.head * head_w;
         int lo = 0, hi = E - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -393,18 +391,17 @@ struct Plan {
         while (true) {
             g.rows = unit_rows(g.e, ru);
             g.tiles = unit_tiles(g.e, ru);
-            w = weight(g.rows);
-            if (r < (long long)g.tiles * w) break;
-            r -= (long long)g.tiles * w;
+            w = unit_weight(g.tiles, g.rows);
+            if (r < w) break;
+            r -= w;
             ++ru;
         }
         g.ru = ru;
-        const long long left = (long long)g.tiles * w - r;
-        const long long take = x1 - x < left ? x1 - x : left;
-        g.tile0 = (int)((r + w - 1) / w);
-        g.tile1 = (int)((r + take + w - 1) / w);
+        const int take = min(x1 - x, w - r), sh = shift(g.rows);
+        g.tile0 = tile_at(r, sh);
+        g.tile1 = tile_at(r + take, sh);
         x += take;
-        g.direct = is_direct(g.e, g.entry, g.rows, g.tiles, g.tile0, g.tile1);
+        g.direct = g.tile0 == 0 && g.tile1 == g.tiles && is_direct(g.e, g.entry, g.rows, g.tiles);
         g.slot = slot_of(g.entry, ru, g.head, blk);
         return g;
     }
@@ -412,47 +409,48 @@ struct Plan {
 
 // Joins the partials of every row that has some (rows whose result went out directly are left alone) and writes 0 for
 // rows that see nothing, NaN for rows of a sequence whose lengths or pages are unusable. One block per row unit of a
-// sequence and KV head, a warp per row; the largest score first, then one pass over the numerators.
+// sequence and KV head. A row's partials are dealt to WPR warps (as many as the block has left for the unit's rows, so
+// that one sequence's long list is read by all of them); a lane looks after one partial's weight, then the warp adds the
+// numerators, all loads of a batch in flight, and the warps of a row join through shared memory.
 constexpr int kMergeThreads = 256;
 
-template <typename T, int D, int RU, int KT, bool DUAL>
+template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
 __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P, Attend a, int nblk) {
+    constexpr int NW = kMergeThreads / 32, VL = D / 32;
     extern __shared__ __align__(16) unsigned char sm_plan[];
     __shared__ int flag;
     __shared__ int units;
-    typedef Plan<RU, KT, DUAL> PlanT;
+    __shared__ float join[NW][D];
+    __shared__ float2 join_stat[NW];
+    typedef Plan<RU, KT, DUAL, LEAD> PlanT;
     PlanT plan(P, a);
     plan.build(sm_plan, &flag, nblk);
-    int* uscan = (int*)(sm_plan + 12 * (plan.E + 1));  // [B+1] row units before each sequence
+    int* uscan = (int*)sm_plan + 2 * (plan.E + 1);    // [B+1] row units before each sequence
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (!plan.broken) {
-        for (int b = tid; b < P.B; b += kMergeThreads)
-            uscan[b + 1] = ((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) * a.G + RU - 1) / RU;
+    if (plan.broken) {
+        if (blockIdx.x == 0 && tid == 0) paged_status(P, kStPage);
+        return;
     }
-    __syncthreads();
     if (warp == 0) {
         int at = 0;
-        for (int i0 = 0; i0 < P.B && !plan.broken; i0 += 32) {
-            int x = i0 + lane < P.B ? uscan[i0 + lane + 1] : 0;
+        for (int i0 = 0; i0 < P.B; i0 += 32) {
+            const int b = i0 + lane;
+            int x = b < P.B ? (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + RU - 1) / RU : 0;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const int xo = __shfl_up_sync(0xffffffffu, x, off);
                 if (lane >= off) x += xo;
             }
-            if (i0 + lane < P.B) uscan[i0 + lane + 1] = at + x;
+            if (b < P.B) uscan[b + 1] = at + x;
             at += __shfl_sync(0xffffffffu, x, 31);
         }
         if (lane == 0) { uscan[0] = 0; units = at; }
     }
     __syncthreads();
-    if (plan.broken) {
-        if (blockIdx.x == 0 && tid == 0) paged_status(P, kStPage);
-        return;
-    }
     pdl_wait();
-    const int items = units * P.Hkv;
+    const int items = units * P.Hkv, chunk = plan.chunk;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const int h = item / units, u = item % units;
+        const int h = item / units, u = item - h * units;
         int lo = 0, hi = P.B - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -460,77 +458,126 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
         }
         const int b = lo, ru = u - uscan[lo], ei = P.groups + b;
         const Entry e = plan.entry(ei);
-        const int rows = plan.unit_rows(e, ru), tiles = plan.unit_tiles(e, ru), w = PlanT::weight(rows);
-        const long long u0 = plan.unit_start(e, ei, ru, h), u1 = u0 + (long long)tiles * w;
-        const int c0 = (int)(u0 / plan.chunk);
-        int c1 = tiles ? (int)((u1 - 1) / plan.chunk) : c0 - 1;
-        if (c1 > c0 && ((long long)c1 * plan.chunk - u0 + w - 1) / w >= tiles) --c1;     // its share is half a tile: the block before did it
-        if (c0 == c1 && plan.is_direct(e, ei, rows, tiles, 0, tiles)) continue;
+        const int rows = plan.unit_rows(e, ru), tiles = plan.unit_tiles(e, ru), w = plan.unit_weight(tiles, rows), sh = PlanT::shift(rows);
+        int u0 = h * plan.head_w + plan.tscan[ei];
+        for (int k = 0; k < ru; ++k) u0 += plan.unit_weight(plan.unit_tiles(e, k), RU);
+        const int c0 = u0 / chunk, c1 = w ? (u0 + w - 1) / chunk : c0 - 1;
+        if (tiles && plan.is_direct(e, ei, rows, tiles)) {
+            // whole in one block: the one that holds the first tile also holds the last
+            const int p = (u0 + LEAD) / chunk;
+            if (PlanT::tile_at(min((p + 1) * chunk, u0 + w) - u0, sh) == tiles) continue;
+        }
         int g = -1;
         Entry ge;
+        ge.bad = ge.rows = ge.tok0 = 0;
         if (P.groups) {
             g = plan.group_of(b);
             ge = plan.entry(g);
             if (!ge.rows) g = -1;                                    // folded (or no rows)
         }
-        const int bad = e.bad | (g >= 0 ? ge.bad : 0);
-        if (bad && lane == 0) paged_status(P, kStPage);
-        for (int r = warp; r < rows; r += kMergeThreads / 32) {
-            const int row = ru * RU + r, tok = e.tok0 + row / a.G, head = h * a.G + row % a.G;
-            float acc[D / 32], m = -INFINITY, l = 0.f;
+        const int bad = e.bad | (g >= 0 ? ge.bad : 0), pt = g >= 0 ? plan.prefix_tiles(ge) : 0;
+        if (bad && tid == 0) paged_status(P, kStPage);
+        const int wpr = rows >= NW ? 1 : rows > 4 ? 1 : rows > 2 ? NW / 4 : rows > 1 ? NW / 2 : NW;   // warps per row
+        for (int r0 = 0; r0 < rows; r0 += NW / wpr) {
+            const int r = r0 + warp / wpr, sub = warp % wpr;
+            float acc[VL], m = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) acc[j] = 0.f;
-            // two passes over the partials: fn(slot)
-            auto each = [&](auto fn) {
-                for (int c = c0; c <= c1; ++c) {
-                    const long long a0 = max((long long)c * plan.chunk, u0) - u0, a1 = min((long long)(c + 1) * plan.chunk, u1) - u0;
-                    const int t0 = (int)((a0 + w - 1) / w), t1 = (int)((a1 + w - 1) / w);
-                    if (t0 >= t1) continue;
-                    const long long s = plan.slot_of(ei, ru, h, c) + r;
-                    fn(s);
-                    if (DUAL && rows <= RU / 2 && t1 - t0 > 1) fn(s + rows);
-                }
-                if (g >= 0) {
-                    const int prow = row + (e.tok0 - ge.tok0) * a.G, pru = prow / RU, pr = prow % RU;
-                    const int prows = plan.unit_rows(ge, pru), pt = plan.prefix_tiles(ge), pw = PlanT::weight(prows);
-                    if (pt) {
-                        const long long v0 = (long long)h * plan.head_w + plan.tscan[g] + (long long)pru * pt * PlanT::weight(RU);
-                        const long long v1 = v0 + (long long)pt * pw;
-                        const int d0 = (int)(v0 / plan.chunk), d1 = (int)((v1 - 1) / plan.chunk);
-                        for (int c = d0; c <= d1; ++c) {
-                            const long long a0 = max((long long)c * plan.chunk, v0) - v0, a1 = min((long long)(c + 1) * plan.chunk, v1) - v0;
-                            const int t0 = (int)((a0 + pw - 1) / pw), t1 = (int)((a1 + pw - 1) / pw);
-                            if (t0 >= t1) continue;
-                            const long long s = plan.slot_of(g, pru, h, c) + pr;
-                            fn(s);
-                            if (DUAL && prows <= RU / 2 && t1 - t0 > 1) fn(s + prows);
+            for (int j = 0; j < VL; ++j) acc[j] = 0.f;
+            // partials of one unit: 1 or 2 of every block in [d0, d1]; v0: the unit's start on the line, vw its weight
+            auto collect = [&](int v0, int vw, int vrows, int d0, int d1, int base) {
+                const int vsh = PlanT::shift(vrows), per = DUAL && !vsh ? 1 : 0, count = (d1 - d0 + 1) << per;
+                for (int i0 = sub * 32; i0 < count; i0 += wpr * 32) {
+                    const int i = i0 + lane, c = d0 + (i >> per), second = i & ((1 << per) - 1);
+                    float2 st = make_float2(-INFINITY, 0.f);
+                    int slot = 0;
+                    bool have = false;
+                    if (i < count) {
+                        const int t0 = PlanT::tile_at(max(c * chunk, v0) - v0, vsh), t1 = PlanT::tile_at(min((c + 1) * chunk, v0 + vw) - v0, vsh);
+                        have = t1 - t0 > second;
+                        slot = base + c * RU + (second ? vrows : 0);
+                    }
+                    if (have) st = __ldcg(a.stat + slot);
+                    float top = st.x;
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                    const float mn = fmaxf(m, top), bs = mn == -INFINITY ? 0.f : mn, al = exp2f(m - bs);
+                    const float f = have ? exp2f(st.x - bs) : 0.f;
+                    float sum = have ? st.y * f : 0.f;
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                    m = mn;
+                    l = l * al + sum;
+#pragma unroll
+                    for (int j = 0; j < VL; ++j) acc[j] *= al;
+                    unsigned todo = __ballot_sync(0xffffffffu, have);
+                    while (todo) {
+                        float x[8][VL], fx[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int src = todo ? __ffs(todo) - 1 : -1;
+                            todo &= todo - 1;
+                            const int s = __shfl_sync(0xffffffffu, slot, src & 31);
+                            fx[k] = __shfl_sync(0xffffffffu, f, src & 31);
+                            if (src < 0) fx[k] = 0.f;
+#pragma unroll
+                            for (int j = 0; j < VL; ++j) x[k][j] = 0.f;
+                            if (src >= 0) {
+                                const float* y = a.part + (long long)s * D + lane * VL;
+                                if constexpr (VL == 4) {
+                                    const float4 v = __ldcg(reinterpret_cast<const float4*>(y));
+                                    x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
+                                } else {
+                                    const float2 v = __ldcg(reinterpret_cast<const float2*>(y));
+                                    x[k][0] = v.x; x[k][1] = v.y;
+                                }
+                            }
                         }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+#pragma unroll
+                            for (int j = 0; j < VL; ++j) acc[j] = fmaf(x[k][j], fx[k], acc[j]);
                     }
                 }
             };
-            each([&](long long s) { m = fmaxf(m, __ldcg(a.stat + s).x); });
-            const float base = m == -INFINITY ? 0.f : m;
-            each([&](long long s) {
-                const float2 st = __ldcg(a.stat + s);
-                const float f = exp2f(st.x - base);
-                l += st.y * f;
-                if constexpr (D == 128) {
-                    const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part + s * D) + lane);
-                    acc[0] = fmaf(x.x, f, acc[0]); acc[1] = fmaf(x.y, f, acc[1]); acc[2] = fmaf(x.z, f, acc[2]); acc[3] = fmaf(x.w, f, acc[3]);
-                } else {
-                    const float2 x = __ldcg(reinterpret_cast<const float2*>(a.part + s * D) + lane);
-                    acc[0] = fmaf(x.x, f, acc[0]); acc[1] = fmaf(x.y, f, acc[1]);
+            if (r < rows) {
+                if (w) collect(u0, w, rows, c0, c1, plan.slot_of(ei, ru, h, 0) + r);
+                if (pt) {
+                    const int prow = ru * RU + r + ((e.tok0 - ge.tok0) << a.g_shift), pru = prow / RU, prows = plan.unit_rows(ge, pru);
+                    const int v0 = h * plan.head_w + plan.tscan[g] + pru * plan.unit_weight(pt, RU), vw = plan.unit_weight(pt, prows);
+                    collect(v0, vw, prows, v0 / chunk, (v0 + vw - 1) / chunk, plan.slot_of(g, pru, h, 0) + prow - pru * RU);
                 }
-            });
+            }
+            if (wpr > 1) {
+                __syncthreads();
+                if (lane == 0) join_stat[warp] = make_float2(m, l);
+#pragma unroll
+                for (int j = 0; j < VL; ++j) join[warp][lane * VL + j] = acc[j];
+                __syncthreads();
+                float mm = -INFINITY;
+                for (int k = 0; k < wpr; ++k) mm = fmaxf(mm, join_stat[warp - sub + k].x);
+                const float bs = mm == -INFINITY ? 0.f : mm;
+                l = 0.f;
+#pragma unroll
+                for (int j = 0; j < VL; ++j) acc[j] = 0.f;
+                for (int k = 0; k < wpr; ++k) {
+                    const float2 st = join_stat[warp - sub + k];
+                    const float f = exp2f(st.x - bs);
+                    l = fmaf(st.y, f, l);
+#pragma unroll
+                    for (int j = 0; j < VL; ++j) acc[j] = fmaf(join[warp - sub + k][lane * VL + j], f, acc[j]);
+                }
+            }
+            if (r >= rows || sub) continue;
             float inv = l == 0.f ? 0.f : 1.f / l;                    // l is NaN where a page was unusable
             if (bad) inv = NAN;
-            T* y = (T*)a.o.p + tok * a.o.ts + head * a.o.hs + lane * (D / 32);
+            const int row = ru * RU + r, tok = e.tok0 + (row >> a.g_shift), head = (h << a.g_shift) + (row & ((1 << a.g_shift) - 1));
+            T* y = (T*)a.o.p + tok * a.o.ts + head * a.o.hs + lane * VL;
             if constexpr (sizeof(T) == 4) {
-                if constexpr (D == 128) *reinterpret_cast<float4*>(y) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+                if constexpr (VL == 4) *reinterpret_cast<float4*>(y) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
                 else *reinterpret_cast<float2*>(y) = make_float2(acc[0] * inv, acc[1] * inv);
             } else {
 #pragma unroll
-                for (int j = 0; j < D / 64; ++j)
+                for (int j = 0; j < VL / 2; ++j)
                     reinterpret_cast<__nv_bfloat162*>(y)[j] = __floats2bfloat162_rn(acc[2 * j] * inv, acc[2 * j + 1] * inv);
             }
         }

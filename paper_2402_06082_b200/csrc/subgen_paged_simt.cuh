@@ -11,7 +11,7 @@
 
 namespace sgk {
 
-constexpr int kSimtKT = 64;
+constexpr int kSimtKT = 64, kSimtLead = 1;
 
 template <int D, int RU>
 struct SimtSmem {
@@ -28,12 +28,12 @@ __global__ void __launch_bounds__(NT) paged_attend_simt_kernel(PagedView P, Atte
     static_assert(RPT * TY == RU, "rows divide");
     extern __shared__ __align__(16) unsigned char dyn[];
     SimtSmem<D, RU>& sm = *reinterpret_cast<SimtSmem<D, RU>*>(dyn);
-    Plan<RU, KT, false> plan(P, a);
+    Plan<RU, KT, false, kSimtLead> plan(P, a);
     plan.build(dyn + ((sizeof(SimtSmem<D, RU>) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
     pdl_trigger();
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    long long x = (long long)blockIdx.x * plan.chunk;
-    const long long x1 = min(plan.total, x + plan.chunk);
+    int x = blockIdx.x * plan.chunk;
+    const int x1 = min(plan.total, x + plan.chunk);
     while (x < x1) {
         const Seg g = plan.next(x, x1, blockIdx.x);
         if (g.tile0 >= g.tile1) continue;
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(NT) paged_attend_simt_kernel(PagedView P, Atte
 #pragma unroll
             for (int e = 0; e < VE; ++e) f[e] = 0.f;
             if (r < g.rows) {
-                const int row = row0 + r, tok = g.e.tok0 + row / a.G, h = g.head * a.G + row % a.G;
+                const int row = row0 + r, tok = g.e.tok0 + (row >> a.g_shift), h = (g.head << a.g_shift) + (row & ((1 << a.g_shift) - 1));
                 Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>((const T*)a.q.p + tok * a.q.ts + h * a.q.hs) + piece), f);
             }
 #pragma unroll
@@ -168,11 +168,11 @@ __global__ void __launch_bounds__(NT) paged_attend_simt_kernel(PagedView P, Atte
                 f = l[i] == 0.f ? 0.f : 1.f / l[i];
                 y = nullptr;
             } else {
-                y = a.part + (g.slot + r) * D;
+                y = a.part + (long long)(g.slot + r) * D;
                 if (tx == 0) a.stat[g.slot + r] = make_float2(m[i], l[i]);
             }
             const int row = row0 + r;
-            T* o = (T*)a.o.p + (g.e.tok0 + row / a.G) * a.o.ts + (g.head * a.G + row % a.G) * a.o.hs;
+            T* o = (T*)a.o.p + (g.e.tok0 + (row >> a.g_shift)) * a.o.ts + ((g.head << a.g_shift) + (row & ((1 << a.g_shift) - 1))) * a.o.hs;
 #pragma unroll
             for (int b = 0; b < D / 64; ++b) {
                 const float4 v = make_float4(acc[i][b * 4] * f, acc[i][b * 4 + 1] * f, acc[i][b * 4 + 2] * f, acc[i][b * 4 + 3] * f);

@@ -1,16 +1,20 @@
 // Attention over a paged bf16 cache on the 5th-generation tensor cores.
 //
 // A block takes a run of key tiles (128 tokens) of one row unit (up to 256 query rows, see Plan) and is one pipeline
-// of ten warps around two score buffers in tensor memory:
-//   producer (warp 8)    walks the block's share of the plan, publishes the runs, and brings Q, K and V by TMA: one copy
-//                        per page and 64 columns into the 128-byte-swizzled layout the MMA reads; a ring of tiles
-//   issuer (warp 9)      S = Q K^T (M = 128 rows, N = 128 tokens), O += P V (P from tensor memory, V as it lies: tokens
+// of warps around two score buffers in tensor memory:
+//   planner (warp 11)    walks the block's share of the plan and publishes its runs
+//   producer (warp 8)    brings Q, K and V by TMA: one copy per page and 64 columns into the 128-byte-swizzled layout
+//                        the MMA reads; a ring of tiles
+//   issuers (warps 9-10) S = Q K^T (M = 128 rows, N = 128 tokens), O += P V (P from tensor memory, V as it lies: tokens
 //                        along K, columns contiguous), both tcgen05.mma bf16 -> fp32
 //   softmax (warps 0-3, 4-7)  one thread per row: read S, running maximum and sum, P in bf16 over S, finally O out
 // A job is one tile against 128 rows; job c uses score buffer, numerator and softmax group c & 1, and S of job c + 2 is
 // issued right after P V of job c, so the tensor cores work for one group while the other exponentiates. More than 128
 // rows: both halves of the unit take every tile in turn. Up to 128: the groups take alternate tiles of the same rows
-// and leave two partial results, so a single sequence's tiles overlap just as well.
+// and leave two partial results, so a single sequence's tiles overlap just as well. Up to 32 rows (single tokens, drafts):
+// Q lies in shared memory four times, so that every warp of a group has all rows in its lanes of tensor memory and
+// takes a quarter of the tile's tokens (the other quarters of its P are zero); the four numerators are added through
+// shared memory at the end of the run. The chain score -> weight -> product is then a quarter as long.
 // The numerator is rescaled only when a row's maximum has risen by more than 2^8 over the one in use (weights up to 256
 // are as exact in bf16, and the sum is fp32); S of job c comes after P V of job c - 2 in the issue order, so a group
 // that has S may change its numerator.
@@ -21,16 +25,18 @@
 #pragma once
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "subgen_paged.cuh"
 
 namespace sgk {
 
-constexpr int kPtThreads = 320, kPtRU = 256, kPtKT = 128, kPtRing = 4;
+constexpr int kPtThreads = 384, kPtRU = 256, kPtKT = 128, kPtRing = 8, kPtLead = 2;
 constexpr unsigned kPtSpins = 1u << 20;
 
 struct SegRec {
-    long long slot;
-    int tile0, tile1, kp, rows, head, ru, tok0, nq, S, P, direct, bad;   // tile1 < 0: no more
+    const int *ptab, *stab;
+    int slot, tile0, tile1, kp, rows, head, ru, tok0, nq, S, P, direct, bad;   // tile1 < 0: no more
 };
 
 template <int D>
@@ -38,8 +44,10 @@ struct PtSmem {                                       // after a 1024-byte align
     static constexpr int kTile = 128 * D * 2, kSlots = 131072 / kTile;
     unsigned char Q[2][kTile];                        // [64-column half][row][128 B swizzled]
     unsigned char KV[kSlots][kTile];                  // K, V, K, V, ...: [half][token][128 B swizzled]
+    float join[2][4][4][D];                           // [group][warp][row][column]: numerators of four rows to be added
+    float2 join_stat[2][4][32];                       // maximum in use, sum
     SegRec seg[kPtRing];
-    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2],
+    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2],
         seg_full[kPtRing], seg_empty[kPtRing], drain;
     unsigned tmem;
     int failed, flag;
@@ -61,13 +69,14 @@ __device__ __forceinline__ bool bar_try(unsigned long long* b, unsigned parity) 
                  : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
     return ok != 0;
 }
-// Bounded; false (and *failed set) when it gives up or another warp has.
+// By a whole warp, with one answer for all lanes. Bounded; false (and *failed set) when it gives up or another warp has.
 __device__ __forceinline__ bool bar_wait(unsigned long long* b, unsigned parity, int* failed) {
-    if (bar_try(b, parity)) return true;
-    for (unsigned i = 0; i < kPtSpins; ++i) {
-        if (bar_try(b, parity)) return true;
-        if ((i & 15) == 15 && *reinterpret_cast<volatile int*>(failed)) return false;
+    bool done = bar_try(b, parity);
+    for (unsigned i = 0; i < kPtSpins && !done; ++i) {
+        done = bar_try(b, parity);
+        if ((i & 15) == 15 && *reinterpret_cast<volatile int*>(failed)) break;
     }
+    if (__all_sync(0xffffffffu, done)) return true;
     *reinterpret_cast<volatile int*>(failed) = 1;
     return false;
 }
@@ -111,6 +120,35 @@ __device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* v) {
                  "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};\n"
                  ::"r"(addr), SGK_I8(v, 0), SGK_I8(v, 8), SGK_I8(v, 16), SGK_I8(v, 24) : "memory");
 }
+__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n"
+                 ::"r"(addr), SGK_I8(v, 0), SGK_I8(v, 8) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}\n"
+        : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}\n"
+        : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+    return r;
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2_approx(float x) {
@@ -130,13 +168,13 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
     extern __shared__ unsigned char dyn_raw[];
     unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~(uintptr_t)1023);
     Smem& sm = *reinterpret_cast<Smem*>(base);
-    typedef Plan<kPtRU, kPtKT, true> PlanT;
+    typedef Plan<kPtRU, kPtKT, true, kPtLead> PlanT;
     PlanT plan(P, a);
     plan.build(base + ((sizeof(Smem) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
     pdl_trigger();
-    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-    long long x = (long long)blockIdx.x * plan.chunk;
-    const long long x1 = min(plan.total, x + plan.chunk);
+    const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
+    int x = blockIdx.x * plan.chunk;
+    const int x1 = min(plan.total, x + plan.chunk);
     if (x >= x1) return;
 
     if (warp == 9) {
@@ -145,142 +183,182 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
     }
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            bar_init(&sm.q_full[i], 1); bar_init(&sm.q_empty[i], 1);
+            bar_init(&sm.q_full[i], 1); bar_init(&sm.q_empty[i], 2);
             bar_init(&sm.s_full[i], 1); bar_init(&sm.p_full[i], 4);
             bar_init(&sm.o_full[i], 1); bar_init(&sm.o_empty[i], 4);
+            bar_init(&sm.join_bar[i], 4);
         }
-        for (int i = 0; i < NS; ++i) { bar_init(&sm.kv_full[i], 1); bar_init(&sm.kv_empty[i], 1); }
-        for (int i = 0; i < kPtRing; ++i) { bar_init(&sm.seg_full[i], 1); bar_init(&sm.seg_empty[i], 9); }
-        bar_init(&sm.drain, 1);
+        for (int i = 0; i < NS; ++i) { bar_init(&sm.kv_full[i], 1); bar_init(&sm.kv_empty[i], 2); }
+        for (int i = 0; i < kPtRing; ++i) { bar_init(&sm.seg_full[i], 1); bar_init(&sm.seg_empty[i], 11); }
+        bar_init(&sm.drain, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sm.failed = 0;
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sm.tmem;
+    const uint32_t tmem = (uint32_t)uniform((int)sm.tmem);
 
-    if (warp == 8) {
-        // ---- producer ----
-        unsigned ns = 0, nq = 0, nk = 0;              // runs, query tiles and ring tiles so far
-        const int pb = min(1 << P.page_shift, 128), chunks = 128 / pb;   // tokens one copy brings; copies for a half tile
-        bool ok = true;
-        while (ok) {
-            SegRec r;
-            const int* ptab = nullptr;
-            const int* stab = nullptr;
-            r.tile1 = -1;
-            while (x < x1) {
-                const Seg g = plan.next(x, x1, blockIdx.x);
-                if (g.tile0 >= g.tile1) continue;
-                r = SegRec{g.slot, g.tile0, g.tile1, g.kp, g.rows, g.head, g.ru, g.e.tok0, g.e.nq, g.e.S, g.e.P, g.direct, g.e.bad};
-                ptab = g.e.ptab;
-                stab = g.e.stab;
-                break;
-            }
-            const int slot = ns % kPtRing;
-            if (ns >= kPtRing && !(ok = bar_wait(&sm.seg_empty[slot], (ns / kPtRing - 1) & 1, &sm.failed))) break;
-            if (lane == 0) {
-                sm.seg[slot] = r;
-                bar_arrive(&sm.seg_full[slot]);
-            }
-            ++ns;
-            if (r.tile1 < 0) break;
-            const int sub = r.rows > 128 ? 2 : 1;
-            for (int i = 0; i < sub && ok; ++i, ++nq) {
-                const int qs = nq & 1;
-                if (nq >= 2 && !(ok = bar_wait(&sm.q_empty[qs], (nq / 2 - 1) & 1, &sm.failed))) break;
+    // registers: three groups of four warps were launched with 168 a thread; 2 x 208 + 88 = 3 x 168
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == 11) {
+            // ---- planner ----
+            unsigned ns = 0;
+            while (true) {
+                SegRec r;
+                r.tile1 = -1;
+                while (x < x1) {
+                    const Seg g = plan.next(x, x1, blockIdx.x);
+                    if (g.tile0 >= g.tile1) continue;
+                    r = SegRec{g.e.ptab, g.e.stab, g.slot, g.tile0, g.tile1, g.kp, g.rows, g.head, g.ru, g.e.tok0, g.e.nq, g.e.S, g.e.P, g.direct, g.e.bad};
+                    break;
+                }
+                const int slot = ns % kPtRing;
+                if (ns >= kPtRing && !bar_wait(&sm.seg_empty[slot], (ns / kPtRing - 1) & 1, &sm.failed)) break;
                 if (lane == 0) {
-                    bar_expect(&sm.q_full[qs], Smem::kTile);
-                    for (int h = 0; h < HALVES; ++h)
-                        tma_load_3d(sm.Q[qs] + h * 16384, &mq, h * 64, r.head * a.G, r.tok0 + (r.ru * kPtRU + i * 128) / a.G, &sm.q_full[qs]);
+                    sm.seg[slot] = r;
+                    bar_arrive(&sm.seg_full[slot]);
                 }
+                __syncwarp();
+                ++ns;
+                if (r.tile1 < 0) break;
             }
-            for (int t = r.tile0; t < r.tile1 && ok; ++t) {
-                const bool pre = t < r.kp;
-                const int first = (pre ? t : t - r.kp) * kPtKT, limit = pre ? r.P : r.S;
-                // lane: chunk = lane / HALVES, half = lane % HALVES
-                const int chunk = lane / HALVES, half = lane % HALVES, pos = first + chunk * pb;
-                bool mine = chunk < chunks && pos < limit;
-                int id = 0;
-                if (mine) {
-                    id = __ldg((pre ? ptab : stab) + (pos >> P.page_shift));
-                    if (id < 0 || id >= P.pages) { mine = false; id = -1; }
-                }
-                if (__any_sync(0xffffffffu, id < 0) && lane == 0) {
-                    *reinterpret_cast<volatile int*>(&sm.seg[slot].bad) = 1;
-                    paged_status(P, kStPage);
-                }
-                const unsigned bytes = __popc(__ballot_sync(0xffffffffu, mine)) * (unsigned)pb * 128u;
-                for (int kv = 0; kv < 2; ++kv, ++nk) {
-                    const int s = nk % NS;
-                    if (nk >= NS && !(ok = bar_wait(&sm.kv_empty[s], (nk / NS - 1) & 1, &sm.failed))) break;
-                    if (lane == 0) bar_expect(&sm.kv_full[s], bytes);
+        } else if (warp == 8) {
+            // ---- producer ----
+            unsigned ns = 0, nq = 0, nk = 0;          // runs, query tiles and ring tiles so far
+            const int pb = min(1 << P.page_shift, 128), chunks = 128 / pb;   // tokens one copy brings; copies for a half tile
+            const int chunk = lane / HALVES, half = lane % HALVES;           // this lane's copy of a tile
+            bool ok = true;
+            while (ok) {
+                const int slot = ns % kPtRing;
+                if (!(ok = bar_wait(&sm.seg_full[slot], (ns / kPtRing) & 1, &sm.failed))) break;
+                SegRec& r = sm.seg[slot];
+                const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, head = r.head, P_ = r.P, S_ = r.S;
+                const int *ptab = r.ptab, *stab = r.stab;
+                if (tile1 < 0) break;
+                // the page of this lane's copy of tile t: -2 nothing to bring, -1 outside the pool
+                auto page_of = [&](int t) {
+                    const bool pre = t < kp;
+                    const int pos = (pre ? t : t - kp) * kPtKT + chunk * pb;
+                    if (t >= tile1 || chunk >= chunks || pos >= (pre ? P_ : S_)) return -2;
+                    const int id = __ldg((pre ? ptab : stab) + (pos >> P.page_shift));
+                    return id < 0 || id >= P.pages ? -1 : id;
+                };
+                int id = page_of(tile0);
+                const int sub = r.rows > 128 ? 2 : 1;
+                for (int i = 0; i < sub && ok; ++i, ++nq) {
+                    const int qs = nq & 1;
+                    if (nq >= 2 && !(ok = bar_wait(&sm.q_empty[qs], (nq / 2 - 1) & 1, &sm.failed))) break;
+                    if (lane == 0) bar_expect(&sm.q_full[qs], Smem::kTile);
                     __syncwarp();
-                    if (mine)
-                        tma_load_4d(sm.KV[s] + half * 16384 + chunk * pb * 128, kv ? &mv : &mk, half * 64, pos & ((1 << P.page_shift) - 1),
-                                    r.head, id, &sm.kv_full[s]);
+                    if (lane < 4 * HALVES) {           // 32 rows at a time, or the same 32 four times
+                        const int step = r.rows > 32 ? 32 >> a.g_shift : 0, tok = r.tok0 + ((r.ru * kPtRU + i * 128) >> a.g_shift);
+                        tma_load_3d(sm.Q[qs] + (lane >> 2) * 16384 + (lane & 3) * 4096, &mq, (lane >> 2) * 64, head << a.g_shift,
+                                    tok + (lane & 3) * step, &sm.q_full[qs]);
+                    }
                 }
+                for (int t = tile0; t < tile1 && ok; ++t) {
+                    const int following = page_of(t + 1);        // asked for a tile early
+                    const int row = ((t < kp ? t : t - kp) * kPtKT + chunk * pb) & ((1 << P.page_shift) - 1);
+                    if (__any_sync(0xffffffffu, id == -1) && lane == 0) {
+                        *reinterpret_cast<volatile int*>(&r.bad) = 1;
+                        paged_status(P, kStPage);
+                    }
+                    const unsigned bytes = __popc(__ballot_sync(0xffffffffu, id >= 0)) * (unsigned)pb * 128u;
+                    for (int kv = 0; kv < 2; ++kv, ++nk) {
+                        const int s = nk % NS;
+                        if (nk >= NS && !(ok = bar_wait(&sm.kv_empty[s], (nk / NS - 1) & 1, &sm.failed))) break;
+                        if (lane == 0) bar_expect(&sm.kv_full[s], bytes);
+                        __syncwarp();
+                        if (id >= 0) tma_load_4d(sm.KV[s] + half * 16384 + chunk * pb * 128, kv ? &mv : &mk, half * 64, row, head, id, &sm.kv_full[s]);
+                    }
+                    id = following;
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sm.seg_empty[slot]);
+                ++ns;
             }
-        }
-        // copies in flight write shared memory: they have to be done before the block ends
-        for (unsigned i = nk > (unsigned)NS ? nk - NS : 0; i < nk; ++i)
-            for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.kv_full[i % NS], (i / NS) & 1); ++j) {}
-        for (unsigned i = nq > 2 ? nq - 2 : 0; i < nq; ++i)
-            for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.q_full[i & 1], (i / 2) & 1); ++j) {}
-    } else if (warp == 9) {
-        // ---- issuer ----
-        struct Cursor { int tile, tile0, tile1, kp, dual, sub, P, S; unsigned seg, q, kv; bool done; };
-        auto enter = [&](Cursor& c) {                  // the run that c.seg counts to
-            const int slot = c.seg % kPtRing;
-            if (!bar_wait(&sm.seg_full[slot], (c.seg / kPtRing) & 1, &sm.failed)) { c.done = true; return; }
-            const SegRec& r = sm.seg[slot];
-            c.tile = c.tile0 = r.tile0; c.tile1 = r.tile1; c.kp = r.kp; c.dual = r.rows > 128; c.sub = 0; c.P = r.P; c.S = r.S;
-            c.done = r.tile1 < 0;
-        };
-        Cursor qk = {0, 0, 0, 0, 0, 0, 0, 0, 0u, 0u, 0u, false}, pv = qk;
-        unsigned jobs_qk = 0, jobs_pv = 0, segs[2] = {0u, 0u};        // segs: runs whose numerator each group has begun
-        bool ok = true;
-        auto issue_qk = [&]() {
-            if (qk.done || !ok) return;
-            const unsigned w = jobs_qk & 1, qt = qk.q + qk.sub, ks = 2 * qk.kv, s = ks % NS;
-            if (qk.tile == qk.tile0 && !(ok = bar_wait(&sm.q_full[qt & 1], (qt / 2) & 1, &sm.failed))) return;
-            if (!(ok = bar_wait(&sm.kv_full[s], (ks / NS) & 1, &sm.failed))) return;
-            const bool last_sub = qk.sub == qk.dual;
-            if (lane == 0) {
-                tc_fence_after();
+            // copies in flight write shared memory: they have to be done before the block ends
+            for (unsigned i = nk > (unsigned)NS ? nk - NS : 0; i < nk; ++i)
+                for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.kv_full[i % NS], (i / NS) & 1); ++j) {}
+            for (unsigned i = nq > 2 ? nq - 2 : 0; i < nq; ++i)
+                for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.q_full[i & 1], (i / 2) & 1); ++j) {}
+        } else {
+            // ---- issuers ----
+            // Everything here is the same in all lanes, and said so by shuffles and votes: an MMA's operands have to be
+            // in uniform registers, and with operands that the compiler takes for divergent each MMA costs some 90 cycles
+            // instead of 64 (128 x 128 x 16). One warp per group, so that a wait of one leaves no gap in the tensor pipe.
+            const int w = warp - 9;
+            struct Cursor { int tile, tile0, tile1, kp, dual, order, rows, P, S, seg, q, kv, jobs, done; };
+            bool ok = true;
+            auto wait = [&](unsigned long long* b, int parity) { return bar_wait(b, (unsigned)parity, &sm.failed); };
+            // The first run from c.seg on in which this group has a job. `release`: give up those in which it has none.
+            auto enter = [&](Cursor& c, bool release) {
+                while (true) {
+                    const int slot = c.seg % kPtRing;
+                    if (!(ok = wait(&sm.seg_full[slot], (c.seg / kPtRing) & 1))) { c.done = 1; return; }
+                    const SegRec& r = sm.seg[slot];
+                    c.tile0 = uniform(r.tile0); c.tile1 = uniform(r.tile1); c.kp = uniform(r.kp);
+                    c.rows = uniform(r.rows); c.P = uniform(r.P); c.S = uniform(r.S);
+                    c.dual = c.rows > 128 ? 1 : 0;
+                    c.order = (w - c.jobs) & 1;
+                    c.done = c.tile1 < 0 ? 1 : 0;
+                    c.tile = c.tile0 + (c.dual ? 0 : c.order);
+                    if (c.done || c.tile < c.tile1) return;
+                    // one tile, and the other group's: the query tile counts both groups all the same (once it is there,
+                    // or the arrival would count for the tile that had its place before)
+                    if (!release && !(ok = wait(&sm.q_full[c.q & 1], (c.q / 2) & 1))) { c.done = 1; return; }
+                    if (lane == 0) bar_arrive(release ? &sm.seg_empty[slot] : &sm.q_empty[c.q & 1]);
+                    __syncwarp();
+                    ++c.seg; ++c.q; ++c.kv; ++c.jobs;
+                }
+            };
+            auto leave = [&](Cursor& c) {
+                const int tiles = c.tile1 - c.tile0;
+                c.q += 1 + c.dual;
+                c.kv += tiles;
+                c.jobs += tiles << c.dual;
+                ++c.seg;
+            };
+            Cursor qk = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}, pv = qk;
+            int segs = 0, mine = 0;                    // runs whose numerator the group has begun, products with V
+            auto issue_qk = [&]() {
+                if (qk.done || !ok) return;
+                const int qt = qk.q + (qk.dual ? qk.order : 0), ks = 2 * (qk.kv + qk.tile - qk.tile0), s = ks % NS, step = 2 - qk.dual;
+                if (qk.tile < qk.tile0 + 2 && !(ok = wait(&sm.q_full[qt & 1], (qt / 2) & 1))) return;
+                if (!(ok = wait(&sm.kv_full[s], (ks / NS) & 1))) return;
+                const bool last = qk.tile + step >= qk.tile1;
                 const uint32_t qa = smem_u32(sm.Q[qt & 1]), ka = smem_u32(sm.KV[s]);
+                tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t off = (uint32_t)((i >> 2) * 16384 + (i & 3) * 32);
-                    tc_mma_ss(tmem + w * 128u, tc_desc(qa + off, 16), tc_desc(ka + off, 16), kIdescS, i ? 1u : 0u);
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = (uint32_t)((i >> 2) * 16384 + (i & 3) * 32);
+                        tc_mma_ss(tmem + w * 128u, tc_desc(qa + off, 16), tc_desc(ka + off, 16), kIdescS, i ? 1u : 0u);
+                    }
+                    tc_commit(&sm.s_full[w]);
+                    tc_commit(&sm.kv_empty[s]);        // a slot counts two: both groups', or this one's twice
+                    if (!qk.dual) tc_commit(&sm.kv_empty[s]);
+                    if (last) {
+                        tc_commit(&sm.q_empty[qt & 1]);
+                        if (qk.dual) tc_commit(&sm.q_empty[qt & 1]);
+                    }
                 }
-                tc_commit(&sm.s_full[w]);
-                if (last_sub) tc_commit(&sm.kv_empty[s]);
-                if (qk.tile == qk.tile1 - 1) tc_commit(&sm.q_empty[qt & 1]);
-            }
-            __syncwarp();
-            ++jobs_qk;
-            if (!last_sub) { qk.sub = 1; return; }
-            qk.sub = 0;
-            ++qk.kv;
-            if (++qk.tile == qk.tile1) {
-                qk.q += 1 + qk.dual;
-                ++qk.seg;
-                enter(qk);
-            }
-        };
-        enter(qk);
-        enter(pv);
-        issue_qk();
-        issue_qk();
-        while (!pv.done && ok) {
-            const unsigned w = jobs_pv & 1, vs = 2 * pv.kv + 1, s = vs % NS;
-            const int i = pv.tile - pv.tile0;
-            const bool fresh = pv.dual ? i == 0 : i < 2, last_sub = pv.sub == pv.dual;
-            const bool final = pv.dual ? pv.tile == pv.tile1 - 1 : pv.tile >= pv.tile1 - 2;
-            if (!(ok = bar_wait(&sm.kv_full[s], (vs / NS) & 1, &sm.failed))) break;
-            if (pv.sub == 0) {
+                __syncwarp();
+                qk.tile += step;
+                if (last) {
+                    leave(qk);
+                    enter(qk, false);
+                }
+            };
+            enter(qk, false);
+            enter(pv, true);
+            issue_qk();
+            while (!pv.done && ok) {
+                const int vs = 2 * (pv.kv + pv.tile - pv.tile0) + 1, s = vs % NS, step = 2 - pv.dual;
+                const bool fresh = pv.tile < pv.tile0 + step, last = pv.tile + step >= pv.tile1;
+                if (!(ok = wait(&sm.kv_full[s], (vs / NS) & 1))) break;
                 const bool pre = pv.tile < pv.kp;
                 const int nv = pre ? pv.P - pv.tile * kPtKT : pv.S - (pv.tile - pv.kp) * kPtKT;
                 if (nv < kPtKT) {                      // the sequence ends in this tile: clear what lies behind
@@ -291,44 +369,105 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-            }
-            if (!(ok = bar_wait(&sm.p_full[w], (jobs_pv / 2) & 1, &sm.failed))) break;
-            if (fresh) {
-                if (segs[w] && !(ok = bar_wait(&sm.o_empty[w], (segs[w] - 1) & 1, &sm.failed))) break;
-                ++segs[w];
-            }
-            if (lane == 0) {
-                tc_fence_after();
-                const uint32_t va = smem_u32(sm.KV[s]);
-#pragma unroll
-                for (int k = 0; k < kPtKT / 16; ++k)
-                    tc_mma_ts(tmem + 256u + w * (uint32_t)D, tmem + w * 128u + k * 8u, tc_desc(va + k * 2048u, 16384), kIdescO, fresh && !k ? 0u : 1u);
-                if (last_sub) tc_commit(&sm.kv_empty[s]);
-                if (final) tc_commit(&sm.o_full[w]);
-            }
-            __syncwarp();
-            ++jobs_pv;
-            if (!last_sub) pv.sub = 1;
-            else {
-                pv.sub = 0;
-                ++pv.kv;
-                if (++pv.tile == pv.tile1) {
-                    if (lane == 0) bar_arrive(&sm.seg_empty[pv.seg % kPtRing]);
-                    ++pv.seg;
-                    enter(pv);
+                if (fresh) {
+                    if (segs && !(ok = wait(&sm.o_empty[w], (segs - 1) & 1))) break;
+                    ++segs;
                 }
+                if (!(ok = wait(&sm.p_full[w], mine & 1))) break;
+                const uint32_t va = smem_u32(sm.KV[s]);
+                const uint32_t first = fresh ? 0u : 1u;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kPtKT / 16; ++k)
+                        tc_mma_ts(tmem + 256u + w * (uint32_t)D, tmem + w * 128u + k * 8u, tc_desc(va + k * 2048u, 16384), kIdescO, k ? 1u : first);
+                    tc_commit(&sm.kv_empty[s]);
+                    if (!pv.dual) tc_commit(&sm.kv_empty[s]);
+                    if (last) tc_commit(&sm.o_full[w]);
+                }
+                __syncwarp();
+                ++mine;
+                pv.tile += step;
+                if (last) {
+                    if (lane == 0) bar_arrive(&sm.seg_empty[pv.seg % kPtRing]);
+                    __syncwarp();
+                    leave(pv);
+                }
+                issue_qk();
+                if (last) enter(pv, true);
             }
-            issue_qk();
+            if (elect_one()) tc_commit(&sm.drain);    // the MMAs read shared memory: done before the block ends
+            __syncwarp();
+            for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.drain, 0); ++j) {}
         }
-        if (lane == 0) tc_commit(&sm.drain);          // the MMAs read shared memory: done before the block ends
-        for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.drain, 0); ++j) {}
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ---- softmax ----
-        const int w = warp >> 2, row128 = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const int w = warp >> 2, quarter = warp & 3;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t tS = tmem + lanes + (uint32_t)w * 128u, tO = tmem + lanes + 256u + (uint32_t)(w * D);
         unsigned ns = 0, job = 0, mine = 0, segs = 0;  // runs, jobs of both groups, jobs and runs of this one
         bool ok = true;
+        float m = 0.f, l = 0.f;                                // of this thread's row: the maximum in use, the sum
+        bool begun = false;
+        unsigned joins = 0;
+        auto joined = [&]() {                          // the group's four warps have come here
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sm.join_bar[w]);
+            return ok = bar_wait(&sm.join_bar[w], joins++ & 1, &sm.failed);
+        };
+        // A new maximum of the row: keep the one in use, or change to the new one and rescale.
+        auto raise = [&](float top) {
+            const bool rise = (top - m) * a.c > 8.f || (m == -INFINITY && top > m);
+            if (__any_sync(0xffffffffu, rise)) {
+                const float f = rise ? ex2_approx((m - top) * a.c) : 1.f;              // 0 when there was no maximum yet
+                if (rise) m = top;
+                l *= f;
+                if (begun) {
+                    uint32_t o[32];
+#pragma unroll 1
+                    for (int i = 0; i < D / 32; ++i) {
+                        tc_ld32(tO + i * 32, o);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                        tc_st32(tO + i * 32, o);
+                    }
+                    tc_wait_st();
+                }
+            }
+        };
+        // N scores of the row -> bf16 weights, two to a register; adds them to the sum
+        auto weigh = [&](auto count, const uint32_t* s, uint32_t* p) {
+            constexpr int N = decltype(count)::value;
+            const float off = m == -INFINITY ? 0.f : -m * a.c;
+            const float2 cc = make_float2(a.c, a.c), oo = make_float2(off, off);
+            float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+                float2 x = fma2(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), cc, oo);
+                float2 y = fma2(make_float2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), cc, oo);
+                x = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                y = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+                l0 = add2(l0, x);
+                l1 = add2(l1, y);
+                const __nv_bfloat162 bx = __float22bfloat162_rn(x), by = __float22bfloat162_rn(y);
+                p[i / 2] = *reinterpret_cast<const uint32_t*>(&bx);
+                p[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&by);
+            }
+            l0 = add2(l0, l1);
+            l += l0.x + l0.y;
+        };
+        auto largest = [&](auto count, const uint32_t* s) {
+            constexpr int N = decltype(count)::value;
+            float t[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < N; i += 8) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t[j] = max3(t[j], __uint_as_float(s[i + 2 * j]), __uint_as_float(s[i + 2 * j + 1]));
+            }
+            return fmaxf(max3(t[0], t[1], t[2]), t[3]);
+        };
         while (ok) {
             const int slot = ns % kPtRing;
             if (!(ok = bar_wait(&sm.seg_full[slot], (ns / kPtRing) & 1, &sm.failed))) break;
@@ -336,70 +475,54 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, rows = r.rows;
             if (tile1 < 0) break;
             const int dual = rows > 128, tiles = tile1 - tile0, order = (w - (int)job) & 1;   // order: this group's half, or turn
-            const int row = dual ? order * 128 + row128 : row128;
-            const bool live = row < rows, some = (row & ~31) < rows;
-            const int urow = r.ru * kPtRU + row;
+            const bool quad = rows <= 32;
+            const int row = quad ? lane : (dual ? order * 128 : 0) + quarter * 32 + lane;
+            const bool live = row < rows, some = quad || (row & ~31) < rows;
+            const int urow = r.ru * kPtRU + row, P_ = r.P;
             Entry e;
             e.S = r.S; e.nq = r.nq;
             const int own = plan.own_limit(e, urow);
-            float m = -INFINITY, l = 0.f;              // m: the maximum in use
-            bool begun = false;
+            m = -INFINITY;
+            l = 0.f;
+            begun = false;
             for (int t = tile0 + (dual ? 0 : order); t < tile1; t += 2 - dual) {
                 if (!(ok = bar_wait(&sm.s_full[w], mine & 1, &sm.failed))) break;
-                if (some) {
+                const bool pre = t < kp;
+                const int lim = pre ? P_ - t * kPtKT : own - (t - kp) * kPtKT;        // tokens of the tile that the row sees
+                if (quad) {
                     tc_fence_after();
-                    uint32_t raw[128];
-                    float s[128];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) tc_ld32(tS + i * 32, raw + i * 32);
+                    uint32_t s[32], p[16];
+                    tc_ld32(tS + quarter * 32, s);
                     tc_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 128; ++i) s[i] = __uint_as_float(raw[i]);
-                    const bool pre = t < kp;
-                    const int lim = pre ? r.P - t * kPtKT : own - (t - kp) * kPtKT;
                     if (__any_sync(0xffffffffu, lim < kPtKT)) {
 #pragma unroll
-                        for (int i = 0; i < 128; ++i) s[i] = i < lim ? s[i] : -INFINITY;
+                        for (int i = 0; i < 32; ++i) s[i] = quarter * 32 + i < lim ? s[i] : 0xff800000u;
                     }
-                    float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
+                    raise(largest(std::integral_constant<int, 32>(), s));
+                    weigh(std::integral_constant<int, 32>(), s, p);
 #pragma unroll
-                    for (int i = 4; i < 128; i += 4) {
-                        m0 = fmaxf(m0, s[i]); m1 = fmaxf(m1, s[i + 1]); m2 = fmaxf(m2, s[i + 2]); m3 = fmaxf(m3, s[i + 3]);
+                    for (int i = 0; i < 16; ++i) s[i] = 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (j == quarter) tc_st16(tS + j * 16, p);
+                        else tc_st16(tS + j * 16, s);
                     }
-                    const float top = fmaxf(m, fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)));
-                    const bool rise = (top - m) * a.c > 8.f || (m == -INFINITY && top > m);
-                    if (__any_sync(0xffffffffu, rise)) {
-                        const float f = rise ? ex2_approx((m - top) * a.c) : 1.f;      // 0 when there was no maximum yet
-                        if (rise) m = top;
-                        l *= f;
-                        if (begun) {
-                            uint32_t o[32];
+                    tc_wait_st();
+                    tc_fence_before();
+                } else if (some) {
+                    tc_fence_after();
+                    uint32_t s[128];
 #pragma unroll
-                            for (int i = 0; i < D / 32; ++i) {
-                                tc_ld32(tO + i * 32, o);
-                                tc_wait_ld();
+                    for (int i = 0; i < 4; ++i) tc_ld32(tS + i * 32, s + i * 32);
+                    tc_wait_ld();
+                    if (__any_sync(0xffffffffu, lim < kPtKT)) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                tc_st32(tO + i * 32, o);
-                            }
-                            tc_wait_st();
-                        }
+                        for (int i = 0; i < 128; ++i) s[i] = i < lim ? s[i] : 0xff800000u;
                     }
-                    const float off = m == -INFINITY ? 0.f : -m * a.c;
-                    float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
-                    uint32_t p[64];
-#pragma unroll
-                    for (int i = 0; i < 128; i += 4) {
-                        const float p0 = ex2_approx(fmaf(s[i], a.c, off)), p1 = ex2_approx(fmaf(s[i + 1], a.c, off));
-                        const float p2 = ex2_approx(fmaf(s[i + 2], a.c, off)), p3 = ex2_approx(fmaf(s[i + 3], a.c, off));
-                        l0 += p0; l1 += p1; l2 += p2; l3 += p3;
-                        const __nv_bfloat162 a0 = __floats2bfloat162_rn(p0, p1), a1 = __floats2bfloat162_rn(p2, p3);
-                        p[i / 2] = *reinterpret_cast<const uint32_t*>(&a0);
-                        p[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&a1);
-                    }
-                    l += (l0 + l1) + (l2 + l3);
-                    tc_st32(tS, p);
-                    tc_st32(tS + 32, p + 32);
+                    raise(largest(std::integral_constant<int, 128>(), s));
+                    weigh(std::integral_constant<int, 128>(), s, s);                   // in place: a pair goes to half its index
+                    tc_st32(tS, s);
+                    tc_st32(tS + 32, s + 32);
                     tc_wait_st();
                     tc_fence_before();
                 }
@@ -414,18 +537,72 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             if (begun) {
                 if (!(ok = bar_wait(&sm.o_full[w], segs & 1, &sm.failed))) break;
                 ++segs;
-                if (some) {
+                const int gs = a.g_shift, bad = *reinterpret_cast<const volatile int*>(&r.bad);
+                const bool direct = r.direct;
+                const int slot0 = r.slot + (dual || order == 0 ? 0 : rows);
+                if (quad) {
+                    // the four warps' numerators, four rows at a time: [warp][row][column] in shared memory, added by one
+                    // thread for four columns
                     tc_fence_after();
-                    if (*reinterpret_cast<const volatile int*>(&r.bad)) l = NAN;
-                    const int G = a.G, tok = r.tok0 + urow / G, head = r.head * G + urow % G;
-                    const long long at = r.slot + (dual || order == 0 ? row : rows + row);
-                    const bool direct = r.direct;
-                    const float f = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-                    uint32_t o[32];
-                    __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
-                    if (live && !direct) a.stat[at] = make_float2(m * a.c, l);
+                    sm.join_stat[w][quarter][lane] = make_float2(m, l);
+                    for (int r0 = 0; r0 < rows; r0 += 4) {
+#pragma unroll 1
+                        for (int i = 0; i < D / 32; ++i) {
+                            uint32_t o[32];
+                            __syncwarp();
+                            tc_ld32(tO + i * 32, o);
+                            tc_wait_ld();
+                            if (lane >= r0 && lane < r0 + 4) {
+                                uint4* z = reinterpret_cast<uint4*>(&sm.join[w][quarter][lane - r0][i * 32]);
 #pragma unroll
+                                for (int j = 0; j < 8; ++j) z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                            }
+                        }
+                        if (!joined()) break;
+                        const int rr = r0 + quarter;             // a warp per row
+                        if (rr < rows) {
+                            float2 st[4];
+                            float M = -INFINITY, L = 0.f;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) { st[k] = sm.join_stat[w][k][rr]; M = fmaxf(M, st[k].x); }
+                            const float base = M == -INFINITY ? 0.f : M;
+                            float z[D / 32];
+#pragma unroll
+                            for (int j = 0; j < D / 32; ++j) z[j] = 0.f;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const float f = ex2_approx((st[k].x - base) * a.c);
+                                L = fmaf(st[k].y, f, L);
+#pragma unroll
+                                for (int j = 0; j < D / 32; ++j) z[j] = fmaf(sm.join[w][k][quarter][j * 32 + lane], f, z[j]);
+                            }
+                            if (bad) L = NAN;
+                            const int gr = r.ru * kPtRU + rr, tok = r.tok0 + (gr >> gs), head = (r.head << gs) + (gr & ((1 << gs) - 1));
+                            if (direct) {
+                                const float f = L == 0.f ? 0.f : 1.f / L;
+                                __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
+#pragma unroll
+                                for (int j = 0; j < D / 32; ++j) y[j * 32 + lane] = __float2bfloat16_rn(z[j] * f);
+                            } else {
+                                float* y = a.part + (long long)(slot0 + rr) * D;
+#pragma unroll
+                                for (int j = 0; j < D / 32; ++j) y[j * 32 + lane] = z[j];
+                                if (lane == 0) a.stat[slot0 + rr] = make_float2(M * a.c, L);
+                            }
+                        }
+                        if (!joined()) break;
+                    }
+                    tc_fence_before();
+                } else if (some) {
+                    tc_fence_after();
+                    if (bad) l = NAN;
+                    const int tok = r.tok0 + (urow >> gs), head = (r.head << gs) + (urow & ((1 << gs) - 1));
+                    const float f = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+                    __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
+                    if (live && !direct) a.stat[slot0 + row] = make_float2(m * a.c, l);
+#pragma unroll 1
                     for (int i = 0; i < D / 32; ++i) {
+                        uint32_t o[32];
                         __syncwarp();
                         tc_ld32(tO + i * 32, o);
                         tc_wait_ld();
@@ -442,7 +619,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                                 *reinterpret_cast<uint4*>(y + i * 32 + j) = v;
                             }
                         } else if (live) {
-                            uint4* z = reinterpret_cast<uint4*>(a.part + at * D + i * 32);
+                            uint4* z = reinterpret_cast<uint4*>(a.part + (long long)(slot0 + row) * D + i * 32);
 #pragma unroll
                             for (int j = 0; j < 8; ++j) z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
                         }

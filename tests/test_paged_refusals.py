@@ -50,7 +50,7 @@ def test_pools(call, kw, word):
 
 @pytest.mark.parametrize("call", [_attend, _append])
 @pytest.mark.parametrize("kw, word", [
-    (dict(B=-1), "B and groups"), (dict(B=2048, groups=1), "at most 2048"), (dict(cu_q=None), "cu_q"), (dict(table_stride=0), "table_stride"),
+    (dict(B=-1), "B and groups"), (dict(B=1024, groups=1), "at most 1024"), (dict(cu_q=None), "cu_q"), (dict(table_stride=0), "table_stride"),
     (dict(table_stride=1 << 27), "2^31"), (dict(groups=1), "cu_group"),
     (dict(groups=1, cu_group=P, prefix_len=P, prefix_table=P, prefix_stride=0), "prefix_stride")])
 def test_batches(call, kw, word):
