@@ -143,9 +143,9 @@ template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
 int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
-    // a block per row unit of a sequence and KV head, as far as the grid goes
-    const long long units = ((long long)P.B + ((long long)a.n << a.g_shift) / RU) * P.Hkv;
-    cfg.gridDim = dim3((unsigned)(units < kSMs * 8 ? units : kSMs * 8));
+    // a block per 32 rows, as far as the grid goes
+    const long long units = ((long long)P.B + ((long long)a.n << a.g_shift) / (RU < 32 ? RU : 32)) * P.Hkv;
+    cfg.gridDim = dim3((unsigned)(units < kSMs * 2 ? units : kSMs * 2));                 // two fit an SM
     cfg.blockDim = dim3(kMergeThreads);
     cfg.dynamicSmemBytes = plan_bytes(P.B + P.groups) + (size_t)4 * (P.B + 1);
     cfg.stream = st;

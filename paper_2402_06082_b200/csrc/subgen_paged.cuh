@@ -408,15 +408,15 @@ struct Plan {
 };
 
 // Joins the partials of every row that has some (rows whose result went out directly are left alone) and writes 0 for
-// rows that see nothing, NaN for rows of a sequence whose lengths or pages are unusable. One block per row unit of a
-// sequence and KV head. A row's partials are dealt to WPR warps (as many as the block has left for the unit's rows, so
+// rows that see nothing, NaN for rows of a sequence whose lengths or pages are unusable. One block per 32 rows of a row unit of
+// a sequence and KV head. A row's partials are dealt to WPR warps (as many as the block has left for the unit's rows, so
 // that one sequence's long list is read by all of them); a lane looks after one partial's weight, then the warp adds the
 // numerators, all loads of a batch in flight, and the warps of a row join through shared memory.
 constexpr int kMergeThreads = 256;
 
 template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
 __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P, Attend a, int nblk) {
-    constexpr int NW = kMergeThreads / 32, VL = D / 32;
+    constexpr int NW = kMergeThreads / 32, VL = D / 32, PART = RU < 32 ? RU : 32;   // PART: rows that one block joins at a time
     extern __shared__ __align__(16) unsigned char sm_plan[];
     __shared__ int flag;
     __shared__ int units;
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
     typedef Plan<RU, KT, DUAL, LEAD> PlanT;
     PlanT plan(P, a);
     plan.build(sm_plan, &flag, nblk);
-    int* uscan = (int*)sm_plan + 2 * (plan.E + 1);    // [B+1] row units before each sequence
+    int* uscan = (int*)sm_plan + 2 * (plan.E + 1);    // [B+1] parts of PART rows before each sequence
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (plan.broken) {
         if (blockIdx.x == 0 && tid == 0) paged_status(P, kStPage);
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
         int at = 0;
         for (int i0 = 0; i0 < P.B; i0 += 32) {
             const int b = i0 + lane;
-            int x = b < P.B ? (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + RU - 1) / RU : 0;
+            int x = b < P.B ? (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + PART - 1) / PART : 0;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const int xo = __shfl_up_sync(0xffffffffu, x, off);
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
             const int mid = (lo + hi + 1) >> 1;
             if (uscan[mid] <= u) lo = mid; else hi = mid - 1;
         }
-        const int b = lo, ru = u - uscan[lo], ei = P.groups + b;
+        const int b = lo, part0 = (u - uscan[lo]) * PART, ru = part0 / RU, ei = P.groups + b;
         const Entry e = plan.entry(ei);
         const int rows = plan.unit_rows(e, ru), tiles = plan.unit_tiles(e, ru), w = plan.unit_weight(tiles, rows), sh = PlanT::shift(rows);
         int u0 = h * plan.head_w + plan.tscan[ei];
@@ -478,7 +478,8 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
         const int bad = e.bad | (g >= 0 ? ge.bad : 0), pt = g >= 0 ? plan.prefix_tiles(ge) : 0;
         if (bad && tid == 0) paged_status(P, kStPage);
         const int wpr = rows >= NW ? 1 : rows > 4 ? 1 : rows > 2 ? NW / 4 : rows > 1 ? NW / 2 : NW;   // warps per row
-        for (int r0 = 0; r0 < rows; r0 += NW / wpr) {
+        const int rows_begin = part0 - ru * RU, rows_end = min(rows, rows_begin + PART);
+        for (int r0 = rows_begin; r0 < rows_end; r0 += NW / wpr) {
             const int r = r0 + warp / wpr, sub = warp % wpr;
             float acc[VL], m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -539,7 +540,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
                     }
                 }
             };
-            if (r < rows) {
+            if (r < rows_end) {
                 if (w) collect(u0, w, rows, c0, c1, plan.slot_of(ei, ru, h, 0) + r);
                 if (pt) {
                     const int prow = ru * RU + r + ((e.tok0 - ge.tok0) << a.g_shift), pru = prow / RU, prows = plan.unit_rows(ge, pru);
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
                     for (int j = 0; j < VL; ++j) acc[j] = fmaf(join[warp - sub + k][lane * VL + j], f, acc[j]);
                 }
             }
-            if (r >= rows || sub) continue;
+            if (r >= rows_end || sub) continue;
             float inv = l == 0.f ? 0.f : 1.f / l;                    // l is NaN where a page was unusable
             if (bad) inv = NAN;
             const int row = ru * RU + r, tok = e.tok0 + (row >> a.g_shift), head = (h << a.g_shift) + (row & ((1 << a.g_shift) - 1));

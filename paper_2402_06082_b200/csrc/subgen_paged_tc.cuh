@@ -32,6 +32,7 @@
 namespace sgk {
 
 constexpr int kPtThreads = 384, kPtRU = 256, kPtKT = 128, kPtRing = 8, kPtLead = 2;
+constexpr int kPtPoly = 2;                            // of 8 pairs of weights, those exponentiated on the fp32 pipe
 constexpr unsigned kPtSpins = 1u << 20;
 
 struct SegRec {
@@ -47,7 +48,7 @@ struct PtSmem {                                       // after a 1024-byte align
     float join[2][4][4][D];                           // [group][warp][row][column]: numerators of four rows to be added
     float2 join_stat[2][4][32];                       // maximum in use, sum
     SegRec seg[kPtRing];
-    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2],
+    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2], turn[2],
         seg_full[kPtRing], seg_empty[kPtRing], drain;
     unsigned tmem;
     int failed, flag;
@@ -66,6 +67,12 @@ __device__ __forceinline__ void bar_expect(unsigned long long* b, unsigned bytes
 __device__ __forceinline__ bool bar_try(unsigned long long* b, unsigned parity) {
     unsigned ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool bar_test(unsigned long long* b, unsigned parity) {       // does not wait
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
                  : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
     return ok != 0;
 }
@@ -88,25 +95,41 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void tc_commit(unsigned long long* b) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
-}
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// shared-memory operand: rows of 128 bytes, 128-byte swizzle, 8-row groups 1024 bytes apart. lbo: bytes between 64-column
-// blocks where the contiguous axis is the MMA's N (V); not used where it is K (Q, K).
-__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lbo) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+// Issued by a whole warp in step; one lane is elected inside. The election sits in the assembly, as a predicate, because an
+// MMA's operands have to be in uniform registers: behind a branch on the election the compiler takes them for divergent
+// and each MMA costs some 90 cycles to issue instead of 64 (128 x 128 x 16).
+__device__ __forceinline__ void tc_commit(unsigned long long* b) {
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(smem_u32(b)) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accum), "r"(0u) : "memory");
+// Shared-memory operands: rows of 128 bytes, 128-byte swizzle, 8-row groups 1024 bytes apart. The descriptor's low word is
+// address >> 4 | distance of 64-column blocks >> 4 << 16 (used where the contiguous axis is the MMA's N: V).
+constexpr uint32_t kDescHigh = 64u | (1u << 14) | (2u << 29);
+#define SGK_MMA_S(off, p) "add.u32 al, %1, " #off ";\n\tadd.u32 bl, %2, " #off ";\n\tmov.b64 a, {al, %4};\n\tmov.b64 b, {bl, %4};\n\t" \
+                          "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, " #p ";\n\t"
+#define SGK_MMA_O(i, off, p) "add.u32 al, %1, " #i ";\n\tadd.u32 bl, %2, " #off ";\n\tmov.b64 b, {bl, %4};\n\t" \
+                             "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [al], b, %3, " #p ";\n\t"
+// S = Q K^T over d in steps of 16: 32 bytes of a row, the second 64 columns 16 KB behind
+template <int D>
+__device__ __forceinline__ void tc_scores(uint32_t d, uint32_t q, uint32_t k, uint32_t idesc) {
+    asm volatile("{\n\t.reg .pred e, z, o;\n\t.reg .b64 a, b;\n\t.reg .b32 al, bl;\n\t"
+                 "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 z, 0, 0;\n\tsetp.eq.b32 o, 0, 0;\n\t"
+                 SGK_MMA_S(0, z) SGK_MMA_S(2, o) SGK_MMA_S(4, o) SGK_MMA_S(6, o) "}\n"
+                 ::"r"(d), "r"((q >> 4) | (1u << 16)), "r"((k >> 4) | (1u << 16)), "r"(idesc), "r"(kDescHigh) : "memory");
+    if constexpr (D == 128)
+        asm volatile("{\n\t.reg .pred e, o;\n\t.reg .b64 a, b;\n\t.reg .b32 al, bl;\n\t"
+                     "elect.sync _|e, 0xffffffff;\n\tsetp.eq.b32 o, 0, 0;\n\t"
+                     SGK_MMA_S(1024, o) SGK_MMA_S(1026, o) SGK_MMA_S(1028, o) SGK_MMA_S(1030, o) "}\n"
+                     ::"r"(d), "r"((q >> 4) | (1u << 16)), "r"((k >> 4) | (1u << 16)), "r"(idesc), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}\n"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accum), "r"(0u) : "memory");
+// O (+)= P V over half a tile's tokens in steps of 16: 8 columns of P, 2 KB of V
+__device__ __forceinline__ void tc_output(uint32_t d, uint32_t p, uint32_t v, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred e, z, o;\n\t.reg .b64 b;\n\t.reg .b32 al, bl;\n\t"
+                 "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 z, %5, 0;\n\tsetp.eq.b32 o, 0, 0;\n\t"
+                 SGK_MMA_O(0, 0, z) SGK_MMA_O(8, 128, o) SGK_MMA_O(16, 256, o) SGK_MMA_O(24, 384, o) "}\n"
+                 ::"r"(d), "r"(p), "r"((v >> 4) | (1024u << 16)), "r"(idesc), "r"(kDescHigh), "r"(accumulate) : "memory");
 }
 #define SGK_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
 #define SGK_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
@@ -124,11 +147,6 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n"
                  ::"r"(addr), SGK_I8(v, 0), SGK_I8(v, 8) : "memory");
 }
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(p));
-    return p != 0;
-}
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 // two fp32 operations in one instruction
 __device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
@@ -143,6 +161,20 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
     asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}\n"
         : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
     return r;
+}
+// 2^x for x <= 8 on the fp32 pipe: 2^round(x) by the exponent, 2^(x - round(x)) by the cubic with the least relative error
+// on [-1/2, 1/2] (Remez, 7.5e-5: a fiftieth of a bf16 half step, which the weight is rounded to). Below 2^-126 it stays
+// near 2^-126, which is nothing beside the row's largest weight (at least 2^-8); rows that see nothing are told by their
+// maximum.
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+    const float2 r = add2(x, make_float2(12582912.f, 12582912.f));        // 1.5 * 2^23: the rounded integer in the low bits
+    const float2 f = fma2(add2(r, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), x);
+    float2 y = fma2(f, make_float2(0.05517167f, 0.05517167f), make_float2(0.24261113f, 0.24261113f));
+    y = fma2(y, f, make_float2(0.69326097f, 0.69326097f));
+    y = fma2(y, f, make_float2(0.99992806f, 0.99992806f));
+    return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(r.x) << 23)),
+                       __int_as_float(__float_as_int(y.y) + (__float_as_int(r.y) << 23)));
 }
 __device__ __forceinline__ float max3(float x, float y, float z) {
     float r;
@@ -186,7 +218,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             bar_init(&sm.q_full[i], 1); bar_init(&sm.q_empty[i], 2);
             bar_init(&sm.s_full[i], 1); bar_init(&sm.p_full[i], 4);
             bar_init(&sm.o_full[i], 1); bar_init(&sm.o_empty[i], 4);
-            bar_init(&sm.join_bar[i], 4);
+            bar_init(&sm.join_bar[i], 4); bar_init(&sm.turn[i], 1);
         }
         for (int i = 0; i < NS; ++i) { bar_init(&sm.kv_full[i], 1); bar_init(&sm.kv_empty[i], 2); }
         for (int i = 0; i < kPtRing; ++i) { bar_init(&sm.seg_full[i], 1); bar_init(&sm.seg_empty[i], 11); }
@@ -234,7 +266,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 const int slot = ns % kPtRing;
                 if (!(ok = bar_wait(&sm.seg_full[slot], (ns / kPtRing) & 1, &sm.failed))) break;
                 SegRec& r = sm.seg[slot];
-                const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, head = r.head, P_ = r.P, S_ = r.S;
+                const int tile0 = uniform(r.tile0), tile1 = uniform(r.tile1), kp = uniform(r.kp), head = uniform(r.head), P_ = r.P, S_ = r.S;
                 const int *ptab = r.ptab, *stab = r.stab;
                 if (tile1 < 0) break;
                 // the page of this lane's copy of tile t: -2 nothing to bring, -1 outside the pool
@@ -260,7 +292,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 }
                 for (int t = tile0; t < tile1 && ok; ++t) {
                     const int following = page_of(t + 1);        // asked for a tile early
-                    const int row = ((t < kp ? t : t - kp) * kPtKT + chunk * pb) & ((1 << P.page_shift) - 1);
+                    const int row = ((t < kp ? t : t - kp) * kPtKT) & ((1 << P.page_shift) - 1);   // pieces of a page start at 0
                     if (__any_sync(0xffffffffu, id == -1) && lane == 0) {
                         *reinterpret_cast<volatile int*>(&r.bad) = 1;
                         paged_status(P, kStPage);
@@ -286,9 +318,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.q_full[i & 1], (i / 2) & 1); ++j) {}
         } else {
             // ---- issuers ----
-            // Everything here is the same in all lanes, and said so by shuffles and votes: an MMA's operands have to be
-            // in uniform registers, and with operands that the compiler takes for divergent each MMA costs some 90 cycles
-            // instead of 64 (128 x 128 x 16). One warp per group, so that a wait of one leaves no gap in the tensor pipe.
+            // Everything here is the same in all lanes, and said so by shuffles and votes. One warp per group, so that a wait
+            // of one leaves no gap in the tensor pipe.
             const int w = warp - 9;
             struct Cursor { int tile, tile0, tile1, kp, dual, order, rows, P, S, seg, q, kv, jobs, done; };
             bool ok = true;
@@ -322,28 +353,31 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 ++c.seg;
             };
             Cursor qk = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}, pv = qk;
-            int segs = 0, mine = 0;                    // runs whose numerator the group has begun, products with V
-            auto issue_qk = [&]() {
+            int segs = 0, mine = 0, turns = 0;         // runs whose numerator the group has begun, products with V, turns taken
+            // Whether Q and K of the next S are there: asked before P V is issued, so that S can follow without a wait.
+            auto issue_ready = [&]() {
+                if (qk.done) return false;
+                const int qt = qk.q + (qk.dual ? qk.order : 0), ks = 2 * (qk.kv + qk.tile - qk.tile0), s = ks % NS;
+                const bool q = qk.tile >= qk.tile0 + 2 || bar_test(&sm.q_full[qt & 1], (qt / 2) & 1);
+                return (bool)__all_sync(0xffffffffu, q && bar_test(&sm.kv_full[s], (ks / NS) & 1));
+            };
+            auto issue_qk = [&](bool there) {
                 if (qk.done || !ok) return;
                 const int qt = qk.q + (qk.dual ? qk.order : 0), ks = 2 * (qk.kv + qk.tile - qk.tile0), s = ks % NS, step = 2 - qk.dual;
-                if (qk.tile < qk.tile0 + 2 && !(ok = wait(&sm.q_full[qt & 1], (qt / 2) & 1))) return;
-                if (!(ok = wait(&sm.kv_full[s], (ks / NS) & 1))) return;
+                if (!there) {
+                    if (qk.tile < qk.tile0 + 2 && !(ok = wait(&sm.q_full[qt & 1], (qt / 2) & 1))) return;
+                    if (!(ok = wait(&sm.kv_full[s], (ks / NS) & 1))) return;
+                }
                 const bool last = qk.tile + step >= qk.tile1;
                 const uint32_t qa = smem_u32(sm.Q[qt & 1]), ka = smem_u32(sm.KV[s]);
                 tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t off = (uint32_t)((i >> 2) * 16384 + (i & 3) * 32);
-                        tc_mma_ss(tmem + w * 128u, tc_desc(qa + off, 16), tc_desc(ka + off, 16), kIdescS, i ? 1u : 0u);
-                    }
-                    tc_commit(&sm.s_full[w]);
-                    tc_commit(&sm.kv_empty[s]);        // a slot counts two: both groups', or this one's twice
-                    if (!qk.dual) tc_commit(&sm.kv_empty[s]);
-                    if (last) {
-                        tc_commit(&sm.q_empty[qt & 1]);
-                        if (qk.dual) tc_commit(&sm.q_empty[qt & 1]);
-                    }
+                tc_scores<D>(tmem + w * 128u, qa, ka, kIdescS);
+                tc_commit(&sm.s_full[w]);
+                tc_commit(&sm.kv_empty[s]);            // a slot counts two: both groups', or this one's twice
+                if (!qk.dual) tc_commit(&sm.kv_empty[s]);
+                if (last) {
+                    tc_commit(&sm.q_empty[qt & 1]);
+                    if (qk.dual) tc_commit(&sm.q_empty[qt & 1]);
                 }
                 __syncwarp();
                 qk.tile += step;
@@ -354,7 +388,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             };
             enter(qk, false);
             enter(pv, true);
-            issue_qk();
+            issue_qk(false);
             while (!pv.done && ok) {
                 const int vs = 2 * (pv.kv + pv.tile - pv.tile0) + 1, s = vs % NS, step = 2 - pv.dual;
                 const bool fresh = pv.tile < pv.tile0 + step, last = pv.tile + step >= pv.tile1;
@@ -373,30 +407,36 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     if (segs && !(ok = wait(&sm.o_empty[w], (segs - 1) & 1))) break;
                     ++segs;
                 }
-                if (!(ok = wait(&sm.p_full[w], mine & 1))) break;
                 const uint32_t va = smem_u32(sm.KV[s]);
                 const uint32_t first = fresh ? 0u : 1u;
+                const bool k_there = issue_ready();
+                // Two groups on the same tiles take turns, P V and the next S of one, then of the other. Left to themselves
+                // both pairs run interleaved, end together, and the tensor pipe waits while both groups exponentiate.
+                const bool turn = pv.dual && (pv.order || pv.tile != pv.tile0);
+                if (turn && !(ok = wait(&sm.turn[w], turns & 1))) break;
+                turns += turn;
+                if (!(ok = wait(&sm.p_full[w], mine & 1))) break;
                 tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < kPtKT / 16; ++k)
-                        tc_mma_ts(tmem + 256u + w * (uint32_t)D, tmem + w * 128u + k * 8u, tc_desc(va + k * 2048u, 16384), kIdescO, k ? 1u : first);
-                    tc_commit(&sm.kv_empty[s]);
-                    if (!pv.dual) tc_commit(&sm.kv_empty[s]);
-                    if (last) tc_commit(&sm.o_full[w]);
-                }
+                const uint32_t td = tmem + 256u + w * (uint32_t)D, tp = tmem + w * 128u;
+                tc_output(td, tp, va, kIdescO, first);
+                tc_output(td, tp + 32u, va + 8192u, kIdescO, 1u);
+                tc_commit(&sm.kv_empty[s]);
+                if (!pv.dual) tc_commit(&sm.kv_empty[s]);
+                if (last) tc_commit(&sm.o_full[w]);
                 __syncwarp();
-                ++mine;
                 pv.tile += step;
+                issue_qk(k_there);
+                ++mine;
+                if (pv.dual && !(pv.order && last) && lane == 0) bar_arrive(&sm.turn[1 - w]);
                 if (last) {
+                    __syncwarp();
                     if (lane == 0) bar_arrive(&sm.seg_empty[pv.seg % kPtRing]);
                     __syncwarp();
                     leave(pv);
+                    enter(pv, true);
                 }
-                issue_qk();
-                if (last) enter(pv, true);
             }
-            if (elect_one()) tc_commit(&sm.drain);    // the MMAs read shared memory: done before the block ends
+            tc_commit(&sm.drain);                     // the MMAs read shared memory: done before the block ends
             __syncwarp();
             for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.drain, 0); ++j) {}
         }
@@ -408,7 +448,9 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         const uint32_t tS = tmem + lanes + (uint32_t)w * 128u, tO = tmem + lanes + 256u + (uint32_t)(w * D);
         unsigned ns = 0, job = 0, mine = 0, segs = 0;  // runs, jobs of both groups, jobs and runs of this one
         bool ok = true;
-        float m = 0.f, l = 0.f;                                // of this thread's row: the maximum in use, the sum
+        float m = 0.f, l = 0.f, edge = 0.f, off = 0.f; // of this thread's row: the maximum in use, the sum, the score from
+                                                       // which on the maximum is replaced, -m * c
+        const float margin = 8.f / a.c;
         bool begun = false;
         unsigned joins = 0;
         auto joined = [&]() {                          // the group's four warps have come here
@@ -418,10 +460,10 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         };
         // A new maximum of the row: keep the one in use, or change to the new one and rescale.
         auto raise = [&](float top) {
-            const bool rise = (top - m) * a.c > 8.f || (m == -INFINITY && top > m);
+            const bool rise = top > edge;
             if (__any_sync(0xffffffffu, rise)) {
                 const float f = rise ? ex2_approx((m - top) * a.c) : 1.f;              // 0 when there was no maximum yet
-                if (rise) m = top;
+                if (rise) { m = top; edge = top + margin; off = -top * a.c; }
                 l *= f;
                 if (begun) {
                     uint32_t o[32];
@@ -440,23 +482,19 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         // N scores of the row -> bf16 weights, two to a register; adds them to the sum
         auto weigh = [&](auto count, const uint32_t* s, uint32_t* p) {
             constexpr int N = decltype(count)::value;
-            const float off = m == -INFINITY ? 0.f : -m * a.c;
             const float2 cc = make_float2(a.c, a.c), oo = make_float2(off, off);
-            float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-            for (int i = 0; i < N; i += 4) {
-                float2 x = fma2(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), cc, oo);
-                float2 y = fma2(make_float2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), cc, oo);
-                x = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                y = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-                l0 = add2(l0, x);
-                l1 = add2(l1, y);
-                const __nv_bfloat162 bx = __float22bfloat162_rn(x), by = __float22bfloat162_rn(y);
-                p[i / 2] = *reinterpret_cast<const uint32_t*>(&bx);
-                p[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&by);
+            for (int i = 0; i < N / 2; ++i) {
+                float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), cc, oo);
+                if (i % 8 < kPtPoly) x = exp2_poly(x);
+                else x = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                sum[i & 1] = add2(sum[i & 1], x);
+                const __nv_bfloat162 b = __float22bfloat162_rn(x);
+                p[i] = *reinterpret_cast<const uint32_t*>(&b);
             }
-            l0 = add2(l0, l1);
-            l += l0.x + l0.y;
+            sum[0] = add2(sum[0], sum[1]);
+            l += sum[0].x + sum[0].y;
         };
         auto largest = [&](auto count, const uint32_t* s) {
             constexpr int N = decltype(count)::value;
@@ -482,19 +520,20 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             Entry e;
             e.S = r.S; e.nq = r.nq;
             const int own = plan.own_limit(e, urow);
-            m = -INFINITY;
-            l = 0.f;
+            m = edge = -INFINITY;
+            l = off = 0.f;
             begun = false;
             for (int t = tile0 + (dual ? 0 : order); t < tile1; t += 2 - dual) {
-                if (!(ok = bar_wait(&sm.s_full[w], mine & 1, &sm.failed))) break;
                 const bool pre = t < kp;
                 const int lim = pre ? P_ - t * kPtKT : own - (t - kp) * kPtKT;        // tokens of the tile that the row sees
+                const bool cut = __any_sync(0xffffffffu, lim < kPtKT);
+                if (!(ok = bar_wait(&sm.s_full[w], mine & 1, &sm.failed))) break;
                 if (quad) {
                     tc_fence_after();
                     uint32_t s[32], p[16];
                     tc_ld32(tS + quarter * 32, s);
                     tc_wait_ld();
-                    if (__any_sync(0xffffffffu, lim < kPtKT)) {
+                    if (cut) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) s[i] = quarter * 32 + i < lim ? s[i] : 0xff800000u;
                     }
@@ -515,20 +554,23 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
 #pragma unroll
                     for (int i = 0; i < 4; ++i) tc_ld32(tS + i * 32, s + i * 32);
                     tc_wait_ld();
-                    if (__any_sync(0xffffffffu, lim < kPtKT)) {
+                    if (cut) {
 #pragma unroll
                         for (int i = 0; i < 128; ++i) s[i] = i < lim ? s[i] : 0xff800000u;
                     }
                     raise(largest(std::integral_constant<int, 128>(), s));
-                    weigh(std::integral_constant<int, 128>(), s, s);                   // in place: a pair goes to half its index
-                    tc_st32(tS, s);
-                    tc_st32(tS + 32, s + 32);
+                    uint32_t p[64];
+                    weigh(std::integral_constant<int, 128>(), s, p);
+                    tc_st32(tS, p);
+                    tc_st32(tS + 32, p + 32);
                     tc_wait_st();
                     tc_fence_before();
                 }
                 begun = true;
                 __syncwarp();
-                if (lane == 0) bar_arrive(&sm.p_full[w]);
+                if (lane == 0) {
+                    bar_arrive(&sm.p_full[w]);
+                }
                 ++mine;
             }
             if (!ok) break;
@@ -576,6 +618,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
 #pragma unroll
                                 for (int j = 0; j < D / 32; ++j) z[j] = fmaf(sm.join[w][k][quarter][j * 32 + lane], f, z[j]);
                             }
+                            if (M == -INFINITY) L = 0.f;
                             if (bad) L = NAN;
                             const int gr = r.ru * kPtRU + rr, tok = r.tok0 + (gr >> gs), head = (r.head << gs) + (gr & ((1 << gs) - 1));
                             if (direct) {
@@ -595,6 +638,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     tc_fence_before();
                 } else if (some) {
                     tc_fence_after();
+                    if (m == -INFINITY) l = 0.f;
                     if (bad) l = NAN;
                     const int tok = r.tok0 + (urow >> gs), head = (r.head << gs) + (urow & ((1 << gs) - 1));
                     const float f = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
