@@ -362,12 +362,20 @@ typedef struct subgen_heads {
     int64_t head_stride;   /* elements from one head to the next */
 } subgen_heads;
 
-/* q, q_out: n tokens of H heads; k, k_out: of Hkv heads. An output may be its input (same strides), otherwise they must
- * not overlap. positions: device [n], any 32-bit value (needed if there is a rotation). wq, wk: device [d] of the
- * dtype, or NULL for no norm. q or k may be NULL (or have p = NULL): then only the other is done. */
-int subgen_qk_norm_rope(const subgen_heads* q, const subgen_heads* k, const subgen_heads* q_out, const subgen_heads* k_out,
-                        int n, int H, int Hkv, int d, int dtype, const int* positions, const subgen_rope* rope,
-                        const void* wq, const void* wk, float eps, void* stream);
+typedef struct subgen_qk_args {
+    subgen_heads q, k, v;     /* n tokens of H (q) and Hkv (k, v) heads; v for subgen_paged_append only */
+    subgen_heads q_out, k_out;/* an output may be its input (same strides), otherwise they must not overlap; k_out for
+                               * subgen_qk_norm_rope only */
+    const int* positions;     /* device [n], any 32-bit value */
+    subgen_rope rope;
+    const void *wq, *wk;      /* device [d] of the dtype, 16-byte aligned; NULL: no norm */
+    int n, H, Hkv, d, dtype;  /* d: 64 or 128; subgen_paged_append takes Hkv, d and dtype from its cache */
+    float eps;
+} subgen_qk_args;
+
+/* q or k may have p = NULL: then only the other is done. positions are needed if there is a rotation. Asynchronous on
+ * `stream`, one kernel. */
+int subgen_qk_norm_rope(const subgen_qk_args* args, void* stream);
 
 /* ---- paged exact cache ------------------------------------------------------------------------- */
 
@@ -404,27 +412,32 @@ typedef struct subgen_batch {
 } subgen_batch;
 
 /* Writes the n new tokens' keys, normed (if wk) and rotated (if rope), and their values into the pages of their
- * sequences, and the queries, normed (if wq) and rotated, to q_out, which may be q (q, q_out may be NULL: keys and values
- * only). positions: device [n], or NULL: a token's position is its place in its sequence, prefix included. Two rows must
- * not have the same slot. Tokens whose own index is negative (more new tokens than the length says) are not written and
- * set SUBGEN_ST_PAGE. Asynchronous on `stream`, one kernel. */
-int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* k, const subgen_heads* v,
-                        const subgen_heads* q, const subgen_heads* q_out, int n, int H, const int* positions,
-                        const subgen_rope* rope, const void* wq, const void* wk, float eps, void* stream);
+ * sequences, and the queries, normed (if wq) and rotated, to q_out, which may be q (q.p may be NULL: keys and values
+ * only). positions NULL: a token's position is its place in its sequence, prefix included. Two rows must not have the
+ * same slot. Tokens whose own index is negative (more new tokens than the length says) are not written and set
+ * SUBGEN_ST_PAGE. Asynchronous on `stream`, one kernel. */
+int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_qk_args* args, void* stream);
+
+typedef struct subgen_attend_args {
+    subgen_heads q, out;      /* n tokens of H heads */
+    void* workspace;          /* device, 256-byte aligned */
+    size_t workspace_bytes;   /* at least subgen_paged_workspace_bytes() */
+    int n, H;
+    float scale;              /* > 0 */
+    int causal;
+} subgen_attend_args;
 
 /* out = softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for each of the n new tokens' H query heads (head h reads KV
  * head h / (H / Hkv); H / Hkv in {1, 2, 4, 8}), the new tokens' keys and values being in the cache already. A token sees
  * its group's whole prefix and, of its own sequence, the tokens up to itself (causal = 1) or all of them (causal = 0).
  * A row that sees nothing (an empty sequence, or one of more new tokens than its length says) is 0. The prefix is read
- * once per group, whatever the number of its sequences. scale > 0. Stored keys and values that some row sees must be
+ * once per group, whatever the number of its sequences. Stored keys and values that some row sees must be
  * finite; what lies behind a sequence's length in its last page may be anything.
  * Scores, maxima, sums and numerators are fp32; on bf16 caches the softmax weights are rounded to bf16 for the product
  * with V. The result does not depend on how blocks are scheduled.
- * workspace: device, subgen_paged_workspace_bytes(), 256-byte aligned, used by this call only until it has run (two calls
- * that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */
+ * The workspace is this call's until it has run (two calls that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */
 size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H);
-int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* q, const subgen_heads* out,
-                        int n, int H, float scale, int causal, void* workspace, size_t workspace_bytes, void* stream);
+int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_attend_args* args, void* stream);
 
 #ifdef __cplusplus
 }

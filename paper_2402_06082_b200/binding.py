@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -73,6 +74,17 @@ class BatchDesc(C.Structure):
                 ("prefix_table", C.c_void_p), ("prefix_stride", C.c_int)]
 
 
+class QkArgs(C.Structure):
+    _fields_ = [(k, Heads) for k in ("q", "k", "v", "q_out", "k_out")] + [
+        ("positions", C.c_void_p), ("rope", RopeDesc), ("wq", C.c_void_p), ("wk", C.c_void_p), ("n", C.c_int), ("H", C.c_int),
+        ("Hkv", C.c_int), ("d", C.c_int), ("dtype", C.c_int), ("eps", C.c_float)]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [("q", Heads), ("out", Heads), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("n", C.c_int),
+                ("H", C.c_int), ("scale", C.c_float), ("causal", C.c_int)]
+
+
 _lib = None
 
 
@@ -128,13 +140,13 @@ def load():
     L.subgen_exact_kcenter_counters.argtypes = [vp, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
     L.subgen_exact_export_tokens.argtypes = [vp, C.c_int, C.c_int, ip, ip]
     L.subgen_exact_attention_noalloc.argtypes = [vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp]
-    hp, rp, pp, bp = C.POINTER(Heads), C.POINTER(RopeDesc), C.POINTER(PagesDesc), C.POINTER(BatchDesc)
+    # descriptors by address, arguments as packed bytes (a call costs a few microseconds on the host, and that counts)
     L.subgen_rope_words.argtypes = [C.POINTER(C.c_double), C.c_int, C.POINTER(C.c_uint64)]
-    L.subgen_qk_norm_rope.argtypes = [hp, hp, hp, hp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp, rp, vp, vp, C.c_float, vp]
-    L.subgen_paged_append.argtypes = [pp, bp, hp, hp, hp, hp, C.c_int, C.c_int, vp, rp, vp, vp, C.c_float, vp]
-    L.subgen_paged_workspace_bytes.argtypes = [pp, bp, C.c_int, C.c_int]
+    L.subgen_qk_norm_rope.argtypes = [C.c_char_p, vp]
+    L.subgen_paged_append.argtypes = [vp, vp, C.c_char_p, vp]
+    L.subgen_paged_workspace_bytes.argtypes = [vp, vp, C.c_int, C.c_int]
     L.subgen_paged_workspace_bytes.restype = C.c_size_t
-    L.subgen_paged_attend.argtypes = [pp, bp, hp, hp, C.c_int, C.c_int, C.c_float, C.c_int, vp, C.c_size_t, vp]
+    L.subgen_paged_attend.argtypes = [vp, vp, C.c_char_p, vp]
     _lib = L
     return L
 
@@ -425,38 +437,43 @@ def exact_attention_noalloc(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, o
 # These calls run on the current stream of their tensors' device and keep nothing between calls: outputs and scratch
 # come from torch's allocator, call by call, so captured graphs and calls on several streams do not share any.
 
-def _raw_stream(index: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(index)
+_QK = struct.Struct("@" + "Pqq" * 5 + "PPiiPP5if")                # QkArgs
+_ATTEND = struct.Struct("@" + "Pqq" * 2 + "PNiifi")               # AttendArgs
+_CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+_NO_ROWS, _NO_ROPE = (0, 0, 0), (0, 0, 0)
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _heads(x: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, n: int, heads: int, d: int) -> Heads:
-    if x.dtype is not dtype or x.device != device or x.shape != (n, heads, d) or (x.stride(2) != 1 and d > 1):
-        raise ValueError("%s must be a %s tensor of shape %s on %s with unit stride along the last axis (got %s %s on %s)" %
-                         (name, dtype, (n, heads, d), device, x.dtype, tuple(x.shape), x.device))
-    return Heads(x.data_ptr(), x.stride(0), x.stride(1))
+def _call(fn, device: int, *args):
+    """fn(*args, current stream of the device) with the device current."""
+    if _current_device() == device:
+        return _check(fn(*args, _raw_stream(device)))
+    with torch.cuda.device(device):
+        return _check(fn(*args, _raw_stream(device)))
 
 
-def _ints(x: Optional[torch.Tensor], name: str, device: torch.device, shape) -> Optional[int]:
+def _rows(x: torch.Tensor, name: str, dtype: torch.dtype, device: int, shape):
+    s = x.stride()
+    if x.dtype is not dtype or x.get_device() != device or x.shape != shape or s[2] != 1:
+        raise ValueError("%s must be a %s tensor of shape %s on cuda:%d with unit stride along the last axis (got %s %s on %s)" %
+                         (name, dtype, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
+    return x.data_ptr(), s[0], s[1]
+
+
+def _whole(x: Optional[torch.Tensor], name: str, dtype: torch.dtype, device: int, shape) -> int:
     if x is None:
-        return None
-    if x.dtype is not torch.int32 or x.device != device or x.shape != shape or not x.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 tensor of shape %s on %s (got %s %s on %s)" %
-                         (name, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
+        return 0
+    if x.dtype is not dtype or x.get_device() != device or x.shape != shape or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d (got %s %s on %s)" %
+                         (name, dtype, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
     return x.data_ptr()
 
 
-def _weight(x: Optional[torch.Tensor], name: str, dtype: torch.dtype, device: torch.device, d: int) -> Optional[int]:
-    if x is None:
-        return None
-    if x.dtype is not dtype or x.device != device or x.shape != (d,) or not x.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape (%d,) on %s" % (name, dtype, d, device))
-    return x.data_ptr()
-
-
-def _cuda(x: torch.Tensor, name: str) -> torch.device:
-    if not x.is_cuda:
+def _cuda(x: torch.Tensor, name: str) -> int:
+    i = x.get_device()
+    if i < 0:
         raise ValueError("%s must be a CUDA tensor: this library has no CPU path" % name)
-    return x.device
+    return i
 
 
 class Rope:
@@ -477,13 +494,13 @@ class Rope:
         _check(load().subgen_rope_words((C.c_double * (r // 2))(*f), r // 2, words.ctypes.data_as(C.POINTER(C.c_uint64))))
         self.d, self.rotary_dim, self.interleaved = int(d), r, bool(interleaved)
         self.words = torch.from_numpy(words.view(np.int64)).to(device)
-        self.device = self.words.device
-        self._desc = RopeDesc(self.words.data_ptr(), r, int(self.interleaved))
+        self.device = self.words.get_device()
+        self._desc = (self.words.data_ptr(), r, int(self.interleaved))
 
-    def _for(self, d: int, device: torch.device):
+    def _for(self, d: int, device: int):
         if self.device != device or self.d != d:
-            raise ValueError("rope was made for d = %d on %s" % (self.d, self.device))
-        return C.byref(self._desc)
+            raise ValueError("rope was made for d = %d on device %d" % (self.d, self.device))
+        return self._desc
 
 
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
@@ -494,26 +511,40 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     q [n, H, d], k [n, Hkv, d]: views with unit stride along d (slices of a fused projection). Returns (q_out, k_out), None for
     what was not given; an output may be its input.
     """
-    x = q if q is not None else k
+    x = k if q is None else q
     if x is None:
         raise ValueError("q and k must not both be None")
-    dev, dt, (n, _, d) = _cuda(x, "q" if q is not None else "k"), x.dtype, x.shape
-    code = _dtype_code(dt)
-    qd = kd = qo = ko = None
-    H = Hkv = 1
-    if q is not None:
-        H = q.shape[1]
-        q_out = torch.empty((n, H, d), dtype=dt, device=dev) if q_out is None else q_out
-        qd, qo = _heads(q, "q", dt, dev, n, H, d), _heads(q_out, "q_out", dt, dev, n, H, d)
-    if k is not None:
+    dev, dt = _cuda(x, "q and k"), x.dtype
+    n, H, d = x.shape
+    Hkv, qp, kp, qo, ko = 1, _NO_ROWS, _NO_ROWS, _NO_ROWS, _NO_ROWS
+    if dt not in _CODES:
+        raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+    if q is None:
+        H, q_out = 1, None
+    else:
+        shape = (n, H, d)
+        qp = _rows(q, "q", dt, dev, shape)
+        if q_out is None:
+            q_out = q.new_empty(shape)
+            qo = (q_out.data_ptr(), H * d, d)
+        else:
+            qo = _rows(q_out, "q_out", dt, dev, shape)
+    if k is None:
+        k_out = None
+    else:
         Hkv = k.shape[1]
-        k_out = torch.empty((n, Hkv, d), dtype=dt, device=dev) if k_out is None else k_out
-        kd, ko = _heads(k, "k", dt, dev, n, Hkv, d), _heads(k_out, "k_out", dt, dev, n, Hkv, d)
-    with torch.cuda.device(dev):
-        _check(load().subgen_qk_norm_rope(qd, kd, qo, ko, n, H, Hkv, d, code, _ints(positions, "positions", dev, (n,)),
-                                          rope._for(d, dev) if rope is not None else None, _weight(wq, "wq", dt, dev, d),
-                                          _weight(wk, "wk", dt, dev, d), eps, _raw_stream(dev.index)))
-    return q_out if q is not None else None, k_out if k is not None else None
+        shape = (n, Hkv, d)
+        kp = _rows(k, "k", dt, dev, shape)
+        if k_out is None:
+            k_out = k.new_empty(shape)
+            ko = (k_out.data_ptr(), Hkv * d, d)
+        else:
+            ko = _rows(k_out, "k_out", dt, dev, shape)
+    args = _QK.pack(*qp, *kp, 0, 0, 0, *qo, *ko, _whole(positions, "positions", torch.int32, dev, (n,)),
+                    *(_NO_ROPE if rope is None else rope._for(d, dev)), _whole(wq, "wq", dt, dev, (d,)), _whole(wk, "wk", dt, dev, (d,)),
+                    n, H, Hkv, d, _CODES[dt], eps)
+    _call(load().subgen_qk_norm_rope, dev, args)
+    return q_out, k_out
 
 
 class PagedBatch:
@@ -535,13 +566,15 @@ class PagedBatch:
         if table.dim() != 2 or (g and prefix_table.dim() != 2):
             raise ValueError("page tables are two-dimensional")
         self.tensors = (cu_q, lengths, table, cu_group, prefix_len, prefix_table)
-        self._desc = BatchDesc(B, _ints(cu_q, "cu_q", dev, (B + 1,)), _ints(lengths, "lengths", dev, (B,)),
-                               _ints(table, "table", dev, (B, table.shape[1])), table.shape[1], g)
+        i32 = torch.int32
+        self._desc = BatchDesc(B, _whole(cu_q, "cu_q", i32, dev, (B + 1,)), _whole(lengths, "lengths", i32, dev, (B,)),
+                               _whole(table, "table", i32, dev, (B, table.shape[1])), table.shape[1], g)
         if g:
-            self._desc.cu_group = _ints(cu_group, "cu_group", dev, (g + 1,))
-            self._desc.prefix_len = _ints(prefix_len, "prefix_len", dev, (g,))
-            self._desc.prefix_table = _ints(prefix_table, "prefix_table", dev, (g, prefix_table.shape[1]))
+            self._desc.cu_group = _whole(cu_group, "cu_group", i32, dev, (g + 1,))
+            self._desc.prefix_len = _whole(prefix_len, "prefix_len", i32, dev, (g,))
+            self._desc.prefix_table = _whole(prefix_table, "prefix_table", i32, dev, (g, prefix_table.shape[1]))
             self._desc.prefix_stride = prefix_table.shape[1]
+        self._at = C.addressof(self._desc)
 
 
 class PagedCache:
@@ -550,53 +583,64 @@ class PagedCache:
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor):
         dev = self.device = _cuda(K, "K")
-        if K.dim() != 4 or K.stride(3) != 1 or V.shape != K.shape or V.stride() != K.stride() or V.dtype is not K.dtype or V.device != dev:
+        if K.dim() != 4 or K.stride(3) != 1 or V.shape != K.shape or V.stride() != K.stride() or V.dtype is not K.dtype or V.get_device() != dev:
             raise ValueError("K and V must be [pages, Hkv, page, d] tensors of one type, device and layout, unit stride along d")
         self._L = load()
         self.K, self.V, self.dtype = K, V, K.dtype
         self.pages, self.Hkv, self.page, self.d = K.shape
-        self._status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self._status = torch.zeros(1, dtype=torch.int32, device=K.device)
+        self._bytes = K.new_empty(0, dtype=torch.uint8)
         self._desc = PagesDesc(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), self.pages, self.page, self.Hkv,
                                self.d, _dtype_code(K.dtype), self._status.data_ptr())
+        self._at = C.addressof(self._desc)
+
+    def _batch(self, batch: PagedBatch) -> int:
+        if batch.device != self.device:
+            raise ValueError("the batch is on device %d, the cache on %d" % (batch.device, self.device))
+        return batch._at
 
     def append(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, *, rope: Optional[Rope] = None,
                positions: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
                q: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Write the new tokens k, v [n, Hkv, d] into their pages, k normed (if wk) and rotated (if rope) on the way; q [n, H, d]
         goes the same way into q_out, which is returned (None without q). One kernel; see subgen_paged_append."""
-        dev, dt, n, H = self.device, self.dtype, k.shape[0], 1
-        kd, vd = _heads(k, "k", dt, dev, n, self.Hkv, self.d), _heads(v, "v", dt, dev, n, self.Hkv, self.d)
-        qd = qo = None
-        if q is not None:
+        dev, dt, d, n, H = self.device, self.dtype, self.d, k.shape[0], 1
+        shape = (n, self.Hkv, d)
+        kp, vp, qp, qo = _rows(k, "k", dt, dev, shape), _rows(v, "v", dt, dev, shape), _NO_ROWS, _NO_ROWS
+        if q is None:
+            q_out = None
+        else:
             H = q.shape[1]
-            q_out = torch.empty((n, H, self.d), dtype=dt, device=dev) if q_out is None else q_out
-            qd, qo = _heads(q, "q", dt, dev, n, H, self.d), _heads(q_out, "q_out", dt, dev, n, H, self.d)
-        if batch.device != dev:
-            raise ValueError("the batch is on %s, the cache on %s" % (batch.device, dev))
-        with torch.cuda.device(dev):
-            _check(self._L.subgen_paged_append(self._desc, batch._desc, kd, vd, qd, qo, n, H, _ints(positions, "positions", dev, (n,)),
-                                               rope._for(self.d, dev) if rope is not None else None,
-                                               _weight(wq, "wq", dt, dev, self.d), _weight(wk, "wk", dt, dev, self.d), eps,
-                                               _raw_stream(dev.index)))
-        return q_out if q is not None else None
+            shape = (n, H, d)
+            qp = _rows(q, "q", dt, dev, shape)
+            if q_out is None:
+                q_out = q.new_empty(shape)
+                qo = (q_out.data_ptr(), H * d, d)
+            else:
+                qo = _rows(q_out, "q_out", dt, dev, shape)
+        args = _QK.pack(*qp, *kp, *vp, *qo, 0, 0, 0, _whole(positions, "positions", torch.int32, dev, (n,)),
+                        *(_NO_ROPE if rope is None else rope._for(d, dev)), _whole(wq, "wq", dt, dev, (d,)),
+                        _whole(wk, "wk", dt, dev, (d,)), n, H, 0, 0, 0, eps)
+        _call(self._L.subgen_paged_append, dev, self._at, self._batch(batch), args)
+        return q_out
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, scale: float = 1.0, causal: bool = True, out: Optional[torch.Tensor] = None):
         """softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for q [n, H, d], whose keys are in the cache already; the prefix is
         read once per group. Rows of `out` behind the last sequence are not written. See subgen_paged_attend."""
-        dev, dt, d = self.device, self.dtype, self.d
-        n, H = q.shape[0], q.shape[1]
-        qd = _heads(q, "q", dt, dev, n, H, d)
-        out = torch.empty((n, H, d), dtype=dt, device=dev) if out is None else out
-        od = _heads(out, "out", dt, dev, n, H, d)
-        if batch.device != dev:
-            raise ValueError("the batch is on %s, the cache on %s" % (batch.device, dev))
-        size = self._L.subgen_paged_workspace_bytes(self._desc, batch._desc, n, H)
+        dev, at = self.device, self._batch(batch)
+        n, H, _ = q.shape
+        shape = (n, H, self.d)
+        qp = _rows(q, "q", self.dtype, dev, shape)
+        if out is None:
+            out = q.new_empty(shape)
+            op = (out.data_ptr(), H * self.d, self.d)
+        else:
+            op = _rows(out, "out", self.dtype, dev, shape)
+        size = self._L.subgen_paged_workspace_bytes(self._at, at, n, H)
         if size == 0:
             raise SubgenError(self._L.subgen_last_error().decode())
-        with torch.cuda.device(dev):
-            ws = torch.empty(size, dtype=torch.uint8, device=dev)     # torch aligns allocations to 512 bytes
-            _check(self._L.subgen_paged_attend(self._desc, batch._desc, qd, od, n, H, scale, int(causal), ws.data_ptr(), size,
-                                               _raw_stream(dev.index)))
+        ws = self._bytes.new_empty(size)                          # torch aligns allocations to 512 bytes
+        _call(self._L.subgen_paged_attend, dev, self._at, at, _ATTEND.pack(*qp, *op, ws.data_ptr(), size, n, H, scale, causal))
         return out
 
     def status(self) -> int:

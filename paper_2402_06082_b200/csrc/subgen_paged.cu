@@ -41,7 +41,7 @@ bool odd_stride(int64_t s, int dtype) { return (s * (int64_t)elem(dtype)) % 16 !
 
 // Also makes the kernel's view of it; the stride of an axis of one is not looked at.
 int check_heads(const char* fn, const char* name, const subgen_heads* x, int n, int heads, int d, int dtype, HeadsView* v) {
-    if (!x || !x->p) return fail(SUBGEN_EINVAL, "%s: %s must not be NULL", fn, name);
+    if (!x->p) return fail(SUBGEN_EINVAL, "%s: %s must not be NULL", fn, name);
     *v = HeadsView{x->p, n == 1 ? (int64_t)heads * d : x->token_stride, heads == 1 ? d : x->head_stride};
     if (v->ts <= 0 || v->hs <= 0) return fail(SUBGEN_EINVAL, "%s: %s: strides must be positive", fn, name);
     if (misaligned(x->p) || odd_stride(v->ts, dtype) || odd_stride(v->hs, dtype))
@@ -58,7 +58,7 @@ int check_shape(const char* fn, int n, int H, int Hkv, int d, int dtype) {
 }
 
 int check_rope(const char* fn, const subgen_rope* r, int d) {
-    if (!r || !r->words) return SUBGEN_OK;
+    if (!r->words) return SUBGEN_OK;
     if (r->rotary_dim <= 0 || r->rotary_dim > d || r->rotary_dim % 16)
         return fail(SUBGEN_EINVAL, "%s: rotary_dim must be a multiple of 16 and at most d", fn);
     return SUBGEN_OK;
@@ -116,6 +116,14 @@ int norm_rope(const NormRope& a, const PagedView& P, int d, int dtype, cudaStrea
     else f32 ? launch_norm_rope<float, 128, PAGED>(a, P, st) : launch_norm_rope<__nv_bfloat16, 128, PAGED>(a, P, st);
     CUDA_TRY(cudaGetLastError());
     return SUBGEN_OK;
+}
+
+void fill_norm_rope(NormRope* a, const subgen_qk_args* x, int H, int Hkv) {
+    a->n = x->n; a->H = H; a->Hkv = Hkv;
+    a->positions = x->positions;
+    a->words = (const unsigned long long*)x->rope.words;
+    a->rot = x->rope.rotary_dim; a->interleaved = x->rope.interleaved;
+    a->wq = x->wq; a->wk = x->wk; a->eps = x->eps;
 }
 
 // ---- attention ----
@@ -249,55 +257,49 @@ int subgen_rope_words(const double* f, int count, uint64_t* words) {
     return SUBGEN_OK;
 }
 
-int subgen_qk_norm_rope(const subgen_heads* q, const subgen_heads* k, const subgen_heads* q_out, const subgen_heads* k_out,
-                        int n, int H, int Hkv, int d, int dtype, const int* positions, const subgen_rope* rope,
-                        const void* wq, const void* wk, float eps, void* stream) {
+int subgen_qk_norm_rope(const subgen_qk_args* x, void* stream) {
     const char* fn = "subgen_qk_norm_rope";
-    const bool has_q = q && q->p, has_k = k && k->p;
-    int rc = check_shape(fn, n, has_q || !has_k ? H : 1, has_k || !has_q ? Hkv : 1, d, dtype);
-    if (!rc) rc = check_rope(fn, rope, d);
-    if (!rc) rc = check_norm(fn, wq, wk, eps);
-    if (rc || n == 0) return rc;
-    if (!has_q && !has_k) rc = fail(SUBGEN_EINVAL, "%s: q and k must not both be NULL", fn);
-    HeadsView vq = {nullptr, 0, 0}, vk = vq, vqo = vq, vko = vq;
-    if (!rc && has_q) rc = check_heads(fn, "q", q, n, H, d, dtype, &vq);
-    if (!rc && has_q) rc = check_heads(fn, "q_out", q_out, n, H, d, dtype, &vqo);
-    if (!rc && has_k) rc = check_heads(fn, "k", k, n, Hkv, d, dtype, &vk);
-    if (!rc && has_k) rc = check_heads(fn, "k_out", k_out, n, Hkv, d, dtype, &vko);
-    const bool turn = rope && rope->words;
-    if (!rc && turn && !positions) rc = fail(SUBGEN_EINVAL, "%s: a rotation needs positions", fn);
+    if (!x) return fail(SUBGEN_EINVAL, "%s: args must not be NULL", fn);
+    const bool has_q = x->q.p, has_k = x->k.p;
+    int rc = check_shape(fn, x->n, has_q || !has_k ? x->H : 1, has_k || !has_q ? x->Hkv : 1, x->d, x->dtype);
+    if (!rc) rc = check_rope(fn, &x->rope, x->d);
+    if (!rc) rc = check_norm(fn, x->wq, x->wk, x->eps);
+    if (rc || x->n == 0) return rc;
+    if (!has_q && !has_k) return fail(SUBGEN_EINVAL, "%s: q and k must not both be NULL", fn);
+    NormRope a;
+    memset(&a, 0, sizeof a);
+    if (has_q) rc = check_heads(fn, "q", &x->q, x->n, x->H, x->d, x->dtype, &a.q);
+    if (!rc && has_q) rc = check_heads(fn, "q_out", &x->q_out, x->n, x->H, x->d, x->dtype, &a.qo);
+    if (!rc && has_k) rc = check_heads(fn, "k", &x->k, x->n, x->Hkv, x->d, x->dtype, &a.k);
+    if (!rc && has_k) rc = check_heads(fn, "k_out", &x->k_out, x->n, x->Hkv, x->d, x->dtype, &a.ko);
+    if (!rc && x->rope.words && !x->positions) rc = fail(SUBGEN_EINVAL, "%s: a rotation needs positions", fn);
     if (rc) return rc;
-    NormRope a = {vq, vk, HeadsView{nullptr, 0, 0}, vqo, vko, n, has_q ? H : 0, has_k ? Hkv : 0, 1, positions,
-                  turn ? (const unsigned long long*)rope->words : nullptr, turn ? rope->rotary_dim : 0, turn ? rope->interleaved : 0,
-                  wq, wk, eps};
+    fill_norm_rope(&a, x, has_q ? x->H : 0, has_k ? x->Hkv : 0);
     PagedView none;
     memset(&none, 0, sizeof none);
-    return norm_rope<false>(a, none, d, dtype, (cudaStream_t)stream);
+    return norm_rope<false>(a, none, x->d, x->dtype, (cudaStream_t)stream);
 }
 
-int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* k, const subgen_heads* v,
-                        const subgen_heads* q, const subgen_heads* q_out, int n, int H, const int* positions,
-                        const subgen_rope* rope, const void* wq, const void* wk, float eps, void* stream) {
+int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_qk_args* x, void* stream) {
     const char* fn = "subgen_paged_append";
     PagedView P;
-    if (!cache || !batch) return fail(SUBGEN_EINVAL, "%s: cache and batch must not be NULL", fn);
-    const bool has_q = q && q->p;
-    int rc = check_shape(fn, n, has_q ? H : 1, cache->Hkv, cache->d, cache->dtype);
+    if (!cache || !batch || !x) return fail(SUBGEN_EINVAL, "%s: cache, batch and args must not be NULL", fn);
+    const bool has_q = x->q.p;
+    const int Hkv = cache->Hkv, d = cache->d, dtype = cache->dtype;
+    int rc = check_shape(fn, x->n, has_q ? x->H : 1, Hkv, d, dtype);
     if (!rc) rc = check_cache(fn, cache, batch, &P);
-    if (!rc) rc = check_rope(fn, rope, cache->d);
-    if (!rc) rc = check_norm(fn, wq, wk, eps);
-    if (rc || n == 0 || batch->B == 0) return rc;
-    HeadsView vk, vv, vq = {nullptr, 0, 0}, vqo = vq;
-    rc = check_heads(fn, "k", k, n, cache->Hkv, cache->d, cache->dtype, &vk);
-    if (!rc) rc = check_heads(fn, "v", v, n, cache->Hkv, cache->d, cache->dtype, &vv);
-    if (!rc && has_q) rc = check_heads(fn, "q", q, n, H, cache->d, cache->dtype, &vq);
-    if (!rc && has_q) rc = check_heads(fn, "q_out", q_out, n, H, cache->d, cache->dtype, &vqo);
+    if (!rc) rc = check_rope(fn, &x->rope, d);
+    if (!rc) rc = check_norm(fn, x->wq, x->wk, x->eps);
+    if (rc || x->n == 0 || batch->B == 0) return rc;
+    NormRope a;
+    memset(&a, 0, sizeof a);
+    rc = check_heads(fn, "k", &x->k, x->n, Hkv, d, dtype, &a.k);
+    if (!rc) rc = check_heads(fn, "v", &x->v, x->n, Hkv, d, dtype, &a.v);
+    if (!rc && has_q) rc = check_heads(fn, "q", &x->q, x->n, x->H, d, dtype, &a.q);
+    if (!rc && has_q) rc = check_heads(fn, "q_out", &x->q_out, x->n, x->H, d, dtype, &a.qo);
     if (rc) return rc;
-    const bool turn = rope && rope->words;
-    NormRope a = {vq, vk, vv, vqo, HeadsView{nullptr, 0, 0}, n, has_q ? H : 0, cache->Hkv, 1, positions,
-                  turn ? (const unsigned long long*)rope->words : nullptr, turn ? rope->rotary_dim : 0, turn ? rope->interleaved : 0,
-                  wq, wk, eps};
-    return norm_rope<true>(a, P, cache->d, cache->dtype, (cudaStream_t)stream);
+    fill_norm_rope(&a, x, has_q ? x->H : 0, Hkv);
+    return norm_rope<true>(a, P, d, dtype, (cudaStream_t)stream);
 }
 
 size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H) {
@@ -308,30 +310,30 @@ size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batc
     return (size_t)slot_count(P, n, H) * (cache->d * sizeof(float) + sizeof(float2));
 }
 
-int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_heads* q, const subgen_heads* out,
-                        int n, int H, float scale, int causal, void* workspace, size_t workspace_bytes, void* stream) {
+int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_attend_args* x, void* stream) {
     const char* fn = "subgen_paged_attend";
     PagedView P;
-    if (!cache || !batch) return fail(SUBGEN_EINVAL, "%s: cache and batch must not be NULL", fn);
-    int rc = check_shape(fn, n, H, cache->Hkv, cache->d, cache->dtype);
+    if (!cache || !batch || !x) return fail(SUBGEN_EINVAL, "%s: cache, batch and args must not be NULL", fn);
+    const int n = x->n, H = x->H, d = cache->d;
+    int rc = check_shape(fn, n, H, cache->Hkv, d, cache->dtype);
     if (!rc) rc = check_cache(fn, cache, batch, &P);
     if (rc) return rc;
-    const int G = H / cache->Hkv, d = cache->d;
+    const int G = H / cache->Hkv;
     if (H % cache->Hkv || (G != 1 && G != 2 && G != 4 && G != 8)) return fail(SUBGEN_EINVAL, "%s: H / Hkv must be 1, 2, 4 or 8", fn);
-    if (!(scale > 0.f) || !isfinite(scale)) return fail(SUBGEN_EINVAL, "%s: scale must be positive and finite", fn);
+    if (!(x->scale > 0.f) || !isfinite(x->scale)) return fail(SUBGEN_EINVAL, "%s: scale must be positive and finite", fn);
     if (n == 0 || batch->B == 0) return SUBGEN_OK;
     HeadsView vq, vo;
-    rc = check_heads(fn, "q", q, n, H, d, cache->dtype, &vq);
-    if (!rc) rc = check_heads(fn, "out", out, n, H, d, cache->dtype, &vo);
+    rc = check_heads(fn, "q", &x->q, n, H, d, cache->dtype, &vq);
+    if (!rc) rc = check_heads(fn, "out", &x->out, n, H, d, cache->dtype, &vo);
     if (rc) return rc;
     const long long slots = slot_count(P, n, H);
     if (slots > 0x7fffffffLL) return fail(SUBGEN_EINVAL, "%s: too many rows in one call", fn);
     const size_t need = (size_t)slots * (d * sizeof(float) + sizeof(float2));
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
+    if (!x->workspace || ((uintptr_t)x->workspace & 255) || x->workspace_bytes < need)
         return fail(SUBGEN_ENOMEM, "%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, need);
     const int g_shift = G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : 3;
-    Attend a = {vq, vo, n, H, g_shift, causal != 0, scale * 1.4426950408889634f, (float*)workspace,
-                (float2*)((float*)workspace + slots * d)};
+    Attend a = {vq, vo, n, H, g_shift, x->causal != 0, x->scale * 1.4426950408889634f, (float*)x->workspace,
+                (float2*)((float*)x->workspace + slots * d)};
     cudaStream_t st = (cudaStream_t)stream;
     if (cache->dtype == SUBGEN_DTYPE_BF16) return d == 64 ? attend_tc<64>(P, a, st) : attend_tc<128>(P, a, st);
     return d == 64 ? attend_simt_rows<float, 64>(P, a, st) : attend_simt_rows<float, 128>(P, a, st);

@@ -234,7 +234,7 @@ struct Plan {
     __device__ Plan(const PagedView& P_, const Attend& a_) : P(P_), a(a_) {}
 
     __device__ __forceinline__ bool folds(int g, int* t0, int* t1) const {
-        const int b0 = __ldg(P.cu_group + g), b1 = __ldg(P.cu_group + g + 1);
+        const int b0 = min(max(__ldg(P.cu_group + g), 0), P.B), b1 = min(max(__ldg(P.cu_group + g + 1), 0), P.B);
         *t0 = __ldg(P.cu_q + b0);
         *t1 = __ldg(P.cu_q + b1);
         return b1 - b0 <= 1 || ((long long)(*t1 - *t0) << a.g_shift) >= (long long)(b1 - b0) * (RU / 2);
@@ -308,32 +308,27 @@ struct Plan {
         int* s = t + E + 1;
         if (threadIdx.x == 0) *flag = 0;
         __syncthreads();
-        bool bad = false;
-        for (int b = threadIdx.x; b <= P.B; b += blockDim.x) {
-            const int x = __ldg(P.cu_q + b);
-            bad |= b == 0 ? x < 0 : x < __ldg(P.cu_q + b - 1);
-            bad |= x > a.n;
-        }
-        for (int g = threadIdx.x; g <= P.groups && P.groups; g += blockDim.x) {
-            const int x = __ldg(P.cu_group + g);
-            bad |= g == 0 ? x != 0 : x < __ldg(P.cu_group + g - 1);
-            bad |= g == P.groups ? x != P.B : x > P.B;
-        }
-        if (bad) *flag = 1;
-        __syncthreads();
-        if (*flag == 0) {
-            for (int i = threadIdx.x; i < E; i += blockDim.x) {
-                const Entry e = entry(i);
-                long long w = 0;
-                int sl = 0;
+        for (int i = threadIdx.x; i < E; i += blockDim.x) {
+            const Entry e = entry(i);
+            bool bad;
+            if (i < P.groups) {
+                const int b0 = __ldg(P.cu_group + i), b1 = __ldg(P.cu_group + i + 1);
+                bad = b0 < 0 || b1 < b0 || b1 > P.B || (i == 0 && b0 != 0) || (i == P.groups - 1 && b1 != P.B);
+            } else {
+                bad = e.tok0 < 0 || e.nq < 0 || (long long)e.tok0 + e.nq > a.n;
+            }
+            long long w = 0;
+            int sl = 0;
+            if (bad) *flag = 1;
+            else {
                 for (int ru = 0; ru * RU < e.rows; ++ru) {
                     const int rows = unit_rows(e, ru);
                     w += unit_weight(unit_tiles(e, ru), rows);
                     sl = ru * RU + (DUAL && rows <= RU / 2 ? 2 * rows : rows);
                 }
-                t[i + 1] = (int)(w > kPlanWeight ? kPlanWeight : w);
-                s[i + 1] = sl;
             }
+            t[i + 1] = (int)(w > kPlanWeight ? kPlanWeight : w);
+            s[i + 1] = sl;
         }
         __syncthreads();
         if (threadIdx.x < 32 && *flag == 0) {

@@ -201,19 +201,14 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
     unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~(uintptr_t)1023);
     Smem& sm = *reinterpret_cast<Smem*>(base);
     typedef Plan<kPtRU, kPtKT, true, kPtLead> PlanT;
-    PlanT plan(P, a);
-    plan.build(base + ((sizeof(Smem) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
-    pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
-    int x = blockIdx.x * plan.chunk;
-    const int x1 = min(plan.total, x + plan.chunk);
-    if (x >= x1) return;
-
+    pdl_trigger();
     if (warp == 9) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (tid == 0) {
+    if (tid == 256) {
+        for (const CUtensorMap* m : {&mq, &mk, &mv}) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
         for (int i = 0; i < 2; ++i) {
             bar_init(&sm.q_full[i], 1); bar_init(&sm.q_empty[i], 2);
             bar_init(&sm.s_full[i], 1); bar_init(&sm.p_full[i], 4);
@@ -227,12 +222,17 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         sm.failed = 0;
     }
     tc_fence_before();
-    __syncthreads();
+    PlanT plan(P, a);
+    plan.build(base + ((sizeof(Smem) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
     tc_fence_after();
+    int x = blockIdx.x * plan.chunk;
+    const int x1 = min(plan.total, x + plan.chunk);
     const uint32_t tmem = (uint32_t)uniform((int)sm.tmem);
 
     // registers: three groups of four warps were launched with 168 a thread; 2 x 208 + 88 = 3 x 168
-    if (warp >= 8) {
+    if (x >= x1) {
+        // nothing of the line is left for this block
+    } else if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 11) {
             // ---- planner ----

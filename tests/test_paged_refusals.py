@@ -27,12 +27,20 @@ def _heads(**kw):
 
 
 def _attend(pages=None, batch=None, q=None, out=None, n=2, H=32, scale=1.0, ws=P, size=1 << 40):
-    return binding.load().subgen_paged_attend(pages or _pages(), batch or _batch(), q or _heads(), out or _heads(), n, H, scale, 1, ws, size, None)
+    pages, batch = pages or _pages(), batch or _batch()
+    args = binding.AttendArgs(q or _heads(), out or _heads(), ws, size, n, H, scale, 1)
+    return binding.load().subgen_paged_attend(C.addressof(pages), C.addressof(batch), bytes(args), None)
 
 
-def _append(pages=None, batch=None, k=None, v=None, q=None, q_out=None, n=2, H=32, rope=None, wk=None, eps=1e-6):
-    return binding.load().subgen_paged_append(pages or _pages(), batch or _batch(), k or _heads(), v or _heads(), q, q_out, n, H, None, rope,
-                                              None, wk, eps, None)
+def _qk(**kw):
+    f = dict(q=_heads(p=None), k=_heads(), v=_heads(), n=2, H=32, Hkv=8, d=128, dtype=1, eps=1e-6)
+    f.update(kw)
+    return binding.QkArgs(**f)
+
+
+def _append(pages=None, batch=None, **kw):
+    pages, batch = pages or _pages(), batch or _batch()
+    return binding.load().subgen_paged_append(C.addressof(pages), C.addressof(batch), bytes(_qk(**kw)), None)
 
 
 def _said():
@@ -68,9 +76,11 @@ def test_attend():
     assert _attend(out=_heads(token_stride=1025)) == -1 and "out" in _said()
     assert _attend(ws=None) == -2 and "workspace" in _said()
     assert _attend(ws=P + 64) == -2 and "aligned" in _said()
-    need = binding.load().subgen_paged_workspace_bytes(_pages(), _batch(), 2, 32)
+    pages, bad, batch = _pages(), _pages(d=32), _batch()
+    need = binding.load().subgen_paged_workspace_bytes(C.addressof(pages), C.addressof(batch), 2, 32)
     assert need > 0 and _attend(size=need - 1) == -2 and str(need) in _said()
-    assert binding.load().subgen_paged_workspace_bytes(_pages(d=32), _batch(), 2, 32) == 0
+    assert binding.load().subgen_paged_workspace_bytes(C.addressof(bad), C.addressof(batch), 2, 32) == 0
+    assert _attend(q=_heads(token_stride=0)) == -1 and "positive" in _said()
 
 
 def test_nothing_to_do():
@@ -81,7 +91,7 @@ def test_nothing_to_do():
 def test_append():
     assert _append(k=_heads(p=None)) == -1 and "k must not" in _said()
     assert _append(v=_heads(head_stride=4)) == -1 and "v:" in _said()
-    assert _append(q=_heads(), q_out=None) == -1 and "q_out" in _said()
+    assert _append(q=_heads()) == -1 and "q_out" in _said()
     assert _append(rope=binding.RopeDesc(P, 24, 0)) == -1 and "rotary_dim" in _said()
     assert _append(rope=binding.RopeDesc(P, 256, 0)) == -1 and "rotary_dim" in _said()
     assert _append(wk=P + 2) == -1 and "aligned" in _said()
@@ -89,15 +99,23 @@ def test_append():
 
 
 def test_qk_norm_rope():
-    f = binding.load().subgen_qk_norm_rope
-    h, r = _heads(), binding.RopeDesc(P, 128, 0)
-    assert f(None, None, None, None, 1, 8, 8, 128, 1, None, None, None, None, 0.0, None) == -1 and "both" in _said()
-    assert f(h, None, None, None, 1, 8, 8, 128, 1, None, None, None, None, 0.0, None) == -1 and "q_out" in _said()
-    assert f(h, h, h, h, 1, 8, 8, 128, 1, None, r, None, None, 0.0, None) == -1 and "positions" in _said()
-    assert f(h, h, h, h, 1, 8, 0, 128, 1, P, r, None, None, 0.0, None) == -1 and "heads" in _said()
-    assert f(h, h, h, h, 1, 8, 8, 80, 1, P, r, None, None, 0.0, None) == -1 and "d must" in _said()
-    assert f(h, h, h, h, 1, 8, 8, 128, 1, P, r, P, None, float("nan"), None) == -1 and "eps" in _said()
-    assert f(h, h, h, h, 0, 8, 8, 128, 1, None, r, None, None, 0.0, None) == 0
+    def f(**kw):
+        return binding.load().subgen_qk_norm_rope(bytes(_qk(**kw)), None)
+    h, none, r = _heads(), _heads(p=None), binding.RopeDesc(P, 128, 0)
+    assert f(k=none) == -1 and "both" in _said()
+    assert f(q=h, k=none) == -1 and "q_out" in _said()
+    assert f(k_out=h, rope=r) == -1 and "positions" in _said()
+    assert f(q=h, q_out=h, k_out=h, Hkv=0) == -1 and "heads" in _said()
+    assert f(k_out=h, d=80) == -1 and "d must" in _said()
+    assert f(k_out=h, positions=P, rope=r, wk=P, eps=float("nan")) == -1 and "eps" in _said()
+    assert f(k_out=h, rope=r, n=0) == 0
+    assert binding.load().subgen_qk_norm_rope(None, None) == -1 and "args" in _said()
+
+
+def test_packed_arguments_are_laid_out_as_the_structures():
+    assert binding._QK.size == C.sizeof(binding.QkArgs) and binding._ATTEND.size == C.sizeof(binding.AttendArgs)
+    a = binding.QkArgs.from_buffer_copy(binding._QK.pack(*range(1, 27), 0.5))
+    assert (a.q.p, a.q_out.head_stride, a.positions, a.rope.words, a.rope.interleaved, a.wk, a.n, a.dtype, a.eps) == (1, 12, 16, 17, 19, 21, 22, 26, 0.5)
 
 
 def test_rope_words():
