@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -85,7 +84,26 @@ class AttendArgs(C.Structure):
                 ("H", C.c_int), ("scale", C.c_float), ("causal", C.c_int)]
 
 
+class SubgenError(RuntimeError):
+    pass
+
+
 _lib = None
+_calls = None
+
+
+def _bind_calls(L):
+    """The calls module (csrc/calls.cpp), which the paged functions go through, over this library."""
+    global _calls
+    try:
+        from . import _calls as module
+    except ImportError as e:
+        raise RuntimeError("_calls.so is missing or was built for another torch: build it with "
+                           "`python paper_2402_06082_b200/build.py`; there is no fallback path") from e
+    at = [C.cast(getattr(L, "subgen_" + f), C.c_void_p).value
+          for f in ("qk_norm_rope", "paged_append", "paged_attend", "paged_workspace_bytes", "last_error")]
+    module.bind(SubgenError, *at)
+    _calls = module
 
 
 def load():
@@ -140,19 +158,16 @@ def load():
     L.subgen_exact_kcenter_counters.argtypes = [vp, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
     L.subgen_exact_export_tokens.argtypes = [vp, C.c_int, C.c_int, ip, ip]
     L.subgen_exact_attention_noalloc.argtypes = [vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp]
-    # descriptors by address, arguments as packed bytes (a call costs a few microseconds on the host, and that counts)
     L.subgen_rope_words.argtypes = [C.POINTER(C.c_double), C.c_int, C.POINTER(C.c_uint64)]
-    L.subgen_qk_norm_rope.argtypes = [C.c_char_p, vp]
-    L.subgen_paged_append.argtypes = [vp, vp, C.c_char_p, vp]
-    L.subgen_paged_workspace_bytes.argtypes = [vp, vp, C.c_int, C.c_int]
+    pp, bp = C.POINTER(PagesDesc), C.POINTER(BatchDesc)
+    L.subgen_qk_norm_rope.argtypes = [C.POINTER(QkArgs), vp]
+    L.subgen_paged_append.argtypes = [pp, bp, C.POINTER(QkArgs), vp]
+    L.subgen_paged_workspace_bytes.argtypes = [pp, bp, C.c_int, C.c_int]
     L.subgen_paged_workspace_bytes.restype = C.c_size_t
-    L.subgen_paged_attend.argtypes = [vp, vp, C.c_char_p, vp]
+    L.subgen_paged_attend.argtypes = [pp, bp, C.POINTER(AttendArgs), vp]
+    _bind_calls(L)
     _lib = L
     return L
-
-
-class SubgenError(RuntimeError):
-    pass
 
 
 def _check(rc: int):
@@ -435,37 +450,14 @@ def exact_attention_noalloc(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, o
 # ---- norms, rotation and the paged exact cache --------------------------------------------------
 #
 # These calls run on the current stream of their tensors' device and keep nothing between calls: outputs and scratch
-# come from torch's allocator, call by call, so captured graphs and calls on several streams do not share any.
+# come from torch's allocator, call by call, so captured graphs and calls on several streams do not share any. They go
+# through the calls module: a step of a small model makes several of them a layer, and ctypes would cost more on the
+# host than their kernels take.
 
-_QK = struct.Struct("@" + "Pqq" * 5 + "PPiiPP5if")                # QkArgs
-_ATTEND = struct.Struct("@" + "Pqq" * 2 + "PNiifi")               # AttendArgs
-_CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
-_NO_ROWS, _NO_ROPE = (0, 0, 0), (0, 0, 0)
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-
-
-def _call(fn, device: int, *args):
-    """fn(*args, current stream of the device) with the device current."""
-    if _current_device() == device:
-        return _check(fn(*args, _raw_stream(device)))
-    with torch.cuda.device(device):
-        return _check(fn(*args, _raw_stream(device)))
-
-
-def _rows(x: torch.Tensor, name: str, dtype: torch.dtype, device: int, shape):
-    s = x.stride()
-    if x.dtype is not dtype or x.get_device() != device or x.shape != shape or s[2] != 1:
-        raise ValueError("%s must be a %s tensor of shape %s on cuda:%d with unit stride along the last axis (got %s %s on %s)" %
-                         (name, dtype, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
-    return x.data_ptr(), s[0], s[1]
-
-
-def _whole(x: Optional[torch.Tensor], name: str, dtype: torch.dtype, device: int, shape) -> int:
-    if x is None:
-        return 0
-    if x.dtype is not dtype or x.get_device() != device or x.shape != shape or not x.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d (got %s %s on %s)" %
-                         (name, dtype, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
+def _whole(x: torch.Tensor, name: str, device: int, shape) -> int:
+    if x.dtype is not torch.int32 or x.get_device() != device or x.shape != shape or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s on cuda:%d (got %s %s on %s)" %
+                         (name, tuple(shape), device, x.dtype, tuple(x.shape), x.device))
     return x.data_ptr()
 
 
@@ -494,13 +486,7 @@ class Rope:
         _check(load().subgen_rope_words((C.c_double * (r // 2))(*f), r // 2, words.ctypes.data_as(C.POINTER(C.c_uint64))))
         self.d, self.rotary_dim, self.interleaved = int(d), r, bool(interleaved)
         self.words = torch.from_numpy(words.view(np.int64)).to(device)
-        self.device = self.words.get_device()
-        self._desc = (self.words.data_ptr(), r, int(self.interleaved))
-
-    def _for(self, d: int, device: int):
-        if self.device != device or self.d != d:
-            raise ValueError("rope was made for d = %d on device %d" % (self.d, self.device))
-        return self._desc
+        self._desc = (self.words.data_ptr(), r, int(self.interleaved), self.d, self.words.get_device())
 
 
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
@@ -511,40 +497,9 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     q [n, H, d], k [n, Hkv, d]: views with unit stride along d (slices of a fused projection). Returns (q_out, k_out), None for
     what was not given; an output may be its input.
     """
-    x = k if q is None else q
-    if x is None:
-        raise ValueError("q and k must not both be None")
-    dev, dt = _cuda(x, "q and k"), x.dtype
-    n, H, d = x.shape
-    Hkv, qp, kp, qo, ko = 1, _NO_ROWS, _NO_ROWS, _NO_ROWS, _NO_ROWS
-    if dt not in _CODES:
-        raise ValueError("dtype must be torch.float32 or torch.bfloat16")
-    if q is None:
-        H, q_out = 1, None
-    else:
-        shape = (n, H, d)
-        qp = _rows(q, "q", dt, dev, shape)
-        if q_out is None:
-            q_out = q.new_empty(shape)
-            qo = (q_out.data_ptr(), H * d, d)
-        else:
-            qo = _rows(q_out, "q_out", dt, dev, shape)
-    if k is None:
-        k_out = None
-    else:
-        Hkv = k.shape[1]
-        shape = (n, Hkv, d)
-        kp = _rows(k, "k", dt, dev, shape)
-        if k_out is None:
-            k_out = k.new_empty(shape)
-            ko = (k_out.data_ptr(), Hkv * d, d)
-        else:
-            ko = _rows(k_out, "k_out", dt, dev, shape)
-    args = _QK.pack(*qp, *kp, 0, 0, 0, *qo, *ko, _whole(positions, "positions", torch.int32, dev, (n,)),
-                    *(_NO_ROPE if rope is None else rope._for(d, dev)), _whole(wq, "wq", dt, dev, (d,)), _whole(wk, "wk", dt, dev, (d,)),
-                    n, H, Hkv, d, _CODES[dt], eps)
-    _call(load().subgen_qk_norm_rope, dev, args)
-    return q_out, k_out
+    if _calls is None:
+        load()
+    return _calls.qk_norm_rope(q, k, positions, None if rope is None else rope._desc, wq, wk, eps, q_out, k_out)
 
 
 class PagedBatch:
@@ -566,13 +521,12 @@ class PagedBatch:
         if table.dim() != 2 or (g and prefix_table.dim() != 2):
             raise ValueError("page tables are two-dimensional")
         self.tensors = (cu_q, lengths, table, cu_group, prefix_len, prefix_table)
-        i32 = torch.int32
-        self._desc = BatchDesc(B, _whole(cu_q, "cu_q", i32, dev, (B + 1,)), _whole(lengths, "lengths", i32, dev, (B,)),
-                               _whole(table, "table", i32, dev, (B, table.shape[1])), table.shape[1], g)
+        self._desc = BatchDesc(B, _whole(cu_q, "cu_q", dev, (B + 1,)), _whole(lengths, "lengths", dev, (B,)),
+                               _whole(table, "table", dev, (B, table.shape[1])), table.shape[1], g)
         if g:
-            self._desc.cu_group = _whole(cu_group, "cu_group", i32, dev, (g + 1,))
-            self._desc.prefix_len = _whole(prefix_len, "prefix_len", i32, dev, (g,))
-            self._desc.prefix_table = _whole(prefix_table, "prefix_table", i32, dev, (g, prefix_table.shape[1]))
+            self._desc.cu_group = _whole(cu_group, "cu_group", dev, (g + 1,))
+            self._desc.prefix_len = _whole(prefix_len, "prefix_len", dev, (g,))
+            self._desc.prefix_table = _whole(prefix_table, "prefix_table", dev, (g, prefix_table.shape[1]))
             self._desc.prefix_stride = prefix_table.shape[1]
         self._at = C.addressof(self._desc)
 
@@ -585,11 +539,10 @@ class PagedCache:
         dev = self.device = _cuda(K, "K")
         if K.dim() != 4 or K.stride(3) != 1 or V.shape != K.shape or V.stride() != K.stride() or V.dtype is not K.dtype or V.get_device() != dev:
             raise ValueError("K and V must be [pages, Hkv, page, d] tensors of one type, device and layout, unit stride along d")
-        self._L = load()
+        load()
         self.K, self.V, self.dtype = K, V, K.dtype
         self.pages, self.Hkv, self.page, self.d = K.shape
         self._status = torch.zeros(1, dtype=torch.int32, device=K.device)
-        self._bytes = K.new_empty(0, dtype=torch.uint8)
         self._desc = PagesDesc(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), self.pages, self.page, self.Hkv,
                                self.d, _dtype_code(K.dtype), self._status.data_ptr())
         self._at = C.addressof(self._desc)
@@ -604,44 +557,13 @@ class PagedCache:
                q: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Write the new tokens k, v [n, Hkv, d] into their pages, k normed (if wk) and rotated (if rope) on the way; q [n, H, d]
         goes the same way into q_out, which is returned (None without q). One kernel; see subgen_paged_append."""
-        dev, dt, d, n, H = self.device, self.dtype, self.d, k.shape[0], 1
-        shape = (n, self.Hkv, d)
-        kp, vp, qp, qo = _rows(k, "k", dt, dev, shape), _rows(v, "v", dt, dev, shape), _NO_ROWS, _NO_ROWS
-        if q is None:
-            q_out = None
-        else:
-            H = q.shape[1]
-            shape = (n, H, d)
-            qp = _rows(q, "q", dt, dev, shape)
-            if q_out is None:
-                q_out = q.new_empty(shape)
-                qo = (q_out.data_ptr(), H * d, d)
-            else:
-                qo = _rows(q_out, "q_out", dt, dev, shape)
-        args = _QK.pack(*qp, *kp, *vp, *qo, 0, 0, 0, _whole(positions, "positions", torch.int32, dev, (n,)),
-                        *(_NO_ROPE if rope is None else rope._for(d, dev)), _whole(wq, "wq", dt, dev, (d,)),
-                        _whole(wk, "wk", dt, dev, (d,)), n, H, 0, 0, 0, eps)
-        _call(self._L.subgen_paged_append, dev, self._at, self._batch(batch), args)
-        return q_out
+        return _calls.append(self._at, self.device, self._batch(batch), k, v, positions, None if rope is None else rope._desc, wk, eps,
+                             q, wq, q_out)
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, scale: float = 1.0, causal: bool = True, out: Optional[torch.Tensor] = None):
         """softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for q [n, H, d], whose keys are in the cache already; the prefix is
         read once per group. Rows of `out` behind the last sequence are not written. See subgen_paged_attend."""
-        dev, at = self.device, self._batch(batch)
-        n, H, _ = q.shape
-        shape = (n, H, self.d)
-        qp = _rows(q, "q", self.dtype, dev, shape)
-        if out is None:
-            out = q.new_empty(shape)
-            op = (out.data_ptr(), H * self.d, self.d)
-        else:
-            op = _rows(out, "out", self.dtype, dev, shape)
-        size = self._L.subgen_paged_workspace_bytes(self._at, at, n, H)
-        if size == 0:
-            raise SubgenError(self._L.subgen_last_error().decode())
-        ws = self._bytes.new_empty(size)                          # torch aligns allocations to 512 bytes
-        _call(self._L.subgen_paged_attend, dev, self._at, at, _ATTEND.pack(*qp, *op, ws.data_ptr(), size, n, H, scale, causal))
-        return out
+        return _calls.attend(self._at, self.device, self._batch(batch), q, scale, causal, out)
 
     def status(self) -> int:
         """Waits for the device's work, returns the status bits that calls on this cache have set (0: none)."""

@@ -101,12 +101,14 @@ int check_cache(const char* fn, const subgen_pages* c, const subgen_batch* b, Pa
 template <typename T, int D, bool PAGED>
 void launch_norm_rope(NormRope a, const PagedView& P, cudaStream_t st) {
     constexpr int RPW = 32 / (D / (16 / (int)sizeof(T)) / 2);
-    const int heads = a.H + (PAGED ? 2 : 1) * a.Hkv, groups = (heads + RPW - 1) / RPW;
+    const int groups = (a.H + RPW - 1) / RPW + (PAGED ? 2 : 1) * ((a.Hkv + RPW - 1) / RPW);
     // enough warps to fill the SMs (16 a SM); beyond that a token stays with one warp
     const int want = (kSMs * 16 + a.n - 1) / a.n;
     a.parts = want < 1 ? 1 : want > groups ? groups : want;
     const long long warps = (long long)a.n * a.parts;
-    norm_rope_kernel<T, D, PAGED><<<(unsigned)((warps + kNrThreads / 32 - 1) / (kNrThreads / 32)), kNrThreads, 0, st>>>(a, P);
+    const unsigned blocks = (unsigned)((warps + kNrThreads / 32 - 1) / (kNrThreads / 32));
+    if (a.parts == 1) norm_rope_kernel<T, D, PAGED, 4><<<blocks, kNrThreads, 0, st>>>(a, P);
+    else norm_rope_kernel<T, D, PAGED, 1><<<blocks, kNrThreads, 0, st>>>(a, P);
 }
 
 template <bool PAGED>

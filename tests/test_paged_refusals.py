@@ -29,7 +29,7 @@ def _heads(**kw):
 def _attend(pages=None, batch=None, q=None, out=None, n=2, H=32, scale=1.0, ws=P, size=1 << 40):
     pages, batch = pages or _pages(), batch or _batch()
     args = binding.AttendArgs(q or _heads(), out or _heads(), ws, size, n, H, scale, 1)
-    return binding.load().subgen_paged_attend(C.addressof(pages), C.addressof(batch), bytes(args), None)
+    return binding.load().subgen_paged_attend(pages, batch, args, None)
 
 
 def _qk(**kw):
@@ -40,7 +40,7 @@ def _qk(**kw):
 
 def _append(pages=None, batch=None, **kw):
     pages, batch = pages or _pages(), batch or _batch()
-    return binding.load().subgen_paged_append(C.addressof(pages), C.addressof(batch), bytes(_qk(**kw)), None)
+    return binding.load().subgen_paged_append(pages, batch, _qk(**kw), None)
 
 
 def _said():
@@ -77,9 +77,9 @@ def test_attend():
     assert _attend(ws=None) == -2 and "workspace" in _said()
     assert _attend(ws=P + 64) == -2 and "aligned" in _said()
     pages, bad, batch = _pages(), _pages(d=32), _batch()
-    need = binding.load().subgen_paged_workspace_bytes(C.addressof(pages), C.addressof(batch), 2, 32)
+    need = binding.load().subgen_paged_workspace_bytes(pages, batch, 2, 32)
     assert need > 0 and _attend(size=need - 1) == -2 and str(need) in _said()
-    assert binding.load().subgen_paged_workspace_bytes(C.addressof(bad), C.addressof(batch), 2, 32) == 0
+    assert binding.load().subgen_paged_workspace_bytes(bad, batch, 2, 32) == 0
     assert _attend(q=_heads(token_stride=0)) == -1 and "positive" in _said()
 
 
@@ -100,7 +100,7 @@ def test_append():
 
 def test_qk_norm_rope():
     def f(**kw):
-        return binding.load().subgen_qk_norm_rope(bytes(_qk(**kw)), None)
+        return binding.load().subgen_qk_norm_rope(_qk(**kw), None)
     h, none, r = _heads(), _heads(p=None), binding.RopeDesc(P, 128, 0)
     assert f(k=none) == -1 and "both" in _said()
     assert f(q=h, k=none) == -1 and "q_out" in _said()
@@ -110,12 +110,6 @@ def test_qk_norm_rope():
     assert f(k_out=h, positions=P, rope=r, wk=P, eps=float("nan")) == -1 and "eps" in _said()
     assert f(k_out=h, rope=r, n=0) == 0
     assert binding.load().subgen_qk_norm_rope(None, None) == -1 and "args" in _said()
-
-
-def test_packed_arguments_are_laid_out_as_the_structures():
-    assert binding._QK.size == C.sizeof(binding.QkArgs) and binding._ATTEND.size == C.sizeof(binding.AttendArgs)
-    a = binding.QkArgs.from_buffer_copy(binding._QK.pack(*range(1, 27), 0.5))
-    assert (a.q.p, a.q_out.head_stride, a.positions, a.rope.words, a.rope.interleaved, a.wk, a.n, a.dtype, a.eps) == (1, 12, 16, 17, 19, 21, 22, 26, 0.5)
 
 
 def test_rope_words():
@@ -155,3 +149,7 @@ def test_python_refusals():
         binding.qk_norm_rope(None, None)
     with pytest.raises(ValueError, match="CUDA"):
         binding.PagedBatch(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        binding.qk_norm_rope(torch.zeros(1, 1, 64).half(), [1.0])
+    with pytest.raises(TypeError):
+        binding._calls.append(1, 2, 3)
