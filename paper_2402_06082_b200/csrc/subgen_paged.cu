@@ -153,9 +153,12 @@ template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
 int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
-    // a block per 32 rows, as far as the grid goes
-    const long long units = ((long long)P.B + ((long long)a.n << a.g_shift) / (RU < 32 ? RU : 32)) * P.Hkv;
-    cfg.gridDim = dim3((unsigned)(units < kSMs * 2 ? units : kSMs * 2));                 // two fit an SM
+        // parts of a row unit that a block joins at a time: 4 rows while the blocks that fit can take all rows at once, else 8,
+    // and 16 for prompts, most of whose rows need none (RU is a multiple of each)
+    const long long rows = (long long)a.n * a.H, once = kSMs * kMergeBlocks;
+    const int part = rows <= once * 4 ? 4 : rows <= once * 8 ? 8 : 16;
+    const long long units = ((long long)P.B + ((long long)a.n << a.g_shift) / part) * P.Hkv;
+    cfg.gridDim = dim3((unsigned)(units < kSMs * kMergeBlocks ? units : kSMs * kMergeBlocks));
     cfg.blockDim = dim3(kMergeThreads);
     cfg.dynamicSmemBytes = plan_bytes(P.B + P.groups) + (size_t)4 * (P.B + 1);
     cfg.stream = st;
@@ -164,7 +167,7 @@ int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t s
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_merge_kernel<T, D, RU, KT, DUAL, LEAD>, P, a, blocks));
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_merge_kernel<T, D, RU, KT, DUAL, LEAD>, P, a, blocks, part));
     return SUBGEN_OK;
 }
 

@@ -430,24 +430,28 @@ struct Plan {
 };
 
 // Joins the partials of every row that has some (rows whose result went out directly are left alone) and writes 0 for
-// rows that see nothing, NaN for rows of a sequence whose lengths or pages are unusable. One block per 32 rows of a row unit of
-// a sequence and KV head. A row's partials are dealt to WPR warps (as many as the block has left for the unit's rows, so
-// that one sequence's long list is read by all of them); a lane looks after one partial's weight, then the warp adds the
-// numerators, all loads of a batch in flight, and the warps of a row join through shared memory.
-constexpr int kMergeThreads = 256;
+// rows that see nothing, NaN for rows of a sequence whose lengths or pages are unusable. An item is up to `part` rows of a row
+// unit of a sequence and KV head; a block's threads first sort out its items that have anything to join (most prompt rows
+// do not), which needs the plan alone and so runs while the attention kernel's last blocks finish. A row's partials are
+// dealt to WPR warps (as many as the block has left for the item's rows, so that one sequence's long list is read by all
+// of them); a lane looks after one partial's weight, then the warp adds the numerators, and the warps of a row join
+// through shared memory. Latency, not bandwidth, is what counts here: one pass over the own and the prefix partials
+// together, and registers for three blocks an SM.
+constexpr int kMergeThreads = 256, kMergeBlocks = 3;
 
 template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
-__global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P, Attend a, int nblk) {
-    constexpr int NW = kMergeThreads / 32, VL = D / 32, PART = RU < 32 ? RU : 32;   // PART: rows that one block joins at a time
+__global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kernel(PagedView P, Attend a, int nblk, int part) {
+    constexpr int NW = kMergeThreads / 32, VL = D / 32;
     extern __shared__ __align__(16) unsigned char sm_plan[];
-    __shared__ int flag;
-    __shared__ int units;
+    __shared__ int flag, units;
+    __shared__ int4 todo[kMergeThreads];              // head, sequence, first row, where its unit starts on the line
+    __shared__ int todo_warp[NW];
     __shared__ float join[NW][D];
     __shared__ float2 join_stat[NW];
     typedef Plan<RU, KT, DUAL, LEAD> PlanT;
     PlanT plan(P, a);
     plan.build(sm_plan, &flag, nblk);
-    int* uscan = (int*)sm_plan + 2 * (plan.E + 1);    // [B+1] parts of PART rows before each sequence
+    int* uscan = (int*)sm_plan + 2 * (plan.E + 1);    // [B+1] parts before each sequence
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (plan.broken) {
         if (blockIdx.x == 0 && tid == 0) paged_status(P, kStPage);
@@ -457,7 +461,7 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
         int at = 0;
         for (int i0 = 0; i0 < P.B; i0 += 32) {
             const int b = i0 + lane;
-            int x = b < P.B ? (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + PART - 1) / PART : 0;
+            int x = b < P.B ? (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + part - 1) / part : 0;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const int xo = __shfl_up_sync(0xffffffffu, x, off);
@@ -469,142 +473,169 @@ __global__ void __launch_bounds__(kMergeThreads) paged_merge_kernel(PagedView P,
         if (lane == 0) { uscan[0] = 0; units = at; }
     }
     __syncthreads();
-    pdl_wait();
     const int items = units * P.Hkv, chunk = plan.chunk;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const int h = item / units, u = item - h * units;
-        int lo = 0, hi = P.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (uscan[mid] <= u) lo = mid; else hi = mid - 1;
-        }
-        const int b = lo, part0 = (u - uscan[lo]) * PART, ru = part0 / RU, ei = P.groups + b;
-        const Entry e = plan.entry(ei);
-        const int rows = plan.unit_rows(e, ru), tiles = plan.unit_tiles(e, ru), w = plan.unit_weight(tiles, rows), sh = PlanT::shift(rows);
+    // first position of the line that belongs to row unit ru of a sequence's entry
+    auto unit_start = [&](const Entry& e, int ei, int h, int ru) {
         int u0 = h * plan.head_w + plan.tscan[ei];
         for (int k = 0; k < ru; ++k) u0 += plan.unit_weight(plan.unit_tiles(e, k), RU);
-        const int c0 = u0 / chunk, c1 = w ? (u0 + w - 1) / chunk : c0 - 1;
-        if (tiles && plan.is_direct(e, ei, rows, tiles)) {
-            // whole in one block: the one that holds the first tile also holds the last
-            const int p = (u0 + LEAD) / chunk;
-            if (PlanT::tile_at(min((p + 1) * chunk, u0 + w) - u0, sh) == tiles) continue;
-        }
-        int g = -1;
-        Entry ge;
-        ge.bad = ge.rows = ge.tok0 = 0;
-        if (P.groups) {
-            g = plan.group_of(b);
-            ge = plan.entry(g);
-            if (!ge.rows) g = -1;                                    // folded (or no rows)
-        }
-        const int bad = e.bad | (g >= 0 ? ge.bad : 0), pt = g >= 0 ? plan.prefix_tiles(ge) : 0;
-        if (bad && tid == 0) paged_status(P, kStPage);
-        const int wpr = rows >= NW ? 1 : rows > 4 ? 1 : rows > 2 ? NW / 4 : rows > 1 ? NW / 2 : NW;   // warps per row
-        const int rows_begin = part0 - ru * RU, rows_end = min(rows, rows_begin + PART);
-        for (int r0 = rows_begin; r0 < rows_end; r0 += NW / wpr) {
-            const int r = r0 + warp / wpr, sub = warp % wpr;
-            float acc[VL], m = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int j = 0; j < VL; ++j) acc[j] = 0.f;
-            // partials of one unit: 1 or 2 of every block in [d0, d1]; v0: the unit's start on the line, vw its weight
-            auto collect = [&](int v0, int vw, int vrows, int d0, int d1, int base) {
-                const int vsh = PlanT::shift(vrows), per = DUAL && !vsh ? 1 : 0, count = (d1 - d0 + 1) << per;
-                for (int i0 = sub * 32; i0 < count; i0 += wpr * 32) {
-                    const int i = i0 + lane, c = d0 + (i >> per), second = i & ((1 << per) - 1);
-                    float2 st = make_float2(-INFINITY, 0.f);
-                    int slot = 0;
-                    bool have = false;
-                    if (i < count) {
-                        const int t0 = PlanT::tile_at(max(c * chunk, v0) - v0, vsh), t1 = PlanT::tile_at(min((c + 1) * chunk, v0 + vw) - v0, vsh);
-                        have = t1 - t0 > second;
-                        slot = base + c * RU + (second ? vrows : 0);
-                    }
-                    if (have) st = __ldcg(a.stat + slot);
-                    float top = st.x;
-#pragma unroll
-                    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                    const float mn = fmaxf(m, top), bs = mn == -INFINITY ? 0.f : mn, al = exp2f(m - bs);
-                    const float f = have ? exp2f(st.x - bs) : 0.f;
-                    float sum = have ? st.y * f : 0.f;
-#pragma unroll
-                    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-                    m = mn;
-                    l = l * al + sum;
-#pragma unroll
-                    for (int j = 0; j < VL; ++j) acc[j] *= al;
-                    unsigned todo = __ballot_sync(0xffffffffu, have);
-                    while (todo) {
-                        float x[8][VL], fx[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const int src = todo ? __ffs(todo) - 1 : -1;
-                            todo &= todo - 1;
-                            const int s = __shfl_sync(0xffffffffu, slot, src & 31);
-                            fx[k] = __shfl_sync(0xffffffffu, f, src & 31);
-                            if (src < 0) fx[k] = 0.f;
-#pragma unroll
-                            for (int j = 0; j < VL; ++j) x[k][j] = 0.f;
-                            if (src >= 0) {
-                                const float* y = a.part + (long long)s * D + lane * VL;
-                                if constexpr (VL == 4) {
-                                    const float4 v = __ldcg(reinterpret_cast<const float4*>(y));
-                                    x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
-                                } else {
-                                    const float2 v = __ldcg(reinterpret_cast<const float2*>(y));
-                                    x[k][0] = v.x; x[k][1] = v.y;
-                                }
-                            }
-                        }
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-#pragma unroll
-                            for (int j = 0; j < VL; ++j) acc[j] = fmaf(x[k][j], fx[k], acc[j]);
-                    }
-                }
-            };
-            if (r < rows_end) {
-                if (w) collect(u0, w, rows, c0, c1, plan.slot_of(ei, ru, h, 0) + r);
-                if (pt) {
-                    const int prow = ru * RU + r + ((e.tok0 - ge.tok0) << a.g_shift), pru = prow / RU, prows = plan.unit_rows(ge, pru);
-                    const int v0 = h * plan.head_w + plan.tscan[g] + pru * plan.unit_weight(pt, RU), vw = plan.unit_weight(pt, prows);
-                    collect(v0, vw, prows, v0 / chunk, (v0 + vw - 1) / chunk, plan.slot_of(g, pru, h, 0) + prow - pru * RU);
-                }
+        return u0;
+    };
+    bool waited = false;
+    for (int first = 0; first * gridDim.x + blockIdx.x < items; first += kMergeThreads) {
+        bool need = false;
+        const int mine = (first + tid) * gridDim.x + blockIdx.x;
+        int4 what = make_int4(0, 0, 0, 0);
+        if (mine < items) {
+            const int h = mine / units, u = mine - h * units;
+            int lo = 0, hi = P.B - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (uscan[mid] <= u) lo = mid; else hi = mid - 1;
             }
-            if (wpr > 1) {
-                __syncthreads();
-                if (lane == 0) join_stat[warp] = make_float2(m, l);
-#pragma unroll
-                for (int j = 0; j < VL; ++j) join[warp][lane * VL + j] = acc[j];
-                __syncthreads();
-                float mm = -INFINITY;
-                for (int k = 0; k < wpr; ++k) mm = fmaxf(mm, join_stat[warp - sub + k].x);
-                const float bs = mm == -INFINITY ? 0.f : mm;
-                l = 0.f;
+            const int b = lo, row0 = (u - uscan[lo]) * part, ei = P.groups + b, ru = row0 / RU;
+            const Entry e = plan.entry(ei);
+            const int rows = plan.unit_rows(e, ru), tiles = plan.unit_tiles(e, ru), w = plan.unit_weight(tiles, rows), u0 = unit_start(e, ei, h, ru);
+            // a direct unit went out whole if the block that holds its first tile also holds the last
+            need = !tiles || !plan.is_direct(e, ei, rows, tiles) ||
+                   PlanT::tile_at(min(((u0 + LEAD) / chunk + 1) * chunk, u0 + w) - u0, PlanT::shift(rows)) != tiles;
+            what = make_int4(h, b, row0, u0);
+        }
+        const unsigned some = __ballot_sync(0xffffffffu, need);
+        __syncthreads();                                             // the list before this one is done with
+        if (lane == 0) todo_warp[warp] = __popc(some);
+        __syncthreads();
+        int before = 0, count = 0;
+        for (int k = 0; k < NW; ++k) { before += k < warp ? todo_warp[k] : 0; count += todo_warp[k]; }
+        if (need) todo[before + __popc(some & ((1u << lane) - 1u))] = what;
+        __syncthreads();
+        if (!waited) { pdl_wait(); waited = true; }
+        for (int it = 0; it < count; ++it) {
+            const int h = todo[it].x, b = todo[it].y, row0 = todo[it].z, u0 = todo[it].w;
+            const int ei = P.groups + b, ru = row0 / RU;
+            const Entry e = plan.entry(ei);
+            const int rows = plan.unit_rows(e, ru), tiles = plan.unit_tiles(e, ru), w = plan.unit_weight(tiles, rows), sh = PlanT::shift(rows);
+            const int c0 = u0 / chunk, c1 = w ? (u0 + w - 1) / chunk : c0 - 1;
+            const int per = DUAL && !sh ? 1 : 0, own = (c1 - c0 + 1) << per;
+            int g = -1;
+            Entry ge;
+            ge.bad = ge.rows = ge.tok0 = ge.P = 0;
+            if (P.groups) {
+                g = plan.group_of(b);
+                ge = plan.entry(g);
+                if (!ge.rows) g = -1;                                // folded (or no rows)
+            }
+            const int bad = e.bad | (g >= 0 ? ge.bad : 0), pt = g >= 0 ? plan.prefix_tiles(ge) : 0;
+            if (bad && tid == 0) paged_status(P, kStPage);
+            const int rows_begin = row0 - ru * RU, rows_end = min(rows, rows_begin + part), here = rows_end - rows_begin;
+            const int wpr = here > 4 ? 1 : here > 2 ? NW / 4 : here > 1 ? NW / 2 : NW;      // warps per row
+            for (int r0 = rows_begin; r0 < rows_end; r0 += NW / wpr) {
+                const int r = r0 + warp / wpr, sub = warp % wpr;
+                float acc[VL], m = -INFINITY, l = 0.f;
 #pragma unroll
                 for (int j = 0; j < VL; ++j) acc[j] = 0.f;
-                for (int k = 0; k < wpr; ++k) {
-                    const float2 st = join_stat[warp - sub + k];
-                    const float f = exp2f(st.x - bs);
-                    l = fmaf(st.y, f, l);
+                if (r < rows_end) {
+                    // partials: 1 or 2 (`per`) of every block of the unit's, then of the prefix's run on the line
+                    int v0 = 0, vw = 0, vrows = RU, vper = 0, vc = 0, vslot = 0, all = own;
+                    if (pt) {
+                        const int prow = ru * RU + r + ((e.tok0 - ge.tok0) << a.g_shift), pru = prow / RU;
+                        vrows = plan.unit_rows(ge, pru);
+                        vw = plan.unit_weight(pt, vrows);
+                        v0 = h * plan.head_w + plan.tscan[g] + pru * plan.unit_weight(pt, RU);
+                        vper = DUAL && !PlanT::shift(vrows) ? 1 : 0;
+                        vc = v0 / chunk;
+                        vslot = plan.slot_of(g, pru, h, 0) + prow - pru * RU;
+                        all += ((v0 + vw - 1) / chunk - vc + 1) << vper;
+                    }
+                    const int oslot = plan.slot_of(ei, ru, h, 0) + r;
+                    for (int i0 = 0; i0 < all; i0 += wpr * 32) {
+                        const int i = i0 + lane * wpr + sub;
+                        const bool pre = i >= own;
+                        const int k = pre ? i - own : i, p = pre ? vper : per, c = (pre ? vc : c0) + (k >> p), second = k & ((1 << p) - 1);
+                        const int z0 = pre ? v0 : u0, zw = pre ? vw : w, zrows = pre ? vrows : rows, zsh = PlanT::shift(zrows);
+                        const int t0 = PlanT::tile_at(max(c * chunk, z0) - z0, zsh), t1 = PlanT::tile_at(min((c + 1) * chunk, z0 + zw) - z0, zsh);
+                        const bool have = i < all && t1 - t0 > second;
+                        const int slot = (pre ? vslot : oslot) + c * RU + (second ? zrows : 0);
+                        float2 st = make_float2(-INFINITY, 0.f);
+                        if (have) st = __ldcg(a.stat + slot);
+                        float top = st.x;
 #pragma unroll
-                    for (int j = 0; j < VL; ++j) acc[j] = fmaf(join[warp - sub + k][lane * VL + j], f, acc[j]);
+                        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                        const float mn = fmaxf(m, top), bs = mn == -INFINITY ? 0.f : mn, al = exp2f(m - bs);
+                        const float f = have ? exp2f(st.x - bs) : 0.f;
+                        float sum = have ? st.y * f : 0.f;
+#pragma unroll
+                        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                        m = mn;
+                        l = l * al + sum;
+#pragma unroll
+                        for (int j = 0; j < VL; ++j) acc[j] *= al;
+                        unsigned left = __ballot_sync(0xffffffffu, have);
+                        while (left) {
+                            float x[8][VL], fx[8];
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                const int src = left ? __ffs(left) - 1 : -1;
+                                left &= left - 1;
+                                const int s = __shfl_sync(0xffffffffu, slot, src & 31);
+                                fx[q] = __shfl_sync(0xffffffffu, f, src & 31);
+                                if (src < 0) fx[q] = 0.f;
+#pragma unroll
+                                for (int j = 0; j < VL; ++j) x[q][j] = 0.f;
+                                if (src >= 0) {
+                                    const float* y = a.part + (long long)s * D + lane * VL;
+                                    if constexpr (VL == 4) {
+                                        const float4 v = __ldcg(reinterpret_cast<const float4*>(y));
+                                        x[q][0] = v.x; x[q][1] = v.y; x[q][2] = v.z; x[q][3] = v.w;
+                                    } else {
+                                        const float2 v = __ldcg(reinterpret_cast<const float2*>(y));
+                                        x[q][0] = v.x; x[q][1] = v.y;
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                                for (int j = 0; j < VL; ++j) acc[j] = fmaf(x[q][j], fx[q], acc[j]);
+                        }
+                    }
                 }
-            }
-            if (r >= rows_end || sub) continue;
-            float inv = l == 0.f ? 0.f : 1.f / l;                    // l is NaN where a page was unusable
-            if (bad) inv = NAN;
-            const int row = ru * RU + r, tok = e.tok0 + (row >> a.g_shift), head = (h << a.g_shift) + (row & ((1 << a.g_shift) - 1));
-            T* y = (T*)a.o.p + tok * a.o.ts + head * a.o.hs + lane * VL;
-            if constexpr (sizeof(T) == 4) {
-                if constexpr (VL == 4) *reinterpret_cast<float4*>(y) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-                else *reinterpret_cast<float2*>(y) = make_float2(acc[0] * inv, acc[1] * inv);
-            } else {
+                if (wpr > 1) {
+                    __syncthreads();
+                    if (lane == 0) join_stat[warp] = make_float2(m, l);
 #pragma unroll
-                for (int j = 0; j < VL / 2; ++j)
-                    reinterpret_cast<__nv_bfloat162*>(y)[j] = __floats2bfloat162_rn(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+                    for (int j = 0; j < VL; ++j) join[warp][lane * VL + j] = acc[j];
+                    __syncthreads();
+                    float mm = -INFINITY;
+                    for (int k = 0; k < wpr; ++k) mm = fmaxf(mm, join_stat[warp - sub + k].x);
+                    const float bs = mm == -INFINITY ? 0.f : mm;
+                    l = 0.f;
+#pragma unroll
+                    for (int j = 0; j < VL; ++j) acc[j] = 0.f;
+                    for (int k = 0; k < wpr; ++k) {
+                        const float2 st = join_stat[warp - sub + k];
+                        const float f = exp2f(st.x - bs);
+                        l = fmaf(st.y, f, l);
+#pragma unroll
+                        for (int j = 0; j < VL; ++j) acc[j] = fmaf(join[warp - sub + k][lane * VL + j], f, acc[j]);
+                    }
+                }
+                if (r >= rows_end || sub) continue;
+                float inv = l == 0.f ? 0.f : 1.f / l;                // l is NaN where a page was unusable
+                if (bad) inv = NAN;
+                const int row = ru * RU + r, tok = e.tok0 + (row >> a.g_shift), head = (h << a.g_shift) + (row & ((1 << a.g_shift) - 1));
+                T* y = (T*)a.o.p + tok * a.o.ts + head * a.o.hs + lane * VL;
+                if constexpr (sizeof(T) == 4) {
+                    if constexpr (VL == 4) *reinterpret_cast<float4*>(y) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+                    else *reinterpret_cast<float2*>(y) = make_float2(acc[0] * inv, acc[1] * inv);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VL / 2; ++j)
+                        reinterpret_cast<__nv_bfloat162*>(y)[j] = __floats2bfloat162_rn(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+                }
             }
         }
     }
+    if (!waited) pdl_wait();
 }
 
 }  // namespace sgk
