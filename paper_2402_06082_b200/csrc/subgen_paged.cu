@@ -213,7 +213,7 @@ EncodeTiled encode_tiled() {
 int make_map(CUtensorMap* m, void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     const EncodeTiled f = encode_tiled();
     if (!f) return fail(SUBGEN_ECUDA, "cuTensorMapEncodeTiled is not available");
-    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     const CUresult r = f(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, p, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(SUBGEN_ECUDA, "cuTensorMapEncodeTiled failed (%d): strides of 2^40 bytes or more?", (int)r);
@@ -239,7 +239,13 @@ int attend_tc(const PagedView& P, const Attend& a, cudaStream_t st) {
     const cuuint64_t strides[3] = {(cuuint64_t)P.ts * 2, (cuuint64_t)P.hs * 2, (cuuint64_t)P.ps * 2};
     const cuuint32_t box[4] = {64, (cuuint32_t)(page < 128 ? page : 128), 1, 1};
     if (!rc) rc = make_map(&mk, P.K, 4, dims, strides, box);
-    if (!rc) rc = make_map(&mv, P.V, 4, dims, strides, box);
+    if (!rc && !paired(P, D)) rc = make_map(&mv, P.V, 4, dims, strides, box);
+    if (!rc && paired(P, D)) {                        // both 64-column halves of a page's rows in one copy
+        const cuuint64_t dims5[5] = {64, (cuuint64_t)page, 2, (cuuint64_t)P.Hkv, (cuuint64_t)P.pages};
+        const cuuint64_t strides5[4] = {strides[0], 128, strides[1], strides[2]};
+        const cuuint32_t box5[5] = {64, box[1], 2, 1, 1};
+        rc = make_map(&mv, P.V, 5, dims5, strides5, box5);
+    }
     if (rc) return rc;
     kern<<<kSMs, kPtThreads, fixed + plan_bytes(P.B + P.groups), st>>>(P, a, mq, mk, mv);
     CUDA_TRY(cudaGetLastError());

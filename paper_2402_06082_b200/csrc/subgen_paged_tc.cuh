@@ -3,8 +3,8 @@
 // A block takes a run of key tiles (128 tokens) of one row unit (up to 256 query rows, see Plan) and is one pipeline
 // of warps around two score buffers in tensor memory:
 //   planner (warp 11)    walks the block's share of the plan and publishes its runs
-//   producer (warp 8)    brings Q, K and V by TMA: one copy per page and 64 columns into the 128-byte-swizzled layout
-//                        the MMA reads; a ring of tiles
+//   producer (warp 8)    brings Q, K and V by TMA: one copy per page (K: and 64 columns) into the 128-byte-swizzled
+//                        layouts the MMA reads; a ring of tiles
 //   issuers (warps 9-10) S = Q K^T (M = 128 rows, N = 128 tokens), O += P V (P from tensor memory, V as it lies: tokens
 //                        along K, columns contiguous), both tcgen05.mma bf16 -> fp32
 //   softmax (warps 0-3, 4-7)  one thread per row: read S, running maximum and sum, P in bf16 over S, finally O out
@@ -44,7 +44,7 @@ template <int D>
 struct PtSmem {                                       // after a 1024-byte aligned base
     static constexpr int kTile = 128 * D * 2, kSlots = 131072 / kTile;
     unsigned char Q[2][kTile];                        // [64-column half][row][128 B swizzled]
-    unsigned char KV[kSlots][kTile];                  // K, V, K, V, ...: [half][token][128 B swizzled]
+    unsigned char KV[kSlots][kTile];                  // K, V, K, V, ...; K: [half][token][128 B swizzled], V: also by pages
     float join[2][4][4][D];                           // [group][warp][row][column]: numerators of four rows to be added
     float2 join_stat[2][4][32];                       // maximum in use, sum
     SegRec seg[kPtRing];
@@ -91,6 +91,10 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
     asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, int v, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(smem_u32(bar)) : "memory");
+}
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, unsigned long long* bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
@@ -109,7 +113,7 @@ __device__ __forceinline__ void tc_commit(unsigned long long* b) {
 constexpr uint32_t kDescHigh = 64u | (1u << 14) | (2u << 29);
 #define SGK_MMA_S(off, p) "add.u32 al, %1, " #off ";\n\tadd.u32 bl, %2, " #off ";\n\tmov.b64 a, {al, %4};\n\tmov.b64 b, {bl, %4};\n\t" \
                           "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, " #p ";\n\t"
-#define SGK_MMA_O(i, off, p) "add.u32 al, %1, " #i ";\n\tadd.u32 bl, %2, " #off ";\n\tmov.b64 b, {bl, %4};\n\t" \
+#define SGK_MMA_O(i, off, p) "add.u32 al, %1, " #i ";\n\t" off "mov.b64 b, {bl, %4};\n\t" \
                              "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [al], b, %3, " #p ";\n\t"
 // S = Q K^T over d in steps of 16: 32 bytes of a row, the second 64 columns 16 KB behind
 template <int D>
@@ -124,12 +128,14 @@ __device__ __forceinline__ void tc_scores(uint32_t d, uint32_t q, uint32_t k, ui
                      SGK_MMA_S(1024, o) SGK_MMA_S(1026, o) SGK_MMA_S(1028, o) SGK_MMA_S(1030, o) "}\n"
                      ::"r"(d), "r"((q >> 4) | (1u << 16)), "r"((k >> 4) | (1u << 16)), "r"(idesc), "r"(kDescHigh) : "memory");
 }
-// O (+)= P V over half a tile's tokens in steps of 16: 8 columns of P, 2 KB of V
-__device__ __forceinline__ void tc_output(uint32_t d, uint32_t p, uint32_t v, uint32_t idesc, uint32_t accumulate) {
+// O (+)= P V over half a tile's tokens in steps of 16: 8 columns of P each; V's low word, and how far behind it the second
+// 16 and the second 32 tokens lie (in units of 16 bytes)
+__device__ __forceinline__ void tc_output(uint32_t d, uint32_t p, uint32_t v, uint32_t second, uint32_t third, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred e, z, o;\n\t.reg .b64 b;\n\t.reg .b32 al, bl;\n\t"
                  "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 z, %5, 0;\n\tsetp.eq.b32 o, 0, 0;\n\t"
-                 SGK_MMA_O(0, 0, z) SGK_MMA_O(8, 128, o) SGK_MMA_O(16, 256, o) SGK_MMA_O(24, 384, o) "}\n"
-                 ::"r"(d), "r"(p), "r"((v >> 4) | (1024u << 16)), "r"(idesc), "r"(kDescHigh), "r"(accumulate) : "memory");
+                 SGK_MMA_O(0, "mov.u32 bl, %2;\n\t", z) SGK_MMA_O(8, "add.u32 bl, %2, %6;\n\t", o)
+                 SGK_MMA_O(16, "add.u32 bl, %2, %7;\n\t", o) SGK_MMA_O(24, "add.u32 bl, bl, %6;\n\t", o) "}\n"
+                 ::"r"(d), "r"(p), "r"(v), "r"(idesc), "r"(kDescHigh), "r"(accumulate), "r"(second), "r"(third) : "memory");
 }
 #define SGK_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
 #define SGK_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
@@ -188,6 +194,11 @@ __device__ __forceinline__ float ex2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+// Pages of 16 tokens: the copies of a tile (16 for K, 16 for V at d = 128) become what the producer spends its time on, so V
+// comes with both 64-column halves of a page in one (long sequences 428 -> 405 us; pages of 64 lose 5 % by it: the bigger
+// copies arrive later).
+__host__ __device__ __forceinline__ bool paired(const PagedView& P, int d) { return d == 128 && P.page_shift == 4; }
 
 template <int D>
 __global__ void __launch_bounds__(kPtThreads, 1)
@@ -261,6 +272,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             unsigned ns = 0, nq = 0, nk = 0;          // runs, query tiles and ring tiles so far
             const int pb = min(1 << P.page_shift, 128), chunks = 128 / pb;   // tokens one copy brings; copies for a half tile
             const int chunk = lane / HALVES, half = lane % HALVES;           // this lane's copy of a tile
+            const bool pairs = paired(P, D);
             bool ok = true;
             while (ok) {
                 const int slot = ns % kPtRing;
@@ -303,7 +315,9 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                         if (nk >= NS && !(ok = bar_wait(&sm.kv_empty[s], (nk / NS - 1) & 1, &sm.failed))) break;
                         if (lane == 0) bar_expect(&sm.kv_full[s], bytes);
                         __syncwarp();
-                        if (id >= 0) tma_load_4d(sm.KV[s] + half * 16384 + chunk * pb * 128, kv ? &mv : &mk, half * 64, row, head, id, &sm.kv_full[s]);
+                        if (id < 0) continue;
+                        if (!pairs || !kv) tma_load_4d(sm.KV[s] + half * 16384 + chunk * pb * 128, kv ? &mv : &mk, half * 64, row, head, id, &sm.kv_full[s]);
+                        else if (!half) tma_load_5d(sm.KV[s] + chunk * pb * 256, &mv, 0, row, 0, head, id, &sm.kv_full[s]);
                     }
                     id = following;
                 }
@@ -321,6 +335,10 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             // Everything here is the same in all lanes, and said so by shuffles and votes. One warp per group, so that a wait
             // of one leaves no gap in the tensor pipe.
             const int w = warp - 9;
+            // V lies as K does, or, in pairs, by pages of 16 tokens and in each of those [half][token][128 B]: in units of 16
+            // bytes, how far apart the halves are, and how far on the second 16, 32 and 64 tokens
+            const bool pairs = paired(P, D);
+            const uint32_t apart = pairs ? 128u : 1024u, second = pairs ? 256u : 128u, third = 2 * second, upper = 4 * second;
             struct Cursor { int tile, tile0, tile1, kp, dual, order, rows, P, S, seg, q, kv, jobs, done; };
             bool ok = true;
             auto wait = [&](unsigned long long* b, int parity) { return bar_wait(b, (unsigned)parity, &sm.failed); };
@@ -398,7 +416,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 if (nv < kPtKT) {                      // the sequence ends in this tile: clear what lies behind
                     for (int p = lane; p < (kPtKT - nv) * 8 * HALVES; p += 32) {
                         const int row = nv + p / (8 * HALVES), c = p % (8 * HALVES);
-                        *reinterpret_cast<uint4*>(sm.KV[s] + (c >> 3) * 16384 + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        const int at = pairs ? (row >> 4) * 4096 + (c >> 3) * 2048 + (row & 15) * 128 : (c >> 3) * 16384 + row * 128;
+                        *reinterpret_cast<uint4*>(sm.KV[s] + at + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -407,7 +426,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     if (segs && !(ok = wait(&sm.o_empty[w], (segs - 1) & 1))) break;
                     ++segs;
                 }
-                const uint32_t va = smem_u32(sm.KV[s]);
+                const uint32_t va = (smem_u32(sm.KV[s]) >> 4) | (apart << 16);
                 const uint32_t first = fresh ? 0u : 1u;
                 const bool k_there = issue_ready();
                 // Two groups on the same tiles take turns, P V and the next S of one, then of the other. Left to themselves
@@ -418,8 +437,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 if (!(ok = wait(&sm.p_full[w], mine & 1))) break;
                 tc_fence_after();
                 const uint32_t td = tmem + 256u + w * (uint32_t)D, tp = tmem + w * 128u;
-                tc_output(td, tp, va, kIdescO, first);
-                tc_output(td, tp + 32u, va + 8192u, kIdescO, 1u);
+                tc_output(td, tp, va, second, third, kIdescO, first);
+                tc_output(td, tp + 32u, va + upper, second, third, kIdescO, 1u);
                 tc_commit(&sm.kv_empty[s]);
                 if (!pv.dual) tc_commit(&sm.kv_empty[s]);
                 if (last) tc_commit(&sm.o_full[w]);
