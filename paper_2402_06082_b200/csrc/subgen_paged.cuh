@@ -333,6 +333,10 @@ struct Plan {
         E = P.groups + P.B;
         int* t = (int*)sm;
         int* s = t + E + 1;
+        // entry() reads these one after the other: asked for at once, so that it finds them in L1
+        auto touch = [](const int* p) { int x; asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(x) : "l"(p)); };
+        for (int b = threadIdx.x; b < P.B; b += blockDim.x) { touch(P.cu_q + b); touch(P.lengths + b); }
+        for (int g = threadIdx.x; g < P.groups; g += blockDim.x) { touch(P.cu_group + g); touch(P.prefix_len + g); }
         if (threadIdx.x == 0) *flag = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < E; i += blockDim.x) {

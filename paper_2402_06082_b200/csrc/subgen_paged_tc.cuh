@@ -606,18 +606,20 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     // thread for four columns
                     tc_fence_after();
                     sm.join_stat[w][quarter][lane] = make_float2(m, l);
-                    for (int r0 = 0; r0 < rows; r0 += 4) {
-#pragma unroll 1
-                        for (int i = 0; i < D / 32; ++i) {
-                            uint32_t o[32];
-                            __syncwarp();
-                            tc_ld32(tO + i * 32, o);
-                            tc_wait_ld();
-                            if (lane >= r0 && lane < r0 + 4) {
-                                uint4* z = reinterpret_cast<uint4*>(&sm.join[w][quarter][lane - r0][i * 32]);
+                    uint32_t o[D];
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                            }
+                    for (int i = 0; i < D / 32; ++i) tc_ld32(tO + i * 32, o + i * 32);
+                    tc_wait_ld();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sm.o_empty[w]);
+                    for (int r0 = 0; r0 < rows; r0 += 4) {
+                        // before the next four rows; the next run's numerators come after everybody's weights for it
+                        if (r0 && !joined()) break;
+                        if (lane >= r0 && lane < r0 + 4) {
+                            uint4* z = reinterpret_cast<uint4*>(&sm.join[w][quarter][lane - r0][0]);
+#pragma unroll
+                            for (int j = 0; j < D / 4; ++j) z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
                         }
                         if (!joined()) break;
                         const int rr = r0 + quarter;             // a warp per row
@@ -652,9 +654,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                                 if (lane == 0) a.stat[slot0 + rr] = make_float2(M * a.c, L);
                             }
                         }
-                        if (!joined()) break;
                     }
-                    tc_fence_before();
                 } else if (some) {
                     tc_fence_after();
                     if (m == -INFINITY) l = 0.f;
@@ -663,35 +663,36 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     const float f = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
                     __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
                     if (live && !direct) a.stat[slot0 + row] = make_float2(m * a.c, l);
-#pragma unroll 1
-                    for (int i = 0; i < D / 32; ++i) {
-                        uint32_t o[32];
-                        __syncwarp();
-                        tc_ld32(tO + i * 32, o);
-                        tc_wait_ld();
-                        if (live && direct) {
-#pragma unroll
-                            for (int j = 0; j < 32; j += 8) {
-                                uint4 v;
-                                uint32_t* vv = &v.x;
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(o[j + 2 * k]) * f, __uint_as_float(o[j + 2 * k + 1]) * f);
-                                    vv[k] = *reinterpret_cast<const uint32_t*>(&b);
-                                }
-                                *reinterpret_cast<uint4*>(y + i * 32 + j) = v;
-                            }
-                        } else if (live) {
-                            uint4* z = reinterpret_cast<uint4*>(a.part + (long long)(slot0 + row) * D + i * 32);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                        }
-                    }
                     __syncwarp();
+                    uint32_t o[D];
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) tc_ld32(tO + i * 32, o + i * 32);
+                    tc_wait_ld();
                     tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sm.o_empty[w]);
+                    if (live && direct) {
+#pragma unroll
+                        for (int j = 0; j < D; j += 8) {
+                            uint4 v;
+                            uint32_t* vv = &v.x;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(o[j + 2 * k]) * f, __uint_as_float(o[j + 2 * k + 1]) * f);
+                                vv[k] = *reinterpret_cast<const uint32_t*>(&b);
+                            }
+                            *reinterpret_cast<uint4*>(y + j) = v;
+                        }
+                    } else if (live) {
+                        uint4* z = reinterpret_cast<uint4*>(a.part + (long long)(slot0 + row) * D);
+#pragma unroll
+                        for (int j = 0; j < D / 4; ++j) z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                    }
+                } else {
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sm.o_empty[w]);
                 }
                 __syncwarp();
-                if (lane == 0) bar_arrive(&sm.o_empty[w]);
             }
             if (lane == 0) bar_arrive(&sm.seg_empty[slot]);
         }
