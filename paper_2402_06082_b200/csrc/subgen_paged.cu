@@ -171,24 +171,25 @@ int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t s
     return SUBGEN_OK;
 }
 
-template <typename T, int D, int RU, int NT>
+template <int D, int RU>
 int attend_simt(const PagedView& P, const Attend& a, cudaStream_t st) {
-    auto kern = paged_attend_simt_kernel<T, D, RU, NT>;
+    typedef SimtShape<D, RU> S;
+    auto kern = paged_attend_simt_kernel<D, RU>;
     static bool done[kMaxDevices];
     constexpr size_t tile = (sizeof(SimtSmem<D, RU>) + 15) & ~(size_t)15;
     const int rc = opt_in(kern, tile + plan_bytes(kPlanMax), done);
     if (rc) return rc;
-    const int blocks = kSMs * 2;
-    kern<<<blocks, NT, tile + plan_bytes(P.B + P.groups), st>>>(P, a);
+    const int blocks = kSMs * S::BLOCKS;
+    kern<<<blocks, S::NT, tile + plan_bytes(P.B + P.groups), st>>>(P, a);
     CUDA_TRY(cudaGetLastError());
-    return launch_merge<T, D, RU, kSimtKT, false, kSimtLead>(P, a, blocks, st);
+    return launch_merge<float, D, RU, S::KT, false, kSimtLead>(P, a, blocks, st);
 }
 
-template <typename T, int D>
+template <int D>
 int attend_simt_rows(const PagedView& P, const Attend& a, cudaStream_t st) {
     // 16-row units while a sequence has up to 16 rows on average, else 64
-    if (((long long)a.n << a.g_shift) <= 16LL * P.B) return attend_simt<T, D, 16, 128>(P, a, st);
-    return attend_simt<T, D, 64, 256>(P, a, st);
+    if (((long long)a.n << a.g_shift) <= 16LL * P.B) return attend_simt<D, 16>(P, a, st);
+    return attend_simt<D, 64>(P, a, st);
 }
 
 // ---- attention, bf16: tensor maps over the pool and the queries ----
@@ -347,7 +348,7 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
                 (float2*)((float*)x->workspace + slots * d)};
     cudaStream_t st = (cudaStream_t)stream;
     if (cache->dtype == SUBGEN_DTYPE_BF16) return d == 64 ? attend_tc<64>(P, a, st) : attend_tc<128>(P, a, st);
-    return d == 64 ? attend_simt_rows<float, 64>(P, a, st) : attend_simt_rows<float, 128>(P, a, st);
+    return d == 64 ? attend_simt_rows<64>(P, a, st) : attend_simt_rows<128>(P, a, st);
 }
 
 }  // extern "C"
