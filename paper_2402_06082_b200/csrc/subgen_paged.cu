@@ -156,7 +156,7 @@ int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t s
         // parts of a row unit that a block joins at a time: 4 rows while the blocks that fit can take all rows at once, else 8,
     // and 16 for prompts, most of whose rows need none (RU is a multiple of each)
     const long long rows = (long long)a.n * a.H, once = kSMs * kMergeBlocks;
-    const int part = rows <= once * 4 ? 4 : rows <= once * 8 ? 8 : 16;
+    const int part = rows <= once * 4 ? 4 : rows <= once * 8 || RU == 8 ? 8 : 16;
     const long long units = ((long long)P.B + ((long long)a.n << a.g_shift) / part) * P.Hkv;
     cfg.gridDim = dim3((unsigned)(units < kSMs * kMergeBlocks ? units : kSMs * kMergeBlocks));
     cfg.blockDim = dim3(kMergeThreads);
@@ -171,25 +171,23 @@ int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t s
     return SUBGEN_OK;
 }
 
-template <int D, int RU>
-int attend_simt(const PagedView& P, const Attend& a, cudaStream_t st) {
-    typedef SimtShape<D, RU> S;
-    auto kern = paged_attend_simt_kernel<D, RU>;
+template <typename S, int D, typename K>
+int attend_fp32_with(K kern, const PagedView& P, const Attend& a, cudaStream_t st) {
     static bool done[kMaxDevices];
-    constexpr size_t tile = (sizeof(SimtSmem<D, RU>) + 15) & ~(size_t)15;
+    constexpr size_t tile = (sizeof(S) + 15) & ~(size_t)15;
     const int rc = opt_in(kern, tile + plan_bytes(kPlanMax), done);
     if (rc) return rc;
     const int blocks = kSMs * S::BLOCKS;
     kern<<<blocks, S::NT, tile + plan_bytes(P.B + P.groups), st>>>(P, a);
     CUDA_TRY(cudaGetLastError());
-    return launch_merge<float, D, RU, S::KT, false, kSimtLead>(P, a, blocks, st);
+    return launch_merge<float, D, S::RU, S::KT, false, kSimtLead>(P, a, blocks, st);
 }
 
 template <int D>
-int attend_simt_rows(const PagedView& P, const Attend& a, cudaStream_t st) {
-    // 16-row units while a sequence has up to 16 rows on average, else 64
-    if (((long long)a.n << a.g_shift) <= 16LL * P.B) return attend_simt<D, 16>(P, a, st);
-    return attend_simt<D, 64>(P, a, st);
+int attend_fp32(const PagedView& P, const Attend& a, cudaStream_t st) {
+    // up to 8 rows a sequence on average: one pass over the cache with little arithmetic to it
+    if (((long long)a.n << a.g_shift) <= 8LL * P.B) return attend_fp32_with<FewSmem<D>, D>(paged_attend_few_kernel<D>, P, a, st);
+    return attend_fp32_with<SimtSmem<D>, D>(paged_attend_simt_kernel<D>, P, a, st);
 }
 
 // ---- attention, bf16: tensor maps over the pool and the queries ----
@@ -348,7 +346,7 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
                 (float2*)((float*)x->workspace + slots * d)};
     cudaStream_t st = (cudaStream_t)stream;
     if (cache->dtype == SUBGEN_DTYPE_BF16) return d == 64 ? attend_tc<64>(P, a, st) : attend_tc<128>(P, a, st);
-    return d == 64 ? attend_simt_rows<64>(P, a, st) : attend_simt_rows<128>(P, a, st);
+    return d == 64 ? attend_fp32<64>(P, a, st) : attend_fp32<128>(P, a, st);
 }
 
 }  // extern "C"

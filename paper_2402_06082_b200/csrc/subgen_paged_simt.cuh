@@ -1,13 +1,14 @@
 // Attention over a paged cache in fp32 arithmetic throughout: the path of fp32 caches.
 //
-// One block takes a run of key tiles of one row unit (see Plan): RU query rows against KT tokens at a time, both products
-// on the fp32 pipes from shared memory, the running maximum and sum of the softmax in registers. A thread holds RPT rows x
-// KT / 16 scores of a tile and RPT rows x D / 16 columns of the numerator; the 16 threads of a row are half a warp, so row
-// reductions are four shuffles.
-// Two sizes. RU = 16 for single tokens and drafts, where the cache is read once and 16 rows of arithmetic per byte stay
-// below what the memory takes: what counts is latency, so the next tile is copied (cp.async) while this one is worked on,
-// in blocks small enough for three an SM. RU = 64 for many rows, where each value read from shared memory serves four rows
-// and two blocks an SM cover for each other's copies.
+// One block takes a run of key tiles of one row unit (see Plan), both products on the fp32 pipes from shared memory, the
+// running maximum and sum of the softmax in registers. Two kernels:
+//   many rows (RU = 64): a thread holds 4 rows x 4 scores of a tile of 64 tokens and 4 rows x D / 16 columns of the
+//     numerator, so each value read from shared memory serves four rows; the 16 threads of a row are half a warp, so row
+//     reductions are four shuffles. Bound by the fp32 pipes; two blocks an SM cover for each other's copies.
+//   few rows (RU = 8): single tokens and drafts, where the cache is read once and the copies must never stop. A warp is on
+//     its own with a quarter of the tile's tokens: its lanes share the tokens' scores for all rows, then each holds
+//     D / 32 columns of the numerator; the next tile is copied (cp.async) meanwhile, three blocks an SM, and the warps'
+//     results are joined at the end of the run.
 #pragma once
 #include "subgen_paged.cuh"
 
@@ -15,16 +16,23 @@ namespace sgk {
 
 constexpr int kSimtLead = 1;
 
-template <int D, int RU> struct SimtShape {
-    static constexpr int KT = RU == 16 && D == 128 ? 32 : 64, STAGES = RU == 16 ? 2 : 1, NT = RU == 16 ? 128 : 256, BLOCKS = RU == 16 ? 3 : 2;
-};
-template <int D, int RU>
+template <int D>
 struct SimtSmem {
-    typedef SimtShape<D, RU> S;
+    static constexpr int RU = 64, KT = 64, NT = 256, BLOCKS = 2;
     float Q[RU][D];
-    float K[S::STAGES][S::KT][D + 4];                 // + 4: sixteen threads read sixteen rows at once
-    float V[S::STAGES][S::KT][D];
-    float P[RU][S::KT];
+    float K[KT][D + 4];                               // + 4: sixteen threads read sixteen rows at once
+    float V[KT][D];
+    float P[RU][KT];
+    int bad, flag;
+};
+template <int D>
+struct FewSmem {
+    static constexpr int RU = 8, KT = D == 128 ? 32 : 64, NT = 128, BLOCKS = 3, SPLIT = NT / KT;    // SPLIT lanes share a token
+    float Q[RU][D];
+    float K[2][KT][D + 4 * SPLIT];                    // eight lanes read all 32 banks
+    float V[2][KT][D];
+    float P[NT / 32][KT / 4][RU];                     // [warp][token][row]
+    float2 stat[NT / 32][RU];
     int bad, flag;
 };
 
@@ -33,15 +41,216 @@ __device__ __forceinline__ void copy16(void* to, const void* from, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
-template <int D, int RU>
-__global__ void __launch_bounds__(SimtShape<D, RU>::NT) paged_attend_simt_kernel(PagedView P, Attend a) {
-    typedef SimtShape<D, RU> S;
-    constexpr int KT = S::KT, NT = S::NT, TK = KT / 16, TY = NT / 16, RPT = RU / TY, LPR = D / 4;
+// Tile t of a run into shared memory: tokens behind the end and unusable pages as zeros.
+template <int KT, int D, int NT>
+__device__ __forceinline__ void bring_tile(const PagedView& P, const Seg& g, int t, float* K, int k_stride, float* V, int* bad) {
+    constexpr int LPR = D / 4;
+    const bool pre = t < g.kp;
+    const int base = (pre ? t : t - g.kp) * KT, limit = pre ? g.e.P : g.e.S;
+    const int* tab = pre ? g.e.ptab : g.e.stab;
+#pragma unroll 4
+    for (int p = threadIdx.x; p < KT * LPR; p += NT) {
+        const int j = p / LPR, piece = p % LPR, pos = base + j;
+        long long off = 0;
+        bool there = pos < limit;
+        if (there) {
+            const int id = __ldg(tab + (pos >> P.page_shift));
+            there = id >= 0 && id < P.pages;
+            if (there) off = id * P.ps + g.head * P.hs + (pos & ((1 << P.page_shift) - 1)) * P.ts + piece * 4;
+            else *bad = 1;
+        }
+        copy16(K + j * k_stride + piece * 4, (const float*)P.K + off, there);
+        copy16(V + j * D + piece * 4, (const float*)P.V + off, there);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int RU, int D, int NT>
+__device__ __forceinline__ void bring_queries(const Attend& a, const Seg& g, float (*Q)[D]) {
+    for (int p = threadIdx.x; p < RU * (D / 4); p += NT) {
+        const int r = p / (D / 4), piece = p % (D / 4);
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < g.rows) {
+            const int row = g.ru * RU + r, tok = g.e.tok0 + (row >> a.g_shift), h = (g.head << a.g_shift) + (row & ((1 << a.g_shift) - 1));
+            f = __ldg(reinterpret_cast<const float4*>((const float*)a.q.p + tok * a.q.ts + h * a.q.hs) + piece);
+        }
+        *reinterpret_cast<float4*>(&Q[r][piece * 4]) = f;
+    }
+}
+// Where row r of a run goes: the output, or its place among the partials.
+template <int RU, int D>
+__device__ __forceinline__ float* result_row(const Attend& a, const Seg& g, int r) {
+    if (!g.direct) return a.part + (long long)(g.slot + r) * D;
+    const int row = g.ru * RU + r;
+    return (float*)a.o.p + (g.e.tok0 + (row >> a.g_shift)) * a.o.ts + ((g.head << a.g_shift) + (row & ((1 << a.g_shift) - 1))) * a.o.hs;
+}
+
+// R rows of a tile by one warp (few rows): scores of its KT / 4 tokens, weights, numerator.
+template <int D, int R>
+__device__ __forceinline__ void few_tile(FewSmem<D>& sm, int at, int first, const int* lim, float c, float* m, float* l, float (*acc)[D / 32]) {
+    typedef FewSmem<D> S;
+    constexpr int SPLIT = S::SPLIT, TOK = S::KT / 4, VL = D / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, split = lane % SPLIT, tok = lane / SPLIT, j = warp * TOK + tok;
+    float s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r] = 0.f;
+#pragma unroll 4
+    for (int f = 0; f < D / 4 / SPLIT; ++f) {
+        const int e = (f * SPLIT + split) * 4;
+        const float4 k = *reinterpret_cast<const float4*>(&sm.K[at][j][e]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float4 q = *reinterpret_cast<const float4*>(&sm.Q[r][e]);
+            s[r] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[r]))));
+        }
+    }
+    bool rise = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int o = 1; o < SPLIT; o <<= 1) s[r] += __shfl_xor_sync(0xffffffffu, s[r], o);
+        s[r] = first + j < lim[r] ? s[r] * c : -INFINITY;
+        rise |= s[r] > m[r];
+    }
+    if (__any_sync(0xffffffffu, rise)) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float top = fmaxf(m[r], s[r]);
+#pragma unroll
+            for (int o = SPLIT; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float al = top == -INFINITY ? 1.f : exp2f(m[r] - top);
+            m[r] = top;
+            l[r] *= al;
+#pragma unroll
+            for (int i = 0; i < VL; ++i) acc[r][i] *= al;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const float p = s[r] == -INFINITY ? 0.f : exp2f(s[r] - m[r]);
+        l[r] += p;                                                   // of this lane's tokens
+        if (split == 0) sm.P[warp][tok][r] = p;
+    }
+    __syncwarp();
+#pragma unroll 4
+    for (int t = 0; t < TOK; ++t) {
+        float p[R], v[VL];
+#pragma unroll
+        for (int r = 0; r < R; r += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(&sm.P[warp][t][r]);
+            p[r] = x.x; p[r + 1] = x.y; p[r + 2] = x.z; p[r + 3] = x.w;
+        }
+        if constexpr (VL == 4) {
+            const float4 x = *reinterpret_cast<const float4*>(&sm.V[at][warp * TOK + t][lane * 4]);
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+        } else {
+            const float2 x = *reinterpret_cast<const float2*>(&sm.V[at][warp * TOK + t][lane * 2]);
+            v[0] = x.x; v[1] = x.y;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < VL; ++i) acc[r][i] = fmaf(p[r], v[i], acc[r][i]);
+    }
+    __syncwarp();
+}
+
+template <int D>
+__global__ void __launch_bounds__(FewSmem<D>::NT, FewSmem<D>::BLOCKS) paged_attend_few_kernel(PagedView P, Attend a) {
+    typedef FewSmem<D> S;
+    constexpr int RU = S::RU, KT = S::KT, NT = S::NT, NW = NT / 32, VL = D / 32;
+    extern __shared__ __align__(16) unsigned char dyn[];
+    S& sm = *reinterpret_cast<S*>(dyn);
+    Plan<RU, KT, false, kSimtLead> plan(P, a);
+    plan.build(dyn + ((sizeof(S) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
+    pdl_trigger();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int x = blockIdx.x * plan.chunk;
+    const int x1 = min(plan.total, x + plan.chunk);
+    while (x < x1) {
+        const Seg g = plan.next(x, x1, blockIdx.x);
+        if (g.tile0 >= g.tile1) continue;
+        __syncthreads();
+        if (tid == 0) sm.bad = g.e.bad;
+        __syncthreads();
+        auto bring = [&](int t) {
+            const int at = (t - g.tile0) & 1;
+            bring_tile<KT, D, NT>(P, g, t, &sm.K[at][0][0], D + 4 * S::SPLIT, &sm.V[at][0][0], &sm.bad);
+        };
+        bring(g.tile0);
+        bring_queries<RU, D, NT>(a, g, sm.Q);
+        float m[RU], l[RU], acc[RU][VL];
+        int own[RU];
+#pragma unroll
+        for (int r = 0; r < RU; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+            own[r] = plan.own_limit(g.e, g.ru * RU + r);
+#pragma unroll
+            for (int i = 0; i < VL; ++i) acc[r][i] = 0.f;
+        }
+        for (int t = g.tile0; t < g.tile1; ++t) {
+            if (t + 1 < g.tile1) {
+                bring(t + 1);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            } else {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            }
+            __syncthreads();
+            const bool pre = t < g.kp;
+            int lim[RU];
+#pragma unroll
+            for (int r = 0; r < RU; ++r) lim[r] = pre ? g.e.P : own[r];
+            const int first = (pre ? t : t - g.kp) * KT, at = (t - g.tile0) & 1;
+            if (g.rows <= 4) few_tile<D, 4>(sm, at, first, lim, a.c, m, l, acc);
+            else few_tile<D, 8>(sm, at, first, lim, a.c, m, l, acc);
+            __syncthreads();                                         // the stage may be filled again
+        }
+        const bool bad = sm.bad != 0;
+        if (bad && tid == 0) paged_status(P, kStPage);
+        // join the four warps: their numerators where K was
+        float (*join)[RU][D] = reinterpret_cast<float (*)[RU][D]>(&sm.K[0][0][0]);
+        static_assert(sizeof(float) * NW * RU * D <= sizeof(sm.K), "the warps' numerators fit");
+#pragma unroll
+        for (int r = 0; r < RU; ++r) {
+#pragma unroll
+            for (int o = S::SPLIT; o < 32; o <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
+            if (lane == 0) sm.stat[warp][r] = make_float2(m[r], l[r]);
+#pragma unroll
+            for (int i = 0; i < VL; ++i) join[warp][r][lane * VL + i] = acc[r][i];
+        }
+        __syncthreads();
+        for (int r = warp; r < g.rows; r += NW) {
+            float M = -INFINITY, L = 0.f, z[VL];
+#pragma unroll
+            for (int i = 0; i < VL; ++i) z[i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) M = fmaxf(M, sm.stat[k][r].x);
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                const float f = sm.stat[k][r].x == -INFINITY ? 0.f : exp2f(sm.stat[k][r].x - M);
+                L = fmaf(sm.stat[k][r].y, f, L);
+#pragma unroll
+                for (int i = 0; i < VL; ++i) z[i] = fmaf(join[k][r][lane * VL + i], f, z[i]);
+            }
+            if (bad) L = NAN;
+            const float f = !g.direct ? 1.f : L == 0.f ? 0.f : 1.f / L;
+            float* y = result_row<RU, D>(a, g, r) + lane * VL;
+            if (!g.direct && lane == 0) a.stat[g.slot + r] = make_float2(M, L);
+            if constexpr (VL == 4) *reinterpret_cast<float4*>(y) = make_float4(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
+            else *reinterpret_cast<float2*>(y) = make_float2(z[0] * f, z[1] * f);
+        }
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(SimtSmem<D>::NT) paged_attend_simt_kernel(PagedView P, Attend a) {
+    typedef SimtSmem<D> S;
+    constexpr int RU = S::RU, KT = S::KT, NT = S::NT, TK = KT / 16, TY = NT / 16, RPT = RU / TY;
     static_assert(RPT * TY == RU, "rows divide");
     extern __shared__ __align__(16) unsigned char dyn[];
-    SimtSmem<D, RU>& sm = *reinterpret_cast<SimtSmem<D, RU>*>(dyn);
+    S& sm = *reinterpret_cast<S*>(dyn);
     Plan<RU, KT, false, kSimtLead> plan(P, a);
-    plan.build(dyn + ((sizeof(SimtSmem<D, RU>) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
+    plan.build(dyn + ((sizeof(S) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
     pdl_trigger();
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     int x = blockIdx.x * plan.chunk;
@@ -53,36 +262,8 @@ __global__ void __launch_bounds__(SimtShape<D, RU>::NT) paged_attend_simt_kernel
         __syncthreads();
         if (tid == 0) sm.bad = g.e.bad;
         __syncthreads();
-        // tile t into a stage; tokens behind the end and unusable pages as zeros
-        auto bring = [&](int t, int stage) {
-            const bool pre = t < g.kp;
-            const int base = (pre ? t : t - g.kp) * KT, limit = pre ? g.e.P : g.e.S;
-            const int* tab = pre ? g.e.ptab : g.e.stab;
-            for (int p = tid; p < KT * LPR; p += NT) {
-                const int j = p / LPR, piece = p % LPR, pos = base + j;
-                long long off = 0;
-                bool there = pos < limit;
-                if (there) {
-                    const int id = __ldg(tab + (pos >> P.page_shift));
-                    there = id >= 0 && id < P.pages;
-                    if (there) off = id * P.ps + g.head * P.hs + (pos & ((1 << P.page_shift) - 1)) * P.ts + piece * 4;
-                    else sm.bad = 1;
-                }
-                copy16(&sm.K[stage][j][piece * 4], (const float*)P.K + off, there);
-                copy16(&sm.V[stage][j][piece * 4], (const float*)P.V + off, there);
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        bring(g.tile0, 0);
-        for (int p = tid; p < RU * LPR; p += NT) {
-            const int r = p / LPR, piece = p % LPR;
-            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < g.rows) {
-                const int row = row0 + r, tok = g.e.tok0 + (row >> a.g_shift), h = (g.head << a.g_shift) + (row & ((1 << a.g_shift) - 1));
-                f = __ldg(reinterpret_cast<const float4*>((const float*)a.q.p + tok * a.q.ts + h * a.q.hs) + piece);
-            }
-            *reinterpret_cast<float4*>(&sm.Q[r][piece * 4]) = f;
-        }
+        bring_tile<KT, D, NT>(P, g, g.tile0, &sm.K[0][0], D + 4, &sm.V[0][0], &sm.bad);
+        bring_queries<RU, D, NT>(a, g, sm.Q);
         float m[RPT], l[RPT], acc[RPT][D / 16];
         int own[RPT];
 #pragma unroll
@@ -95,14 +276,9 @@ __global__ void __launch_bounds__(SimtShape<D, RU>::NT) paged_attend_simt_kernel
         }
         for (int t = g.tile0; t < g.tile1; ++t) {
             const bool pre = t < g.kp;
-            const int base = (pre ? t : t - g.kp) * KT, limit = pre ? g.e.P : g.e.S, at = (t - g.tile0) % S::STAGES;
-            if (S::STAGES > 1 && t + 1 < g.tile1) {
-                bring(t + 1, (t + 1 - g.tile0) % S::STAGES);
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
-            } else {
-                if (S::STAGES == 1 && t > g.tile0) bring(t, 0);
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-            }
+            const int base = (pre ? t : t - g.kp) * KT, limit = pre ? g.e.P : g.e.S;
+            if (t > g.tile0) bring_tile<KT, D, NT>(P, g, t, &sm.K[0][0], D + 4, &sm.V[0][0], &sm.bad);
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncthreads();
             float s[RPT][TK];
 #pragma unroll
@@ -113,7 +289,7 @@ __global__ void __launch_bounds__(SimtShape<D, RU>::NT) paged_attend_simt_kernel
             for (int e = 0; e < D; e += 4) {
                 float4 kv[TK];
 #pragma unroll
-                for (int j = 0; j < TK; ++j) kv[j] = *reinterpret_cast<const float4*>(&sm.K[at][tx + 16 * j][e]);
+                for (int j = 0; j < TK; ++j) kv[j] = *reinterpret_cast<const float4*>(&sm.K[tx + 16 * j][e]);
 #pragma unroll
                 for (int i = 0; i < RPT; ++i) {
                     const float4 qv = *reinterpret_cast<const float4*>(&sm.Q[ty * RPT + i][e]);
@@ -157,7 +333,7 @@ __global__ void __launch_bounds__(SimtShape<D, RU>::NT) paged_attend_simt_kernel
                 for (int q = 0; q < 4; ++q) {
 #pragma unroll
                     for (int b = 0; b < D / 64; ++b) {
-                        const float4 v = *reinterpret_cast<const float4*>(&sm.V[at][j + q][b * 64 + tx * 4]);
+                        const float4 v = *reinterpret_cast<const float4*>(&sm.V[j + q][b * 64 + tx * 4]);
 #pragma unroll
                         for (int i = 0; i < RPT; ++i) {
                             const float w = q == 0 ? p[i].x : q == 1 ? p[i].y : q == 2 ? p[i].z : p[i].w;
@@ -169,7 +345,7 @@ __global__ void __launch_bounds__(SimtShape<D, RU>::NT) paged_attend_simt_kernel
                     }
                 }
             }
-            __syncthreads();                                         // the stage may be filled again
+            __syncthreads();                                         // the tile may be filled again
         }
         const bool bad = sm.bad != 0;
         if (bad && tid == 0) paged_status(P, kStPage);
@@ -180,10 +356,8 @@ __global__ void __launch_bounds__(SimtShape<D, RU>::NT) paged_attend_simt_kernel
             const int r = ty * RPT + i;
             if (bad) l[i] = NAN;
             if (r < g.rows) {
-                const int row = row0 + r;
                 const float f = !g.direct ? 1.f : l[i] == 0.f ? 0.f : 1.f / l[i];
-                float* y = g.direct ? (float*)a.o.p + (g.e.tok0 + (row >> a.g_shift)) * a.o.ts + ((g.head << a.g_shift) + (row & ((1 << a.g_shift) - 1))) * a.o.hs
-                                    : a.part + (long long)(g.slot + r) * D;
+                float* y = result_row<RU, D>(a, g, r);
                 if (!g.direct && tx == 0) a.stat[g.slot + r] = make_float2(m[i], l[i]);
 #pragma unroll
                 for (int b = 0; b < D / 64; ++b)
