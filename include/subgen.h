@@ -383,7 +383,7 @@ int subgen_qk_norm_rope(const subgen_qk_args* args, void* stream);
  * pointers are device pointers; the functions below keep nothing between calls, so lengths and tables may change on
  * the device (also inside a captured graph). Indices are checked on the device: a page outside [0, pages) or a length
  * beyond its table is neither read nor written, sets SUBGEN_ST_PAGE in *status and makes the outputs that needed it
- * NaN. */
+ * NaN. The first call of each kind on a device loads its kernels: make it before starting any stream capture. */
 typedef struct subgen_pages {
     void *K, *V;            /* element (page, head, row, x) of each at page * page_stride + head * head_stride + row * row_stride + x */
     int64_t page_stride, head_stride, row_stride;   /* elements; multiples of 16 bytes */
@@ -435,7 +435,7 @@ typedef struct subgen_attend_args {
  * finite; what lies behind a sequence's length in its last page may be anything.
  * Scores, maxima, sums and numerators are fp32; on bf16 caches the softmax weights are rounded to bf16 for the product
  * with V. The result does not depend on how blocks are scheduled.
- * The workspace is this call's until it has run (two calls that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */
+ * out must not overlap q. The workspace is this call's until it has run (two calls that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */
 size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H);
 int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_attend_args* args, void* stream);
 

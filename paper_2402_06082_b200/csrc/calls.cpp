@@ -9,6 +9,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <climits>
 #include <stdexcept>
 #include <string>
 
@@ -56,6 +57,7 @@ subgen_heads rows(const at::Tensor& x, const char* name, const Like& w, int64_t 
         x.size(2) != d || x.stride(2) != 1)
         refuse(std::string(name) + " must be a " + at::toString(w.type) + " tensor of shape (" + std::to_string(n) + "," + std::to_string(heads) + "," +
                std::to_string(d) + ") on cuda:" + std::to_string(w.device) + " with unit stride along the last axis " + said(x));
+    if (n > INT_MAX || heads > INT_MAX) refuse(std::string(name) + ": too many rows");
     return subgen_heads{x.data_ptr(), x.stride(0), x.stride(1)};
 }
 const void* whole(PyObject* o, const char* name, at::ScalarType type, int device, int64_t n) {

@@ -132,9 +132,12 @@ void fill_norm_rope(NormRope* a, const subgen_qk_args* x, int H, int Hkv) {
 size_t plan_bytes(int E) { return ((size_t)8 * (E + 1) + 15) & ~(size_t)15; }
 
 long long slot_count(const PagedView& P, int n, int H) {
-    // every row once per entry it belongs to, twice where two halves of a block share its tiles, and a row unit of up
-    // to 256 rows for every block that shares a unit with the block before it
-    return (long long)n * H * 2 * (P.groups ? 2 : 1) + 256LL * kSMs * 2;
+    // every row once per entry it belongs to; up to 128 rows of an entry's last unit twice, where the two groups of a block
+    // share its tiles; and a unit of up to 256 rows (64 where a launch has more blocks) for every block that shares a unit
+    // with the block before it
+    const long long rows = (long long)n * H, unit = 128LL * P.Hkv;
+    auto entries = [&](long long count) { return rows + (rows < unit * count ? rows : unit * count); };
+    return entries(P.B) + (P.groups ? entries(P.groups) : 0) + 256LL * kSMs;
 }
 
 template <typename K>
@@ -178,6 +181,7 @@ int attend_fp32_with(K kern, const PagedView& P, const Attend& a, cudaStream_t s
     const int rc = opt_in(kern, tile + plan_bytes(kPlanMax), done);
     if (rc) return rc;
     const int blocks = kSMs * S::BLOCKS;
+    static_assert(S::RU * S::BLOCKS <= 256, "slot_count");
     kern<<<blocks, S::NT, tile + plan_bytes(P.B + P.groups), st>>>(P, a);
     CUDA_TRY(cudaGetLastError());
     return launch_merge<float, D, S::RU, S::KT, false, kSimtLead>(P, a, blocks, st);
@@ -330,12 +334,13 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
     if (rc) return rc;
     const int G = H / cache->Hkv;
     if (H % cache->Hkv || (G != 1 && G != 2 && G != 4 && G != 8)) return fail(SUBGEN_EINVAL, "%s: H / Hkv must be 1, 2, 4 or 8", fn);
-    if (!(x->scale > 0.f) || !isfinite(x->scale)) return fail(SUBGEN_EINVAL, "%s: scale must be positive and finite", fn);
+    if (!(x->scale > 0.f) || !isfinite(x->scale * 1.4426950408889634f)) return fail(SUBGEN_EINVAL, "%s: scale must be positive and finite", fn);
     if (n == 0 || batch->B == 0) return SUBGEN_OK;
     HeadsView vq, vo;
     rc = check_heads(fn, "q", &x->q, n, H, d, cache->dtype, &vq);
     if (!rc) rc = check_heads(fn, "out", &x->out, n, H, d, cache->dtype, &vo);
     if (rc) return rc;
+    if (vo.p == vq.p) return fail(SUBGEN_EINVAL, "%s: out must not be q", fn);
     const long long slots = slot_count(P, n, H);
     if (slots > 0x7fffffffLL) return fail(SUBGEN_EINVAL, "%s: too many rows in one call", fn);
     const size_t need = (size_t)slots * (d * sizeof(float) + sizeof(float2));

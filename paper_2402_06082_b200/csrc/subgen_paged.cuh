@@ -57,14 +57,19 @@ struct NormRope {
 
 constexpr int kNrThreads = 128;
 
-// index of the last i in [0, count) with edges[i] <= x, or -1; edges non-decreasing. One warp, all lanes get it.
+// Index of the last i in [0, count) with edges[i] <= x, or -1; -2 where edges that are above x come before ones that are
+// not. One warp, all lanes get it.
 __device__ __forceinline__ int warp_find(const int* edges, int count, int x) {
     int found = 0;
+    bool over = false, broken = false;
     for (int i = 0; i < count; i += 32) {
         const int j = i + (threadIdx.x & 31);
-        found += __popc(__ballot_sync(0xffffffffu, j < count && __ldg(edges + j) <= x));
+        const unsigned below = __ballot_sync(0xffffffffu, j < count && __ldg(edges + j) <= x);
+        broken |= (below & (below + 1)) != 0 || (over && below);
+        over |= below != 0xffffffffu;
+        found += __popc(below);
     }
-    return found - 1;
+    return broken ? -2 : found - 1;
 }
 
 template <typename T, int VE>
@@ -95,10 +100,15 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     int pos = 0;
     if constexpr (PAGED) {
         const int b = warp_find(P.cu_q, P.B + 1, tok);
-        if (b < 0 || b >= P.B) return;                               // behind the last sequence
-        const int own = __ldg(P.lengths + b) - __ldg(P.cu_q + b + 1) + tok;
-        const int pg = own >> P.page_shift;
-        if (own >= 0 && pg < P.table_stride) {
+        const int end = b >= 0 && b < P.B ? __ldg(P.cu_q + b + 1) : 0;
+        if (b == -2 || end > a.n) {
+            if (lane == 0) paged_status(P, kStPage);
+            return;
+        }
+        if (b < 0 || b >= P.B) return;                               // before the first sequence, behind the last
+        const long long place = (long long)__ldg(P.lengths + b) - end + tok, pg = place >> P.page_shift;
+        const int own = (int)place;
+        if (place >= 0 && pg < P.table_stride) {
             const int id = __ldg(P.table + (long long)b * P.table_stride + pg);
             if (id >= 0 && id < P.pages) slot = (long long)id * P.ps + (long long)(own & ((1 << P.page_shift) - 1)) * P.ts;
         }
@@ -107,7 +117,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
         if (a.positions) pos = __ldg(a.positions + tok);
         else if (P.groups) {
             const int g = warp_find(P.cu_group, P.groups + 1, b);
-            if (g >= 0 && g < P.groups) pos += __ldg(P.prefix_len + g);
+            if (g >= 0 && g < P.groups) pos = (int)((unsigned)pos + (unsigned)__ldg(P.prefix_len + g));
         }
     } else {
         if (a.words) pos = __ldg(a.positions + tok);
@@ -459,6 +469,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (plan.broken) {
         if (blockIdx.x == 0 && tid == 0) paged_status(P, kStPage);
+        pdl_wait();                                   // this kernel's end stands for the attention kernel's
         return;
     }
     if (warp == 0) {

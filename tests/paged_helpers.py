@@ -89,8 +89,9 @@ def attend(q, K, V, cu, lengths, table, scale, causal=True, cu_group=(), prefix_
         y = torch.einsum("thgl,hld->thgd", w, v)
         a = torch.einsum("thgl,hld->thgd", w, v.abs())
         # weights: e^(2 ds) from the scores, exp2 and its argument (|s| up to its range: 2^-21 with the fp32 rounding of an
-        # argument of up to 64), L sums and as many joins; bf16: the weight itself
-        rel = 2 * torch.expm1(ds) + 2.0 ** -20 + 2 * (L + 64) * U32 + (u if q.dtype == torch.bfloat16 else 0)
+        # argument of up to 64), L sums and as many joins; bf16: the weight itself, and 7.5e-5 of the cubic that some of the
+        # weights are made with, which the sum of the weights has as well
+        rel = 2 * torch.expm1(ds) + 2.0 ** -20 + 2 * (L + 64) * U32 + (u + 2 * 7.5e-5 if q.dtype == torch.bfloat16 else 0)
         out[t0:t1] = y.reshape(t1 - t0, H, d)
         bound[t0:t1] = (rel * a + u * (y.abs() + rel * a)).reshape(t1 - t0, H, d) + 1e-30
     return out, bound

@@ -149,6 +149,33 @@ def test_append_leaves_bad_pages_alone():
     assert torch.equal(changed, want)
 
 
+@pytest.mark.parametrize("what", ["falls", "passes n", "starts late"])
+def test_append_broken_offsets(what):
+    """Rows that two sequences claim, or that there are not, are written for nobody; rows before cu_q[0] belong to nobody."""
+    s = ph.Setting([1, 2, 1], [40, 30, 20], 4, 2, 64, FP32, 16)
+    cache, K0 = s.cache(), s.K.clone()
+    q_out = torch.full_like(s.q, 7.0)
+    if what == "falls":
+        s.cu_q.copy_(torch.tensor([0, 3, 1, 4], dtype=torch.int32))
+        ours, tokens, status = [], [0, 3], 8          # rows 0 and 3 still have one sequence: [0, 3) and [1, 4) by the edges
+    elif what == "passes n":
+        s.cu_q[3] = 9
+        ours, tokens, status = [(0, 39), (1, 28), (1, 29)], [0, 1, 2], 8
+    else:
+        s.cu_q.copy_(torch.tensor([1, 1, 3, 4], dtype=torch.int32))
+        ours, tokens, status = [(1, 28), (1, 29), (2, 19)], [1, 2, 3], 0
+    cache.append(s.batch(), s.k, s.v, q=s.q, q_out=q_out)
+    assert cache.status() == status
+    if what != "falls":
+        changed = (torch.nan_to_num(s.K) != torch.nan_to_num(K0)).any(-1).any(1)
+        want = torch.zeros_like(changed)
+        for b, j in ours:
+            want[int(s.table[b, j // 16]), j % 16] = True
+        assert torch.equal(changed, want)
+    for i in range(4):
+        assert bool((q_out[i] == 7).all()) == (i not in tokens)
+
+
 # ---- attention ------------------------------------------------------------------------------------
 
 ATTENDS = {  # new, own, edges, prefix, behind
@@ -381,3 +408,5 @@ def test_other_device_and_type_are_refused():
         cache.attend(batch, s.q, scale=-1.0)
     with pytest.raises(binding.SubgenError):
         cache.attend(batch, s.q[:, :3])
+    with pytest.raises(binding.SubgenError):
+        cache.attend(batch, s.q, out=s.q)

@@ -28,8 +28,8 @@ def _heads(**kw):
 
 def _attend(pages=None, batch=None, q=None, out=None, n=2, H=32, scale=1.0, ws=P, size=1 << 40):
     pages, batch = pages or _pages(), batch or _batch()
-    args = binding.AttendArgs(q or _heads(), out or _heads(), ws, size, n, H, scale, 1)
-    return binding.load().subgen_paged_attend(pages, batch, args, None)
+    args = binding.AttendArgs(q or _heads(), out or _heads(p=2 * P), ws, size, n, H, scale, 1)
+    return binding.load().subgen_paged_attend(pages, batch, args, None)             # (q and out differ unless a test says so)
 
 
 def _qk(**kw):
@@ -68,11 +68,12 @@ def test_batches(call, kw, word):
 def test_attend():
     assert _attend(H=12) == -1 and "H / Hkv" in _said()
     assert _attend(H=128) == -1 and "H / Hkv" in _said()
-    for scale in (0.0, -1.0, float("nan"), float("inf")):
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 3e38):
         assert _attend(scale=scale) == -1 and "scale" in _said()
     assert _attend(n=-1) == -1 and "n must" in _said()
     assert _attend(n=1 << 30) == -1 and "rows" in _said()
     assert _attend(q=_heads(p=None)) == -1 and "q must not" in _said()
+    assert _attend(out=_heads(p=P)) == -1 and "out must not be q" in _said()
     assert _attend(out=_heads(token_stride=1025)) == -1 and "out" in _said()
     assert _attend(ws=None) == -2 and "workspace" in _said()
     assert _attend(ws=P + 64) == -2 and "aligned" in _said()
