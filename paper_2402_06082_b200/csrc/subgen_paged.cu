@@ -156,10 +156,11 @@ template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
 int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
-        // parts of a row unit that a block joins at a time: 4 rows while the blocks that fit can take all rows at once, else 8,
-    // and 16 for prompts, most of whose rows need none (RU is a multiple of each)
+        // parts of a row unit that a block joins at a time: as few rows as let the blocks that fit take all of them at once, up
+    // to 16 for prompts, most of whose rows need none (RU is a multiple of each)
     const long long rows = (long long)a.n * a.H, once = kSMs * kMergeBlocks;
-    const int part = rows <= once * 4 ? 4 : rows <= once * 8 || RU == 8 ? 8 : 16;
+    int part = 1;
+    while (part < 16 && part < RU && rows > once * part) part *= 2;
     const long long units = ((long long)P.B + ((long long)a.n << a.g_shift) / part) * P.Hkv;
     cfg.gridDim = dim3((unsigned)(units < kSMs * kMergeBlocks ? units : kSMs * kMergeBlocks));
     cfg.blockDim = dim3(kMergeThreads);

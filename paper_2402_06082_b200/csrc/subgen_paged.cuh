@@ -585,10 +585,12 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
 #pragma unroll
                         for (int j = 0; j < VL; ++j) acc[j] *= al;
                         unsigned left = __ballot_sync(0xffffffffu, have);
-                        while (left) {
-                            float x[8][VL], fx[8];
+                        // W numerators, all loads in flight
+                        auto add = [&](auto width) {
+                            constexpr int W = decltype(width)::value;
+                            float x[W][VL], fx[W];
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) {
+                            for (int q = 0; q < W; ++q) {
                                 const int src = left ? __ffs(left) - 1 : -1;
                                 left &= left - 1;
                                 const int s = __shfl_sync(0xffffffffu, slot, src & 31);
@@ -608,9 +610,13 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
                                 }
                             }
 #pragma unroll
-                            for (int q = 0; q < 8; ++q)
+                            for (int q = 0; q < W; ++q)
 #pragma unroll
                                 for (int j = 0; j < VL; ++j) acc[j] = fmaf(x[q][j], fx[q], acc[j]);
+                        };
+                        while (left) {
+                            if (__popc(left) > 3) add(std::integral_constant<int, 8>());
+                            else add(std::integral_constant<int, 3>());
                         }
                     }
                 }
