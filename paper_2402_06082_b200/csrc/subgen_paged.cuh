@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
 // then sequences (own tokens against the sequence's rows). An entry's rows (tokens x G heads, in packed order, so a
 // group's rows are one range of tokens) are cut into row units of RU rows, each unit's keys into tiles of KT tokens.
 // A unit with tiles has weight LEAD (what starting and ending a run costs, in tiles) plus 1 for each tile, or 2 where
-// both halves of its rows are in use. All weights of all heads lie on one line; block c takes [c * chunk, (c+1) * chunk)
+// more than half of 128 or 256 rows are in use. All weights of all heads lie on one line; block c takes [c * chunk, (c+1) * chunk)
 // of it, so every block has the same work whatever the lengths are, and a unit that several blocks share leaves one
 // partial result (numerator, largest score, sum) per block.
 // A group folds its prefix into the sequences' entries (own tiles follow the prefix's tiles there) when that costs no
@@ -333,7 +333,7 @@ struct Plan {
         const int last = min(e.rows, (ru + 1) * RU) - 1;
         return prefix_tiles(e) + (own_limit(e, last) + KT - 1) / KT;
     }
-    __device__ static __forceinline__ int shift(int rows) { return DUAL && rows > RU / 2 ? 1 : 0; }     // a tile weighs 1 << shift
+    __device__ static __forceinline__ int shift(int rows) { return RU >= 128 && rows > RU / 2 ? 1 : 0; }     // a tile weighs 1 << shift
     __device__ __forceinline__ int unit_weight(int tiles, int rows) const { return tiles ? LEAD + (tiles << shift(rows)) : 0; }
     // tiles of a unit before position p of its weight
     __device__ static __forceinline__ int tile_at(int p, int sh) { return p <= LEAD ? 0 : (p - LEAD + sh) >> sh; }

@@ -2,9 +2,12 @@
 //
 // One block takes a run of key tiles of one row unit (see Plan), both products on the fp32 pipes from shared memory, the
 // running maximum and sum of the softmax in registers. Two kernels:
-//   many rows (RU = 64): a thread holds 4 rows x 4 scores of a tile of 64 tokens and 4 rows x D / 16 columns of the
-//     numerator, so each value read from shared memory serves four rows; the 16 threads of a row are half a warp, so row
-//     reductions are four shuffles. Bound by the fp32 pipes; two blocks an SM cover for each other's copies.
+//   many rows (RU = d): a thread holds up to d / 16 rows (1, 2, 4 or 8, as many as the unit's rows need) x 4 scores of a
+//     tile of 64 tokens and as many rows x d / 16 columns of the numerator; the 16 threads of a row are half a warp, so row
+//     reductions are four shuffles. Bound by what shared memory delivers (8 rows: 12 16-byte loads for 128 multiply-adds,
+//     4 rows: 8 for 64), then by the fp32 pipes. K and V are copied (cp.async) as soon as the one before has been read: K
+//     during P V, V during the next Q K^T. At d = 128 one block of 128 rows an SM against two of 64: 860 and 920 us (1000
+//     new tokens x 32 heads behind 1000 to 1700 others, 32 TFLOP/s); at d = 64 two blocks of 64 rows are ahead, 192 and 200.
 //   few rows (RU = 8): single tokens and drafts, where the cache is read once and the copies must never stop. A warp is on
 //     its own with a quarter of the tile's tokens: its lanes share the tokens' scores for all rows, then each holds
 //     D / 32 columns of the numerator; the next tile is copied (cp.async) meanwhile, three blocks an SM, and the warps'
@@ -18,7 +21,7 @@ constexpr int kSimtLead = 1;
 
 template <int D>
 struct SimtSmem {
-    static constexpr int RU = 64, KT = 64, NT = 256, BLOCKS = 2;
+    static constexpr int RU = D, KT = 64, NT = 256, BLOCKS = D == 64 ? 2 : 1;
     float Q[RU][D];
     float K[KT][D + 4];                               // + 4: sixteen threads read sixteen rows at once
     float V[KT][D];
@@ -41,8 +44,9 @@ __device__ __forceinline__ void copy16(void* to, const void* from, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
-// Tile t of a run into shared memory: tokens behind the end and unusable pages as zeros.
-template <int KT, int D, int NT>
+// Tile t of a run into shared memory, K or V or (one loop, one look at the page) both: tokens behind the end and unusable
+// pages as zeros. One group of copies.
+template <int KT, int D, int NT, bool HAS_K, bool HAS_V>
 __device__ __forceinline__ void bring_tile(const PagedView& P, const Seg& g, int t, float* K, int k_stride, float* V, int* bad) {
     constexpr int LPR = D / 4;
     const bool pre = t < g.kp;
@@ -59,8 +63,8 @@ __device__ __forceinline__ void bring_tile(const PagedView& P, const Seg& g, int
             if (there) off = id * P.ps + g.head * P.hs + (pos & ((1 << P.page_shift) - 1)) * P.ts + piece * 4;
             else *bad = 1;
         }
-        copy16(K + j * k_stride + piece * 4, (const float*)P.K + off, there);
-        copy16(V + j * D + piece * 4, (const float*)P.V + off, there);
+        if (HAS_K) copy16(K + j * k_stride + piece * 4, (const float*)P.K + off, there);
+        if (HAS_V) copy16(V + j * D + piece * 4, (const float*)P.V + off, there);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
 }
@@ -174,7 +178,7 @@ __global__ void __launch_bounds__(FewSmem<D>::NT, FewSmem<D>::BLOCKS) paged_atte
         __syncthreads();
         auto bring = [&](int t) {
             const int at = (t - g.tile0) & 1;
-            bring_tile<KT, D, NT>(P, g, t, &sm.K[at][0][0], D + 4 * S::SPLIT, &sm.V[at][0][0], &sm.bad);
+            bring_tile<KT, D, NT, true, true>(P, g, t, &sm.K[at][0][0], D + 4 * S::SPLIT, &sm.V[at][0][0], &sm.bad);
         };
         bring(g.tile0);
         bring_queries<RU, D, NT>(a, g, sm.Q);
@@ -242,11 +246,96 @@ __global__ void __launch_bounds__(FewSmem<D>::NT, FewSmem<D>::BLOCKS) paged_atte
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(SimtSmem<D>::NT) paged_attend_simt_kernel(PagedView P, Attend a) {
+// One tile against 16 * R rows (many rows); thread (tx, ty) has rows ty + 16 i, tokens tx + 16 j and columns tx * 4 + 64 b.
+// K of the tile is there, V on its way; asks for K and V of the next one when these have been read.
+template <int D, int R>
+__device__ __forceinline__ void simt_tile(SimtSmem<D>& sm, const PagedView& P, const Seg& g, int t, const int* own, float c, float* m, float* l,
+                                          float (*acc)[D / 16]) {
     typedef SimtSmem<D> S;
-    constexpr int RU = S::RU, KT = S::KT, NT = S::NT, TK = KT / 16, TY = NT / 16, RPT = RU / TY;
-    static_assert(RPT * TY == RU, "rows divide");
+    constexpr int KT = S::KT, NT = S::NT, TK = KT / 16;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const bool pre = t < g.kp, more = t + 1 < g.tile1;
+    const int base = (pre ? t : t - g.kp) * KT;
+    float s[R][TK];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < TK; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < D; e += 4) {
+        float4 kv[TK];
+#pragma unroll
+        for (int j = 0; j < TK; ++j) kv[j] = *reinterpret_cast<const float4*>(&sm.K[tx + 16 * j][e]);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float4 qv = *reinterpret_cast<const float4*>(&sm.Q[ty + 16 * i][e]);
+#pragma unroll
+            for (int j = 0; j < TK; ++j) s[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, s[i][j]))));
+        }
+    }
+    __syncthreads();                                                 // K has been read
+    if (more) {
+        bring_tile<KT, D, NT, true, false>(P, g, t + 1, &sm.K[0][0], D + 4, nullptr, &sm.bad);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");         // V of this tile
+    } else {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int lim = (pre ? g.e.P : own[i]) - base;
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < TK; ++j) {
+            s[i][j] = tx + 16 * j < lim ? s[i][j] * c : -INFINITY;
+            top = fmaxf(top, s[i][j]);
+        }
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const float mn = fmaxf(m[i], top), b = mn == -INFINITY ? 0.f : mn;
+        const float al = exp2f(m[i] - b);
+        m[i] = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < TK; ++j) {
+            const float p = exp2f(s[i][j] - b);
+            sum += p;
+            sm.P[ty + 16 * i][tx + 16 * j] = p;
+        }
+        l[i] = l[i] * al + sum;                                      // this thread's share; the 16 are added at the end
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) acc[i][j] *= al;
+    }
+    __syncthreads();                                                 // V is there for all (P would need its half-warp only)
+#pragma unroll 4
+    for (int j = 0; j < KT; j += 4) {
+        float4 p[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) p[i] = *reinterpret_cast<const float4*>(&sm.P[ty + 16 * i][j]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int b = 0; b < D / 64; ++b) {
+                const float4 v = *reinterpret_cast<const float4*>(&sm.V[j + q][b * 64 + tx * 4]);
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const float w = q == 0 ? p[i].x : q == 1 ? p[i].y : q == 2 ? p[i].z : p[i].w;
+                    acc[i][b * 4 + 0] = fmaf(w, v.x, acc[i][b * 4 + 0]);
+                    acc[i][b * 4 + 1] = fmaf(w, v.y, acc[i][b * 4 + 1]);
+                    acc[i][b * 4 + 2] = fmaf(w, v.z, acc[i][b * 4 + 2]);
+                    acc[i][b * 4 + 3] = fmaf(w, v.w, acc[i][b * 4 + 3]);
+                }
+            }
+        }
+    }
+    __syncthreads();                                                 // V has been read
+    if (more) bring_tile<KT, D, NT, false, true>(P, g, t + 1, nullptr, 0, &sm.V[0][0], &sm.bad);
+}
+
+template <int D>
+__global__ void __launch_bounds__(SimtSmem<D>::NT, SimtSmem<D>::BLOCKS) paged_attend_simt_kernel(PagedView P, Attend a) {
+    typedef SimtSmem<D> S;
+    constexpr int RU = S::RU, KT = S::KT, NT = S::NT, RPT = RU / 16;
+    static_assert(NT == 256, "16 x 16 threads");
     extern __shared__ __align__(16) unsigned char dyn[];
     S& sm = *reinterpret_cast<S*>(dyn);
     Plan<RU, KT, false, kSimtLead> plan(P, a);
@@ -258,11 +347,11 @@ __global__ void __launch_bounds__(SimtSmem<D>::NT) paged_attend_simt_kernel(Page
     while (x < x1) {
         const Seg g = plan.next(x, x1, blockIdx.x);
         if (g.tile0 >= g.tile1) continue;
-        const int row0 = g.ru * RU;
         __syncthreads();
         if (tid == 0) sm.bad = g.e.bad;
         __syncthreads();
-        bring_tile<KT, D, NT>(P, g, g.tile0, &sm.K[0][0], D + 4, &sm.V[0][0], &sm.bad);
+        bring_tile<KT, D, NT, true, false>(P, g, g.tile0, &sm.K[0][0], D + 4, nullptr, &sm.bad);
+        bring_tile<KT, D, NT, false, true>(P, g, g.tile0, nullptr, 0, &sm.V[0][0], &sm.bad);
         bring_queries<RU, D, NT>(a, g, sm.Q);
         float m[RPT], l[RPT], acc[RPT][D / 16];
         int own[RPT];
@@ -270,90 +359,25 @@ __global__ void __launch_bounds__(SimtSmem<D>::NT) paged_attend_simt_kernel(Page
         for (int i = 0; i < RPT; ++i) {
             m[i] = -INFINITY;
             l[i] = 0.f;
-            own[i] = plan.own_limit(g.e, row0 + ty * RPT + i);
+            own[i] = plan.own_limit(g.e, g.ru * RU + ty + 16 * i);
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) acc[i][j] = 0.f;
         }
         for (int t = g.tile0; t < g.tile1; ++t) {
-            const bool pre = t < g.kp;
-            const int base = (pre ? t : t - g.kp) * KT, limit = pre ? g.e.P : g.e.S;
-            if (t > g.tile0) bring_tile<KT, D, NT>(P, g, t, &sm.K[0][0], D + 4, &sm.V[0][0], &sm.bad);
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            asm volatile("cp.async.wait_group 1;" ::: "memory");     // K of this tile
             __syncthreads();
-            float s[RPT][TK];
-#pragma unroll
-            for (int i = 0; i < RPT; ++i)
-#pragma unroll
-                for (int j = 0; j < TK; ++j) s[i][j] = 0.f;
-#pragma unroll 4
-            for (int e = 0; e < D; e += 4) {
-                float4 kv[TK];
-#pragma unroll
-                for (int j = 0; j < TK; ++j) kv[j] = *reinterpret_cast<const float4*>(&sm.K[tx + 16 * j][e]);
-#pragma unroll
-                for (int i = 0; i < RPT; ++i) {
-                    const float4 qv = *reinterpret_cast<const float4*>(&sm.Q[ty * RPT + i][e]);
-#pragma unroll
-                    for (int j = 0; j < TK; ++j)
-                        s[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, s[i][j]))));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < RPT; ++i) {
-                const int lim = (pre ? limit : own[i]) - base;
-                float top = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < TK; ++j) {
-                    s[i][j] = tx + 16 * j < lim ? s[i][j] * a.c : -INFINITY;
-                    top = fmaxf(top, s[i][j]);
-                }
-#pragma unroll
-                for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                const float mn = fmaxf(m[i], top), b = mn == -INFINITY ? 0.f : mn;
-                const float al = exp2f(m[i] - b);
-                m[i] = mn;
-                float sum = 0.f;
-#pragma unroll
-                for (int j = 0; j < TK; ++j) {
-                    const float p = exp2f(s[i][j] - b);
-                    sum += p;
-                    sm.P[ty * RPT + i][tx + 16 * j] = p;
-                }
-                l[i] = l[i] * al + sum;                              // this thread's share; the 16 are added at the end
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) acc[i][j] *= al;
-            }
-            __syncwarp();                                            // a row's scores come from and go to one half-warp
-#pragma unroll 4
-            for (int j = 0; j < KT; j += 4) {
-                float4 p[RPT];
-#pragma unroll
-                for (int i = 0; i < RPT; ++i) p[i] = *reinterpret_cast<const float4*>(&sm.P[ty * RPT + i][j]);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-#pragma unroll
-                    for (int b = 0; b < D / 64; ++b) {
-                        const float4 v = *reinterpret_cast<const float4*>(&sm.V[j + q][b * 64 + tx * 4]);
-#pragma unroll
-                        for (int i = 0; i < RPT; ++i) {
-                            const float w = q == 0 ? p[i].x : q == 1 ? p[i].y : q == 2 ? p[i].z : p[i].w;
-                            acc[i][b * 4 + 0] = fmaf(w, v.x, acc[i][b * 4 + 0]);
-                            acc[i][b * 4 + 1] = fmaf(w, v.y, acc[i][b * 4 + 1]);
-                            acc[i][b * 4 + 2] = fmaf(w, v.z, acc[i][b * 4 + 2]);
-                            acc[i][b * 4 + 3] = fmaf(w, v.w, acc[i][b * 4 + 3]);
-                        }
-                    }
-                }
-            }
-            __syncthreads();                                         // the tile may be filled again
+            if (g.rows <= 16) simt_tile<D, 1>(sm, P, g, t, own, a.c, m, l, acc);
+            else if (g.rows <= 32) simt_tile<D, 2>(sm, P, g, t, own, a.c, m, l, acc);
+            else if (RU == 64 || g.rows <= 64) simt_tile<D, 4>(sm, P, g, t, own, a.c, m, l, acc);
+            else simt_tile<D, RU / 16>(sm, P, g, t, own, a.c, m, l, acc);
         }
-        const bool bad = sm.bad != 0;
+        const bool bad = sm.bad != 0;                                // last written before the last tile's barriers
         if (bad && tid == 0) paged_status(P, kStPage);
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
 #pragma unroll
             for (int off = 8; off > 0; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
-            const int r = ty * RPT + i;
+            const int r = ty + 16 * i;
             if (bad) l[i] = NAN;
             if (r < g.rows) {
                 const float f = !g.direct ? 1.f : l[i] == 0.f ? 0.f : 1.f / l[i];
