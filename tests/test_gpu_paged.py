@@ -1,6 +1,7 @@
 """GPU tests of the head norms with rotation, the paged append and the paged attention, against 64-bit statements."""
 import math
 import os
+import random
 import sys
 
 import pytest
@@ -323,6 +324,98 @@ def test_attend_on_two_streams_at_once(dtype):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(x, alone[i]) for x in outs[i])
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_attend_two_graphs_at_once(dtype):
+    s = ph.Setting([1] * 12, [2000 + 31 * i for i in range(12)], 8, 2, 128, dtype, 16, [0, 12], [3000], seed=1)
+    cache, batch = s.cache(), s.batch()
+    alone = cache.attend(batch, s.q, scale=0.1)
+    torch.cuda.synchronize()
+    graphs, outs, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(cache.attend(batch, s.q, scale=0.1))
+        graphs.append(g)
+    for _ in range(10):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, alone) for o in outs)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_as_many_sequences_as_there_may_be(dtype):
+    """1000 sequences in 24 groups, some of them empty, and one more than there may be."""
+    from paper_2402_06082_b200 import binding
+    B, G = 1000, 24
+    new = [i % 3 for i in range(B)]
+    own = [new[i] + (7 * i) % 40 for i in range(B)]
+    edges = sorted((i * i * B // (G * G)) for i in range(G + 1))
+    s = ph.Setting(new, own, 2, 1, 64, dtype, 16, edges, [11 * i for i in range(G)], seed=1, behind=3)
+    cache = s.cache()
+    out = cache.attend(s.batch(), s.q, scale=0.2)
+    want, bound = s.want(0.2)
+    m = s.cu[-1]
+    ph.assert_within(out[:m], want[:m], bound[:m])
+    assert cache.status() == 0
+    more = ph.Setting([1] * 1025, [1] * 1025, 2, 1, 64, dtype, 16)
+    with pytest.raises(binding.SubgenError):
+        more.cache().attend(more.batch(), more.q)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_sequences_that_read_the_same_pages(dtype):
+    s = ph.Setting([2, 2, 1], [90, 90, 300], 4, 2, 128, dtype, 16, seed=5)
+    s.table[1] = s.table[0]
+    s.q[2:4] = s.q[0:2]
+    out = s.cache().attend(s.batch(), s.q, scale=0.1)
+    want, bound = s.want(0.1)
+    ph.assert_within(out, want, bound)
+    assert torch.equal(out[0:2], out[2:4])
+
+
+def random_setting(seed):
+    r = random.Random(seed)
+    dtype, d, page = r.choice([BF16, BF16, FP32]), r.choice([64, 128]), r.choice([16, 32, 64, 128, 256, 1024])
+    G, Hkv, B = r.choice([1, 2, 4, 8]), r.choice([1, 2, 3, 5]), r.randint(1, 20)
+    top, long = r.choice([1, 1, 3, 9, 70, 300]), r.choice([1, 20, 130, 600, 3000])
+    new = [r.choice([0, 1, r.randint(0, top)]) for _ in range(B)]
+    new[r.randrange(B)] += 1
+    own = [r.choice([k, k + r.randint(0, long), max(0, k - 1)]) for k in new]
+    edges, prefix = [], []
+    if r.random() < 0.7:
+        g = r.randint(1, min(B, 4))
+        edges = [0] + sorted(r.randint(0, B) for _ in range(g - 1)) + [B]
+        prefix = [r.choice([0, r.randint(0, 40), r.randint(0, 2500)]) for _ in range(g)]
+    return ph.Setting(new, own, G * Hkv, Hkv, d, dtype, page, edges, prefix, seed=seed, behind=r.choice([0, 0, 5]), rows_first=r.random() < 0.3), r
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_attend_random(seed):
+    s, r = random_setting(seed)
+    scale, causal, m = r.choice([0.05, s.d ** -0.5, 0.7]), r.random() < 0.8, s.cu[-1]
+    cache = s.cache()
+    out = cache.attend(s.batch(), s.q, scale=scale, causal=causal)
+    want, bound = s.want(scale, causal)
+    ph.assert_within(out[:m], want[:m], bound[:m], "seed %d" % seed)
+    assert cache.status() == 0
+
+
+def test_nothing_at_all():
+    from paper_2402_06082_b200 import binding
+    s = ph.Setting([1], [5], 4, 2, 64, BF16)
+    none = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    empty = binding.PagedBatch(none(1), none(0), none(0, 4))
+    cache = s.cache()
+    assert cache.attend(empty, s.q).shape == s.q.shape and cache.append(empty, s.k, s.v) is None
+    assert cache.attend(s.batch(), s.q[:0]).shape == (0, 4, 64) and cache.append(s.batch(), s.k[:0], s.v[:0], q=s.q[:0]).shape == (0, 4, 64)
+    assert cache.status() == 0
 
 
 def test_offsets_beyond_32_bits():
