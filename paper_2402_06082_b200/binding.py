@@ -1,6 +1,7 @@
 """Thin ctypes binding of libsubgen.so (declared in include/subgen.h).
 
-Argument marshalling only: every step of the path runs in the library's CUDA kernels. torch is used
+Argument marshalling only: every step of the path runs in the library's CUDA kernels (the paged functions are called
+through the C++ module _calls.so instead of ctypes). torch is used
 for device memory and streams. There is no CPU path: loading fails loudly if the shared library is
 missing, and every call fails if no CUDA device is usable.
 """

@@ -239,6 +239,23 @@ def test_attend_strided_queries(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("page", [16, 64])
+def test_pools_that_are_halves_of_one_tensor(dtype, page):
+    """K and V as [:, 0] and [:, 1] of [pages, 2, Hkv, page, d], and one head of several."""
+    from paper_2402_06082_b200 import binding
+    s = ph.Setting([1, 3], [200, 90], 4, 2, 128, dtype, page, [0, 2], [70], seed=6)
+    both = torch.stack((s.K, s.V), 1)
+    cache = binding.PagedCache(both[:, 0], both[:, 1])
+    want, bound = s.want(0.1)
+    ph.assert_within(cache.attend(s.batch(), s.q, scale=0.1), want, bound)
+    one = binding.PagedCache(both[:, 0, 1:], both[:, 1, 1:])           # the second KV head and its two query heads
+    ph.assert_within(one.attend(s.batch(), s.q[:, 2:], scale=0.1), want[:, 2:], bound[:, 2:])
+    cache.append(s.batch(), s.k, s.v)
+    assert torch.equal(both[int(s.table[0, 199 // page]), 0, :, 199 % page], s.k[0])
+    assert torch.equal(both[int(s.table[1, 89 // page]), 1, :, 89 % page], s.v[3])
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_attend_bad_pages_and_lengths(dtype):
     """A page outside the pool or a length beyond its table: NaN for the rows that needed it, the others as ever."""
     s = ph.Setting([1, 1, 2, 1, 1, 1], [300, 20, 200, 5, 9, 40], 8, 2, 128, dtype, 16, [0, 5, 6], [100, 30], seed=3)
