@@ -283,6 +283,7 @@ struct Plan {
     }
     __device__ __forceinline__ int group_of(int b) const {
         int lo = 0, hi = P.groups - 1;
+#pragma unroll 1
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (__ldg(P.cu_group + mid) <= b) lo = mid; else hi = mid - 1;
@@ -345,10 +346,13 @@ struct Plan {
         int* s = t + E + 1;
         // entry() reads these one after the other: asked for at once, so that it finds them in L1
         auto touch = [](const int* p) { int x; asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(x) : "l"(p)); };
+#pragma unroll 1
         for (int b = threadIdx.x; b < P.B; b += blockDim.x) { touch(P.cu_q + b); touch(P.lengths + b); }
+#pragma unroll 1
         for (int g = threadIdx.x; g < P.groups; g += blockDim.x) { touch(P.cu_group + g); touch(P.prefix_len + g); }
         if (threadIdx.x == 0) *flag = 0;
         __syncthreads();
+#pragma unroll 1
         for (int i = threadIdx.x; i < E; i += blockDim.x) {
             const Entry e = entry(i);
             bool bad;
@@ -362,6 +366,7 @@ struct Plan {
             int sl = 0;
             if (bad) *flag = 1;
             else {
+#pragma unroll 1
                 for (int ru = 0; ru * RU < e.rows; ++ru) {
                     const int rows = unit_rows(e, ru);
                     w += unit_weight(unit_tiles(e, ru), rows);
@@ -372,26 +377,30 @@ struct Plan {
             s[i + 1] = sl;
         }
         __syncthreads();
-        if (threadIdx.x < 32 && *flag == 0) {
-            long long at = 0;
-            int as = 0;
+        if (threadIdx.x < 32) {
+            // sums that stay at kPlanWeight once they reach it. Loops as they stand: a block starts with no code in its caches,
+            // and each new 128 bytes of it (8 instructions) cost over 300 cycles; unrolled, this took 3500 to 11000.
+            const int lane = threadIdx.x;
+            unsigned at = 0, as = 0;
+#pragma unroll 1
             for (int i0 = 0; i0 < E; i0 += 32) {
-                const int i = i0 + (int)threadIdx.x;
-                long long x = i < E ? t[i + 1] : 0;
-                int y = i < E ? s[i + 1] : 0;
-#pragma unroll
+                const int i = i0 + lane;
+                unsigned x = i < E ? t[i + 1] : 0, y = i < E ? s[i + 1] : 0;
+#pragma unroll 1
                 for (int off = 1; off < 32; off <<= 1) {
-                    const long long xo = __shfl_up_sync(0xffffffffu, x, off);
-                    const int yo = __shfl_up_sync(0xffffffffu, y, off);
-                    if ((int)threadIdx.x >= off) { x += xo; y += yo; }
+                    const unsigned xo = __shfl_up_sync(0xffffffffu, x, off), yo = __shfl_up_sync(0xffffffffu, y, off);
+                    x = lane >= off ? min(x + xo, (unsigned)kPlanWeight) : x;
+                    y += lane >= off ? yo : 0;
                 }
-                if (i < E) { t[i + 1] = (int)(at + x); s[i + 1] = as + y; }
-                at += __shfl_sync(0xffffffffu, x, 31);
-                as += __shfl_sync(0xffffffffu, y, 31);
+                x = min(at + x, (unsigned)kPlanWeight);
+                y += as;
+                if (i < E) { t[i + 1] = (int)x; s[i + 1] = (int)y; }
+                at = __shfl_sync(0xffffffffu, x, 31);
+                as = __shfl_sync(0xffffffffu, y, 31);
             }
-            if (threadIdx.x == 0) {
+            if (lane == 0) {
                 t[0] = s[0] = 0;
-                if (at * P.Hkv > kPlanWeight) *flag = 1;
+                if ((long long)at * P.Hkv >= kPlanWeight) *flag = 1;
             }
         }
         __syncthreads();
@@ -415,6 +424,7 @@ struct Plan {
         g.head = x / head_w;
         int r = x - g.head * head_w;
         int lo = 0, hi = E - 1;
+#pragma unroll 1
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (tscan[mid] <= r) lo = mid; else hi = mid - 1;
@@ -424,6 +434,7 @@ struct Plan {
         g.e = entry(lo);
         g.kp = prefix_tiles(g.e);
         int ru = 0, w;
+#pragma unroll 1
         while (true) {
             g.rows = unit_rows(g.e, ru);
             g.tiles = unit_tiles(g.e, ru);
@@ -474,10 +485,11 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
     }
     if (warp == 0) {
         int at = 0;
+#pragma unroll 1
         for (int i0 = 0; i0 < P.B; i0 += 32) {
             const int b = i0 + lane;
             int x = b < P.B ? (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + part - 1) / part : 0;
-#pragma unroll
+#pragma unroll 1
             for (int off = 1; off < 32; off <<= 1) {
                 const int xo = __shfl_up_sync(0xffffffffu, x, off);
                 if (lane >= off) x += xo;
@@ -492,6 +504,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
     // first position of the line that belongs to row unit ru of a sequence's entry
     auto unit_start = [&](const Entry& e, int ei, int h, int ru) {
         int u0 = h * plan.head_w + plan.tscan[ei];
+#pragma unroll 1
         for (int k = 0; k < ru; ++k) u0 += plan.unit_weight(plan.unit_tiles(e, k), RU);
         return u0;
     };
@@ -503,7 +516,8 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
         if (mine < items) {
             const int h = mine / units, u = mine - h * units;
             int lo = 0, hi = P.B - 1;
-            while (lo < hi) {
+    #pragma unroll 1
+        while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (uscan[mid] <= u) lo = mid; else hi = mid - 1;
             }
@@ -562,6 +576,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
                         all += ((v0 + vw - 1) / chunk - vc + 1) << vper;
                     }
                     const int oslot = plan.slot_of(ei, ru, h, 0) + r;
+#pragma unroll 1
                     for (int i0 = 0; i0 < all; i0 += wpr * 32) {
                         const int i = i0 + lane * wpr + sub;
                         const bool pre = i >= own;
@@ -573,12 +588,12 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
                         float2 st = make_float2(-INFINITY, 0.f);
                         if (have) st = __ldcg(a.stat + slot);
                         float top = st.x;
-#pragma unroll
+#pragma unroll 1
                         for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
                         const float mn = fmaxf(m, top), bs = mn == -INFINITY ? 0.f : mn, al = exp2f(m - bs);
                         const float f = have ? exp2f(st.x - bs) : 0.f;
                         float sum = have ? st.y * f : 0.f;
-#pragma unroll
+#pragma unroll 1
                         for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
                         m = mn;
                         l = l * al + sum;
@@ -627,11 +642,13 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
                     for (int j = 0; j < VL; ++j) join[warp][lane * VL + j] = acc[j];
                     __syncthreads();
                     float mm = -INFINITY;
+#pragma unroll 1
                     for (int k = 0; k < wpr; ++k) mm = fmaxf(mm, join_stat[warp - sub + k].x);
                     const float bs = mm == -INFINITY ? 0.f : mm;
                     l = 0.f;
 #pragma unroll
                     for (int j = 0; j < VL; ++j) acc[j] = 0.f;
+#pragma unroll 1
                     for (int k = 0; k < wpr; ++k) {
                         const float2 st = join_stat[warp - sub + k];
                         const float f = exp2f(st.x - bs);
