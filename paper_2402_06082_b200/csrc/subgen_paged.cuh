@@ -274,7 +274,7 @@ struct Plan {
         const int b0 = min(max(__ldg(P.cu_group + g), 0), P.B), b1 = min(max(__ldg(P.cu_group + g + 1), 0), P.B);
         *t0 = __ldg(P.cu_q + b0);
         *t1 = __ldg(P.cu_q + b1);
-        return b1 - b0 <= 1 || ((long long)(*t1 - *t0) << a.g_shift) >= (long long)(b1 - b0) * (RU / 2);
+        return b1 - b0 <= 1 || (((long long)*t1 - *t0) << a.g_shift) >= (long long)(b1 - b0) * (RU / 2);
     }
     __device__ __forceinline__ int clipped(int len, int stride, int* bad) const {
         const long long cap = (long long)stride << P.page_shift;
@@ -355,12 +355,11 @@ struct Plan {
 #pragma unroll 1
         for (int i = threadIdx.x; i < E; i += blockDim.x) {
             const Entry e = entry(i);
-            bool bad;
+            // a group's rows too: the loop below is as long as they are many
+            bool bad = e.tok0 < 0 || e.nq < 0 || (long long)e.tok0 + e.nq > a.n;
             if (i < P.groups) {
                 const int b0 = __ldg(P.cu_group + i), b1 = __ldg(P.cu_group + i + 1);
-                bad = b0 < 0 || b1 < b0 || b1 > P.B || (i == 0 && b0 != 0) || (i == P.groups - 1 && b1 != P.B);
-            } else {
-                bad = e.tok0 < 0 || e.nq < 0 || (long long)e.tok0 + e.nq > a.n;
+                bad |= b0 < 0 || b1 < b0 || b1 > P.B || (i == 0 && b0 != 0) || (i == P.groups - 1 && b1 != P.B);
             }
             long long w = 0;
             int sl = 0;

@@ -298,6 +298,20 @@ def test_attend_broken_offsets(dtype, what):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("heads", [(4, 2), (8, 1)])
+@pytest.mark.parametrize("edges", [[0, 1, 3, 2**31 - 1], [0, 2**31 - 1, 3, 4], [0, 1, -2**31, 4], [-2**31, 1, 3, 2**31 - 1], [0, 2**28, 2**29, 2**30]])
+@pytest.mark.parametrize("groups", [[0, 3], [0, 1, 3]])
+def test_attend_offsets_far_out(dtype, heads, edges, groups):
+    """Offsets that would make rows by the billion of a group or a sequence: refused like any that pass n."""
+    s = ph.Setting([1, 2, 1], [40, 30, 20], *heads, 64, dtype, 16, groups, [10] * (len(groups) - 1), seed=3)
+    s.cu_q.copy_(torch.tensor(edges, dtype=torch.int32))
+    out = torch.full_like(s.q, 7.0)
+    cache = s.cache()
+    cache.attend(s.batch(), s.q, out=out)
+    assert cache.status() == 8 and bool((out == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_attend_in_a_graph_with_lengths_that_grow(dtype):
     from paper_2402_06082_b200 import binding
     s = ph.Setting([1, 1, 1], [200, 90, 130], 8, 2, 128, dtype, 16, [0, 3], [260], seed=3)
