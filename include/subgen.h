@@ -397,7 +397,7 @@ typedef struct subgen_pages {
  * its lengths[b] own tokens; own token j lies in page table[b][j / page], row j % page. Rows from cu_q[B] on belong to
  * nobody: they are neither read nor written. Sequences cu_group[g] .. cu_group[g+1] - 1 share prefix g: prefix_len[g]
  * tokens (any number) in the pages prefix_table[g], which come before their own tokens. groups = 0: no prefixes.
- * B + groups <= 1024. */
+ * B + groups <= 1024; a row of a table stands for fewer than 2^31 - 1024 tokens (table_stride * page). */
 typedef struct subgen_batch {
     int B;
     const int* cu_q;        /* [B + 1], non-decreasing from >= 0 to <= the rows of the call */

@@ -87,8 +87,9 @@ int check_cache(const char* fn, const subgen_pages* c, const subgen_batch* b, Pa
         return fail(SUBGEN_EINVAL, "%s: cu_q, lengths and table must not be NULL, table_stride must be positive", fn);
     if (b->groups && (!b->cu_group || !b->prefix_len || !b->prefix_table || b->prefix_stride <= 0))
         return fail(SUBGEN_EINVAL, "%s: cu_group, prefix_len and prefix_table must not be NULL, prefix_stride must be positive", fn);
-    if ((long long)b->table_stride * c->page > 0x7fffffffLL || (b->groups && (long long)b->prefix_stride * c->page > 0x7fffffffLL))
-        return fail(SUBGEN_EINVAL, "%s: a page table must hold fewer than 2^31 tokens", fn);
+    const long long cap = 0x7fffffffLL - 1024;        // a token's index rounded up to tiles stays an int
+    if ((long long)b->table_stride * c->page > cap || (b->groups && (long long)b->prefix_stride * c->page > cap))
+        return fail(SUBGEN_EINVAL, "%s: a page table must hold fewer than 2^31 - 1024 tokens", fn);
     int shift = 0;
     while ((1 << shift) < c->page) ++shift;
     *v = PagedView{(char*)c->K, (char*)c->V, c->page_stride, c->head_stride, c->row_stride, c->pages, shift, c->Hkv,
@@ -156,7 +157,7 @@ template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
 int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
-        // parts of a row unit that a block joins at a time: as few rows as let the blocks that fit take all of them at once, up
+    // parts of a row unit that a block joins at a time: as few rows as let the blocks that fit take all of them at once, up
     // to 16 for prompts, most of whose rows need none (RU is a multiple of each)
     const long long rows = (long long)a.n * a.H, once = kSMs * kMergeBlocks;
     int part = 1;

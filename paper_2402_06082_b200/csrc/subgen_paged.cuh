@@ -515,8 +515,8 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
         if (mine < items) {
             const int h = mine / units, u = mine - h * units;
             int lo = 0, hi = P.B - 1;
-    #pragma unroll 1
-        while (lo < hi) {
+#pragma unroll 1
+            while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (uscan[mid] <= u) lo = mid; else hi = mid - 1;
             }

@@ -65,6 +65,17 @@ def test_batches(call, kw, word):
     assert call(batch=_batch(**kw)) == -1 and word in _said()
 
 
+@pytest.mark.parametrize("call", [_attend, _append])
+@pytest.mark.parametrize("page", [16, 128, 1024])
+def test_longest_tables(call, page):
+    """Lengths end far enough below 2^31 for an index that is rounded up to a tile to stay an int."""
+    most = (2**31 - 1024) // page - 1
+    for n, rc in ((most, 0), (most + 1, -1)):
+        assert call(pages=_pages(page=page), batch=_batch(table_stride=n), n=0) == rc
+        groups = dict(groups=1, cu_group=P, prefix_len=P, prefix_table=P, prefix_stride=n)
+        assert call(pages=_pages(page=page), batch=_batch(**groups), n=0) == rc
+
+
 def test_attend():
     assert _attend(H=12) == -1 and "H / Hkv" in _said()
     assert _attend(H=128) == -1 and "H / Hkv" in _said()
