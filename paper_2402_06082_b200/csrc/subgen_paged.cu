@@ -141,19 +141,21 @@ long long slot_count(const PagedView& P, int n, int H) {
     return entries(P.B) + (P.groups ? entries(P.groups) : 0) + 256LL * kSMs;
 }
 
-template <typename K>
-int opt_in(K kern, size_t smem, bool* done) {
-    int dev = -1;
-    CUDA_TRY(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= kMaxDevices) return fail(SUBGEN_EINVAL, "device index %d not supported", dev);
-    if (!done[dev]) {
-        CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        done[dev] = true;
-    }
+// Once per device: loads a kernel and the merge that follows it, so that both may be captured later.
+template <typename K, typename M>
+int opt_in(K kern, M merge, size_t smem) {
+    cudaFuncAttributes at;
+    CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CUDA_TRY(cudaFuncGetAttributes(&at, merge));
+    return SUBGEN_OK;
+}
+int this_device(int* dev) {
+    CUDA_TRY(cudaGetDevice(dev));
+    if (*dev < 0 || *dev >= kMaxDevices) return fail(SUBGEN_EINVAL, "device index %d not supported", *dev);
     return SUBGEN_OK;
 }
 
-template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
+template <typename T, int D, int RU, int KT, int DUAL, int LEAD>
 int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
@@ -178,19 +180,28 @@ int launch_merge(const PagedView& P, const Attend& a, int blocks, cudaStream_t s
 
 template <typename S, int D, typename K>
 int attend_fp32_with(K kern, const PagedView& P, const Attend& a, cudaStream_t st) {
-    static bool done[kMaxDevices];
     constexpr size_t tile = (sizeof(S) + 15) & ~(size_t)15;
-    const int rc = opt_in(kern, tile + plan_bytes(kPlanMax), done);
-    if (rc) return rc;
     const int blocks = kSMs * S::BLOCKS;
     static_assert(S::RU * S::BLOCKS <= 256, "slot_count");
     kern<<<blocks, S::NT, tile + plan_bytes(P.B + P.groups), st>>>(P, a);
     CUDA_TRY(cudaGetLastError());
-    return launch_merge<float, D, S::RU, S::KT, false, kSimtLead>(P, a, blocks, st);
+    return launch_merge<float, D, S::RU, S::KT, 0, kSimtLead>(P, a, blocks, st);
+}
+template <typename S, int D, typename K>
+int opt_in_fp32(K kern) {
+    return opt_in(kern, paged_merge_kernel<float, D, S::RU, S::KT, 0, kSimtLead>, ((sizeof(S) + 15) & ~(size_t)15) + plan_bytes(kPlanMax));
 }
 
 template <int D>
 int attend_fp32(const PagedView& P, const Attend& a, cudaStream_t st) {
+    static bool done[kMaxDevices];
+    int dev, rc = this_device(&dev);
+    if (!rc && !done[dev]) {                          // both kinds, whichever this call takes
+        rc = opt_in_fp32<FewSmem<D>, D>(paged_attend_few_kernel<D>);
+        if (!rc) rc = opt_in_fp32<SimtSmem<D>, D>(paged_attend_simt_kernel<D>);
+        done[dev] = !rc;
+    }
+    if (rc) return rc;
     // Up to 8 rows a sequence on average: one pass over the cache with little arithmetic to it (16 sequences of 2000 tokens,
     // 8 heads, 8 rows each: 93 us against 216; 12 rows, which take two units there: 191 against 218, but 110 against 82 at
     // d = 64 behind a shared prefix).
@@ -229,10 +240,15 @@ int make_map(CUtensorMap* m, void* p, int rank, const cuuint64_t* dims, const cu
 
 template <int D>
 int attend_tc(const PagedView& P, const Attend& a, cudaStream_t st) {
-    auto kern = paged_attend_tc_kernel<D>;
+    typedef __nv_bfloat16 T;
     static bool done[kMaxDevices];
     constexpr size_t fixed = 1024 + ((sizeof(PtSmem<D>) + 15) & ~(size_t)15);
-    int rc = opt_in(kern, fixed + plan_bytes(kPlanMax), done);
+    int dev, rc = this_device(&dev);
+    if (!rc && !done[dev]) {                          // both kinds, whichever this call takes
+        rc = opt_in(paged_attend_tc_kernel<D, false>, paged_merge_kernel<T, D, kPtRU, kPtKT, 1, kPtLead>, fixed + plan_bytes(kPlanMax));
+        if (!rc) rc = opt_in(paged_attend_tc_kernel<D, true>, paged_merge_kernel<T, D, kPtRU, kPtKT, 2, kPtLead>, fixed + plan_bytes(kPlanMax));
+        done[dev] = !rc;
+    }
     if (rc) return rc;
     CUtensorMap mq, mk, mv;
     {
@@ -254,9 +270,18 @@ int attend_tc(const PagedView& P, const Attend& a, cudaStream_t st) {
         rc = make_map(&mv, P.V, 5, dims5, strides5, box5);
     }
     if (rc) return rc;
-    kern<<<kSMs, kPtThreads, fixed + plan_bytes(P.B + P.groups), st>>>(P, a, mq, mk, mv);
+    const size_t smem = fixed + plan_bytes(P.B + P.groups);
+    // The two groups' results of a unit of up to 32 rows are joined in the block where most units are one block's: no prefixes
+    // and a unit for each block at least (128 sequences of 1024 tokens, 8 KV heads: 107 -> 102 us; but 95 -> 98 with
+    // prefixes, whose partials go to the merge anyway, and 15.4 -> 16.1 for one short sequence, all of it split).
+    if (!P.groups && (long long)P.B * P.Hkv >= kSMs) {
+        paged_attend_tc_kernel<D, true><<<kSMs, kPtThreads, smem, st>>>(P, a, mq, mk, mv);
+        CUDA_TRY(cudaGetLastError());
+        return launch_merge<T, D, kPtRU, kPtKT, 2, kPtLead>(P, a, kSMs, st);
+    }
+    paged_attend_tc_kernel<D, false><<<kSMs, kPtThreads, smem, st>>>(P, a, mq, mk, mv);
     CUDA_TRY(cudaGetLastError());
-    return launch_merge<__nv_bfloat16, D, kPtRU, kPtKT, true, kPtLead>(P, a, kSMs, st);
+    return launch_merge<T, D, kPtRU, kPtKT, 1, kPtLead>(P, a, kSMs, st);
 }
 
 }  // namespace

@@ -258,7 +258,7 @@ struct Attend {
     float2* stat;                                     // [slots] largest score * c, sum
 };
 
-template <int RU, int KT, bool DUAL, int LEAD>
+template <int RU, int KT, int DUAL, int LEAD>
 struct Plan {
     const PagedView& P;
     const Attend& a;
@@ -322,6 +322,9 @@ struct Plan {
         }
         return e;
     }
+    // Units of up to 128 rows, whose tiles two groups of a block share, leave two partials (DUAL 1), or one where the block
+    // joins them (DUAL 2: units of up to 32 rows).
+    __device__ static __forceinline__ int twice(int rows) { return DUAL && rows <= RU / 2 && (DUAL == 1 || rows > 32) ? 1 : 0; }
     // own tokens that row r of an entry sees
     __device__ __forceinline__ int own_limit(const Entry& e, int r) const {
         if (!a.causal) return e.S;
@@ -369,7 +372,7 @@ struct Plan {
                 for (int ru = 0; ru * RU < e.rows; ++ru) {
                     const int rows = unit_rows(e, ru);
                     w += unit_weight(unit_tiles(e, ru), rows);
-                    sl = ru * RU + (DUAL && rows <= RU / 2 ? 2 * rows : rows);
+                    sl = ru * RU + (rows << twice(rows));
                 }
             }
             t[i + 1] = (int)(w > kPlanWeight ? kPlanWeight : w);
@@ -415,7 +418,7 @@ struct Plan {
     }
     __device__ __forceinline__ bool is_direct(const Entry& e, int i, int rows, int tiles) const {
         if (i < P.groups || (P.groups && !e.ptab)) return false;     // partials of the group's entry join in
-        return !DUAL || rows > RU / 2 || tiles == 1;
+        return tiles == 1 || !twice(rows);
     }
     // The run of tiles that starts at x (< x1 <= total) on the line; moves x behind it. May be empty (tile0 == tile1).
     __device__ Seg next(int& x, int x1, int blk) const {
@@ -463,7 +466,7 @@ struct Plan {
 // together, and registers for three blocks an SM.
 constexpr int kMergeThreads = 256, kMergeBlocks = 3;
 
-template <typename T, int D, int RU, int KT, bool DUAL, int LEAD>
+template <typename T, int D, int RU, int KT, int DUAL, int LEAD>
 __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kernel(PagedView P, Attend a, int nblk, int part) {
     constexpr int NW = kMergeThreads / 32, VL = D / 32;
     extern __shared__ __align__(16) unsigned char sm_plan[];
@@ -543,7 +546,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
             const Entry e = plan.entry(ei);
             const int rows = plan.unit_rows(e, ru), tiles = plan.unit_tiles(e, ru), w = plan.unit_weight(tiles, rows), sh = PlanT::shift(rows);
             const int c0 = u0 / chunk, c1 = w ? (u0 + w - 1) / chunk : c0 - 1;
-            const int per = DUAL && !sh ? 1 : 0, own = (c1 - c0 + 1) << per;
+            const int per = PlanT::twice(rows), own = (c1 - c0 + 1) << per;
             int g = -1;
             Entry ge;
             ge.bad = ge.rows = ge.tok0 = ge.P = 0;
@@ -569,7 +572,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
                         vrows = plan.unit_rows(ge, pru);
                         vw = plan.unit_weight(pt, vrows);
                         v0 = h * plan.head_w + plan.tscan[g] + pru * plan.unit_weight(pt, RU);
-                        vper = DUAL && !PlanT::shift(vrows) ? 1 : 0;
+                        vper = PlanT::twice(vrows);
                         vc = v0 / chunk;
                         vslot = plan.slot_of(g, pru, h, 0) + prow - pru * RU;
                         all += ((v0 + vw - 1) / chunk - vc + 1) << vper;

@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(FewSmem<D>::NT, FewSmem<D>::BLOCKS) paged_atte
     constexpr int RU = S::RU, KT = S::KT, NT = S::NT, NW = NT / 32, VL = D / 32;
     extern __shared__ __align__(16) unsigned char dyn[];
     S& sm = *reinterpret_cast<S*>(dyn);
-    Plan<RU, KT, false, kSimtLead> plan(P, a);
+    Plan<RU, KT, 0, kSimtLead> plan(P, a);
     plan.build(dyn + ((sizeof(S) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(SimtSmem<D>::NT, SimtSmem<D>::BLOCKS) paged_at
     static_assert(NT == 256, "16 x 16 threads");
     extern __shared__ __align__(16) unsigned char dyn[];
     S& sm = *reinterpret_cast<S*>(dyn);
-    Plan<RU, KT, false, kSimtLead> plan(P, a);
+    Plan<RU, KT, 0, kSimtLead> plan(P, a);
     plan.build(dyn + ((sizeof(S) + 15) & ~(size_t)15), &sm.flag, gridDim.x);
     pdl_trigger();
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;

@@ -15,6 +15,8 @@
 // Q lies in shared memory four times, so that every warp of a group has all rows in its lanes of tensor memory and
 // takes a quarter of the tile's tokens (the other quarters of its P are zero); the four numerators are added through
 // shared memory at the end of the run. The chain score -> weight -> product is then a quarter as long.
+// HAND: the second group hands the rows of such a unit over to the first, warp to warp, so that a run leaves one result,
+// and a whole sequence nothing for the merge.
 // The numerator is rescaled only when a row's maximum has risen by more than 2^8 over the one in use (weights up to 256
 // are as exact in bf16, and the sum is fp32); S of job c comes after P V of job c - 2 in the issue order, so a group
 // that has S may change its numerator.
@@ -47,8 +49,10 @@ struct PtSmem {                                       // after a 1024-byte align
     unsigned char KV[kSlots][kTile];                  // K, V, K, V, ...; K: [half][token][128 B swizzled], V: also by pages
     float join[2][4][4][D];                           // [group][warp][row][column]: numerators of four rows to be added
     float2 join_stat[2][4][32];                       // maximum in use, sum
+    float hand[4][2][D];                              // [warp][which][column]: a row's numerator from the second group to the first
+    float2 hand_stat[4][2];
     SegRec seg[kPtRing];
-    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2], turn[2],
+    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2], turn[2], hand_full[4][2], hand_empty[4][2],
         seg_full[kPtRing], seg_empty[kPtRing], drain;
     unsigned tmem;
     int failed, flag;
@@ -200,7 +204,7 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // copies arrive later).
 __host__ __device__ __forceinline__ bool paired(const PagedView& P, int d) { return d == 128 && P.page_shift == 4; }
 
-template <int D>
+template <int D, bool HAND>
 __global__ void __launch_bounds__(kPtThreads, 1)
 paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                        const __grid_constant__ CUtensorMap mv) {
@@ -211,7 +215,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
     extern __shared__ unsigned char dyn_raw[];
     unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~(uintptr_t)1023);
     Smem& sm = *reinterpret_cast<Smem*>(base);
-    typedef Plan<kPtRU, kPtKT, true, kPtLead> PlanT;
+    typedef Plan<kPtRU, kPtKT, HAND ? 2 : 1, kPtLead> PlanT;
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
     pdl_trigger();
     if (warp == 9) {
@@ -231,6 +235,10 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         bar_init(&sm.drain, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sm.failed = 0;
+    }
+    if (HAND && warp == 10 && lane < 16) {
+        bar_init((lane & 8 ? &sm.hand_empty[0][0] : &sm.hand_full[0][0]) + (lane & 7), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     tc_fence_before();
     PlanT plan(P, a);
@@ -471,7 +479,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                                                        // which on the maximum is replaced, -m * c
         const float margin = 8.f / a.c;
         bool begun = false;
-        unsigned joins = 0;
+        unsigned joins = 0, hands = 0;                 // hands: rows that this warp has handed over or taken
         auto joined = [&]() {                          // the group's four warps have come here
             __syncwarp();
             if (lane == 0) bar_arrive(&sm.join_bar[w]);
@@ -600,7 +608,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 ++segs;
                 const int gs = a.g_shift, bad = *reinterpret_cast<const volatile int*>(&r.bad);
                 const bool direct = r.direct;
-                const int slot0 = r.slot + (dual || order == 0 ? 0 : rows);
+                const int slot0 = r.slot + (order == 0 || !PlanT::twice(rows) ? 0 : rows);
                 if (quad) {
                     // the four warps' numerators, four rows at a time: [warp][row][column] in shared memory, added by one
                     // thread for four columns
@@ -641,6 +649,29 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                             }
                             if (M == -INFINITY) L = 0.f;
                             if (bad) L = NAN;
+                            if (HAND && tiles > 1) {                     // the other group has the other tiles' share of the row
+                                const int at = hands & 1, parity = (hands >> 1) & 1;
+                                ++hands;
+                                if (w) {
+                                    if (hands > 2 && !(ok = bar_wait(&sm.hand_empty[quarter][at], parity ^ 1, &sm.failed))) break;
+#pragma unroll
+                                    for (int j = 0; j < D / 32; ++j) sm.hand[quarter][at][j * 32 + lane] = z[j];
+                                    if (lane == 0) sm.hand_stat[quarter][at] = make_float2(M, L);
+                                    __syncwarp();
+                                    if (lane == 0) bar_arrive(&sm.hand_full[quarter][at]);
+                                    continue;
+                                }
+                                if (!(ok = bar_wait(&sm.hand_full[quarter][at], parity, &sm.failed))) break;
+                                const float2 other = sm.hand_stat[quarter][at];
+                                const float both = fmaxf(M, other.x), b = both == -INFINITY ? 0.f : both;
+                                const float f = ex2_approx((M - b) * a.c), fo = ex2_approx((other.x - b) * a.c);
+                                M = both;
+                                L = L * f + other.y * fo;
+#pragma unroll
+                                for (int j = 0; j < D / 32; ++j) z[j] = fmaf(sm.hand[quarter][at][j * 32 + lane], fo, z[j] * f);
+                                __syncwarp();
+                                if (lane == 0) bar_arrive(&sm.hand_empty[quarter][at]);
+                            }
                             const int gr = r.ru * kPtRU + rr, tok = r.tok0 + (gr >> gs), head = (r.head << gs) + (gr & ((1 << gs) - 1));
                             if (direct) {
                                 const float f = L == 0.f ? 0.f : 1.f / L;

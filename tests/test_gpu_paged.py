@@ -278,6 +278,64 @@ def test_attend_bad_pages_and_lengths(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H, Hkv, B, most_new, most_own", [
+    (8, 2, 74, 1, 700), (8, 2, 80, 8, 1300), (32, 4, 37, 12, 600), (4, 4, 40, 40, 300), (16, 2, 150, 3, 140), (8, 8, 19, 2, 3000), (1, 1, 148, 33, 257)])
+def test_attend_wide_batches(dtype, d, H, Hkv, B, most_new, most_own):
+    """Without prefixes and with at least as many sequences and KV heads as blocks; empty ones and more new than own among them."""
+    g = torch.Generator().manual_seed(B + most_own)
+    own = torch.randint(0, most_own + 1, (B,), generator=g).tolist()
+    new = torch.randint(0, most_new + 1, (B,), generator=g).tolist()
+    own[B // 3] = most_own
+    new[B // 3] = most_new
+    s = ph.Setting(new, own, H, Hkv, d, dtype, 64 if d == 64 else 16, seed=B, behind=2)
+    cache, out = s.cache(), torch.full_like(s.q, 7.0)
+    for causal in (True, False):
+        cache.attend(s.batch(), s.q, scale=0.13, causal=causal, out=out)
+        want, bound = s.want(0.13, causal)
+        ph.assert_within(out[:s.cu[-1]], want[:s.cu[-1]], bound[:s.cu[-1]])
+        assert bool((out[s.cu[-1]:] == 7).all())
+    assert cache.status() == 0
+    again = cache.attend(s.batch(), s.q, scale=0.13, causal=False)
+    assert torch.equal(again[:s.cu[-1]], out[:s.cu[-1]])
+    if s.cu[B // 3 + 1] > s.cu[B // 3]:
+        s.table[B // 3, 0] = -3                        # its first page: all of its rows need it
+        want[s.cu[B // 3]:s.cu[B // 3 + 1]] = math.nan
+        ph.assert_within(cache.attend(s.batch(), s.q, scale=0.13, causal=False)[:s.cu[-1]], want[:s.cu[-1]], bound[:s.cu[-1]])
+        assert cache.status() == 8
+
+
+CAPTURE = """
+import sys, torch
+sys.path.insert(0, "tests")
+import paged_helpers as ph
+for dtype in (torch.bfloat16, torch.float32):
+    one = ph.Setting([1], [40], 4, 2, 64, dtype)
+    one.cache().attend(one.batch(), one.q)
+    for new, own in (([1] * 80, [100] * 80), ([50, 60], [70, 80])):
+        s = ph.Setting(new, own, 4, 2, 64, dtype)
+        cache, batch, out = s.cache(), s.batch(), torch.zeros_like(s.q)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cache.attend(batch, s.q, scale=0.2, out=out)
+        graph.replay()
+        ph.assert_within(out, *s.want(0.2))
+print("captured")
+"""
+
+
+def test_capture_of_sizes_that_have_not_run():
+    """One call of a type and d loads what calls of other sizes need."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", CAPTURE], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("what", ["falls", "passes n", "negative", "groups end early", "groups fall"])
 def test_attend_broken_offsets(dtype, what):
     s = ph.Setting([1, 2, 1], [40, 30, 20], 4, 2, 64, dtype, 16, [0, 1, 3], [10, 20], seed=3)
