@@ -380,29 +380,34 @@ struct Plan {
         }
         __syncthreads();
         if (threadIdx.x < 32) {
-            // sums that stay at kPlanWeight once they reach it. Loops as they stand: a block starts with no code in its caches,
-            // and each new 128 bytes of it (8 instructions) cost over 300 cycles; unrolled, this took 3500 to 11000.
-            const int lane = threadIdx.x;
-            unsigned at = 0, as = 0;
+            // Sums that stay at kPlanWeight once they reach it. A lane has `per` entries in a row (an odd number, so that the lanes
+            // are in different banks). Loops as they stand: a block starts with no code in its caches, and each new 128 bytes of
+            // it (8 instructions) cost over 300 cycles; unrolled, 32 entries at a time, this took 3500 to 11000.
+            const int lane = threadIdx.x, per = (E + 31) / 32 | 1, i0 = lane * per, i1 = min(E, i0 + per);
+            unsigned x = 0, y = 0;
 #pragma unroll 1
-            for (int i0 = 0; i0 < E; i0 += 32) {
-                const int i = i0 + lane;
-                unsigned x = i < E ? t[i + 1] : 0, y = i < E ? s[i + 1] : 0;
+            for (int i = i0; i < i1; ++i) { x = min(x + t[i + 1], (unsigned)kPlanWeight); y += s[i + 1]; }
+            unsigned at = x, as = y;
 #pragma unroll 1
-                for (int off = 1; off < 32; off <<= 1) {
-                    const unsigned xo = __shfl_up_sync(0xffffffffu, x, off), yo = __shfl_up_sync(0xffffffffu, y, off);
-                    x = lane >= off ? min(x + xo, (unsigned)kPlanWeight) : x;
-                    y += lane >= off ? yo : 0;
-                }
-                x = min(at + x, (unsigned)kPlanWeight);
-                y += as;
-                if (i < E) { t[i + 1] = (int)x; s[i + 1] = (int)y; }
-                at = __shfl_sync(0xffffffffu, x, 31);
-                as = __shfl_sync(0xffffffffu, y, 31);
+            for (int off = 1; off < 32; off <<= 1) {
+                const unsigned xo = __shfl_up_sync(0xffffffffu, at, off), yo = __shfl_up_sync(0xffffffffu, as, off);
+                at = lane >= off ? min(at + xo, (unsigned)kPlanWeight) : at;
+                as += lane >= off ? yo : 0;
+            }
+            const unsigned all = __shfl_sync(0xffffffffu, at, 31);
+            at = __shfl_up_sync(0xffffffffu, at, 1);
+            as -= y;
+            if (lane == 0) at = 0;
+#pragma unroll 1
+            for (int i = i0; i < i1; ++i) {
+                at = min(at + t[i + 1], (unsigned)kPlanWeight);
+                as += s[i + 1];
+                t[i + 1] = (int)at;
+                s[i + 1] = (int)as;
             }
             if (lane == 0) {
                 t[0] = s[0] = 0;
-                if ((long long)at * P.Hkv >= kPlanWeight) *flag = 1;
+                if ((long long)all * P.Hkv >= kPlanWeight) *flag = 1;
             }
         }
         __syncthreads();
@@ -486,20 +491,25 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
         return;
     }
     if (warp == 0) {
-        int at = 0;
+        const int per = (P.B + 31) / 32 | 1, b0 = lane * per, b1 = min(P.B, b0 + per);
+        int x = 0;
 #pragma unroll 1
-        for (int i0 = 0; i0 < P.B; i0 += 32) {
-            const int b = i0 + lane;
-            int x = b < P.B ? (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + part - 1) / part : 0;
-#pragma unroll 1
-            for (int off = 1; off < 32; off <<= 1) {
-                const int xo = __shfl_up_sync(0xffffffffu, x, off);
-                if (lane >= off) x += xo;
-            }
-            if (b < P.B) uscan[b + 1] = at + x;
-            at += __shfl_sync(0xffffffffu, x, 31);
+        for (int b = b0; b < b1; ++b) {
+            const int y = (((__ldg(P.cu_q + b + 1) - __ldg(P.cu_q + b)) << a.g_shift) + part - 1) / part;
+            uscan[b + 1] = y;
+            x += y;
         }
-        if (lane == 0) { uscan[0] = 0; units = at; }
+        int at = x;
+#pragma unroll 1
+        for (int off = 1; off < 32; off <<= 1) {
+            const int xo = __shfl_up_sync(0xffffffffu, at, off);
+            if (lane >= off) at += xo;
+        }
+        if (lane == 31) units = at;
+        at -= x;
+#pragma unroll 1
+        for (int b = b0; b < b1; ++b) { at += uscan[b + 1]; uscan[b + 1] = at; }
+        if (lane == 0) uscan[0] = 0;
     }
     __syncthreads();
     const int items = units * P.Hkv, chunk = plan.chunk;
