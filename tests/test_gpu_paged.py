@@ -280,7 +280,7 @@ def test_attend_bad_pages_and_lengths(dtype):
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("H, Hkv, B, most_new, most_own", [
-    (8, 2, 74, 1, 700), (8, 2, 80, 8, 1300), (32, 4, 37, 12, 600), (4, 4, 40, 40, 300), (16, 2, 150, 3, 140), (8, 8, 19, 2, 3000), (1, 1, 148, 33, 257)])
+    (8, 2, 74, 1, 700), (8, 2, 80, 8, 1300), (32, 4, 37, 12, 600), (4, 4, 40, 40, 300), (16, 2, 150, 3, 140), (8, 8, 19, 2, 3000), (1, 1, 148, 33, 257), (8, 1, 150, 45, 400)])
 def test_attend_wide_batches(dtype, d, H, Hkv, B, most_new, most_own):
     """Without prefixes and with at least as many sequences and KV heads as blocks; empty ones and more new than own among them."""
     g = torch.Generator().manual_seed(B + most_own)
