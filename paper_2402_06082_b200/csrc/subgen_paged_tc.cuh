@@ -186,9 +186,10 @@ __device__ __forceinline__ float2 exp2_poly(float2 x) {
     return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(r.x) << 23)),
                        __int_as_float(__float_as_int(y.y) + (__float_as_int(r.y) << 23)));
 }
+// the largest, or NaN if there is one
 __device__ __forceinline__ float max3(float x, float y, float z) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -478,7 +479,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         float m = 0.f, l = 0.f, edge = 0.f, off = 0.f; // of this thread's row: the maximum in use, the sum, the score from
                                                        // which on the maximum is replaced, -m * c
         const float margin = 8.f / a.c;
-        bool begun = false;
+        bool begun = false, live = false;              // live: the row is one of the unit's (other lanes may hold anything)
         unsigned joins = 0, hands = 0;                 // hands: rows that this warp has handed over or taken
         auto joined = [&]() {                          // the group's four warps have come here
             __syncwarp();
@@ -487,7 +488,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         };
         // A new maximum of the row: keep the one in use, or change to the new one and rescale.
         auto raise = [&](float top) {
-            const bool rise = top > edge;
+            const bool rise = live && !(top <= edge);  // a NaN becomes the maximum, and the sum NaN with it
             if (__any_sync(0xffffffffu, rise)) {
                 const float f = rise ? ex2_approx((m - top) * a.c) : 1.f;              // 0 when there was no maximum yet
                 if (rise) { m = top; edge = top + margin; off = -top * a.c; }
@@ -531,7 +532,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
 #pragma unroll
                 for (int j = 0; j < 4; ++j) t[j] = max3(t[j], __uint_as_float(s[i + 2 * j]), __uint_as_float(s[i + 2 * j + 1]));
             }
-            return fmaxf(max3(t[0], t[1], t[2]), t[3]);
+            return max3(max3(t[0], t[1], t[2]), t[3], t[3]);
         };
         while (ok) {
             const int slot = ns % kPtRing;
@@ -542,7 +543,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             const int dual = rows > 128, tiles = tile1 - tile0, order = (w - (int)job) & 1;   // order: this group's half, or turn
             const bool quad = rows <= 32;
             const int row = quad ? lane : (dual ? order * 128 : 0) + quarter * 32 + lane;
-            const bool live = row < rows, some = quad || (row & ~31) < rows;
+            const bool some = quad || (row & ~31) < rows;
+            live = row < rows;
             const int urow = r.ru * kPtRU + row, P_ = r.P;
             Entry e;
             e.S = r.S; e.nq = r.nq;
@@ -550,7 +552,11 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             m = edge = -INFINITY;
             l = off = 0.f;
             begun = false;
-            for (int t = tile0 + (dual ? 0 : order); t < tile1; t += 2 - dual) {
+            // Whether this group's share of the run has a token that the row sees. If so and no score is finite, the row is NaN;
+            // a maximum of -infinity alone would not tell it from a row that sees nothing, which is 0.
+            const int t_first = tile0 + (dual ? 0 : order);
+            const bool sees = t_first < kp || own > (t_first - kp) * kPtKT;
+            for (int t = t_first; t < tile1; t += 2 - dual) {
                 const bool pre = t < kp;
                 const int lim = pre ? P_ - t * kPtKT : own - (t - kp) * kPtKT;        // tokens of the tile that the row sees
                 const bool cut = __any_sync(0xffffffffu, lim < kPtKT);
@@ -614,6 +620,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     // thread for four columns
                     tc_fence_after();
                     sm.join_stat[w][quarter][lane] = make_float2(m, l);
+                    const unsigned seen = __ballot_sync(0xffffffffu, sees);
                     uint32_t o[D];
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) tc_ld32(tO + i * 32, o + i * 32);
@@ -647,7 +654,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
 #pragma unroll
                                 for (int j = 0; j < D / 32; ++j) z[j] = fmaf(sm.join[w][k][quarter][j * 32 + lane], f, z[j]);
                             }
-                            if (M == -INFINITY) L = 0.f;
+                            if (M == -INFINITY) L = (seen >> rr) & 1 ? NAN : 0.f;
                             if (bad) L = NAN;
                             if (HAND && tiles > 1) {                     // the other group has the other tiles' share of the row
                                 const int at = hands & 1, parity = (hands >> 1) & 1;
@@ -688,7 +695,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     }
                 } else if (some) {
                     tc_fence_after();
-                    if (m == -INFINITY) l = 0.f;
+                    if (!(fabsf(m) < INFINITY)) l = sees ? NAN : 0.f;
                     if (bad) l = NAN;
                     const int tok = r.tok0 + (urow >> gs), head = (r.head << gs) + (urow & ((1 << gs) - 1));
                     const float f = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
