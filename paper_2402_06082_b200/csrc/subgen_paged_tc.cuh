@@ -172,17 +172,17 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
         : "=f"(r.x), "=f"(r.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
     return r;
 }
-// 2^x for x <= 8 on the fp32 pipe: 2^round(x) by the exponent, 2^(x - round(x)) by the cubic with the least relative error
-// on [-1/2, 1/2] (Remez, 7.5e-5: a fiftieth of a bf16 half step, which the weight is rounded to). Below 2^-126 it stays
-// near 2^-126, which is nothing beside the row's largest weight (at least 2^-8); rows that see nothing are told by their
-// maximum.
+// 2^(x + 1/2) for x <= 7.5 on the fp32 pipe: 2^round(x) by the exponent, 2^(x - round(x) + 1/2) in [1, 2) by the cubic with the
+// least relative error (Remez, 7.5e-5: a fiftieth of a bf16 half step, which the weight is rounded to). The half is what lets
+// x end at -127.5: with r = -127 the exponent field is 0 and the value a denormal, 7e-42 at the end, which bf16 rounds to 0. So
+// a masked token's weight is 0 and its V of any finite size adds nothing (2^-126 of bf16's lowest value would be 4).
 __device__ __forceinline__ float2 exp2_poly(float2 x) {
-    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+    x = make_float2(fmaxf(x.x, -127.4990234375f), fmaxf(x.y, -127.4990234375f));      // -127.5 + 2^-10: the cubic is above 1
     const float2 r = add2(x, make_float2(12582912.f, 12582912.f));        // 1.5 * 2^23: the rounded integer in the low bits
     const float2 f = fma2(add2(r, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), x);
-    float2 y = fma2(f, make_float2(0.05517167f, 0.05517167f), make_float2(0.24261113f, 0.24261113f));
-    y = fma2(y, f, make_float2(0.69326097f, 0.69326097f));
-    y = fma2(y, f, make_float2(0.99992806f, 0.99992806f));
+    float2 y = fma2(f, make_float2(0.07802452f, 0.07802452f), make_float2(0.34310395f, 0.34310395f));
+    y = fma2(y, f, make_float2(0.98041904f, 0.98041904f));
+    y = fma2(y, f, make_float2(1.4141119f, 1.4141119f));
     return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(r.x) << 23)),
                        __int_as_float(__float_as_int(y.y) + (__float_as_int(r.y) << 23)));
 }
@@ -510,11 +510,11 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         // N scores of the row -> bf16 weights, two to a register; adds them to the sum
         auto weigh = [&](auto count, const uint32_t* s, uint32_t* p) {
             constexpr int N = decltype(count)::value;
-            const float2 cc = make_float2(a.c, a.c), oo = make_float2(off, off);
+            const float2 cc = make_float2(a.c, a.c), oo = make_float2(off, off), oh = make_float2(off - 0.5f, off - 0.5f);
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
-                float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), cc, oo);
+                float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), cc, i % 8 < kPtPoly ? oh : oo);
                 if (i % 8 < kPtPoly) x = exp2_poly(x);
                 else x = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                 sum[i & 1] = add2(sum[i & 1], x);

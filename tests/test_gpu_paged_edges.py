@@ -65,3 +65,34 @@ def test_rows_that_see_nothing_of_queries_that_are_not_finite(dtype):
     for t in (0, 1, 2, 5, 14):
         s.q[t] = math.nan
     ph.assert_within(s.cache().attend(s.batch(), s.q, scale=0.1), want, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new, own, G", [(4, 5, 1), (8, 300, 1), (8, 8, 2), (20, 20, 4), (60, 61, 4), (200, 700, 1), (300, 300, 1)])
+def test_extreme_values_that_a_row_does_not_see(dtype, d, new, own, G):
+    """V of tokens behind a row's own is finite but the type's lowest: a weight that is not exactly 0 would show."""
+    s = ph.Setting([new], [own], 2 * G, 2, d, dtype, 16, seed=3)
+    want, bound = s.want(0.1)
+    first = own - new + 1 if new < 64 else own - 20    # tokens from here on: rows up to the one before do not see them
+    for j in range(first, own):
+        s.V[int(s.table[0, j // 16]), :, j % 16] = torch.finfo(dtype).min
+    rows = first - (own - new)
+    out = s.cache().attend(s.batch(), s.q, scale=0.1)
+    ph.assert_within(out[:rows], want[:rows], bound[:rows])
+
+
+def test_weights_of_the_cubic():
+    """One token's weight against the largest's, from even to 2^-140 of it, by the place in the tile: within the bf16 bound."""
+    n, d = 64, 64
+    s = ph.Setting([1], [n], 1, 1, d, BF16, 64, seed=1)
+    s.q.zero_()
+    s.q[0, 0, 0] = 1
+    K, V = s.K[int(s.table[0, 0]), 0], s.V[int(s.table[0, 0]), 0]
+    for shift in (0.0, 0.37, 20.0):
+        for last in (n - 1, n - 10):                   # the largest score by the cubic or not
+            K.zero_()
+            K[:, 0] = -torch.linspace(0, 97, n, device="cuda").to(BF16) - shift
+            K[last, 0] = shift
+            want, bound = s.want(1.0)
+            ph.assert_within(s.cache().attend(s.batch(), s.q, scale=1.0), want, bound)
