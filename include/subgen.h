@@ -413,9 +413,11 @@ typedef struct subgen_batch {
 
 /* Writes the n new tokens' keys, normed (if wk) and rotated (if rope), and their values into the pages of their
  * sequences, and the queries, normed (if wq) and rotated, to q_out, which may be q (q.p may be NULL: keys and values
- * only). positions NULL: a token's position is its place in its sequence, prefix included. Two rows must not have the
- * same slot. Tokens whose own index is negative (more new tokens than the length says) are not written and set
- * SUBGEN_ST_PAGE. Asynchronous on `stream`, one kernel. */
+ * only). positions NULL: a token's position is its place in its sequence, prefix included; with a rotation, a token whose
+ * position cannot be told (no group or several claim its sequence, or the prefix's length is negative or beyond its table)
+ * gets neither key, value nor query written and sets SUBGEN_ST_PAGE. Two rows must not have the same slot. Tokens whose own
+ * index is negative (more new tokens than the length says) are not written to the cache and set SUBGEN_ST_PAGE.
+ * Asynchronous on `stream`, one kernel. */
 int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_qk_args* args, void* stream);
 
 typedef struct subgen_attend_args {

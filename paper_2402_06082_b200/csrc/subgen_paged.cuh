@@ -72,6 +72,27 @@ __device__ __forceinline__ int warp_find(const int* edges, int count, int x) {
     return broken ? -2 : found - 1;
 }
 
+// The group of sequence b; -1 where none or several claim it. Edges that fall, do not start at 0 or do not end at B set the
+// status. One warp, all lanes get it.
+__device__ __forceinline__ int warp_group(const PagedView& P, int b) {
+    int found = -1, claims = 0;
+    bool broken = false;
+    for (int i = 0; i < P.groups; i += 32) {
+        const int g = i + (threadIdx.x & 31);
+        bool mine = false;
+        if (g < P.groups) {
+            const int e0 = __ldg(P.cu_group + g), e1 = __ldg(P.cu_group + g + 1);
+            mine = e0 <= b && b < e1;
+            broken |= e1 < e0 || (g == 0 && e0 != 0) || (g == P.groups - 1 && e1 != P.B);
+        }
+        const unsigned who = __ballot_sync(0xffffffffu, mine);
+        claims += __popc(who);
+        if (who) found = i + __ffs(who) - 1;
+    }
+    if (__any_sync(0xffffffffu, broken) && (threadIdx.x & 31) == 0) paged_status(P, kStPage);
+    return claims == 1 ? found : -1;
+}
+
 template <typename T, int VE>
 __device__ __forceinline__ uint4 pack_row(const float* f) {
     uint4 r;
@@ -115,9 +136,13 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
         if (slot < 0 && lane == 0) paged_status(P, kStPage);
         pos = own;
         if (a.positions) pos = __ldg(a.positions + tok);
-        else if (P.groups) {
-            const int g = warp_find(P.cu_group, P.groups + 1, b);
-            if (g >= 0 && g < P.groups) pos = (int)((unsigned)pos + (unsigned)__ldg(P.prefix_len + g));
+        else if (P.groups && a.words) {                              // its prefix comes before it
+            const int g = warp_group(P, b), len = g >= 0 ? __ldg(P.prefix_len + g) : -1;
+            if (len < 0 || len > (long long)P.prefix_stride << P.page_shift) {         // no position: nothing is written
+                if (lane == 0) paged_status(P, kStPage);
+                return;
+            }
+            pos = (int)((unsigned)pos + (unsigned)len);
         }
     } else {
         if (a.words) pos = __ldg(a.positions + tok);

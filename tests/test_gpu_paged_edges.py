@@ -96,3 +96,94 @@ def test_weights_of_the_cubic():
             K[last, 0] = shift
             want, bound = s.want(1.0)
             ph.assert_within(s.cache().attend(s.batch(), s.q, scale=1.0), want, bound)
+
+
+# ---- append ---------------------------------------------------------------------------------------
+
+def _written(s, K0, tokens):
+    """Exactly the slots of these tokens of s have changed."""
+    where = [(b, s.own[b] - s.new[b] + i) for b in range(len(s.new)) for i in range(s.new[b])]
+    changed = (torch.nan_to_num(s.K) != torch.nan_to_num(K0)).any(-1).any(1)
+    want = torch.zeros_like(changed)
+    for t in tokens:
+        b, j = where[t]
+        want[int(s.table[b, j // s.page]), j % s.page] = True
+    assert torch.equal(changed, want)
+
+
+BROKEN_GROUPS = {  # cu_group (of [0, 1, 3]), prefix_len (of [10, 20], tables of 32 tokens) -> tokens whose position is known, status
+    "as it should be": ([0, 1, 3], [10, 20], [0, 1, 2, 3], 0),
+    "whole tables": ([0, 1, 3], [32, 32], [0, 1, 2, 3], 0),
+    "empty prefix": ([0, 0, 3], [10, 0], [0, 1, 2, 3], 0),
+    "falls": ([0, 2, 1], [10, 20], [0, 1, 2], 8),
+    "falls below 0": ([0, -1, 3], [10, 20], [0, 1, 2, 3], 8),
+    "falls from the end": ([0, 3, 1], [10, 20], [0, 1, 2, 3], 8),
+    "starts late": ([1, 2, 3], [10, 20], [1, 2, 3], 8),
+    "ends early": ([0, 1, 2], [10, 20], [0, 1, 2], 8),
+    "ends late": ([0, 1, 4], [10, 20], [0, 1, 2, 3], 8),
+    "negative length": ([0, 1, 3], [10, -1], [0], 8),
+    "beyond its table": ([0, 1, 3], [33, 20], [1, 2, 3], 8),
+}
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("name", list(BROKEN_GROUPS))
+def test_append_with_broken_groups(dtype, name):
+    """A position that cannot be told is not made up: neither the key nor the query is written, and the status says so."""
+    from paper_2402_06082_b200 import binding
+    edges, lens, tokens, status = BROKEN_GROUPS[name]
+    s = ph.Setting([1, 2, 1], [40, 30, 20], 4, 2, 64, dtype, 16, [0, 1, 3], [32, 32], seed=3)
+    s.groups["cu_group"].copy_(_ints(edges))
+    s.groups["prefix_len"].copy_(_ints(lens))
+    rope = binding.Rope(64)
+    cache, K0, q_out = s.cache(), s.K.clone(), torch.full_like(s.q, 7.0)
+    cache.append(s.batch(), s.k, s.v, rope=rope, q=s.q, q_out=q_out)
+    assert cache.status() == status
+    _written(s, K0, tokens)
+    seq = [0, 1, 1, 2]
+    for t in range(4):
+        if t not in tokens:
+            assert bool((q_out[t] == 7).all())
+            continue
+        g = next(i for i in (0, 1) if edges[i] <= seq[t] < edges[i + 1])
+        pos = torch.tensor([lens[g] + [39, 28, 29, 19][t]])
+        ph.assert_within(q_out[t:t + 1], *ph.norm_rope(s.q[t:t + 1], pos, None, ph.freqs(64), 64, False, 0.0))
+
+
+def test_append_where_two_groups_claim_a_sequence():
+    from paper_2402_06082_b200 import binding
+    s = ph.Setting([1, 2, 1], [40, 30, 20], 4, 2, 64, BF16, 16, [0, 1, 2, 3], [7, 7, 7], seed=3)
+    s.groups["cu_group"].copy_(_ints([0, 3, 1, 3]))                # the first has all, the third the second and third sequence
+    cache, K0 = s.cache(), s.K.clone()
+    cache.append(s.batch(), s.k, s.v, rope=binding.Rope(64))
+    assert cache.status() == 8
+    _written(s, K0, [0])
+
+
+def test_append_that_needs_no_prefix_length():
+    """With positions, or without a rotation, groups are not looked at."""
+    from paper_2402_06082_b200 import binding
+    s = ph.Setting([1, 2, 1], [40, 30, 20], 4, 2, 64, BF16, 16, [0, 1, 3], [32, 32], seed=3)
+    s.groups["prefix_len"].fill_(-1)
+    cache, K0 = s.cache(), s.K.clone()
+    cache.append(s.batch(), s.k, s.v)
+    _written(s, K0, [0, 1, 2, 3])
+    pos = _ints([3, 4, 5, 6])
+    q = cache.append(s.batch(), s.k, s.v, rope=binding.Rope(64), positions=pos, q=s.q)
+    ph.assert_within(q, *ph.norm_rope(s.q, pos, None, ph.freqs(64), 64, False, 0.0))
+    assert cache.status() == 0
+
+
+@pytest.mark.parametrize("G", [40, 100])
+def test_append_positions_behind_many_groups(G):
+    """More groups than a warp has lanes, some of them empty."""
+    from paper_2402_06082_b200 import binding
+    B = 120
+    edges = sorted((i * i * B // (G * G)) for i in range(G + 1))
+    prefix = [5 * i for i in range(G)]
+    s = ph.Setting([1] * B, [1 + i % 30 for i in range(B)], 2, 1, 64, FP32, 16, edges, prefix, seed=1)
+    cache = s.cache()
+    q = cache.append(s.batch(), s.k, s.v, rope=binding.Rope(64), q=s.q)
+    pos = torch.tensor([next(prefix[g] for g in range(G) if edges[g] <= b < edges[g + 1]) + b % 30 for b in range(B)])
+    ph.assert_within(q, *ph.norm_rope(s.q, pos, None, ph.freqs(64), 64, False, 0.0))
+    assert cache.status() == 0
