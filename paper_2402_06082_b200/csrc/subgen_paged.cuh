@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     if (tok >= a.n) return;
 
     long long slot = -1;                                             // element offset of the token's row in head 0 of its page
-    int pos = 0;
+    long long pos = 0;                                               // prefix and own tokens together may pass 2^31
     if constexpr (PAGED) {
         const int b = warp_find(P.cu_q, P.B + 1, tok);
         const int end = b >= 0 && b < P.B ? __ldg(P.cu_q + b + 1) : 0;
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
                 if (lane == 0) paged_status(P, kStPage);
                 return;
             }
-            pos = (int)((unsigned)pos + (unsigned)len);
+            pos += len;
         }
     } else {
         if (a.words) pos = __ldg(a.positions + tok);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     if (turn) {
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
-            const unsigned long long turns = (unsigned long long)(long long)pos * __ldg(a.words + l * VE + e);
+            const unsigned long long turns = (unsigned long long)pos * __ldg(a.words + l * VE + e);
             sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &si[e], &co[e]);   // 2^-31: half turns
         }
     }

@@ -187,3 +187,22 @@ def test_append_positions_behind_many_groups(G):
     pos = torch.tensor([next(prefix[g] for g in range(G) if edges[g] <= b < edges[g + 1]) + b % 30 for b in range(B)])
     ph.assert_within(q, *ph.norm_rope(s.q, pos, None, ph.freqs(64), 64, False, 0.0))
     assert cache.status() == 0
+
+
+def test_append_positions_beyond_31_bits():
+    """The longest prefix and the longest sequence that tables can hold, all in one page."""
+    from paper_2402_06082_b200 import binding
+    page, most = 1024, 2 ** 21 - 2
+    far = most * page
+    K, V = (torch.zeros(1, 1, page, 64, device="cuda") for _ in "KV")
+    cache, table = binding.PagedCache(K, V), torch.zeros(1, most, dtype=torch.int32, device="cuda")
+    batch = binding.PagedBatch(_ints([0, 1]), _ints([far]), table, _ints([0, 1]), _ints([far]), table)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k = (torch.randn(1, 1, 64, generator=g, device="cuda") for _ in "qk")
+    out = cache.append(batch, k, k, rope=binding.Rope(64), q=q)
+    assert cache.status() == 0
+    pos = torch.tensor([2 * far - 1])
+    ph.assert_within(out, *ph.norm_rope(q, pos, None, ph.freqs(64), 64, False, 0.0))
+    want, bound = ph.norm_rope(k, pos, None, ph.freqs(64), 64, False, 0.0)
+    ph.assert_within(K[0, :, page - 1], want[0], bound[0])
+    assert torch.equal(V[0, :, page - 1], k[0])
