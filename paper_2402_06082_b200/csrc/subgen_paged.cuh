@@ -121,8 +121,9 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     long long pos = 0;                                               // prefix and own tokens together may pass 2^31
     if constexpr (PAGED) {
         const int b = warp_find(P.cu_q, P.B + 1, tok);
-        const int end = b >= 0 && b < P.B ? __ldg(P.cu_q + b + 1) : 0;
-        if (b == -2 || end > a.n) {
+        const int start = b >= 0 && b < P.B ? __ldg(P.cu_q + b) : 0, end = b >= 0 && b < P.B ? __ldg(P.cu_q + b + 1) : 0;
+        if (w == 0 && lane == 0 && (__ldg(P.cu_q) < 0 || __ldg(P.cu_q + P.B) > a.n)) paged_status(P, kStPage);    // no token may tell
+        if (b == -2 || start < 0 || end > a.n) {
             if (lane == 0) paged_status(P, kStPage);
             return;
         }

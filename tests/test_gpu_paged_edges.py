@@ -206,3 +206,19 @@ def test_append_positions_beyond_31_bits():
     want, bound = ph.norm_rope(k, pos, None, ph.freqs(64), 64, False, 0.0)
     ph.assert_within(K[0, :, page - 1], want[0], bound[0])
     assert torch.equal(V[0, :, page - 1], k[0])
+
+
+@pytest.mark.parametrize("edges, tokens, status", [
+    ([0, 1, 3, 4], [0, 1, 2, 3], 0), ([-1, 1, 3, 4], [1, 2, 3], 8), ([0, 1, 4, 6], [], 8), ([0, 1, 3, 2 ** 31 - 1], [0, 1, 2], 8),
+    ([-2 ** 31, 1, 3, 4], [1, 2, 3], 8), ([-3, -2, -1, 4], [], 8)])
+def test_append_edges_outside_the_rows(edges, tokens, status):
+    """Edges below 0 or past n set the status also where no row of the call is theirs."""
+    s = ph.Setting([1, 2, 1], [40, 30, 20], 4, 2, 64, FP32, 16)
+    s.cu_q.copy_(_ints(edges))
+    cache, K0, q_out = s.cache(), s.K.clone(), torch.full_like(s.q, 7.0)
+    cache.append(s.batch(), s.k, s.v, q=s.q, q_out=q_out)
+    assert cache.status() == status
+    if edges[1:3] == [1, 3]:
+        _written(s, K0, tokens)
+        for t in range(4):
+            assert bool((q_out[t] == 7).all()) == (t not in tokens)
