@@ -371,6 +371,7 @@ typedef struct subgen_qk_args {
     const void *wq, *wk;      /* device [d] of the dtype, 16-byte aligned; NULL: no norm */
     int n, H, Hkv, d, dtype;  /* d: 64 or 128; subgen_paged_append takes Hkv, d and dtype from its cache */
     float eps;
+    int fresh;                /* subgen_paged_append: q_out holds nothing yet, so a token that is left out becomes NaN there */
 } subgen_qk_args;
 
 /* q or k may have p = NULL: then only the other is done. positions are needed if there is a rotation. Asynchronous on
@@ -415,7 +416,8 @@ typedef struct subgen_batch {
  * sequences, and the queries, normed (if wq) and rotated, to q_out, which may be q (q.p may be NULL: keys and values
  * only). positions NULL: a token's position is its place in its sequence, prefix included; with a rotation, a token whose
  * position cannot be told (no group or several claim its sequence, or the prefix's length is negative or beyond its table)
- * gets neither key, value nor query written and sets SUBGEN_ST_PAGE. Two rows must not have the same slot. Tokens whose own
+ * gets neither key, value nor query written and sets SUBGEN_ST_PAGE. So does a token that two sequences claim or whose
+ * sequence begins below row 0 or ends behind row n. Two rows must not have the same slot. Tokens whose own
  * index is negative (more new tokens than the length says) are not written to the cache and set SUBGEN_ST_PAGE.
  * Asynchronous on `stream`, one kernel. */
 int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, const subgen_qk_args* args, void* stream);
@@ -427,6 +429,7 @@ typedef struct subgen_attend_args {
     int n, H;
     float scale;              /* > 0 */
     int causal;
+    int fresh;                /* out holds nothing yet: NaN to all n rows where nothing can be computed */
 } subgen_attend_args;
 
 /* out = softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for each of the n new tokens' H query heads (head h reads KV
@@ -435,6 +438,8 @@ typedef struct subgen_attend_args {
  * A row that sees nothing (an empty sequence, or one of more new tokens than its length says) is 0. The prefix is read
  * once per group, whatever the number of its sequences. Stored keys and values that some row sees must be
  * finite; what lies behind a sequence's length in its last page may be anything.
+ * Where cu_q or cu_group are not what they have to be, nothing is computed: SUBGEN_ST_PAGE is set, and `out` is left as it was,
+ * or NaN if it is `fresh`.
  * Scores, maxima, sums and numerators are fp32; on bf16 caches the softmax weights are rounded to bf16 for the product
  * with V. The result does not depend on how blocks are scheduled.
  * out must not overlap q. The workspace is this call's until it has run (two calls that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */

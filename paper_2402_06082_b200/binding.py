@@ -77,12 +77,12 @@ class BatchDesc(C.Structure):
 class QkArgs(C.Structure):
     _fields_ = [(k, Heads) for k in ("q", "k", "v", "q_out", "k_out")] + [
         ("positions", C.c_void_p), ("rope", RopeDesc), ("wq", C.c_void_p), ("wk", C.c_void_p), ("n", C.c_int), ("H", C.c_int),
-        ("Hkv", C.c_int), ("d", C.c_int), ("dtype", C.c_int), ("eps", C.c_float)]
+        ("Hkv", C.c_int), ("d", C.c_int), ("dtype", C.c_int), ("eps", C.c_float), ("fresh", C.c_int)]
 
 
 class AttendArgs(C.Structure):
     _fields_ = [("q", Heads), ("out", Heads), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("n", C.c_int),
-                ("H", C.c_int), ("scale", C.c_float), ("causal", C.c_int)]
+                ("H", C.c_int), ("scale", C.c_float), ("causal", C.c_int), ("fresh", C.c_int)]
 
 
 class SubgenError(RuntimeError):
@@ -557,13 +557,16 @@ class PagedCache:
                positions: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
                q: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Write the new tokens k, v [n, Hkv, d] into their pages, k normed (if wk) and rotated (if rope) on the way; q [n, H, d]
-        goes the same way into q_out, which is returned (None without q). One kernel; see subgen_paged_append."""
+        goes the same way into q_out, which is returned (None without q). A token that broken offsets or groups leave out (status())
+        keeps its row of a q_out that was given, and is NaN in a new one. One kernel; see subgen_paged_append."""
         return _calls.append(self._at, self.device, self._batch(batch), k, v, positions, None if rope is None else rope._desc, wk, eps,
                              q, wq, q_out)
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, scale: float = 1.0, causal: bool = True, out: Optional[torch.Tensor] = None):
         """softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for q [n, H, d], whose keys are in the cache already; the prefix is
-        read once per group. Rows of `out` behind the last sequence are not written. See subgen_paged_attend."""
+        read once per group. Rows of `out` behind the last sequence are not written (of a new one: undefined). Broken offsets
+        leave an `out` that was given as it is and make NaN of a new one; status() tells. See
+        subgen_paged_attend."""
         return _calls.attend(self._at, self.device, self._batch(batch), q, scale, causal, out)
 
     def status(self) -> int:

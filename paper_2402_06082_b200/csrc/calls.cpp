@@ -197,6 +197,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t got) {
             if (q->dim() != 3) refuse("q must have the axes tokens, heads, d " + said(*q));
             p.H = (int)q->size(1);
             p.q = rows(*q, "q", w, n, p.H, d);
+            p.fresh = qo.o == Py_None;
             p.q_out = output(qo.o, "q_out", *q, w, n, p.H, d);
             qo.mine = true;
         }
@@ -224,6 +225,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t got) {
         subgen_attend_args p{};
         p.q = rows(*q, "q", w, n, H, d);
         Held out(a[6]);
+        p.fresh = out.o == Py_None;
         p.out = output(out.o, "out", *q, w, n, H, d);
         out.mine = true;
         p.workspace_bytes = f_bytes(c, b, (int)n, (int)H);

@@ -126,7 +126,7 @@ void fill_norm_rope(NormRope* a, const subgen_qk_args* x, int H, int Hkv) {
     a->positions = x->positions;
     a->words = (const unsigned long long*)x->rope.words;
     a->rot = x->rope.rotary_dim; a->interleaved = x->rope.interleaved;
-    a->wq = x->wq; a->wk = x->wk; a->eps = x->eps;
+    a->wq = x->wq; a->wk = x->wk; a->eps = x->eps; a->fresh = x->fresh != 0;
 }
 
 // ---- attention ----
@@ -377,7 +377,7 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
         return fail(SUBGEN_ENOMEM, "%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, need);
     const int g_shift = G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : 3;
     Attend a = {vq, vo, n, H, g_shift, x->causal != 0, x->scale * 1.4426950408889634f, (float*)x->workspace,
-                (float2*)((float*)x->workspace + slots * d)};
+                (float2*)((float*)x->workspace + slots * d), x->fresh != 0};
     cudaStream_t st = (cudaStream_t)stream;
     if (cache->dtype == SUBGEN_DTYPE_BF16) return d == 64 ? attend_tc<64>(P, a, st) : attend_tc<128>(P, a, st);
     return d == 64 ? attend_fp32<64>(P, a, st) : attend_fp32<128>(P, a, st);

@@ -53,6 +53,7 @@ struct NormRope {
     int rot, interleaved;
     const void *wq, *wk;                              // NULL: no norm
     float eps;
+    int fresh;                                        // qo holds nothing yet: a token that is left out becomes NaN
 };
 
 constexpr int kNrThreads = 128;
@@ -123,10 +124,13 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
         const int b = warp_find(P.cu_q, P.B + 1, tok);
         const int start = b >= 0 && b < P.B ? __ldg(P.cu_q + b) : 0, end = b >= 0 && b < P.B ? __ldg(P.cu_q + b + 1) : 0;
         if (w == 0 && lane == 0 && (__ldg(P.cu_q) < 0 || __ldg(P.cu_q + P.B) > a.n)) paged_status(P, kStPage);    // no token may tell
-        if (b == -2 || start < 0 || end > a.n) {
+        auto leave_out = [&]() {                                     // the token: nothing is written
             if (lane == 0) paged_status(P, kStPage);
-            return;
-        }
+            if (!a.fresh || !a.q.p) return;
+            for (int i = part * 32 + lane; i < a.H * (D / VE); i += a.parts * 32)
+                *reinterpret_cast<uint4*>((T*)a.qo.p + tok * a.qo.ts + i / (D / VE) * a.qo.hs + i % (D / VE) * VE) = make_uint4(~0u, ~0u, ~0u, ~0u);
+        };
+        if (b == -2 || start < 0 || end > a.n) return leave_out();
         if (b < 0 || b >= P.B) return;                               // before the first sequence, behind the last
         const long long place = (long long)__ldg(P.lengths + b) - end + tok, pg = place >> P.page_shift;
         const int own = (int)place;
@@ -139,10 +143,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
         if (a.positions) pos = __ldg(a.positions + tok);
         else if (P.groups && a.words) {                              // its prefix comes before it
             const int g = warp_group(P, b), len = g >= 0 ? __ldg(P.prefix_len + g) : -1;
-            if (len < 0 || len > (long long)P.prefix_stride << P.page_shift) {         // no position: nothing is written
-                if (lane == 0) paged_status(P, kStPage);
-                return;
-            }
+            if (len < 0 || len > (long long)P.prefix_stride << P.page_shift) return leave_out();     // no position
             pos += len;
         }
     } else {
@@ -282,6 +283,7 @@ struct Attend {
     float c;                                          // scale * log2(e)
     float* part;                                      // [slots][D] numerators
     float2* stat;                                     // [slots] largest score * c, sum
+    int fresh;                                        // o holds nothing yet: NaN where nothing can be computed
 };
 
 template <int RU, int KT, int DUAL, int LEAD>
@@ -497,6 +499,17 @@ struct Plan {
 // together, and registers for three blocks an SM.
 constexpr int kMergeThreads = 256, kMergeBlocks = 3;
 
+// All rows of an output. Out of line: no part of what the kernel's code caches hold.
+template <typename T, int D>
+__device__ __noinline__ void fill_nan(T* o, long long ts, long long hs, int n, int H) {
+    constexpr int PIECES = D * (int)sizeof(T) / 16;
+    const long long count = (long long)n * H * PIECES, step = (long long)gridDim.x * blockDim.x;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += step) {
+        const long long row = i / PIECES;
+        *reinterpret_cast<uint4*>(o + row / H * ts + row % H * hs + i % PIECES * (16 / (int)sizeof(T))) = make_uint4(~0u, ~0u, ~0u, ~0u);
+    }
+}
+
 template <typename T, int D, int RU, int KT, int DUAL, int LEAD>
 __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kernel(PagedView P, Attend a, int nblk, int part) {
     constexpr int NW = kMergeThreads / 32, VL = D / 32;
@@ -514,6 +527,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
     if (plan.broken) {
         if (blockIdx.x == 0 && tid == 0) paged_status(P, kStPage);
         pdl_wait();                                   // this kernel's end stands for the attention kernel's
+        if (a.fresh) fill_nan<T, D>((T*)a.o.p, a.o.ts, a.o.hs, a.n, a.H);
         return;
     }
     if (warp == 0) {

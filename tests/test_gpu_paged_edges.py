@@ -222,3 +222,42 @@ def test_append_edges_outside_the_rows(edges, tokens, status):
         _written(s, K0, tokens)
         for t in range(4):
             assert bool((q_out[t] == 7).all()) == (t not in tokens)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_new_outputs_of_tokens_left_out(dtype):
+    """Without q_out the tokens that are left out are NaN, the others as ever."""
+    from paper_2402_06082_b200 import binding
+    s = ph.Setting([1, 2, 1], [40, 30, 20], 40, 5, 64, dtype, 16, [0, 1, 3], [32, 32], seed=3)
+    rope, cache = binding.Rope(64), s.cache()
+    good = cache.append(s.batch(), s.k, s.v, rope=rope, q=s.q)
+    assert torch.isfinite(good).all() and cache.status() == 0
+    s.groups["prefix_len"][0] = 33
+    q = cache.append(s.batch(), s.k, s.v, rope=rope, q=s.q)
+    assert torch.isnan(q[0]).all() and torch.equal(q[1:], good[1:]) and cache.status() == 8
+    s.groups["prefix_len"][0] = 32
+    s.cu_q[3] = 9
+    q = cache.append(s.batch(), s.k, s.v, rope=rope, q=s.q)
+    assert torch.isnan(q[3]).all() and torch.equal(q[:3], good[:3])
+    many = ph.Setting([3000], [3000], 8, 2, 64, dtype, 64, seed=1)  # a warp a token
+    many.cu_q[1] = 3001
+    assert torch.isnan(many.cache().append(many.batch(), many.k, many.v, q=many.q)).all()
+
+
+# ---- attention that computes nothing --------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("new", [[1, 2, 1], [40, 300, 7]])
+@pytest.mark.parametrize("d, H, Hkv", [(64, 4, 2), (128, 8, 8)])
+def test_new_outputs_of_broken_offsets(dtype, new, d, H, Hkv):
+    """All NaN, status 8; an output that was given stays as it is."""
+    s = ph.Setting(new, [k + 20 for k in new], H, Hkv, d, dtype, 16, [0, 1, 3], [10, 20], seed=3, behind=2)
+    cache, batch = s.cache(), s.batch()
+    s.cu_q[1] = s.cu[2] + 1
+    assert torch.isnan(cache.attend(batch, s.q)).all() and cache.status() == 8
+    out = torch.full_like(s.q, 7.0)
+    cache.attend(batch, s.q, out=out)
+    assert bool((out == 7).all())
+    s.cu_q[1] = s.cu[1]
+    s.groups["cu_group"][2] = 2
+    assert torch.isnan(cache.attend(batch, s.q)).all()
