@@ -72,6 +72,7 @@ extern "C" {
 #define SUBGEN_ST_TIMEOUT 4  /* a bounded wait inside a kernel ran out (not expected; the state is unusable) */
 #define SUBGEN_ST_PAGE 8     /* paged calls: a page outside the pool, a length beyond its page table, or offsets that
                               * decrease or pass the number of rows */
+#define SUBGEN_ST_SIZE 16    /* subgen_paged_attend: more work in one call than it can divide (see there); nothing was computed */
 
 typedef struct subgen subgen_t;
 typedef struct subgen_exact subgen_exact_t;
@@ -439,7 +440,9 @@ typedef struct subgen_attend_args {
  * once per group, whatever the number of its sequences. Stored keys and values that some row sees must be
  * finite; what lies behind a sequence's length in its last page may be anything.
  * Where cu_q or cu_group are not what they have to be, nothing is computed: SUBGEN_ST_PAGE is set, and `out` is left as it was,
- * or NaN if it is `fresh`.
+ * or NaN if it is `fresh`. The same with SUBGEN_ST_SIZE where the key tiles that all row units of all KV heads take come to 2^30 or
+ * more (bf16: tiles of 128 tokens, units of up to 256 rows, which above 128 rows count twice; fp32: 32 or 64 tokens, units of up to
+ * 8, 64 or 128 rows; and one or two more for each unit).
  * Scores, maxima, sums and numerators are fp32; on bf16 caches the softmax weights are rounded to bf16 for the product
  * with V. The result does not depend on how blocks are scheduled.
  * out must not overlap q. The workspace is this call's until it has run (two calls that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */

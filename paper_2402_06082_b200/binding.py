@@ -18,7 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsubgen.so")
 
 DTYPE_FP32, DTYPE_BF16 = 0, 1
-ST_CAPACITY, ST_RANGE, ST_TIMEOUT, ST_PAGE = 1, 2, 4, 8
+ST_CAPACITY, ST_RANGE, ST_TIMEOUT, ST_PAGE, ST_SIZE = 1, 2, 4, 8, 16
 STEP_MODES = {"auto": 0, "fused": 1, "split": 2}
 
 EXPORTS = [
@@ -564,8 +564,8 @@ class PagedCache:
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, scale: float = 1.0, causal: bool = True, out: Optional[torch.Tensor] = None):
         """softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for q [n, H, d], whose keys are in the cache already; the prefix is
-        read once per group. Rows of `out` behind the last sequence are not written (of a new one: undefined). Broken offsets
-        leave an `out` that was given as it is and make NaN of a new one; status() tells. See
+        read once per group. Rows of `out` behind the last sequence are not written (of a new one: undefined). Broken offsets and
+        batches that are too long leave an `out` that was given as it is and make NaN of a new one; status() tells. See
         subgen_paged_attend."""
         return _calls.attend(self._at, self.device, self._batch(batch), q, scale, causal, out)
 

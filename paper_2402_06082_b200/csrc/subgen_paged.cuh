@@ -9,7 +9,7 @@
 
 namespace sgk {
 
-constexpr int kStTimeout = 4, kStPage = 8;            // SUBGEN_ST_TIMEOUT, SUBGEN_ST_PAGE
+constexpr int kStTimeout = 4, kStPage = 8, kStSize = 16;     // SUBGEN_ST_TIMEOUT, SUBGEN_ST_PAGE, SUBGEN_ST_SIZE
 
 struct HeadsView {                                    // [tokens, heads, d]: unit stride along d, strides in elements
     void* p;
@@ -262,7 +262,8 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
 // tensor work: one sequence in it, or at least RU / 2 rows per sequence, so that the row units are full without
 // packing several sequences into one; that spares the rows' second partial.
 constexpr int kPlanMax = 1024;                        // groups + sequences of one call
-constexpr long long kPlanWeight = 1 << 30;            // longest line; some 10^13 (query row, key) pairs
+constexpr long long kPlanWeight = 1 << 30;            // the line is shorter: of full units 10^13 (query row, key) pairs in bf16,
+                                                      // 10^11 where 8 fp32 rows meet 32 tokens
 
 struct Entry {
     int tok0, rows;                                   // first token; rows = tokens * G
@@ -294,7 +295,7 @@ struct Plan {
     const int* sscan;                                 // [E+1] partial slots before each entry, per head
     int E;
     int head_w, total, chunk;
-    bool broken;                                      // cu_q or cu_group is not what it has to be: nothing is computed
+    int broken;                                       // nothing is computed: 1 cu_q or cu_group is not what it has to be, 2 a line too long
 
     __device__ Plan(const PagedView& P_, const Attend& a_) : P(P_), a(a_) {}
 
@@ -435,11 +436,11 @@ struct Plan {
             }
             if (lane == 0) {
                 t[0] = s[0] = 0;
-                if ((long long)all * P.Hkv >= kPlanWeight) *flag = 1;
+                if (!*flag && (long long)all * P.Hkv >= kPlanWeight) *flag = 2;
             }
         }
         __syncthreads();
-        broken = *flag != 0;
+        broken = *flag;
         tscan = t;
         sscan = s;
         head_w = broken ? 0 : t[E];
@@ -525,7 +526,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
     int* uscan = (int*)sm_plan + 2 * (plan.E + 1);    // [B+1] parts before each sequence
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (plan.broken) {
-        if (blockIdx.x == 0 && tid == 0) paged_status(P, kStPage);
+        if (blockIdx.x == 0 && tid == 0) paged_status(P, plan.broken == 2 ? kStSize : kStPage);
         pdl_wait();                                   // this kernel's end stands for the attention kernel's
         if (a.fresh) fill_nan<T, D>((T*)a.o.p, a.o.ts, a.o.hs, a.n, a.H);
         return;

@@ -261,3 +261,22 @@ def test_new_outputs_of_broken_offsets(dtype, new, d, H, Hkv):
     s.cu_q[1] = s.cu[1]
     s.groups["cu_group"][2] = 2
     assert torch.isnan(cache.attend(batch, s.q)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_more_work_than_can_be_divided(dtype):
+    """128 heads of a sequence that is as long as a table can hold (its pages are all the same one): refused on the device."""
+    from paper_2402_06082_b200 import binding
+    page, most, Hkv = 1024, 2 ** 21 - 2, 128
+    K = torch.zeros(1, Hkv, page, 64, dtype=dtype, device="cuda")
+    cache = binding.PagedCache(K, K)
+    batch = binding.PagedBatch(_ints([0, 1]), _ints([most * page]), torch.zeros(1, most, dtype=torch.int32, device="cuda"))
+    q = torch.zeros(1, Hkv, 64, dtype=dtype, device="cuda")
+    out = torch.full_like(q, 7.0)
+    cache.attend(batch, q, out=out)
+    assert bool((out == 7).all()) and cache.status() == 16
+    assert torch.isnan(cache.attend(batch, q)).all()
+    batch.tensors[0][1] = 2                            # broken offsets as well: these are told
+    cache = binding.PagedCache(K, K)
+    cache.attend(batch, q, out=out)
+    assert cache.status() == 8
