@@ -98,9 +98,24 @@ int check_cache(const char* fn, const subgen_pages* c, const subgen_batch* b, Pa
     return SUBGEN_OK;
 }
 
+int this_device(int* dev) {
+    CUDA_TRY(cudaGetDevice(dev));
+    if (*dev < 0 || *dev >= kMaxDevices) return fail(SUBGEN_EINVAL, "device index %d not supported", *dev);
+    return SUBGEN_OK;
+}
+
 // ---- norms, rotation, append ----
 template <typename T, int D, bool PAGED>
-void launch_norm_rope(NormRope a, const PagedView& P, cudaStream_t st) {
+int launch_norm_rope(NormRope a, const PagedView& P, cudaStream_t st) {
+    static bool done[kMaxDevices];
+    int dev, rc = this_device(&dev);
+    if (rc) return rc;
+    if (!done[dev]) {                                 // loads both, so that a call of any size may be captured later
+        cudaFuncAttributes at;
+        CUDA_TRY(cudaFuncGetAttributes(&at, norm_rope_kernel<T, D, PAGED, 4>));
+        CUDA_TRY(cudaFuncGetAttributes(&at, norm_rope_kernel<T, D, PAGED, 1>));
+        done[dev] = true;
+    }
     constexpr int RPW = 32 / (D / (16 / (int)sizeof(T)) / 2);
     const int groups = (a.H + RPW - 1) / RPW + (PAGED ? 2 : 1) * ((a.Hkv + RPW - 1) / RPW);
     // enough warps to fill the SMs (16 a SM); beyond that a token stays with one warp
@@ -110,15 +125,15 @@ void launch_norm_rope(NormRope a, const PagedView& P, cudaStream_t st) {
     const unsigned blocks = (unsigned)((warps + kNrThreads / 32 - 1) / (kNrThreads / 32));
     if (a.parts == 1) norm_rope_kernel<T, D, PAGED, 4><<<blocks, kNrThreads, 0, st>>>(a, P);
     else norm_rope_kernel<T, D, PAGED, 1><<<blocks, kNrThreads, 0, st>>>(a, P);
+    CUDA_TRY(cudaGetLastError());
+    return SUBGEN_OK;
 }
 
 template <bool PAGED>
 int norm_rope(const NormRope& a, const PagedView& P, int d, int dtype, cudaStream_t st) {
     const bool f32 = dtype == SUBGEN_DTYPE_FP32;
-    if (d == 64) f32 ? launch_norm_rope<float, 64, PAGED>(a, P, st) : launch_norm_rope<__nv_bfloat16, 64, PAGED>(a, P, st);
-    else f32 ? launch_norm_rope<float, 128, PAGED>(a, P, st) : launch_norm_rope<__nv_bfloat16, 128, PAGED>(a, P, st);
-    CUDA_TRY(cudaGetLastError());
-    return SUBGEN_OK;
+    if (d == 64) return f32 ? launch_norm_rope<float, 64, PAGED>(a, P, st) : launch_norm_rope<__nv_bfloat16, 64, PAGED>(a, P, st);
+    return f32 ? launch_norm_rope<float, 128, PAGED>(a, P, st) : launch_norm_rope<__nv_bfloat16, 128, PAGED>(a, P, st);
 }
 
 void fill_norm_rope(NormRope* a, const subgen_qk_args* x, int H, int Hkv) {
@@ -147,11 +162,6 @@ int opt_in(K kern, M merge, size_t smem) {
     cudaFuncAttributes at;
     CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     CUDA_TRY(cudaFuncGetAttributes(&at, merge));
-    return SUBGEN_OK;
-}
-int this_device(int* dev) {
-    CUDA_TRY(cudaGetDevice(dev));
-    if (*dev < 0 || *dev >= kMaxDevices) return fail(SUBGEN_EINVAL, "device index %d not supported", *dev);
     return SUBGEN_OK;
 }
 

@@ -280,3 +280,38 @@ def test_more_work_than_can_be_divided(dtype):
     cache = binding.PagedCache(K, K)
     cache.attend(batch, q, out=out)
     assert cache.status() == 8
+
+
+# ---- captures and streams -------------------------------------------------------------------------
+
+CAPTURE = """
+import sys, torch
+sys.path[:0] = [".", "tests"]
+import paged_helpers as ph
+from paper_2402_06082_b200 import binding
+for dtype in (torch.bfloat16, torch.float32):
+    for d, first, then in ((64, 1, 4000), (128, 4000, 1)):
+        a, b = (ph.Setting([n], [n], 4, 4, d, dtype, 64, seed=n) for n in (first, then))
+        rope = binding.Rope(d)
+        for paged in (False, True):
+            calls = []
+            for s in (a, b):
+                pos = torch.arange(s.n, dtype=torch.int32, device="cuda")
+                cache, batch = s.cache(), s.batch()
+                if paged: calls.append(lambda s=s, cache=cache, batch=batch: cache.append(batch, s.k, s.v, rope=rope, q=s.q))
+                else: calls.append(lambda s=s, pos=pos: binding.qk_norm_rope(s.q, s.k, pos, rope)[0])
+            calls[0]()
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                q = calls[1]()
+            graph.replay()
+            ph.assert_within(q, *ph.norm_rope(b.q, torch.arange(then), None, ph.freqs(d), d, False, 0.0))
+print("captured")
+"""
+
+
+def test_capture_of_rotations_of_sizes_that_have_not_run():
+    """One call of an operator, type and d loads what calls of other sizes need."""
+    r = subprocess.run([sys.executable, "-c", CAPTURE], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
