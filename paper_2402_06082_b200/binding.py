@@ -93,9 +93,11 @@ _lib = None
 _calls = None
 
 
-def _bind_calls(L):
-    """The calls module (csrc/calls.cpp), which the paged functions go through, over this library."""
+def _bind_calls():
+    """The calls module (csrc/calls.cpp), which the paged functions go through, over this library. At the first of these calls:
+    the rest of the library does without it, whatever torch is installed."""
     global _calls
+    L = load()
     try:
         from . import _calls as module
     except ImportError as e:
@@ -166,7 +168,6 @@ def load():
     L.subgen_paged_workspace_bytes.argtypes = [pp, bp, C.c_int, C.c_int]
     L.subgen_paged_workspace_bytes.restype = C.c_size_t
     L.subgen_paged_attend.argtypes = [pp, bp, C.POINTER(AttendArgs), vp]
-    _bind_calls(L)
     _lib = L
     return L
 
@@ -499,7 +500,7 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     what was not given; an output may be its input.
     """
     if _calls is None:
-        load()
+        _bind_calls()
     return _calls.qk_norm_rope(q, k, positions, None if rope is None else rope._desc, wq, wk, eps, q_out, k_out)
 
 
@@ -540,7 +541,8 @@ class PagedCache:
         dev = self.device = _cuda(K, "K")
         if K.dim() != 4 or K.stride(3) != 1 or V.shape != K.shape or V.stride() != K.stride() or V.dtype is not K.dtype or V.get_device() != dev:
             raise ValueError("K and V must be [pages, Hkv, page, d] tensors of one type, device and layout, unit stride along d")
-        load()
+        if _calls is None:
+            _bind_calls()
         self.K, self.V, self.dtype = K, V, K.dtype
         self.pages, self.Hkv, self.page, self.d = K.shape
         self._status = torch.zeros(1, dtype=torch.int32, device=K.device)
