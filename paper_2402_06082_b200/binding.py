@@ -98,11 +98,14 @@ def _bind_calls():
     the rest of the library does without it, whatever torch is installed."""
     global _calls
     L = load()
+    from .build import built_for
+    advice = "build it with `python paper_2402_06082_b200/build.py`; there is no fallback path"
     try:
         from . import _calls as module
     except ImportError as e:
-        raise RuntimeError("_calls.so is missing or was built for another torch: build it with "
-                           "`python paper_2402_06082_b200/build.py`; there is no fallback path") from e
+        raise RuntimeError("_calls.so is missing or was built for another torch: " + advice) from e
+    if module.built_for != "built for " + built_for():
+        raise RuntimeError("_calls.so was %s, this is %s: %s" % (module.built_for, built_for(), advice))
     at = [C.cast(getattr(L, "subgen_" + f), C.c_void_p).value
           for f in ("qk_norm_rope", "paged_append", "paged_attend", "paged_workspace_bytes", "last_error")]
     module.bind(SubgenError, *at)

@@ -21,6 +21,19 @@ def _stale(out: str, sources) -> bool:
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in sources)
 
 
+def built_for() -> str:
+    """What the calls module depends on besides its sources; compiled into it."""
+    import torch
+    return "torch %s, python %d.%d" % (torch.__version__, *sys.version_info[:2])
+
+
+def _calls_stale() -> bool:
+    if _stale(CALLS, CALLS_SOURCES):
+        return True
+    with open(CALLS, "rb") as f:
+        return ("built for " + built_for()).encode() + b"\0" not in f.read()
+
+
 def _calls_command(out: str):
     """calls.cpp against the headers and libraries of the torch that runs this."""
     import sysconfig
@@ -30,7 +43,8 @@ def _calls_command(out: str):
     inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
            os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"), sysconfig.get_paths()["include"]]
     lib = os.path.join(root, "lib")
-    return (["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    return (["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+             '-DSUBGEN_BUILT_FOR="built for %s"' % built_for()]
             + ["-I" + d for d in inc] + ["-o", out, os.path.join(CSRC, "calls.cpp"), "-L" + lib]
             + ["-l" + x for x in ("torch_python", "torch", "torch_cpu", "c10", "c10_cuda")] + ["-Wl,-rpath," + lib])
 
@@ -45,7 +59,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             cmd.insert(1, "-Xptxas")
             cmd.insert(2, "-v")
         jobs.append((LIB, cmd, subprocess.Popen(cmd)))
-    if force or _stale(CALLS, CALLS_SOURCES):
+    if force or _calls_stale():
         cmd = _calls_command(CALLS + ".tmp")
         jobs.append((CALLS, cmd, subprocess.Popen(cmd)))
     codes = [p.wait() for _, _, p in jobs]
