@@ -92,6 +92,11 @@ float real(PyObject* o) {
     if (x == -1.0 && PyErr_Occurred()) { PyErr_Clear(); refuse("a number is wanted"); }
     return (float)x;
 }
+bool truth(PyObject* o, const char* name) {
+    const int x = PyObject_IsTrue(o);
+    if (x < 0) { PyErr_Clear(); refuse(std::string(name) + " has no truth value"); }
+    return x != 0;
+}
 // rope: None or (words, rotary_dim, interleaved, d, device)
 subgen_rope rope_of(PyObject* o, int64_t d, int device) {
     if (o == Py_None) return subgen_rope{nullptr, 0, 0};
@@ -232,7 +237,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t got) {
         if (!p.workspace_bytes) throw Failed(f_error());
         const at::Tensor space = at::empty({(int64_t)p.workspace_bytes}, q->options().dtype(at::kByte));   // torch aligns to 512 bytes
         p.workspace = space.data_ptr();
-        p.n = (int)n; p.H = (int)H; p.scale = real(a[4]); p.causal = PyObject_IsTrue(a[5]) == 1;
+        p.n = (int)n; p.H = (int)H; p.scale = real(a[4]); p.causal = truth(a[5], "causal");
         check(f_attend(c, b, &p, c10::cuda::getCurrentCUDAStream(w.device).stream()));
         return out.release();
     });

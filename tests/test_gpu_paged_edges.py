@@ -315,3 +315,11 @@ def test_capture_of_rotations_of_sizes_that_have_not_run():
     """One call of an operator, type and d loads what calls of other sizes need."""
     r = subprocess.run([sys.executable, "-c", CAPTURE], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+def test_causal_without_a_truth_value():
+    s = ph.Setting([1], [5], 4, 2, 64, BF16)
+    cache, batch = s.cache(), s.batch()
+    with pytest.raises(ValueError, match="causal"):
+        cache.attend(batch, s.q, causal=torch.ones(2))
+    assert torch.equal(cache.attend(batch, s.q, causal=torch.ones(1)), cache.attend(batch, s.q, causal=1))
