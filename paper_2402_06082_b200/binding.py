@@ -549,6 +549,8 @@ class PagedCache:
         self.K, self.V, self.dtype = K, V, K.dtype
         self.pages, self.Hkv, self.page, self.d = K.shape
         self._status = torch.zeros(1, dtype=torch.int32, device=K.device)
+        if not torch.cuda.is_current_stream_capturing():   # 0 before a call on any stream may set a bit (made once a pool)
+            torch.cuda.current_stream(dev).synchronize()
         self._desc = PagesDesc(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), self.pages, self.page, self.Hkv,
                                self.d, _dtype_code(K.dtype), self._status.data_ptr())
         self._at = C.addressof(self._desc)

@@ -323,3 +323,33 @@ def test_causal_without_a_truth_value():
     with pytest.raises(ValueError, match="causal"):
         cache.attend(batch, s.q, causal=torch.ones(2))
     assert torch.equal(cache.attend(batch, s.q, causal=torch.ones(1)), cache.attend(batch, s.q, causal=1))
+
+
+def test_status_of_a_cache_that_a_busy_stream_made():
+    """A call on another stream right after the cache was made: the bit that it sets stays."""
+    s = ph.Setting([1], [5], 4, 2, 64, BF16)
+    s.table[0, 0] = -1
+    batch = s.batch()
+    s.cache().append(batch, s.k, s.v)
+    torch.cuda.synchronize()
+    busy, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(busy):
+        torch.cuda._sleep(200_000_000)                 # a tenth of a second
+        cache = s.cache()
+    with torch.cuda.stream(other):
+        cache.append(batch, s.k, s.v)
+    assert cache.status() == 8
+
+
+def test_a_cache_made_in_a_capture():
+    s = ph.Setting([1, 2], [40, 30], 4, 2, 64, BF16)
+    batch = s.batch()
+    s.cache().attend(batch, s.q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache = s.cache()
+        out = cache.attend(batch, s.q, scale=0.2)
+    graph.replay()
+    ph.assert_within(out, *s.want(0.2))
+    assert cache.status() == 0
