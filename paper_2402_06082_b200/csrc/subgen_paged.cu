@@ -7,6 +7,8 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <initializer_list>
+
 #include "subgen_paged.cuh"
 #include "subgen_paged_simt.cuh"
 #include "subgen_paged_tc.cuh"
@@ -46,6 +48,25 @@ int check_heads(const char* fn, const char* name, const subgen_heads* x, int n, 
     if (v->ts <= 0 || v->hs <= 0) return fail(SUBGEN_EINVAL, "%s: %s: strides must be positive", fn, name);
     if (misaligned(x->p) || odd_stride(v->ts, dtype) || odd_stride(v->hs, dtype))
         return fail(SUBGEN_EINVAL, "%s: %s: pointer and strides must be multiples of 16 bytes", fn, name);
+    return SUBGEN_OK;
+}
+
+// An output whose rows overlap each other, or that starts where an input does and lies otherwise (`same`: the one that it may be).
+// Outputs that overlap an input further on are the caller's to avoid.
+int check_output(const char* fn, const char* name, const HeadsView& o, int n, int heads, int d, const HeadsView& same,
+                 std::initializer_list<const void*> others) {
+    bool overlap = (n > 1 && o.ts < d) || (heads > 1 && o.hs < d);
+    // rows (t, h) and (t + dt, h - dh) are dt * ts - dh * hs apart; where one axis lies within a step of the other there are none
+    if (!overlap && o.ts < (heads - 1) * o.hs + d && o.hs < (n - 1) * o.ts + d)
+        for (long long dh = 1; dh < heads && !overlap; ++dh) {
+            const long long dt = dh * o.hs / o.ts, off = dh * o.hs - dt * o.ts;
+            overlap = (dt > 0 && dt < n && off < d) || (dt + 1 < n && o.ts - off < d);
+        }
+    if (overlap) return fail(SUBGEN_EINVAL, "%s: %s: rows overlap", fn, name);
+    if (o.p == same.p && (o.ts != same.ts || o.hs != same.hs))
+        return fail(SUBGEN_EINVAL, "%s: %s: an output that is its input must have its strides", fn, name);
+    for (const void* p : others)
+        if (p && o.p == p) return fail(SUBGEN_EINVAL, "%s: %s must not be another tensor of the call", fn, name);
     return SUBGEN_OK;
 }
 
@@ -326,6 +347,8 @@ int subgen_qk_norm_rope(const subgen_qk_args* x, void* stream) {
     if (!rc && has_k) rc = check_heads(fn, "k", &x->k, x->n, x->Hkv, x->d, x->dtype, &a.k);
     if (!rc && has_k) rc = check_heads(fn, "k_out", &x->k_out, x->n, x->Hkv, x->d, x->dtype, &a.ko);
     if (!rc && x->rope.words && !x->positions) rc = fail(SUBGEN_EINVAL, "%s: a rotation needs positions", fn);
+    if (!rc && has_q) rc = check_output(fn, "q_out", a.qo, x->n, x->H, x->d, a.q, {a.k.p, a.ko.p});
+    if (!rc && has_k) rc = check_output(fn, "k_out", a.ko, x->n, x->Hkv, x->d, a.k, {a.q.p});
     if (rc) return rc;
     fill_norm_rope(&a, x, has_q ? x->H : 0, has_k ? x->Hkv : 0);
     PagedView none;
@@ -350,6 +373,7 @@ int subgen_paged_append(const subgen_pages* cache, const subgen_batch* batch, co
     if (!rc) rc = check_heads(fn, "v", &x->v, x->n, Hkv, d, dtype, &a.v);
     if (!rc && has_q) rc = check_heads(fn, "q", &x->q, x->n, x->H, d, dtype, &a.q);
     if (!rc && has_q) rc = check_heads(fn, "q_out", &x->q_out, x->n, x->H, d, dtype, &a.qo);
+    if (!rc && has_q) rc = check_output(fn, "q_out", a.qo, x->n, x->H, d, a.q, {a.k.p, a.v.p, P.K, P.V});
     if (rc) return rc;
     fill_norm_rope(&a, x, has_q ? x->H : 0, Hkv);
     return norm_rope<true>(a, P, d, dtype, (cudaStream_t)stream);
@@ -385,6 +409,8 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
     const size_t need = (size_t)slots * (d * sizeof(float) + sizeof(float2));
     if (!x->workspace || ((uintptr_t)x->workspace & 255) || x->workspace_bytes < need)
         return fail(SUBGEN_ENOMEM, "%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, need);
+    rc = check_output(fn, "out", vo, n, H, d, vq, {P.K, P.V});
+    if (rc) return rc;
     const int g_shift = G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : 3;
     Attend a = {vq, vo, n, H, g_shift, x->causal != 0, x->scale * 1.4426950408889634f, (float*)x->workspace,
                 (float2*)((float*)x->workspace + slots * d), x->fresh != 0};
