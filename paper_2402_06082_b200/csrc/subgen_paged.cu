@@ -405,7 +405,8 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
     if (rc) return rc;
     if (vo.p == vq.p) return fail(SUBGEN_EINVAL, "%s: out must not be q", fn);
     const long long slots = slot_count(P, n, H);
-    if (slots > 0x7fffffffLL) return fail(SUBGEN_EINVAL, "%s: too many rows in one call", fn);
+    // (the merge counts parts of rows for each sequence and KV head, those without new tokens among them)
+    if (slots > 0x7fffffffLL || (long long)n * H + (long long)P.B * P.Hkv > 0x7f000000LL) return fail(SUBGEN_EINVAL, "%s: too many rows in one call", fn);
     const size_t need = (size_t)slots * (d * sizeof(float) + sizeof(float2));
     if (!x->workspace || ((uintptr_t)x->workspace & 255) || x->workspace_bytes < need)
         return fail(SUBGEN_ENOMEM, "%s: the workspace must be 256-byte aligned and hold %zu bytes", fn, need);

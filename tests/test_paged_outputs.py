@@ -76,3 +76,13 @@ def test_another_tensor_of_the_call():
         assert _append(q, _heads(p, 4 * D, D)) == -1 and "another" in _said()
     for p in (6, 7):
         assert _attend(q, _heads(p, 4 * D, D)) == -1 and "another" in _said()
+
+
+def test_more_heads_than_can_be_counted():
+    """Sequences without new tokens count as well."""
+    wide = 1 << 21
+    pages = binding.PagesDesc(K=6 * P, V=7 * P, page_stride=wide * 16 * D, head_stride=16 * D, row_stride=D, pages=10, page=16, Hkv=wide, d=D, dtype=0)
+    batch = _batch()
+    batch.B = 1024
+    args = binding.AttendArgs(_heads(1, wide * D, D), _heads(2, wide * D, D), 8 * P, 1 << 40, 1, wide, 1.0, 1)
+    assert binding.load().subgen_paged_attend(pages, batch, args, None) == -1 and "too many rows" in _said()
