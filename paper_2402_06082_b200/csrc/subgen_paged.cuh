@@ -360,6 +360,12 @@ struct Plan {
         const int lim = e.S - e.nq + 1 + (r >> a.g_shift);
         return lim < 0 ? 0 : lim > e.S ? e.S : lim;
     }
+    // 1 / sum of row r, which sees `prefix` tokens before its own. A sum of 0: nothing to see, and the result is 0, or nothing
+    // but scores of -infinity, and it is NaN as the formula's.
+    __device__ __forceinline__ float inverse(float sum, int prefix, const Entry& e, int r) const {
+        if (sum == 0.f) return prefix > 0 || own_limit(e, r) > 0 ? NAN : 0.f;
+        return 1.f / sum;
+    }
     __device__ __forceinline__ int unit_rows(const Entry& e, int ru) const { return min(RU, e.rows - ru * RU); }
     __device__ __forceinline__ int prefix_tiles(const Entry& e) const { return (e.P + KT - 1) / KT; }
     __device__ __forceinline__ int unit_tiles(const Entry& e, int ru) const {
@@ -711,9 +717,16 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
                     }
                 }
                 if (r >= rows_end || sub) continue;
-                float inv = l == 0.f ? 0.f : 1.f / l;                // l is NaN where a page was unusable
+                const int row = ru * RU + r;
+                float inv = 1.f / l;                                 // l is NaN where a page was unusable
+                if (__builtin_expect(l == 0.f, 0)) {
+                    int b2 = b;                                      // told anew, so that nothing is kept for it
+                    asm volatile("" : "+r"(b2));
+                    const Entry e2 = plan.entry(P.groups + b2);
+                    inv = plan.inverse(l, P.groups ? __ldg(P.prefix_len + plan.group_of(b2)) : 0, e2, row);
+                }
                 if (bad) inv = NAN;
-                const int row = ru * RU + r, tok = e.tok0 + (row >> a.g_shift), head = (h << a.g_shift) + (row & ((1 << a.g_shift) - 1));
+                const int tok = e.tok0 + (row >> a.g_shift), head = (h << a.g_shift) + (row & ((1 << a.g_shift) - 1));
                 T* y = (T*)a.o.p + tok * a.o.ts + head * a.o.hs + lane * VL;
                 if constexpr (sizeof(T) == 4) {
                     if constexpr (VL == 4) *reinterpret_cast<float4*>(y) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);

@@ -88,10 +88,6 @@ __device__ __forceinline__ float* result_row(const Attend& a, const Seg& g, int 
     return (float*)a.o.p + (g.e.tok0 + (row >> a.g_shift)) * a.o.ts + ((g.head << a.g_shift) + (row & ((1 << a.g_shift) - 1))) * a.o.hs;
 }
 
-// Whether a run has a token that a row of the unit sees, which has `own` own ones to see. If so and no score is above
-// -infinity, the row is NaN; one that sees nothing is 0.
-__device__ __forceinline__ bool sees_any(const Seg& g, int own, int kt) { return g.tile0 < g.kp || own > (g.tile0 - g.kp) * kt; }
-
 // R rows of a tile by one warp (few rows): scores of its KT / 4 tokens, weights, numerator.
 template <int D, int R>
 __device__ __forceinline__ void few_tile(FewSmem<D>& sm, int at, int first, const int* lim, float c, float* m, float* l, float (*acc)[D / 32]) {
@@ -240,8 +236,8 @@ __global__ void __launch_bounds__(FewSmem<D>::NT, FewSmem<D>::BLOCKS) paged_atte
 #pragma unroll
                 for (int i = 0; i < VL; ++i) z[i] = fmaf(join[k][r][lane * VL + i], f, z[i]);
             }
-            if (bad || (M == -INFINITY && sees_any(g, plan.own_limit(g.e, g.ru * RU + r), KT))) L = NAN;
-            const float f = !g.direct ? 1.f : L == 0.f ? 0.f : 1.f / L;
+            if (bad) L = NAN;
+            const float f = !g.direct ? 1.f : plan.inverse(L, g.e.P, g.e, g.ru * RU + r);
             float* y = result_row<RU, D>(a, g, r) + lane * VL;
             if (!g.direct && lane == 0) a.stat[g.slot + r] = make_float2(M, L);
             if constexpr (VL == 4) *reinterpret_cast<float4*>(y) = make_float4(z[0] * f, z[1] * f, z[2] * f, z[3] * f);
@@ -382,9 +378,9 @@ __global__ void __launch_bounds__(SimtSmem<D>::NT, SimtSmem<D>::BLOCKS) paged_at
 #pragma unroll
             for (int off = 8; off > 0; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
             const int r = ty + 16 * i;
-            if (bad || (m[i] == -INFINITY && sees_any(g, own[i], KT))) l[i] = NAN;
+            if (bad) l[i] = NAN;
             if (r < g.rows) {
-                const float f = !g.direct ? 1.f : l[i] == 0.f ? 0.f : 1.f / l[i];
+                const float f = !g.direct ? 1.f : plan.inverse(l[i], g.e.P, g.e, g.ru * RU + r);
                 float* y = result_row<RU, D>(a, g, r);
                 if (!g.direct && tx == 0) a.stat[g.slot + r] = make_float2(m[i], l[i]);
 #pragma unroll

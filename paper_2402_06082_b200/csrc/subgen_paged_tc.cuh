@@ -552,11 +552,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             m = edge = -INFINITY;
             l = off = 0.f;
             begun = false;
-            // Whether this group's share of the run has a token that the row sees. If so and no score is finite, the row is NaN;
-            // a maximum of -infinity alone would not tell it from a row that sees nothing, which is 0.
-            const int t_first = tile0 + (dual ? 0 : order);
-            const bool sees = t_first < kp || own > (t_first - kp) * kPtKT;
-            for (int t = t_first; t < tile1; t += 2 - dual) {
+            for (int t = tile0 + (dual ? 0 : order); t < tile1; t += 2 - dual) {
                 const bool pre = t < kp;
                 const int lim = pre ? P_ - t * kPtKT : own - (t - kp) * kPtKT;        // tokens of the tile that the row sees
                 const bool cut = __any_sync(0xffffffffu, lim < kPtKT);
@@ -620,7 +616,6 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     // thread for four columns
                     tc_fence_after();
                     sm.join_stat[w][quarter][lane] = make_float2(m, l);
-                    const unsigned seen = __ballot_sync(0xffffffffu, sees);
                     uint32_t o[D];
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) tc_ld32(tO + i * 32, o + i * 32);
@@ -654,7 +649,6 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
 #pragma unroll
                                 for (int j = 0; j < D / 32; ++j) z[j] = fmaf(sm.join[w][k][quarter][j * 32 + lane], f, z[j]);
                             }
-                            if (M == -INFINITY) L = (seen >> rr) & 1 ? NAN : 0.f;
                             if (bad) L = NAN;
                             if (HAND && tiles > 1) {                     // the other group has the other tiles' share of the row
                                 const int at = hands & 1, parity = (hands >> 1) & 1;
@@ -681,7 +675,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                             }
                             const int gr = r.ru * kPtRU + rr, tok = r.tok0 + (gr >> gs), head = (r.head << gs) + (gr & ((1 << gs) - 1));
                             if (direct) {
-                                const float f = L == 0.f ? 0.f : 1.f / L;
+                                const float f = plan.inverse(L, P_, e, gr);
                                 __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
 #pragma unroll
                                 for (int j = 0; j < D / 32; ++j) y[j * 32 + lane] = __float2bfloat16_rn(z[j] * f);
@@ -695,10 +689,10 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     }
                 } else if (some) {
                     tc_fence_after();
-                    if (!(fabsf(m) < INFINITY)) l = sees ? NAN : 0.f;
+                    if (!(fabsf(m) < INFINITY)) l = m == -INFINITY ? 0.f : NAN;       // no score above -infinity here, or NaN
                     if (bad) l = NAN;
                     const int tok = r.tok0 + (urow >> gs), head = (r.head << gs) + (urow & ((1 << gs) - 1));
-                    const float f = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+                    const float f = direct ? plan.inverse(l, P_, e, urow) : 1.f;
                     __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
                     if (live && !direct) a.stat[slot0 + row] = make_float2(m * a.c, l);
                     __syncwarp();

@@ -69,6 +69,31 @@ def test_rows_that_see_nothing_of_queries_that_are_not_finite(dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new, own, prefix, low", [
+    (1, 256, 0, range(128)), (1, 256, 0, range(128, 256)), (1, 40, 0, range(39)), (2, 9000, 0, range(5000)), (60, 700, 0, range(500)),
+    (300, 900, 0, range(128, 500)), (3, 200, 300, range(-300, 0)), (3, 200, 300, range(-300, 150)), (1, 129, 128, range(129)),
+    (1, 40, 0, range(40)), (2, 9000, 0, range(9000)), (3, 200, 300, range(-300, 200)), (90, 300, 0, range(250))])
+def test_scores_of_minus_infinity(dtype, d, new, own, prefix, low):
+    """Keys whose products overflow have no weight, also where a block, a group of warps or a whole part of the row has no other;
+    a row that sees none but those is NaN. Own tokens count from 0, the prefix's from -prefix."""
+    s = ph.Setting([new], [own], 4, 2, d, dtype, 16, [0, 1] if prefix else [], [prefix] if prefix else [], seed=5)
+    s.q.abs_().add_(1)
+    scale, at = 0.25, []
+    for j in low:
+        row, i = (s.table[0], j) if j >= 0 else (s.ptable[0], prefix + j)
+        at.append((int(row[i // 16]), i % 16))
+    where = tuple(torch.tensor(x, device="cuda") for x in zip(*at))
+    s.K[where[0], :, where[1]] = -8.0                  # d * 1 * 8 * scale = 128 below and more: no weight either
+    want, bound = s.want(scale)
+    s.K[where[0], :, where[1]] = torch.finfo(dtype).min
+    for i in range(new):
+        if all(j in low for j in range(-prefix, own - new + 1 + i)):
+            want[i] = math.nan
+    ph.assert_within(s.cache().attend(s.batch(), s.q, scale=scale), want, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("new, own, G", [(4, 5, 1), (8, 300, 1), (8, 8, 2), (20, 20, 4), (60, 61, 4), (200, 700, 1), (300, 300, 1)])
 def test_extreme_values_that_a_row_does_not_see(dtype, d, new, own, G):
     """V of tokens behind a row's own is finite but the type's lowest: a weight that is not exactly 0 would show."""
