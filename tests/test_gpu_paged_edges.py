@@ -107,6 +107,22 @@ def test_extreme_values_that_a_row_does_not_see(dtype, d, new, own, G):
     ph.assert_within(out[:rows], want[:rows], bound[:rows])
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new, own, G", [(4, 5, 1), (8, 300, 1), (20, 20, 4), (60, 61, 4), (200, 700, 1), (300, 300, 1)])
+@pytest.mark.parametrize("value", ["lowest", "largest"])
+def test_extreme_keys_that_a_row_does_not_see(dtype, d, new, own, G, value):
+    """Keys behind a row's own whose products overflow, to either side or to NaN."""
+    s = ph.Setting([new], [own], 2 * G, 2, d, dtype, 16, seed=4)
+    want, bound = s.want(0.1)
+    first = own - 2
+    for j in range(first, own):
+        s.K[int(s.table[0, j // 16]), :, j % 16] = torch.finfo(dtype).min if value == "lowest" else torch.finfo(dtype).max
+    rows = first - (own - new)
+    out = s.cache().attend(s.batch(), s.q, scale=0.1)
+    ph.assert_within(out[:rows], want[:rows], bound[:rows])
+
+
 def test_weights_of_the_cubic():
     """One token's weight against the largest's, from even to 2^-140 of it, by the place in the tile: within the bf16 bound."""
     n, d = 64, 64
