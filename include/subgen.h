@@ -345,7 +345,8 @@ int subgen_exact_attention_noalloc(const void* q, const void* K, const void* V, 
  *   y = rot(position, w * x / sqrt(mean(x^2) + eps))
  * per head, the norm only where w is given; rot turns the pair (a, b) of coordinates (i, i + r/2), or (2i, 2i + 1) if
  * interleaved, i < r/2, by the angle position * f_i: (a cos - b sin, b cos + a sin). Coordinates from r on pass.
- * Arithmetic in fp32, one rounding at the end; angles are exact to 2^-33 of a turn for any 31-bit position. */
+ * Arithmetic in fp32, one rounding at the end. position * f_i is exact to 2^-32 of a turn for positions below 2^32; sine and
+ * cosine are taken of that rounded to 24 bits, so an angle is off by at most 2^-26 of a turn (1e-7 rad) near half a turn. */
 typedef struct subgen_rope {
     const uint64_t* words;  /* device, [rotary_dim / 2], from subgen_rope_words; NULL: no rotation */
     int rotary_dim;         /* r: a multiple of 16, at most d */
@@ -384,8 +385,10 @@ int subgen_qk_norm_rope(const subgen_qk_args* args, void* stream);
 /* A pool of pages that any number of sequences share, owned by the caller, and what a call has to know about them. All
  * pointers are device pointers; the functions below keep nothing between calls, so lengths and tables may change on
  * the device (also inside a captured graph). Indices are checked on the device: a page outside [0, pages) or a length
- * beyond its table is neither read nor written, sets SUBGEN_ST_PAGE in *status and makes the outputs that needed it
- * NaN. The first call of each kind on a device loads its kernels: make it before starting any stream capture. */
+ * beyond its table is neither read nor written, sets SUBGEN_ST_PAGE in *status and makes the attention's outputs that needed
+ * it NaN (other new tokens of the same sequence, whose rows are worked on together with theirs, may become NaN as well).
+ * After SUBGEN_ST_TIMEOUT the outputs of the call are unspecified. The first call of an operator with a dtype and d on a
+ * device loads its kernels for all sizes: make it before starting any stream capture. */
 typedef struct subgen_pages {
     void *K, *V;            /* element (page, head, row, x) of each at page * page_stride + head * head_stride + row * row_stride + x */
     int64_t page_stride, head_stride, row_stride;   /* elements; multiples of 16 bytes */
@@ -436,15 +439,18 @@ typedef struct subgen_attend_args {
 /* out = softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for each of the n new tokens' H query heads (head h reads KV
  * head h / (H / Hkv); H / Hkv in {1, 2, 4, 8}), the new tokens' keys and values being in the cache already. A token sees
  * its group's whole prefix and, of its own sequence, the tokens up to itself (causal = 1) or all of them (causal = 0).
- * A row that sees nothing (an empty sequence, or one of more new tokens than its length says) is 0. The prefix is read
- * once per group, whatever the number of its sequences. Stored keys and values that some row sees must be
- * finite; what lies behind a sequence's length in its last page may be anything.
+ * A row that sees nothing (an empty sequence, or one of more new tokens than its length says) is 0. The rows (new tokens x
+ * H / Hkv) of a group's sequences are worked on together, and its prefix is read once for each unit of them, not for each
+ * sequence: up to 256 rows on bf16 caches, on fp32 ones 128 (d = 128) or 64, or 8 in calls of at most 8 rows a sequence on
+ * average. (Sequences of half a unit's rows or more read it themselves, unit by unit.) Stored keys and values that some row
+ * sees must be finite; what lies behind a sequence's length in its last page may be anything. A query that is not finite,
+ * or whose scores all overflow to -infinity, makes its own row NaN (if it sees anything) and no other.
  * Where cu_q or cu_group are not what they have to be, nothing is computed: SUBGEN_ST_PAGE is set, and `out` is left as it was,
  * or NaN if it is `fresh`. The same with SUBGEN_ST_SIZE where the key tiles that all row units of all KV heads take come to 2^30 or
  * more (bf16: tiles of 128 tokens, units of up to 256 rows, which above 128 rows count twice; fp32: 32 or 64 tokens, units of up to
  * 8, 64 or 128 rows; and one or two more for each unit).
  * Scores, maxima, sums and numerators are fp32; on bf16 caches the softmax weights are rounded to bf16 for the product
- * with V. The result does not depend on how blocks are scheduled.
+ * with V, and a quarter of them are made with a relative error of up to 7.5e-5 before (a fiftieth of that rounding). The result does not depend on how blocks are scheduled.
  * out must not overlap q. The workspace is this call's until it has run (two calls that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */
 size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H);
 int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_attend_args* args, void* stream);

@@ -235,7 +235,8 @@ int attend_fp32(const PagedView& P, const Attend& a, cudaStream_t st) {
     if (rc) return rc;
     // Up to 8 rows a sequence on average: one pass over the cache with little arithmetic to it (16 sequences of 2000 tokens,
     // 8 heads, 8 rows each: 93 us against 216; 12 rows, which take two units there: 191 against 218, but 110 against 82 at
-    // d = 64 behind a shared prefix).
+    // d = 64 behind a shared prefix). The mean is all that is looked at: a chunk of a prompt among many single tokens, or many of
+    // those behind one prefix, comes in units of 8 rows here, each of which reads all that it sees.
     if (((long long)a.n << a.g_shift) <= 8LL * P.B) return attend_fp32_with<FewSmem<D>, D>(paged_attend_few_kernel<D>, P, a, st);
     return attend_fp32_with<SimtSmem<D>, D>(paged_attend_simt_kernel<D>, P, a, st);
 }

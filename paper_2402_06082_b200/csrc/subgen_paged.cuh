@@ -35,16 +35,18 @@ __device__ __forceinline__ void paged_status(const PagedView& P, int bit) {
 //
 // y = rot(pos, w * x / sqrt(mean(x^2) + eps)) per head, pairs (a, b) -> (a cos - b sin, b cos + a sin); fp32 inside, one
 // rounding at the end. The angle of pair i is pos * f_i; f_i comes as word_i = round(f_i / 2pi * 2^64), so pos * word_i
-// mod 2^64 is the angle's fraction of a turn, exact to 2^-33 of a turn for every 31-bit position (a product in fp32
-// would be off by 2^-24 * pos radians), and the top 32 bits go through sincospi.
+// mod 2^64 is the angle's fraction of a turn, off by 2^-33 of a turn at most for positions below 2^32 (a product in fp32
+// would be off by 2^-24 * pos radians). Its top 32 bits, converted to fp32 half turns, go through sincospi: the conversion
+// rounds to 24 bits, 2^-26 of a turn near half a turn, as much as fp32 holds of an angle; more would take a second product
+// and a correction for each pair (fp32 results are 6.9e-8 from the exact ones, 6.3e-8 with 64-bit angles).
 //
 // Memory bound: each element is read once and written once (n = 16384, 64 heads, d = 128, bf16: 537 MB, floor 83 us).
 // A row (one head of one token) is held by D / 16 bytes / 2 lanes, each with two 16-byte pieces that contain both
 // members of its pairs, so the rotation needs no exchange and the norm a few shuffles. A warp stays with one token and
 // walks over its heads: the sines are computed once per token and lane, and the loads of U row groups go out before the
 // first is used. With few tokens a token's heads are dealt to several warps (`parts`), which repeat the sines but shorten
-// the chain; then U = 1. U = 4 in 96 registers: 97 us for the above (5.5 TB/s), 156 us for 11.7 K tokens x 96 heads
-// appended to pages (6.2 TB/s of 6.5 measured for a copy); U = 1 took 132 and 201, U = 2 103 and 162.
+// the chain; then U = 1. U = 4 in 96 registers: 97 to 102 us for the above by the box (5.3 to 5.5 TB/s), 158 us for 19.7 K
+// tokens x 96 heads appended to pages (6.1 TB/s of 6.5 measured for a copy); U = 1 took 132 and 201, U = 2 103 and 162.
 struct NormRope {
     HeadsView q, k, v, qo, ko;                        // ko: unless the keys go into pages
     int n, H, Hkv, parts;
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
 //
 // out = softmax(scale q [Kp; Ko]^T) [Vp; Vo]: every query row (a new token's head) sees its group's prefix p in full and
 // of its sequence's own tokens o those up to its own position (causal) or all. Entries of the plan, per KV head:
-// groups first (their prefix against the rows of all their sequences at once: the prefix is read once per group),
+// groups first (their prefix against the rows of all their sequences at once: the prefix is read once per row unit),
 // then sequences (own tokens against the sequence's rows). An entry's rows (tokens x G heads, in packed order, so a
 // group's rows are one range of tokens) are cut into row units of RU rows, each unit's keys into tiles of KT tokens.
 // A unit with tiles has weight LEAD (what starting and ending a run costs, in tiles) plus 1 for each tile, or 2 where
