@@ -444,7 +444,8 @@ typedef struct subgen_attend_args {
  * sequence: up to 256 rows on bf16 caches, on fp32 ones 128 (d = 128) or 64, or 8 in calls of at most 8 rows a sequence on
  * average. (Sequences of half a unit's rows or more read it themselves, unit by unit.) Stored keys and values that some row
  * sees must be finite; what lies behind a sequence's length in its last page may be anything. A query that is not finite,
- * or whose scores all overflow to -infinity, makes its own row NaN (if it sees anything) and no other.
+ * whose scores all overflow to -infinity or whose largest one, times scale and log2(e), overflows makes its own row NaN (if it
+ * sees anything) and no other.
  * Where cu_q or cu_group are not what they have to be, nothing is computed: SUBGEN_ST_PAGE is set, and `out` is left as it was,
  * or NaN if it is `fresh`. The same with SUBGEN_ST_SIZE where the key tiles that all row units of all KV heads take come to 2^30 or
  * more (bf16: tiles of 128 tokens, units of up to 256 rows, which above 128 rows count twice; fp32: 32 or 64 tokens, units of up to

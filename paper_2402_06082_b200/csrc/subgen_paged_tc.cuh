@@ -476,8 +476,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         const uint32_t tS = tmem + lanes + (uint32_t)w * 128u, tO = tmem + lanes + 256u + (uint32_t)(w * D);
         unsigned ns = 0, job = 0, mine = 0, segs = 0;  // runs, jobs of both groups, jobs and runs of this one
         bool ok = true;
-        float m = 0.f, l = 0.f, edge = 0.f, off = 0.f; // of this thread's row: the maximum in use, the sum, the score from
-                                                       // which on the maximum is replaced, -m * c
+        float m = 0.f, l = 0.f, edge = 0.f, off = 0.f, cr = 0.f;   // of this thread's row: the maximum in use, the sum, the score
+                                                       // from which on the maximum is replaced, -m * cr, c or less
         const float margin = 8.f / a.c;
         bool begun = false, live = false;              // live: the row is one of the unit's (other lanes may hold anything)
         unsigned joins = 0, hands = 0;                 // hands: rows that this warp has handed over or taken
@@ -491,7 +491,17 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             const bool rise = live && !(top <= edge);  // a NaN becomes the maximum, and the sum NaN with it
             if (__any_sync(0xffffffffu, rise)) {
                 const float f = rise ? ex2_approx((m - top) * a.c) : 1.f;              // 0 when there was no maximum yet
-                if (rise) { m = top; edge = top + margin; off = -top * a.c; }
+                if (rise) {
+                    m = top;
+                    edge = top + margin;
+                    // -m * c is rounded once more than s * c + off: by 2^-4 at 2^20, by more than any exponent holds at 2^31. A
+                    // score is no better known there (d sums rounded to 2^-24 of it), so from 2^21 on a factor that is smaller
+                    // by a power of two does as well: scores that sums over d = 64 can tell apart stay 17 octaves apart. Sums
+                    // are joined by c as ever.
+                    const int e = max((__float_as_int(top * a.c) >> 23) & 255, 127 + 20);
+                    cr = a.c * __int_as_float((127 + 127 + 20 - e) << 23);
+                    off = -top * cr;
+                }
                 l *= f;
                 if (begun) {
                     uint32_t o[32];
@@ -510,7 +520,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         // N scores of the row -> bf16 weights, two to a register; adds them to the sum
         auto weigh = [&](auto count, const uint32_t* s, uint32_t* p) {
             constexpr int N = decltype(count)::value;
-            const float2 cc = make_float2(a.c, a.c), oo = make_float2(off, off), oh = make_float2(off - 0.5f, off - 0.5f);
+            const float2 cc = make_float2(cr, cr), oo = make_float2(off, off), oh = make_float2(off - 0.5f, off - 0.5f);
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
@@ -551,6 +561,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             const int own = plan.own_limit(e, urow);
             m = edge = -INFINITY;
             l = off = 0.f;
+            cr = a.c;
             begun = false;
             for (int t = tile0 + (dual ? 0 : order); t < tile1; t += 2 - dual) {
                 const bool pre = t < kp;
@@ -606,6 +617,10 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             job += dual ? 2 * tiles : tiles;
             ++ns;
             if (begun) {
+                // no score above -infinity here, or one that is not finite
+                if (!(fabsf(m * a.c) < INFINITY)) l = m == -INFINITY ? 0.f : NAN;
+                // a whole row without weights: nothing to see (0), or nothing but scores of -infinity (NaN, as the formula's)
+                const float none = P_ > 0 || own > 0 ? NAN : 0.f;
                 if (!(ok = bar_wait(&sm.o_full[w], segs & 1, &sm.failed))) break;
                 ++segs;
                 const int gs = a.g_shift, bad = *reinterpret_cast<const volatile int*>(&r.bad);
@@ -633,6 +648,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                         }
                         if (!joined()) break;
                         const int rr = r0 + quarter;             // a warp per row
+                        const float rr_none = __shfl_sync(0xffffffffu, none, rr & 31);
                         if (rr < rows) {
                             float2 st[4];
                             float M = -INFINITY, L = 0.f;
@@ -675,7 +691,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                             }
                             const int gr = r.ru * kPtRU + rr, tok = r.tok0 + (gr >> gs), head = (r.head << gs) + (gr & ((1 << gs) - 1));
                             if (direct) {
-                                const float f = plan.inverse(L, P_, e, gr);
+                                const float f = L == 0.f ? rr_none : 1.f / L;
                                 __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
 #pragma unroll
                                 for (int j = 0; j < D / 32; ++j) y[j * 32 + lane] = __float2bfloat16_rn(z[j] * f);
@@ -689,10 +705,9 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     }
                 } else if (some) {
                     tc_fence_after();
-                    if (!(fabsf(m) < INFINITY)) l = m == -INFINITY ? 0.f : NAN;       // no score above -infinity here, or NaN
                     if (bad) l = NAN;
                     const int tok = r.tok0 + (urow >> gs), head = (r.head << gs) + (urow & ((1 << gs) - 1));
-                    const float f = direct ? plan.inverse(l, P_, e, urow) : 1.f;
+                    const float f = direct ? (l == 0.f ? none : 1.f / l) : 1.f;
                     __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
                     if (live && !direct) a.stat[slot0 + row] = make_float2(m * a.c, l);
                     __syncwarp();

@@ -94,6 +94,37 @@ def test_scores_of_minus_infinity(dtype, d, new, own, prefix, low):
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("scale", [3e4, 1e7, 1e9, 1e12, 1e30])
+def test_scores_beyond_a_float_exponent(dtype, d, name, scale):
+    """Finite scores of any size: where the largest is ahead by more than its rounding and 200, it has all the weight."""
+    new, own, edges, prefix, H, Hkv = SHAPES[name]
+    s = ph.Setting(new, own, H, Hkv, d, dtype, 16, edges, prefix, seed=8)
+    got = s.cache().attend(s.batch(), s.q, scale=scale).cpu().double()
+    clear = 0
+    for b in range(len(new)):
+        g = next((i for i in range(len(prefix)) if edges[i] <= b < edges[i + 1]), None)
+        parts = ([(s.ptable[g], prefix[g])] if g is not None else []) + [(s.table[b], own[b])]
+        k, v = (torch.cat([ph.own_tokens(pool, row, n) for row, n in parts], 1) for pool in (s.K, s.V))
+        x = s.q[s.cu[b]:s.cu[b + 1]].cpu().double().view(new[b], Hkv, H // Hkv, d)
+        sc = torch.einsum("thgd,hld->thgl", x, k) * scale
+        size = torch.einsum("thgd,hld->thgl", x.abs(), k.abs()).amax(-1) * scale
+        last = k.shape[1] - new[b] + torch.arange(new[b])
+        sc.masked_fill_((torch.arange(k.shape[1]) > last[:, None])[:, None, None], -math.inf)
+        two = torch.cat([sc, torch.full_like(sc[..., :1], -math.inf)], -1).topk(2, -1)
+        ahead = (two.values[..., 0] - two.values[..., 1] > 200 + 4 * (d + 4) * ph.U32 * size).view(new[b], H)
+        want = torch.stack([v[h][two.indices[:, h, :, 0].clamp(max=k.shape[1] - 1)] for h in range(Hkv)], 1).view(new[b], H, d)
+        # its weight is any power of two up to 2^13, in the sum as it is, for the product rounded to bf16 (2^-8), perhaps by the
+        # cubic in one and the same; 1 / sum, a product and the rounding of the output
+        bound = (2 ** -7 + 2 ** -20 if dtype == BF16 else 2.0 ** -20) * want.abs()
+        off = ((got[s.cu[b]:s.cu[b + 1]] - want).abs() > bound).any(-1)
+        assert not (off & ahead).any() and torch.isfinite(got[s.cu[b]:s.cu[b + 1]]).all()
+        clear += int(ahead.sum())
+    assert clear > s.n * H // 2
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("new, own, G", [(4, 5, 1), (8, 300, 1), (8, 8, 2), (20, 20, 4), (60, 61, 4), (200, 700, 1), (300, 300, 1)])
 def test_extreme_values_that_a_row_does_not_see(dtype, d, new, own, G):
     """V of tokens behind a row's own is finite but the type's lowest: a weight that is not exactly 0 would show."""
