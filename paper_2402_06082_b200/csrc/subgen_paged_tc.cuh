@@ -52,10 +52,10 @@ struct PtSmem {                                       // after a 1024-byte align
     float hand[4][2][D];                              // [warp][which][column]: a row's numerator from the second group to the first
     float2 hand_stat[4][2];
     SegRec seg[kPtRing];
-    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2], turn[2], hand_full[4][2], hand_empty[4][2],
+    unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2], hand_full[4][2], hand_empty[4][2],
         seg_full[kPtRing], seg_empty[kPtRing], drain;
     unsigned tmem;
-    int failed, flag;
+    int failed, flag, turns[2];                       // turns: tiles shared by both groups that a group's issuer has done with
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -86,6 +86,19 @@ __device__ __forceinline__ bool bar_wait(unsigned long long* b, unsigned parity,
     for (unsigned i = 0; i < kPtSpins && !done; ++i) {
         done = bar_try(b, parity);
         if ((i & 15) == 15 && *reinterpret_cast<volatile int*>(failed)) break;
+    }
+    if (__all_sync(0xffffffffu, done)) return true;
+    *reinterpret_cast<volatile int*>(failed) = 1;
+    return false;
+}
+// Waits until *count, which only grows, is `target` or more; as bar_wait. A count, not a barrier: one group's issuer may be two
+// turns ahead of the other's wait (the last of one run and the first of the next), and a barrier's parity would then stand for
+// a turn that never comes.
+__device__ __forceinline__ bool count_wait(const int* count, int target, int* failed) {
+    bool done = *reinterpret_cast<const volatile int*>(count) >= target;
+    for (unsigned i = 0; i < 8 * kPtSpins && !done; ++i) {
+        done = *reinterpret_cast<const volatile int*>(count) >= target;
+        if ((i & 255) == 255 && *reinterpret_cast<volatile int*>(failed)) break;
     }
     if (__all_sync(0xffffffffu, done)) return true;
     *reinterpret_cast<volatile int*>(failed) = 1;
@@ -229,7 +242,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             bar_init(&sm.q_full[i], 1); bar_init(&sm.q_empty[i], 2);
             bar_init(&sm.s_full[i], 1); bar_init(&sm.p_full[i], 4);
             bar_init(&sm.o_full[i], 1); bar_init(&sm.o_empty[i], 4);
-            bar_init(&sm.join_bar[i], 4); bar_init(&sm.turn[i], 1);
+            bar_init(&sm.join_bar[i], 4);
+            sm.turns[i] = 0;
         }
         for (int i = 0; i < NS; ++i) { bar_init(&sm.kv_full[i], 1); bar_init(&sm.kv_empty[i], 2); }
         for (int i = 0; i < kPtRing; ++i) { bar_init(&sm.seg_full[i], 1); bar_init(&sm.seg_empty[i], 11); }
@@ -380,7 +394,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 ++c.seg;
             };
             Cursor qk = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}, pv = qk;
-            int segs = 0, mine = 0, turns = 0;         // runs whose numerator the group has begun, products with V, turns taken
+            int segs = 0, mine = 0, turns = 0;         // runs whose numerator the group has begun, products with V, those of shared tiles
             // Whether Q and K of the next S are there: asked before P V is issued, so that S can follow without a wait.
             auto issue_ready = [&]() {
                 if (qk.done) return false;
@@ -441,8 +455,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 // Two groups on the same tiles take turns, P V and the next S of one, then of the other. Left to themselves
                 // both pairs run interleaved, end together, and the tensor pipe waits while both groups exponentiate.
                 const bool turn = pv.dual && (pv.order || pv.tile != pv.tile0);
-                if (turn && !(ok = wait(&sm.turn[w], turns & 1))) break;
-                turns += turn;
+                if (turn && !(ok = count_wait(&sm.turns[1 - w], turns + pv.order, &sm.failed))) break;
                 if (!(ok = wait(&sm.p_full[w], mine & 1))) break;
                 tc_fence_after();
                 const uint32_t td = tmem + 256u + w * (uint32_t)D, tp = tmem + w * 128u;
@@ -455,7 +468,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 pv.tile += step;
                 issue_qk(k_there);
                 ++mine;
-                if (pv.dual && !(pv.order && last) && lane == 0) bar_arrive(&sm.turn[1 - w]);
+                turns += pv.dual;
+                if (pv.dual && lane == 0) *reinterpret_cast<volatile int*>(&sm.turns[w]) = turns;
                 if (last) {
                     __syncwarp();
                     if (lane == 0) bar_arrive(&sm.seg_empty[pv.seg % kPtRing]);

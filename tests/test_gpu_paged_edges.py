@@ -170,6 +170,30 @@ def test_weights_of_the_cubic():
             ph.assert_within(s.cache().attend(s.batch(), s.q, scale=1.0), want, bound)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G, Hkv", [(8, 3), (8, 8), (4, 5), (1, 8)])
+@pytest.mark.parametrize("seed", range(4))
+def test_many_short_runs_of_two_halves(d, G, Hkv, seed):
+    """Row units of more than 128 rows over a tile or two, between ones of one group alone: the groups' issuers get far apart."""
+    g = torch.Generator().manual_seed(100 * seed + G)
+    B = 150
+    rows = torch.tensor([3, 40, 130, 180, 256, 300])[torch.randint(0, 6, (B,), generator=g)]
+    new = ((rows + G - 1) // G).tolist()
+    own = torch.tensor([1, 5, 60, 128, 129, 200, 300, 900])[torch.randint(0, 8, (B,), generator=g)].tolist()
+    s = ph.Setting(new, own, G * Hkv, Hkv, d, BF16, 128, seed=seed)
+    cache, batch = s.cache(), s.batch()
+    want, bound = s.want(0.1)
+    out = torch.full_like(s.q, 7.0)
+    cache.attend(batch, s.q, scale=0.1, out=out)
+    assert cache.status() == 0
+    ph.assert_within(out, want, bound)
+    for _ in range(20):
+        again = torch.full_like(s.q, 7.0)
+        cache.attend(batch, s.q, scale=0.1, out=again)
+        assert torch.equal(again, out)
+    assert cache.status() == 0
+
+
 # ---- append ---------------------------------------------------------------------------------------
 
 def _written(s, K0, tokens):
