@@ -571,9 +571,9 @@ class PagedCache:
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, scale: float = 1.0, causal: bool = True, out: Optional[torch.Tensor] = None):
         """softmax(scale q [Kprefix; Kown]^T) [Vprefix; Vown] for q [n, H, d], whose keys are in the cache already; a prefix is
-        read for the rows of its group's sequences together. Rows of `out` behind the last sequence are not written (of a new one: undefined). Broken offsets and
-        batches that are too long leave an `out` that was given as it is and make NaN of a new one; status() tells. See
-        subgen_paged_attend."""
+        read for the rows of its group's sequences together. Rows of `out` behind the last sequence are not written (of a new
+        one: undefined). Broken offsets and batches that are too long leave an `out` that was given as it is and make NaN of a
+        new one; status() tells. See subgen_paged_attend."""
         return _calls.attend(self._at, self.device, self._batch(batch), q, scale, causal, out)
 
     def status(self) -> int:
