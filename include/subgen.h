@@ -451,7 +451,9 @@ typedef struct subgen_attend_args {
  * more (bf16: tiles of 128 tokens, units of up to 256 rows, which above 128 rows count twice; fp32: 32 or 64 tokens, units of up to
  * 8, 64 or 128 rows; and one or two more for each unit).
  * Scores, maxima, sums and numerators are fp32; on bf16 caches the softmax weights are rounded to bf16 for the product
- * with V, and a quarter of them are made with a relative error of up to 7.5e-5 before (a fiftieth of that rounding). The result does not depend on how blocks are scheduled.
+ * with V, and a quarter of them are made with a relative error of up to 7.5e-5 before (a fiftieth of that rounding); weights are
+ * up to 2^8 until they are divided by their sum, so values of 2^100 and more may overflow there. The result does not depend on how
+ * blocks are scheduled.
  * out must not overlap q. The workspace is this call's until it has run (two calls that can overlap on the GPU need two). Asynchronous on `stream`, two kernels. */
 size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H);
 int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_attend_args* args, void* stream);
