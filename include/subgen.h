@@ -458,6 +458,85 @@ typedef struct subgen_attend_args {
 size_t subgen_paged_workspace_bytes(const subgen_pages* cache, const subgen_batch* batch, int n, int H);
 int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, const subgen_attend_args* args, void* stream);
 
+/* ---- paged cache in 4 bits ---------------------------------------------------------------------- */
+
+/* Pages as above, at 4.5 bits a value. 16 consecutive coordinates of a head are a group with a scale S: the group's largest
+ * magnitude, rounded up to 4 significant bits (below 2^-14: to a multiple of 2^-17). A coordinate x has the code
+ * n = min(15, floor(8 x / S) + 8), which stands for (n - 7.5) S / 8: |x| is off by S / 16 at most, and every value is exact in
+ * fp32, bf16 and fp16. A group whose largest magnitude is above 61440 or that holds anything that is not finite reads as NaN (in
+ * any row that attends to tokens of its page tile) and sets SUBGEN_ST_RANGE. A group of zeros reads as zeros.
+ * 16 tokens of a page (rows 16 i .. 16 i + 15) have a cell in each head: their keys' codes [16][d / 2], their keys' scales
+ * [16][d / 16], their values' codes and scales: 2304 bytes at d = 128, 1152 at d = 64. A page has page / 16 of them on end in
+ * each head. Eight codes are a 32-bit word, least byte first: codes 0, 2, 4, 6 (least first) in the low half, 1, 3, 5, 7 in the high
+ * half, each half rotated left by 2. A scale is the upper byte of the 15 bits that an fp16 has below its sign; 255 is NaN.
+ * All 8-bit contents are valid, so a pool needs no initial values. */
+typedef struct subgen_pages4 {
+    void* pool;             /* device; cell (page, head, i) at pool + page * page_stride + head * head_stride + i * cell bytes */
+    int64_t page_stride, head_stride;   /* bytes, multiples of 16; at least page / 16 cells (not looked at for one page, one head) */
+    int pages;              /* in the pool */
+    int page;               /* tokens per page: 16, 32, 64, ... 1024 (a power of two) */
+    int Hkv, d;             /* d: 64 or 128 */
+    int* status;            /* sticky SUBGEN_ST_* bits, or NULL */
+} subgen_pages4;
+
+/* As subgen_paged_append, with keys and values rounded into their cells (a key once, from its normed and rotated fp32 value);
+ * args->dtype is that of q, k, v. Other tokens of the same cells are left as they are. Asynchronous on `stream`, one kernel. */
+int subgen_paged4_append(const subgen_pages4* cache, const subgen_batch* batch, const subgen_qk_args* args, void* stream);
+
+/* Tokens by their slots as dense rows: K row i, V row i [Hkv, d] = the values of slot slots[i] = page * cache->page + row (device
+ * int64), exact. What subgen_prefill and the exact caches take, or the read-back of what an append has rounded. A slot below
+ * 0 (padding) gives zeros; one behind the pool gives NaN and sets SUBGEN_ST_PAGE. K->p or V->p may be NULL: then only the
+ * other is read. dtype: of K and V. Asynchronous on `stream`, one kernel. */
+int subgen_paged4_load(const subgen_pages4* cache, const int64_t* slots, int n, const subgen_heads* K, const subgen_heads* V, int dtype, void* stream);
+
+/* As subgen_paged_attend, over the values of the cells; dtype: of q and out. What that says of units of rows, with these numbers:
+ * bf16 queries in units of 8 rows (new tokens x H / Hkv) in calls of at most 8 rows a sequence on average (a group, where there
+ * are any), 16 up to 16 rows, else 256; fp32 queries in units of 8. Key tiles have 128 tokens.
+ * Units of 8 and 16 rows take queries and softmax weights in fp16 (fp32 queries: as two fp16 each, 22 bits), queries scaled by
+ * a power of two first, so that what is below 2^-29 of a row's largest coordinate is rounded more coarsely; weights below 2^-31 of
+ * the largest count for the sum alone. Units of 256 rows take them in bf16 as the bf16 cache does. */
+size_t subgen_paged4_workspace_bytes(const subgen_pages4* cache, const subgen_batch* batch, int n, int H);
+int subgen_paged4_attend(const subgen_pages4* cache, const subgen_batch* batch, const subgen_attend_args* args, int dtype, void* stream);
+
+/* ---- the tables of a step ----------------------------------------------------------------------- */
+
+/* Which pages the sequences of a paged cache have, kept on the device: B rows (requests) with lengths[b] tokens in the pages
+ * table[b][0 .. ceil(lengths[b] / page) - 1], and a stack of free pages, free_pages[0 .. *free_count - 1]. One call makes a step's
+ * tables, from device arrays alone (so it can be captured and replayed):
+ * 1. Rows with ended[b] != 0 give their pages back: pushed in order of rows and places; the row's length becomes 0.
+ * 2. Every row asks for added[b] >= 0 tokens. It is served if the pages that it and all rows before it lack are on the stack, its
+ *    tokens and those asked for before it are at most n, and its pages fit into its row of the table. (A row that lacks no
+ *    page, or asks for no token, is not held up by the pages, or tokens, of others.) Pages are taken from the top of the stack in
+ *    order of rows and places and written to the table behind the row's own. A row that is not served stays as it is: it gets no
+ *    new tokens, and SUBGEN_ST_CAPACITY is set.
+ * 3. cu_q[b] .. cu_q[b + 1] - 1 are the new tokens of row b; slots[i] = table entry * page + row in it of new token i, positions[i] = its
+ *    index in its sequence, plus first[b] where given (the length of a prefix). From cu_q[B] on up to n: -1 and 0.
+ * cu_q, lengths_out and table are what a subgen_batch takes, slots what subgen_paged4_load takes, positions what
+ * subgen_qk_norm_rope takes. lengths_out may be lengths, free_count_out may be free_count; the table and the stack change in
+ * place. No other two arrays may overlap.
+ * A length outside its row, a negative number of tokens (served as 0), a count outside [0, pages], more pages given back than the
+ * stack has room for (they are dropped) or a table entry outside the pool (slot -1) set SUBGEN_ST_PAGE; a row with such a length
+ * gets and gives nothing. Asynchronous on `stream`, one kernel. */
+typedef struct subgen_page_step_args {
+    int B, n;               /* rows: 1 to 1024; new tokens that slots and positions hold */
+    int pages, page;        /* in the pool; tokens per page: 16, 32, 64, ... 1024 (a power of two) */
+    int* table;             /* device [B, table_stride] */
+    int table_stride;       /* pages a row of the table holds; fewer than 2^31 - 1024 tokens */
+    int* free_pages;        /* device [pages] */
+    const int* free_count;  /* device [1] */
+    const int* lengths;     /* device [B] */
+    const int* added;       /* device [B] */
+    const int* ended;       /* device [B], or NULL: none */
+    const int* first;       /* device [B], or NULL */
+    int* free_count_out;    /* device [1] */
+    int* lengths_out;       /* device [B] */
+    int* cu_q;              /* device [B + 1] */
+    int64_t* slots;         /* device [n] */
+    int* positions;         /* device [n] */
+    int* status;            /* sticky SUBGEN_ST_* bits, or NULL */
+} subgen_page_step_args;
+int subgen_page_step(const subgen_page_step_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

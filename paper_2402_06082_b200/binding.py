@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -30,6 +30,7 @@ EXPORTS = [
     "subgen_exact_launch_count", "subgen_exact_attention_noalloc",
     "subgen_exact_kcenter_compress", "subgen_exact_kcenter_counters", "subgen_exact_export_tokens",
     "subgen_rope_words", "subgen_qk_norm_rope", "subgen_paged_append", "subgen_paged_workspace_bytes", "subgen_paged_attend",
+    "subgen_paged4_append", "subgen_paged4_load", "subgen_paged4_workspace_bytes", "subgen_paged4_attend", "subgen_page_step",
 ]
 
 
@@ -68,6 +69,11 @@ class PagesDesc(C.Structure):
                 ("dtype", C.c_int), ("status", C.c_void_p)]
 
 
+class Pages4Desc(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("pages", C.c_int), ("page", C.c_int),
+                ("Hkv", C.c_int), ("d", C.c_int), ("status", C.c_void_p)]
+
+
 class BatchDesc(C.Structure):
     _fields_ = [("B", C.c_int), ("cu_q", C.c_void_p), ("lengths", C.c_void_p), ("table", C.c_void_p),
                 ("table_stride", C.c_int), ("groups", C.c_int), ("cu_group", C.c_void_p), ("prefix_len", C.c_void_p),
@@ -83,6 +89,12 @@ class QkArgs(C.Structure):
 class AttendArgs(C.Structure):
     _fields_ = [("q", Heads), ("out", Heads), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("n", C.c_int),
                 ("H", C.c_int), ("scale", C.c_float), ("causal", C.c_int), ("fresh", C.c_int)]
+
+
+class PageStepArgs(C.Structure):
+    _fields_ = [("B", C.c_int), ("n", C.c_int), ("pages", C.c_int), ("page", C.c_int), ("table", C.c_void_p), ("table_stride", C.c_int)] + [
+        (k, C.c_void_p) for k in ("free_pages", "free_count", "lengths", "added", "ended", "first", "free_count_out", "lengths_out", "cu_q",
+                                  "slots", "positions", "status")]
 
 
 class SubgenError(RuntimeError):
@@ -107,7 +119,8 @@ def _bind_calls():
     if module.built_for != "built for " + built_for():
         raise RuntimeError("_calls.so was %s, this is %s: %s" % (module.built_for, built_for(), advice))
     at = [C.cast(getattr(L, "subgen_" + f), C.c_void_p).value
-          for f in ("qk_norm_rope", "paged_append", "paged_attend", "paged_workspace_bytes", "last_error")]
+          for f in ("qk_norm_rope", "paged_append", "paged_attend", "paged_workspace_bytes", "paged4_append", "paged4_load", "paged4_attend",
+                    "paged4_workspace_bytes", "page_step", "last_error")]
     module.bind(SubgenError, *at)
     _calls = module
 
@@ -171,6 +184,13 @@ def load():
     L.subgen_paged_workspace_bytes.argtypes = [pp, bp, C.c_int, C.c_int]
     L.subgen_paged_workspace_bytes.restype = C.c_size_t
     L.subgen_paged_attend.argtypes = [pp, bp, C.POINTER(AttendArgs), vp]
+    qp = C.POINTER(Pages4Desc)
+    L.subgen_paged4_append.argtypes = [qp, bp, C.POINTER(QkArgs), vp]
+    L.subgen_paged4_load.argtypes = [qp, vp, C.c_int, C.POINTER(Heads), C.POINTER(Heads), C.c_int, vp]
+    L.subgen_paged4_workspace_bytes.argtypes = [qp, bp, C.c_int, C.c_int]
+    L.subgen_paged4_workspace_bytes.restype = C.c_size_t
+    L.subgen_paged4_attend.argtypes = [qp, bp, C.POINTER(AttendArgs), C.c_int, vp]
+    L.subgen_page_step.argtypes = [C.POINTER(PageStepArgs), vp]
     _lib = L
     return L
 
@@ -579,4 +599,109 @@ class PagedCache:
     def status(self) -> int:
         """Waits for the device's work, returns the status bits that calls on this cache have set (0: none)."""
         torch.cuda.synchronize(self.device)
+        return int(self._status.item())
+
+
+class PagedCache4:
+    """A cache in pages that holds keys and values in 4 bits, 4.5 with their scales (see subgen_pages4): pool [pages, Hkv, bytes] uint8
+    with bytes(page, d) on end for each head, owned by the caller (any strides of pages and heads, multiples of 16). Takes fp32 and bf16
+    queries, keys and values, call by call."""
+
+    def __init__(self, pool: torch.Tensor, page: int, d: int):
+        dev = self.device = _cuda(pool, "pool")
+        if pool.dtype is not torch.uint8 or pool.dim() != 3 or pool.stride(2) != 1 or pool.shape[2] != self.bytes(page, d):
+            raise ValueError("pool must be a uint8 tensor [pages, Hkv, %d] with unit stride along the last axis (got %s %s)" %
+                             (self.bytes(page, d), pool.dtype, tuple(pool.shape)))
+        if _calls is None:
+            _bind_calls()
+        self.pool, self.page, self.d = pool, int(page), int(d)
+        self.pages, self.Hkv = pool.shape[:2]
+        self._status = torch.zeros(1, dtype=torch.int32, device=pool.device)
+        if not torch.cuda.is_current_stream_capturing():   # 0 before a call on any stream may set a bit (made once a pool)
+            torch.cuda.current_stream(dev).synchronize()
+        self._desc = Pages4Desc(pool.data_ptr(), pool.stride(0), pool.stride(1), self.pages, self.page, self.Hkv, self.d, self._status.data_ptr())
+        self._at = C.addressof(self._desc)
+
+    @staticmethod
+    def bytes(page: int, d: int) -> int:
+        """What a page takes in one head: codes and scales of its keys and values."""
+        return int(page) * 2 * (int(d) // 2 + int(d) // 16)
+
+    def _batch(self, batch: PagedBatch) -> int:
+        if batch.device != self.device:
+            raise ValueError("the batch is on device %d, the cache on %d" % (batch.device, self.device))
+        return batch._at
+
+    def append(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, *, rope: Optional[Rope] = None,
+               positions: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               q: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
+        """PagedCache.append with keys and values rounded to 4 bits on the way. One kernel; see subgen_paged4_append."""
+        return _calls.append4(self._at, self.device, self._batch(batch), k, v, positions, None if rope is None else rope._desc, wk, eps,
+                              q, wq, q_out)
+
+    def attend(self, batch: PagedBatch, q: torch.Tensor, scale: float = 1.0, causal: bool = True, out: Optional[torch.Tensor] = None):
+        """PagedCache.attend over the values that the cells stand for. See subgen_paged4_attend."""
+        return _calls.attend4(self._at, self.device, self._batch(batch), q, scale, causal, out)
+
+    def load(self, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None):
+        """Keys and values [n, Hkv, d] of the tokens in `slots` (int64, page * tokens per page + row; below 0: zeros), exact: what a
+        SubGen.prefill or an exact cache takes. K, V: outputs, views with unit stride along d. See subgen_paged4_load."""
+        return _calls.load4(self._at, self.device, slots, _dtype_code(dtype), K, V)
+
+    def status(self) -> int:
+        """Waits for the device's work, returns the status bits that calls on this cache have set (0: none)."""
+        torch.cuda.synchronize(self.device)
+        return int(self._status.item())
+
+
+class PageStep(NamedTuple):
+    """What page_step gives: cu_q [B + 1], lengths [B], free_count [1], slots [n] (int64; -1 behind the last token), positions [n]."""
+    cu_q: torch.Tensor
+    lengths: torch.Tensor
+    free_count: torch.Tensor
+    slots: torch.Tensor
+    positions: torch.Tensor
+
+
+def page_step(lengths: torch.Tensor, table: torch.Tensor, free: torch.Tensor, free_count: torch.Tensor, added: torch.Tensor, page: int, n: int,
+              *, ended: Optional[torch.Tensor] = None, first: Optional[torch.Tensor] = None, in_place: bool = True, cu_q: Optional[torch.Tensor] = None,
+              slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> PageStep:
+    """The tables of a step, on the device (see subgen_page_step): rows that ended give their pages back, rows with new tokens get pages.
+
+    lengths, added, ended, first [B], table [B, m], free [pages], free_count, status [1]: int32. The table and the stack of free pages change
+    in place; lengths and free_count too, or (in_place=False) into new tensors. n: rows of the step's tensors, which slots and positions are
+    made for. added may ask for more than there is: rows that are not served get no new tokens.
+    """
+    if _calls is None:
+        _bind_calls()
+    return PageStep._make(_calls.page_step(lengths, table, free, free_count, added, page, n, ended, first, lengths if in_place else None,
+                                           free_count if in_place else None, cu_q, slots, positions, status))
+
+
+class PageTables:
+    """Lengths, page tables and free pages of B requests over a pool, kept on the device, and the batch that a paged cache's calls take.
+
+    step() serves a step's new tokens and moves on; a captured graph may hold it and the calls behind it, since batch, slots and positions
+    stay where they are. A row's request is over when `ended` says so, and the row is free for the next one, in the same step if it has to be.
+    """
+
+    def __init__(self, B: int, pages_per_row: int, pages: int, page: int, n: int, device="cuda"):
+        ints = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=device)  # noqa: E731
+        self.page, self.n = int(page), int(n)
+        self.lengths, self.table, self.cu_q, self._status = ints(B), ints(B, pages_per_row), ints(B + 1), ints(1)
+        self.free = torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device)      # page 0 is on top
+        self.free_count = torch.full((1,), pages, dtype=torch.int32, device=device)
+        self.slots, self.positions = torch.full((self.n,), -1, dtype=torch.int64, device=device), ints(self.n)
+        self.batch = PagedBatch(self.cu_q, self.lengths, self.table)
+        torch.cuda.current_stream(self.lengths.device).synchronize()                       # before a call on any stream
+
+    def step(self, added: torch.Tensor, ended: Optional[torch.Tensor] = None) -> PageStep:
+        """added [B]: the tokens that each request gets now; ended [B]: nonzero where a request is over (both int32). What is given back is
+        what the object holds: the next step changes it."""
+        return page_step(self.lengths, self.table, self.free, self.free_count, added, self.page, self.n, ended=ended, cu_q=self.cu_q,
+                         slots=self.slots, positions=self.positions, status=self._status)
+
+    def status(self) -> int:
+        """Waits for the device's work, returns the status bits that steps have set: ST_CAPACITY where a row was not served (0: none)."""
+        torch.cuda.synchronize(self.lengths.device)
         return int(self._status.item())

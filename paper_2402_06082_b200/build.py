@@ -10,8 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsubgen.so")
 CALLS = os.path.join(HERE, "_calls.so")
 CALLS_SOURCES = ["calls.cpp", os.path.join("..", "..", "include", "subgen.h")]
-SOURCES = ["subgen.cu", "subgen_paged.cu"]
-HEADERS = ["subgen_device.cuh", "subgen_kernels.cuh", "subgen_query_mma.cuh", "subgen_insert_mma.cuh", "subgen_step_fused.cuh", "subgen_prefill.cuh", "subgen_score_tc.cuh", "subgen_prefill_persist.cuh", "subgen_exact_mma.cuh", "subgen_kcenter.cuh", "subgen_paged.cuh", "subgen_paged_simt.cuh", "subgen_paged_tc.cuh", os.path.join("..", "..", "include", "subgen.h")]
+SOURCES = ["subgen.cu", "subgen_paged.cu", "subgen_paged4.cu"]
+HEADERS = ["subgen_device.cuh", "subgen_kernels.cuh", "subgen_query_mma.cuh", "subgen_insert_mma.cuh", "subgen_step_fused.cuh", "subgen_prefill.cuh", "subgen_score_tc.cuh", "subgen_prefill_persist.cuh", "subgen_exact_mma.cuh", "subgen_kcenter.cuh", "subgen_paged.cuh", "subgen_paged_simt.cuh", "subgen_paged_tc.cuh", "subgen_paged_host.cuh", "subgen_codes4.cuh", "subgen_paged4.cuh", "subgen_paged4_few.cuh", os.path.join("..", "..", "include", "subgen.h")]
 
 
 def _stale(out: str, sources) -> bool:

@@ -21,6 +21,11 @@ decltype(&subgen_qk_norm_rope) f_qk;
 decltype(&subgen_paged_append) f_append;
 decltype(&subgen_paged_attend) f_attend;
 decltype(&subgen_paged_workspace_bytes) f_bytes;
+decltype(&subgen_paged4_append) f_append4;
+decltype(&subgen_paged4_load) f_load4;
+decltype(&subgen_paged4_attend) f_attend4;
+decltype(&subgen_paged4_workspace_bytes) f_bytes4;
+decltype(&subgen_page_step) f_step;
 decltype(&subgen_last_error) f_error;
 PyObject* g_error;                                    // SubgenError
 
@@ -183,36 +188,76 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t got) {
 const subgen_pages* cache_at(PyObject* o) { return (const subgen_pages*)PyLong_AsVoidPtr(o); }
 const subgen_batch* batch_at(PyObject* o) { return (const subgen_batch*)PyLong_AsVoidPtr(o); }
 
+const subgen_pages4* cache4_at(PyObject* o) { return (const subgen_pages4*)PyLong_AsVoidPtr(o); }
+
+// call(args) appends; `w`: type and device of the tensors
+template <typename F>
+PyObject* append_with(PyObject* const* a, const Like& w, int Hkv, int64_t d, F call) {
+    const at::Tensor *k = tensor(a[3], "k"), *v = tensor(a[4], "v"), *q = tensor(a[9], "q");
+    if (!k || !v || k->dim() != 3) refuse("k and v must have the axes tokens, heads, d");
+    const int64_t n = k->size(0);
+    const c10::cuda::CUDAGuard on((c10::DeviceIndex)w.device);
+    subgen_qk_args p{};
+    p.k = rows(*k, "k", w, n, Hkv, d);
+    p.v = rows(*v, "v", w, n, Hkv, d);
+    Held qo(q ? a[11] : Py_None);
+    p.H = 1;
+    if (q) {
+        if (q->dim() != 3) refuse("q must have the axes tokens, heads, d " + said(*q));
+        p.H = (int)q->size(1);
+        p.q = rows(*q, "q", w, n, p.H, d);
+        p.fresh = qo.o == Py_None;
+        p.q_out = output(qo.o, "q_out", *q, w, n, p.H, d);
+        qo.mine = true;
+    }
+    p.positions = (const int*)whole(a[5], "positions", at::kInt, w.device, n);
+    p.rope = rope_of(a[6], d, w.device);
+    p.wk = whole(a[7], "wk", w.type, w.device, d);
+    p.wq = whole(a[10], "wq", w.type, w.device, d);
+    p.n = (int)n; p.eps = real(a[8]); p.dtype = dtype_of(w);
+    check(call(&p, c10::cuda::getCurrentCUDAStream(w.device).stream()));
+    return qo.release();
+}
+
+// call(args) attends; bytes(n, H): of the workspace
+template <typename B, typename F>
+PyObject* attend_with(PyObject* const* a, const at::Tensor& q, const Like& w, int64_t d, B bytes, F call) {
+    const int64_t n = q.size(0), H = q.size(1);
+    const c10::cuda::CUDAGuard on((c10::DeviceIndex)w.device);
+    subgen_attend_args p{};
+    p.q = rows(q, "q", w, n, H, d);
+    Held out(a[6]);
+    p.fresh = out.o == Py_None;
+    p.out = output(out.o, "out", q, w, n, H, d);
+    out.mine = true;
+    p.workspace_bytes = bytes((int)n, (int)H);
+    if (!p.workspace_bytes) throw Failed(f_error());
+    const at::Tensor space = at::empty({(int64_t)p.workspace_bytes}, q.options().dtype(at::kByte));   // torch aligns to 512 bytes
+    p.workspace = space.data_ptr();
+    p.n = (int)n; p.H = (int)H; p.scale = real(a[4]); p.causal = truth(a[5], "causal");
+    check(call(&p, c10::cuda::getCurrentCUDAStream(w.device).stream()));
+    return out.release();
+}
+
 // (cache, device, batch, k, v, positions, rope, wk, eps, q, wq, q_out) -> q_out or None; cache, batch: addresses of descriptors
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t got) {
     if (!count(got, 12)) return nullptr;
     return guarded([&]() -> PyObject* {
         const subgen_pages* c = cache_at(a[0]);
         const Like w{c->dtype == SUBGEN_DTYPE_FP32 ? at::kFloat : at::kBFloat16, integer(a[1])};
-        const at::Tensor *k = tensor(a[3], "k"), *v = tensor(a[4], "v"), *q = tensor(a[9], "q");
-        if (!k || !v || k->dim() != 3) refuse("k and v must have the axes tokens, heads, d");
-        const int64_t n = k->size(0), d = c->d;
-        const c10::cuda::CUDAGuard on((c10::DeviceIndex)w.device);
-        subgen_qk_args p{};
-        p.k = rows(*k, "k", w, n, c->Hkv, d);
-        p.v = rows(*v, "v", w, n, c->Hkv, d);
-        Held qo(q ? a[11] : Py_None);
-        p.H = 1;
-        if (q) {
-            if (q->dim() != 3) refuse("q must have the axes tokens, heads, d " + said(*q));
-            p.H = (int)q->size(1);
-            p.q = rows(*q, "q", w, n, p.H, d);
-            p.fresh = qo.o == Py_None;
-            p.q_out = output(qo.o, "q_out", *q, w, n, p.H, d);
-            qo.mine = true;
-        }
-        p.positions = (const int*)whole(a[5], "positions", at::kInt, w.device, n);
-        p.rope = rope_of(a[6], d, w.device);
-        p.wk = whole(a[7], "wk", w.type, w.device, d);
-        p.wq = whole(a[10], "wq", w.type, w.device, d);
-        p.n = (int)n; p.eps = real(a[8]);
-        check(f_append(c, batch_at(a[2]), &p, c10::cuda::getCurrentCUDAStream(w.device).stream()));
-        return qo.release();
+        return append_with(a, w, c->Hkv, c->d, [&](const subgen_qk_args* p, void* st) { return f_append(c, batch_at(a[2]), p, st); });
+    });
+}
+
+// the same for a cache in 4 bits
+PyObject* append4(PyObject*, PyObject* const* a, Py_ssize_t got) {
+    if (!count(got, 12)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const subgen_pages4* c = cache4_at(a[0]);
+        const at::Tensor* k = tensor(a[3], "k");
+        if (!k) refuse("k and v must have the axes tokens, heads, d");
+        const Like w{like(*k, "k").type, integer(a[1])};
+        return append_with(a, w, c->Hkv, c->d, [&](const subgen_qk_args* p, void* st) { return f_append4(c, batch_at(a[2]), p, st); });
     });
 }
 
@@ -225,41 +270,121 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t got) {
         const Like w{c->dtype == SUBGEN_DTYPE_FP32 ? at::kFloat : at::kBFloat16, integer(a[1])};
         const at::Tensor* q = tensor(a[3], "q");
         if (!q || q->dim() != 3) refuse("q must have the axes tokens, heads, d");
-        const int64_t n = q->size(0), H = q->size(1), d = c->d;
-        const c10::cuda::CUDAGuard on((c10::DeviceIndex)w.device);
-        subgen_attend_args p{};
-        p.q = rows(*q, "q", w, n, H, d);
-        Held out(a[6]);
-        p.fresh = out.o == Py_None;
-        p.out = output(out.o, "out", *q, w, n, H, d);
-        out.mine = true;
-        p.workspace_bytes = f_bytes(c, b, (int)n, (int)H);
-        if (!p.workspace_bytes) throw Failed(f_error());
-        const at::Tensor space = at::empty({(int64_t)p.workspace_bytes}, q->options().dtype(at::kByte));   // torch aligns to 512 bytes
-        p.workspace = space.data_ptr();
-        p.n = (int)n; p.H = (int)H; p.scale = real(a[4]); p.causal = truth(a[5], "causal");
-        check(f_attend(c, b, &p, c10::cuda::getCurrentCUDAStream(w.device).stream()));
-        return out.release();
+        return attend_with(a, *q, w, c->d, [&](int n, int H) { return f_bytes(c, b, n, H); },
+                           [&](const subgen_attend_args* p, void* st) { return f_attend(c, b, p, st); });
     });
 }
 
-// (SubgenError, addresses of subgen_qk_norm_rope, _paged_append, _paged_attend, _paged_workspace_bytes, _last_error)
-PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t got) {
+// the same for a cache in 4 bits
+PyObject* attend4(PyObject*, PyObject* const* a, Py_ssize_t got) {
+    if (!count(got, 7)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const subgen_pages4* c = cache4_at(a[0]);
+        const subgen_batch* b = batch_at(a[2]);
+        const at::Tensor* q = tensor(a[3], "q");
+        if (!q) refuse("q must have the axes tokens, heads, d");
+        const Like w{like(*q, "q").type, integer(a[1])};
+        return attend_with(a, *q, w, c->d, [&](int n, int H) { return f_bytes4(c, b, n, H); },
+                           [&](const subgen_attend_args* p, void* st) { return f_attend4(c, b, p, dtype_of(w), st); });
+    });
+}
+
+// (cache, device, slots, dtype code, K or None, V or None) -> (K, V)
+PyObject* load4(PyObject*, PyObject* const* a, Py_ssize_t got) {
     if (!count(got, 6)) return nullptr;
-    void* p[5];
-    for (int i = 0; i < 5; ++i) {
+    return guarded([&]() -> PyObject* {
+        const subgen_pages4* c = cache4_at(a[0]);
+        const Like w{integer(a[3]) == SUBGEN_DTYPE_FP32 ? at::kFloat : at::kBFloat16, integer(a[1])};
+        const at::Tensor* slots = tensor(a[2], "slots");
+        if (!slots || slots->dim() != 1) refuse("slots must be a tensor of one axis");
+        const int64_t n = slots->size(0);
+        if (n > INT_MAX) refuse("slots: too many rows");
+        const c10::cuda::CUDAGuard on((c10::DeviceIndex)w.device);
+        const void* at_slots = whole(a[2], "slots", at::kLong, w.device, n);
+        const at::Tensor none = at::empty({0}, slots->options().dtype(w.type));
+        Held k(a[4]), v(a[5]);
+        const subgen_heads hk = output(k.o, "K", none, w, n, c->Hkv, c->d);
+        k.mine = true;
+        const subgen_heads hv = output(v.o, "V", none, w, n, c->Hkv, c->d);
+        v.mine = true;
+        check(f_load4(c, (const int64_t*)at_slots, (int)n, &hk, &hv, dtype_of(w), c10::cuda::getCurrentCUDAStream(w.device).stream()));
+        PyObject* both = PyTuple_New(2);
+        if (!both) throw std::bad_alloc();
+        PyTuple_SET_ITEM(both, 0, k.release());
+        PyTuple_SET_ITEM(both, 1, v.release());
+        return both;
+    });
+}
+
+// (lengths, table, free, free_count, added, page, n, ended, first, lengths_out, free_count_out, cu_q, slots, positions, status)
+// -> (cu_q, lengths_out, free_count_out, slots, positions); outputs that are None are made
+PyObject* page_step(PyObject*, PyObject* const* a, Py_ssize_t got) {
+    if (!count(got, 15)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor *lengths = tensor(a[0], "lengths"), *table = tensor(a[1], "table"), *free = tensor(a[2], "free");
+        if (!lengths || !table || !free || lengths->dim() != 1 || table->dim() != 2 || free->dim() != 1) refuse("lengths, table and free must be tensors of one, two and one axes");
+        if (!lengths->is_cuda()) refuse("lengths must be a CUDA tensor: this library has no CPU path");
+        const int dev = (int)lengths->get_device();
+        const int64_t B = lengths->size(0), n = integer(a[6]);
+        const c10::cuda::CUDAGuard on((c10::DeviceIndex)dev);
+        if (table->scalar_type() != at::kInt || !table->is_cuda() || table->get_device() != dev || table->size(0) != B || !table->is_contiguous() || table->size(1) > INT_MAX)
+            refuse("table must be a contiguous Int tensor with " + std::to_string(B) + " rows on cuda:" + std::to_string(dev) + " " + said(*table));
+        if (B > INT_MAX || free->size(0) > INT_MAX || n < 0) refuse("lengths, free and n must be in range");
+        subgen_page_step_args p{};
+        p.B = (int)B; p.n = (int)n; p.page = integer(a[5]); p.pages = (int)free->size(0); p.table_stride = (int)table->size(1);
+        p.lengths = (const int*)whole(a[0], "lengths", at::kInt, dev, B);
+        p.table = (int*)table->data_ptr();
+        p.free_pages = (int*)whole(a[2], "free", at::kInt, dev, p.pages);
+        p.free_count = (const int*)whole(a[3], "free_count", at::kInt, dev, 1);
+        p.added = (const int*)whole(a[4], "added", at::kInt, dev, B);
+        p.ended = (const int*)whole(a[7], "ended", at::kInt, dev, B);
+        p.first = (const int*)whole(a[8], "first", at::kInt, dev, B);
+        p.status = (int*)whole(a[14], "status", at::kInt, dev, 1);
+        PyObject* five = PyTuple_New(5);
+        if (!five) throw std::bad_alloc();
+        Held held(five);
+        held.mine = true;
+        auto out = [&](int i, PyObject* o, const char* name, at::ScalarType type, int64_t count) {
+            if (o == Py_None) {
+                o = THPVariable_Wrap(at::empty({count}, lengths->options().dtype(type)));
+                if (!o) throw std::bad_alloc();
+            } else {
+                Py_INCREF(o);
+            }
+            PyTuple_SET_ITEM(five, i, o);
+            return const_cast<void*>(whole(o, name, type, dev, count));
+        };
+        p.cu_q = (int*)out(0, a[11], "cu_q", at::kInt, B + 1);
+        p.lengths_out = (int*)out(1, a[9], "lengths_out", at::kInt, B);
+        p.free_count_out = (int*)out(2, a[10], "free_count_out", at::kInt, 1);
+        p.slots = (int64_t*)out(3, a[12], "slots", at::kLong, n);
+        p.positions = (int*)out(4, a[13], "positions", at::kInt, n);
+        check(f_step(&p, c10::cuda::getCurrentCUDAStream(dev).stream()));
+        return held.release();
+    });
+}
+
+// (SubgenError, addresses of subgen_qk_norm_rope, _paged_append, _paged_attend, _paged_workspace_bytes, the same three of paged4 and
+// _paged4_load behind the first, _page_step, _last_error)
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t got) {
+    if (!count(got, 11)) return nullptr;
+    void* p[10];
+    for (int i = 0; i < 10; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i + 1]);
         if (!p[i]) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address"); return nullptr; }
     }
     Py_INCREF(a[0]);
     Py_XSETREF(g_error, a[0]);
     f_qk = (decltype(f_qk))p[0]; f_append = (decltype(f_append))p[1]; f_attend = (decltype(f_attend))p[2];
-    f_bytes = (decltype(f_bytes))p[3]; f_error = (decltype(f_error))p[4];
+    f_bytes = (decltype(f_bytes))p[3];
+    f_append4 = (decltype(f_append4))p[4]; f_load4 = (decltype(f_load4))p[5]; f_attend4 = (decltype(f_attend4))p[6];
+    f_bytes4 = (decltype(f_bytes4))p[7]; f_step = (decltype(f_step))p[8]; f_error = (decltype(f_error))p[9];
     Py_RETURN_NONE;
 }
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(bind), ENTRY(qk_norm_rope), ENTRY(append), ENTRY(attend), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ENTRY(bind), ENTRY(qk_norm_rope), ENTRY(append), ENTRY(attend),
+                         ENTRY(append4), ENTRY(load4), ENTRY(attend4), ENTRY(page_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

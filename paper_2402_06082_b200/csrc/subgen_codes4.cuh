@@ -1,0 +1,100 @@
+// Heads in 4 bits: 16 coordinates share a scale, a cell of 16 tokens holds codes and scales.
+#pragma once
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+namespace sgk {
+
+// A group is 16 consecutive coordinates of a head. S = the largest magnitude, rounded up to 4 significant bits (below 2^-14 to
+// a multiple of 2^-17); code n = min(15, floor(8 x / S) + 8) stands for (n - 7.5) S / 8, so a coordinate is off by S / 16 at most.
+// Why these: S has 4 significant bits and 2 n - 15 has 4, so every value is exact in bf16 and in fp16 (at most 8 bits, from 2^-21
+// to 57600) and no product that the attention makes of it rounds the cache a second time. S is kept as the upper byte of the
+// 15 bits that an fp16 has below its sign: 4.5 bits a value in all. A group whose largest magnitude is above 61440 or not
+// finite has the byte 255, an fp16 NaN.
+//
+// A cell is what 16 tokens of a page have in one head: K codes [16][D / 2], K scales [16][D / 16], V codes, V scales: 2304 bytes at
+// D = 128, one bulk copy. Eight coordinates are a 32-bit word, the even ones in the low half and the odd ones in the high
+// half, each half rotated left by 2: three of the four pairs (c0 c1, c2 c3, ...) come into the top mantissa bits of two fp16 by
+// one shift and one mask or a mask alone, the fourth by a byte permutation, and one fma takes the offset off and scales.
+template <int D>
+struct Cell4 {
+    static constexpr int kCodes = D / 2, kScales = D / 16;           // bytes a token
+    static constexpr int kHalf = 16 * (kCodes + kScales), kBytes = 2 * kHalf, kScaleAt = 16 * kCodes;
+};
+
+constexpr unsigned kMaxMagnitude4 = 0x47700000u;                     // 61440.f
+
+// ---- rounding: once a token, so exactness comes before speed ----
+
+// The scale byte of a group whose largest magnitude has the bits `top` (without sign; NaN counts as the largest).
+__device__ __forceinline__ unsigned scale4(unsigned top) {
+    if (top > kMaxMagnitude4) return 255u;
+    if (top >= 0x38800000u) return ((top + 0xfffffu) >> 20) - (112u << 3);                  // 2^-14 and more
+    return (unsigned)__float2int_ru(__uint_as_float(top) * 131072.f);                       // 2^17
+}
+// S / 8 of a scale byte; 1 where there is none (the codes do not matter there)
+__device__ __forceinline__ float step4(unsigned byte) {
+    const float s = byte >= 8 ? __uint_as_float((byte + (112u << 3)) << 20) : (float)byte * 7.62939453125e-06f;
+    return byte == 0 || byte == 255 ? 1.f : s * 0.125f;
+}
+// min(15, floor(x / step) + 8) exactly: the quotient by a reciprocal is off by less than 1, and the signs of x - f step and
+// x - (f + 1) step, each one rounding of the exact difference, tell the floor.
+__device__ __forceinline__ unsigned code4(float x, float step, float rcp) {
+    const float big = 12582912.f;                                    // 1.5 * 2^23
+    float f = __fadd_rd(x * rcp, big) - big;
+    if (fmaf(-f, step, x) < 0.f) f -= 1.f;
+    else if (fmaf(-(f + 1.f), step, x) >= 0.f) f += 1.f;
+    return (unsigned)min((int)f + 8, 15) & 15u;
+}
+// eight coordinates
+__device__ __forceinline__ uint32_t word4(const float* x, float step, float rcp) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w |= code4(x[i], step, rcp) << ((i & 1) * 16 + (i >> 1) * 4);
+    return ((w << 2) & 0xfffcfffcu) | ((w >> 14) & 0x00030003u);
+}
+
+// ---- reading ----
+//
+// Values come as fp16 pairs of value / 8: with S / 64 instead of S / 8 the offset 23.5 S / 64 of the fma below stays finite for all
+// scales, and the smallest value (2^-24) is still an fp16.
+
+// S / 64 twice and -23.5 S / 64 twice of byte `k` of `bytes`
+__device__ __forceinline__ void scale_pair4(uint32_t bytes, unsigned k, __half2* s, __half2* o) {
+    const uint32_t u = __byte_perm(bytes, 0, 0x0404u | k << 4 | k << 12) >> 1;
+    const __half2 h = *reinterpret_cast<const __half2*>(&u);
+    *s = __hmul2(h, __half2half2(__ushort_as_half(0x2400)));         // 2^-6
+    *o = __hmul2(h, __half2half2(__ushort_as_half(0xb5e0)));         // -47 / 128
+}
+// S / 64 and -23.5 S / 64 of two tokens, whose bytes are byte 0 of `a` and of `b`
+__device__ __forceinline__ void scale_two4(uint32_t a, uint32_t b, __half2* s, __half2* o) {
+    const uint32_t u = (a << 7) | (b << 23);
+    const __half2 h = *reinterpret_cast<const __half2*>(&u);
+    *s = __hmul2(h, __half2half2(__ushort_as_half(0x2400)));
+    *o = __hmul2(h, __half2half2(__ushort_as_half(0xb5e0)));
+}
+// value / 8 of nibble i of both halves of x: 16 + n by the mantissa's top bits of an fp16 in [16, 32), then (16 + n) s - 23.5 s
+template <int I>
+__device__ __forceinline__ uint32_t pair4(uint32_t x, __half2 s, __half2 o) {
+    const uint32_t y = I == 0 ? x << 4 : I == 1 ? x : I == 2 ? x >> 4 : __byte_perm(x, 0, 0x2301);
+    const uint32_t e = (y & 0x03c003c0u) | 0x4c004c00u;
+    const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&e), s, o);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+
+// The same as bf16 pairs of the value itself, for tiles in shared memory: 16 + n in [16, 32), - 23.5, times S / 8; each exact.
+__device__ __forceinline__ uint32_t scale_bf16_4(unsigned byte) {    // S / 8 twice
+    const float s = byte == 255u ? __uint_as_float(0x7fc00000u) : byte >= 8 ? __uint_as_float((byte + (109u << 3)) << 20) : (float)byte * 9.5367431640625e-07f;
+    return __byte_perm(__float_as_uint(s), 0, 0x3232);
+}
+template <int I>
+__device__ __forceinline__ uint32_t pair4_bf16(uint32_t x, uint32_t s) {
+    const uint32_t y = I == 0 ? x << 1 : I == 1 ? x >> 3 : I == 2 ? x >> 7 : __byte_perm(x, 0, 0x2301) >> 3;
+    const uint32_t e = (y & 0x00780078u) | 0x41804180u;
+    uint32_t v;
+    asm("{\n\t.reg .b32 z;\n\tadd.rn.bf16x2 z, %1, %2;\n\tmul.rn.bf16x2 %0, z, %3;\n\t}\n" : "=r"(v) : "r"(e), "r"(0xc1bcc1bcu), "r"(s));
+    return v;
+}
+
+}  // namespace sgk

@@ -5,11 +5,12 @@
 
 #include <type_traits>
 
+#include "subgen_codes4.cuh"
 #include "subgen_device.cuh"
 
 namespace sgk {
 
-constexpr int kStTimeout = 4, kStPage = 8, kStSize = 16;     // SUBGEN_ST_TIMEOUT, SUBGEN_ST_PAGE, SUBGEN_ST_SIZE
+constexpr int kStCapacity = 1, kStRange = 2, kStTimeout = 4, kStPage = 8, kStSize = 16;     // SUBGEN_ST_*
 
 struct HeadsView {                                    // [tokens, heads, d]: unit stride along d, strides in elements
     void* p;
@@ -112,7 +113,10 @@ __device__ __forceinline__ uint4 pack_row(const float* f) {
     return r;
 }
 
-template <typename T, int D, bool PAGED, int U>
+// PAGED: 0 keys to an output, 1 keys and values into exact pages, 2 into 4-bit cells (P.K: the pool, strides in bytes). There a
+// lane rounds the two pieces that follow each other (16 coordinates in bf16; 8 in fp32, whose scale two lanes share); keys that
+// were rotated in halves lie apart and change lanes through shared memory first.
+template <typename T, int D, int PAGED, int U>
 __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(NormRope a, PagedView P) {
     constexpr int VE = 16 / sizeof(T), LPR = D / VE / 2, RPW = 32 / LPR;
     const int lane = threadIdx.x & 31, l = lane % LPR, sub = lane / LPR;
@@ -121,6 +125,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     if (tok >= a.n) return;
 
     long long slot = -1;                                             // element offset of the token's row in head 0 of its page
+    [[maybe_unused]] int cell_row = 0;                               // PAGED 2: slot is its cell's, in bytes
     long long pos = 0;                                               // prefix and own tokens together may pass 2^31
     if constexpr (PAGED) {
         const int b = warp_find(P.cu_q, P.B + 1, tok);
@@ -138,7 +143,11 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
         const int own = (int)place;
         if (place >= 0 && pg < P.table_stride) {
             const int id = __ldg(P.table + (long long)b * P.table_stride + pg);
-            if (id >= 0 && id < P.pages) slot = (long long)id * P.ps + (long long)(own & ((1 << P.page_shift) - 1)) * P.ts;
+            if (id >= 0 && id < P.pages) {
+                const int row = own & ((1 << P.page_shift) - 1);
+                if constexpr (PAGED == 2) { slot = (long long)id * P.ps + (row >> 4) * Cell4<D>::kBytes; cell_row = row & 15; }
+                else slot = (long long)id * P.ps + (long long)row * P.ts;
+            }
         }
         if (slot < 0 && lane == 0) paged_status(P, kStPage);
         pos = own;
@@ -155,9 +164,9 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     // this lane's two pieces; rotated lanes hold pairs l*VE .. l*VE+VE-1
     const int rl = a.words ? a.rot / (2 * VE) : 0;                   // lanes of a row that rotate
     const bool turn = l < rl;
-    int ca, cb;                                                      // pieces
-    if (!turn || a.interleaved) { ca = 2 * l; cb = 2 * l + 1; }      // also the pieces behind the rotated ones
-    else { ca = l; cb = l + rl; }
+    int ca_, cb_;                                                    // pieces
+    if (!turn || a.interleaved) { ca_ = 2 * l; cb_ = 2 * l + 1; }    // also the pieces behind the rotated ones
+    else { ca_ = l; cb_ = l + rl; }
     float co[VE], si[VE];
     if (turn) {
 #pragma unroll
@@ -172,8 +181,11 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     const int per = (total + a.parts - 1) / a.parts, g0 = part * per, g1 = min(total, g0 + per);
 
     // Groups [lo, hi) of one kind: 0 queries, 1 keys, 2 values.
+    [[maybe_unused]] __shared__ float change[PAGED == 2 ? kNrThreads / 32 : 1][PAGED == 2 ? RPW * D : 1];
     auto run = [&](auto kind_, int lo, int hi, const HeadsView& src, T* dst, long long dst_hs, const T* wt) {
         constexpr int KIND = decltype(kind_)::value;
+        constexpr bool kCodes = PAGED == 2 && KIND > 0;
+        const int ca = kCodes && KIND == 2 ? 2 * l : ca_, cb = kCodes && KIND == 2 ? 2 * l + 1 : cb_;
         const int heads = KIND == 0 ? a.H : a.Hkv;
         const T* x = (const T*)src.p + tok * src.ts;
         uint4 wa = make_uint4(0, 0, 0, 0), wb = wa;
@@ -195,11 +207,11 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int h = (g + u) * RPW + sub;
-                if (KIND < 2 && (wt || turn)) {                      // else the bits go through as they are
-                    float xa[VE], xb[VE];
+                if (kCodes || (KIND < 2 && (wt || turn))) {          // else the bits go through as they are
+                    float x2[2 * VE], *const xa = x2, *const xb = x2 + VE;
                     Elem<T>::unpack(ra[u], xa);
                     Elem<T>::unpack(rb[u], xb);
-                    if (wt) {
+                    if (KIND < 2 && wt) {
                         float ss = 0.f;
 #pragma unroll
                         for (int e = 0; e < VE; ++e) ss = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], ss));
@@ -212,7 +224,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
 #pragma unroll
                         for (int e = 0; e < VE; ++e) { xa[e] *= r * fa[e]; xb[e] *= r * fb[e]; }
                     }
-                    if (turn) {
+                    if (KIND < 2 && turn) {
                         if (a.interleaved) {
 #pragma unroll
                             for (int e = 0; e < VE / 2; ++e) {
@@ -231,6 +243,34 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
                             }
                         }
                     }
+                    if constexpr (kCodes) {
+                        if (KIND == 1 && a.words && !a.interleaved) {            // the same for the whole grid
+                            float* row = change[threadIdx.x >> 5] + sub * D;
+                            __syncwarp();
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) { row[ca * VE + e] = xa[e]; row[cb * VE + e] = xb[e]; }
+                            __syncwarp();
+#pragma unroll
+                            for (int e = 0; e < 2 * VE; ++e) x2[e] = row[2 * l * VE + e];
+                        }
+                        unsigned top = 0;
+#pragma unroll
+                        for (int e = 0; e < 2 * VE; ++e) top = max(top, __float_as_uint(x2[e]) & 0x7fffffffu);
+                        if constexpr (VE == 4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                        const unsigned byte = scale4(top);
+                        const float step = step4(byte), rcp = 1.f / step;
+                        const uint32_t w0 = word4(x2, step, rcp);
+                        [[maybe_unused]] uint32_t w1 = 0;
+                        if constexpr (VE == 8) w1 = word4(x2 + 8, step, rcp);
+                        if (g + u < hi && h < heads) {
+                            unsigned char* at = (unsigned char*)dst + h * dst_hs;
+                            if constexpr (VE == 8) *reinterpret_cast<uint2*>(at + cell_row * (D / 2) + l * 8) = make_uint2(w0, w1);
+                            else *reinterpret_cast<uint32_t*>(at + cell_row * (D / 2) + l * 4) = w0;
+                            if (VE == 8 || !(l & 1)) at[Cell4<D>::kScaleAt + cell_row * (D / 16) + l * VE / 8] = (unsigned char)byte;
+                            if (byte == 255u) paged_status(P, kStRange);
+                        }
+                        continue;
+                    }
                     ra[u] = pack_row<T, VE>(xa);
                     rb[u] = pack_row<T, VE>(xb);
                 }
@@ -243,10 +283,11 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
     };
     if (a.q.p) run(std::integral_constant<int, 0>(), g0, min(g1, gq), a.q, (T*)a.qo.p + tok * a.qo.ts, a.qo.hs, (const T*)a.wq);
     if (a.k.p && (!PAGED || slot >= 0))
-        run(std::integral_constant<int, 1>(), max(g0 - gq, 0), min(g1 - gq, gk), a.k, PAGED ? (T*)P.K + slot : (T*)a.ko.p + tok * a.ko.ts,
+        run(std::integral_constant<int, 1>(), max(g0 - gq, 0), min(g1 - gq, gk), a.k, PAGED == 2 ? (T*)(P.K + slot) : PAGED ? (T*)P.K + slot : (T*)a.ko.p + tok * a.ko.ts,
             PAGED ? P.hs : a.ko.hs, (const T*)a.wk);
     if (PAGED && slot >= 0)
-        run(std::integral_constant<int, 2>(), max(g0 - gq - gk, 0), g1 - gq - gk, a.v, (T*)P.V + slot, P.hs, (const T*)nullptr);
+        run(std::integral_constant<int, 2>(), max(g0 - gq - gk, 0), g1 - gq - gk, a.v, PAGED == 2 ? (T*)(P.K + slot + Cell4<D>::kHalf) : (T*)P.V + slot, P.hs,
+            (const T*)nullptr);
 }
 
 // ---- the division of an attention call's work ---------------------------------------------------

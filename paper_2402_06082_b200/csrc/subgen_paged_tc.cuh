@@ -33,7 +33,7 @@
 
 namespace sgk {
 
-constexpr int kPtThreads = 384, kPtRU = 256, kPtKT = 128, kPtRing = 8, kPtLead = 2;
+constexpr int kPtThreads = 384, kPtThreads4 = 512, kPtRU = 256, kPtKT = 128, kPtRing = 8, kPtLead = 2;
 constexpr int kPtPoly = 2;                            // of 8 pairs of weights, those exponentiated on the fp32 pipe
 constexpr unsigned kPtSpins = 1u << 20;
 
@@ -218,8 +218,89 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // copies arrive later).
 __host__ __device__ __forceinline__ bool paired(const PagedView& P, int d) { return d == 128 && P.page_shift == 4; }
 
-template <int D, bool HAND>
-__global__ void __launch_bounds__(kPtThreads, 1)
+// Warps 12 to 15 of a CODES block: every tile of the block's runs from the pool's cells into the ring, K and V in turn.
+template <int D>
+__device__ __forceinline__ void expand_tiles(PtSmem<D>& sm, const PagedView& P) {
+    typedef Cell4<D> C;
+    constexpr int NS = PtSmem<D>::kSlots, PIECES = D / 32;           // of 32 codes, 16 bytes, two scales
+    const int lane = threadIdx.x & 31, row = threadIdx.x - 384;
+    unsigned ns = 0, nk = 0;
+    struct Raw { uint4 code[PIECES]; uint32_t scale[D / 64]; };      // of this thread's token: K or V
+    bool ok = true;
+    while (ok) {
+        const int slot = ns % kPtRing;
+        if (!(ok = bar_wait(&sm.seg_full[slot], (ns / kPtRing) & 1, &sm.failed))) break;
+        SegRec& r = sm.seg[slot];
+        const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, P_ = r.P, S_ = r.S;
+        const int *ptab = r.ptab, *stab = r.stab;
+        const long long head = r.head * P.hs;
+        if (tile1 < 0) break;
+        // the token's cell in tile t: NULL nothing to bring
+        auto cell_of = [&](int t) -> const char* {
+            const bool pre = t < kp;
+            const int pos = (pre ? t : t - kp) * kPtKT + row;
+            if (t >= tile1 || pos >= (pre ? P_ : S_)) return nullptr;
+            const int id = __ldg((pre ? ptab : stab) + (pos >> P.page_shift));
+            if (id < 0 || id >= P.pages) {
+                *reinterpret_cast<volatile int*>(&r.bad) = 1;
+                paged_status(P, kStPage);
+                return nullptr;
+            }
+            return P.K + id * P.ps + head + ((pos & ((1 << P.page_shift) - 1)) >> 4) * C::kBytes;
+        };
+        auto fetch = [&](const char* cell, int kv, Raw& x) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) x.code[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) x.scale[i] = 0;         // and scales of 0 make zeros
+            if (!cell) return;
+            const char* y = cell + kv * C::kHalf;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) x.code[i] = __ldg(reinterpret_cast<const uint4*>(y + (row & 15) * C::kCodes) + i);
+            const uint32_t* z = reinterpret_cast<const uint32_t*>(y + C::kScaleAt + (row & 15) * C::kScales);
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) x.scale[i] = __ldg(z + i);
+        };
+        auto store = [&](const Raw& x) {
+            const int s = nk % NS;
+            if (nk >= NS && !(ok = bar_wait(&sm.kv_empty[s], (nk / NS - 1) & 1, &sm.failed))) return;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const uint32_t w[4] = {x.code[i].x, x.code[i].y, x.code[i].z, x.code[i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t sc = scale_bf16_4((x.scale[i / 2] >> ((i & 1) * 16 + (j >> 1) * 8)) & 255u);
+                    *reinterpret_cast<uint4*>(sm.KV[s] + (i >> 1) * 16384 + row * 128 + ((((i & 1) * 4 + j) ^ (row & 7)) << 4)) =
+                        make_uint4(pair4_bf16<0>(w[j], sc), pair4_bf16<1>(w[j], sc), pair4_bf16<2>(w[j], sc), pair4_bf16<3>(w[j], sc));
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sm.kv_full[s]);
+            ++nk;
+        };
+        Raw k, v;
+        const char* cell = cell_of(tile0);
+        fetch(cell, 0, k);
+        for (int t = tile0; t < tile1 && ok; ++t) {
+            fetch(cell, 1, v);
+            store(k);
+            if (!ok) break;
+            cell = cell_of(t + 1);
+            fetch(cell, 0, k);
+            store(v);
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sm.seg_empty[slot]);
+        ++ns;
+    }
+}
+
+// CODES: a cache in 4-bit cells (P.K: the pool, strides in bytes). Four more warps take the producer's part for K and V: a thread
+// a token, the next tile's codes asked for while this one's become bf16 values (exact) in the same swizzled layout, zeros behind
+// the sequence's end. mk and mv are not used.
+template <int D, bool HAND, bool CODES = false>
+__global__ void __launch_bounds__(CODES ? kPtThreads4 : kPtThreads, 1)
 paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                        const __grid_constant__ CUtensorMap mv) {
     typedef PtSmem<D> Smem;
@@ -245,8 +326,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             bar_init(&sm.join_bar[i], 4);
             sm.turns[i] = 0;
         }
-        for (int i = 0; i < NS; ++i) { bar_init(&sm.kv_full[i], 1); bar_init(&sm.kv_empty[i], 2); }
-        for (int i = 0; i < kPtRing; ++i) { bar_init(&sm.seg_full[i], 1); bar_init(&sm.seg_empty[i], 11); }
+        for (int i = 0; i < NS; ++i) { bar_init(&sm.kv_full[i], CODES ? 4 : 1); bar_init(&sm.kv_empty[i], 2); }
+        for (int i = 0; i < kPtRing; ++i) { bar_init(&sm.seg_full[i], 1); bar_init(&sm.seg_empty[i], CODES ? 15 : 11); }
         bar_init(&sm.drain, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sm.failed = 0;
@@ -263,11 +344,13 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
     const int x1 = min(plan.total, x + plan.chunk);
     const uint32_t tmem = (uint32_t)uniform((int)sm.tmem);
 
-    // registers: three groups of four warps were launched with 168 a thread; 2 x 208 + 88 = 3 x 168
+    // registers: three groups of four warps were launched with 168 a thread; 2 x 208 + 88 = 3 x 168. CODES: four groups with 128;
+    // 2 x 192 + 2 x 64 = 4 x 128
     if (x >= x1) {
         // nothing of the line is left for this block
     } else if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if constexpr (CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 11) {
             // ---- planner ----
             unsigned ns = 0;
@@ -290,12 +373,14 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 ++ns;
                 if (r.tile1 < 0) break;
             }
+        } else if (CODES && warp >= 12) {
+            expand_tiles<D>(sm, P);
         } else if (warp == 8) {
             // ---- producer ----
             unsigned ns = 0, nq = 0, nk = 0;          // runs, query tiles and ring tiles so far
             const int pb = min(1 << P.page_shift, 128), chunks = 128 / pb;   // tokens one copy brings; copies for a half tile
             const int chunk = lane / HALVES, half = lane % HALVES;           // this lane's copy of a tile
-            const bool pairs = paired(P, D);
+            const bool pairs = !CODES && paired(P, D);
             bool ok = true;
             while (ok) {
                 const int slot = ns % kPtRing;
@@ -312,7 +397,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     const int id = __ldg((pre ? ptab : stab) + (pos >> P.page_shift));
                     return id < 0 || id >= P.pages ? -1 : id;
                 };
-                int id = page_of(tile0);
+                int id = CODES ? -2 : page_of(tile0);
                 const int sub = r.rows > 128 ? 2 : 1;
                 for (int i = 0; i < sub && ok; ++i, ++nq) {
                     const int qs = nq & 1;
@@ -325,7 +410,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                                     tok + (lane & 3) * step, &sm.q_full[qs]);
                     }
                 }
-                for (int t = tile0; t < tile1 && ok; ++t) {
+                for (int t = tile0; !CODES && t < tile1 && ok; ++t) {
                     const int following = page_of(t + 1);        // asked for a tile early
                     const int row = ((t < kp ? t : t - kp) * kPtKT) & ((1 << P.page_shift) - 1);   // pieces of a page start at 0
                     if (__any_sync(0xffffffffu, id == -1) && lane == 0) {
@@ -360,7 +445,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             const int w = warp - 9;
             // V lies as K does, or, in pairs, by pages of 16 tokens and in each of those [half][token][128 B]: in units of 16
             // bytes, how far apart the halves are, and how far on the second 16, 32 and 64 tokens
-            const bool pairs = paired(P, D);
+            const bool pairs = !CODES && paired(P, D);
             const uint32_t apart = pairs ? 128u : 1024u, second = pairs ? 256u : 128u, third = 2 * second, upper = 4 * second;
             struct Cursor { int tile, tile0, tile1, kp, dual, order, rows, P, S, seg, q, kv, jobs, done; };
             bool ok = true;
@@ -436,7 +521,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 if (!(ok = wait(&sm.kv_full[s], (vs / NS) & 1))) break;
                 const bool pre = pv.tile < pv.kp;
                 const int nv = pre ? pv.P - pv.tile * kPtKT : pv.S - (pv.tile - pv.kp) * kPtKT;
-                if (nv < kPtKT) {                      // the sequence ends in this tile: clear what lies behind
+                if (!CODES && nv < kPtKT) {            // the sequence ends in this tile: clear what lies behind
                     for (int p = lane; p < (kPtKT - nv) * 8 * HALVES; p += 32) {
                         const int row = nv + p / (8 * HALVES), c = p % (8 * HALVES);
                         const int at = pairs ? (row >> 4) * 4096 + (c >> 3) * 2048 + (row & 15) * 128 : (c >> 3) * 16384 + row * 128;
@@ -483,7 +568,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.drain, 0); ++j) {}
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        if constexpr (CODES) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ---- softmax ----
         const int w = warp >> 2, quarter = warp & 3;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
