@@ -59,29 +59,40 @@ __device__ __forceinline__ uint32_t word4(const float* x, float step, float rcp)
 // Values come as fp16 pairs of value / 8: with S / 64 instead of S / 8 the offset 23.5 S / 64 of the fma below stays finite for all
 // scales, and the smallest value (2^-24) is still an fp16.
 
-// S / 64 twice and -23.5 S / 64 twice of byte `k` of `bytes`
-__device__ __forceinline__ void scale_pair4(uint32_t bytes, unsigned k, __half2* s, __half2* o) {
-    const uint32_t u = __byte_perm(bytes, 0, 0x0404u | k << 4 | k << 12) >> 1;
+//
+// Logic, shifts and permutations share one pipe, 2 cycles each for a warp; fp16 pairs take the other, 2 cycles as well, where an integer
+// multiply-add takes 1. So shifts to the left are products with a factor that the compiler does not see through (`opaque`).
+__device__ __forceinline__ uint32_t opaque(uint32_t x) {
+    asm volatile("" : "+r"(x));
+    return x;
+}
+// The constants of an expansion, in registers: as immediates mask and exponent would take two logic operations instead of one.
+struct Consts4 {
+    uint32_t f16, f128, f64k, mask, top;
+    __device__ __forceinline__ Consts4() : f16(opaque(16u)), f128(opaque(128u)), f64k(opaque(65536u)), mask(opaque(0x03c003c0u)), top(opaque(0x4c004c00u)) {}
+};
+
+// S / 64 twice and -23.5 S / 64 twice, from S's byte in the low byte of both halves
+__device__ __forceinline__ void scale_pair4(uint32_t bytes, const Consts4& c, __half2* s, __half2* o) {
+    const uint32_t u = bytes * c.f128;
     const __half2 h = *reinterpret_cast<const __half2*>(&u);
     *s = __hmul2(h, __half2half2(__ushort_as_half(0x2400)));         // 2^-6
     *o = __hmul2(h, __half2half2(__ushort_as_half(0xb5e0)));         // -47 / 128
 }
-// S / 64 and -23.5 S / 64 of two tokens, whose bytes are byte 0 of `a` and of `b`
-__device__ __forceinline__ void scale_two4(uint32_t a, uint32_t b, __half2* s, __half2* o) {
-    const uint32_t u = (a << 7) | (b << 23);
-    const __half2 h = *reinterpret_cast<const __half2*>(&u);
-    *s = __hmul2(h, __half2half2(__ushort_as_half(0x2400)));
-    *o = __hmul2(h, __half2half2(__ushort_as_half(0xb5e0)));
+// Values / 8 of 8 codes x (or of 4 codes of each of two tokens): pair i = nibble i of both halves. 16 + n by the mantissa's top
+// bits of an fp16 in [16, 32), then (16 + n) s - 23.5 s, which is exact. Nibbles 0 and 2 lie 4 bits below their place, 2 and 3
+// after the bytes of each half have changed places.
+__device__ __forceinline__ void pairs4(uint32_t x, __half2 s, __half2 o, const Consts4& c, uint32_t* v) {
+    const uint32_t y = __byte_perm(x, 0, 0x2301);
+    const uint32_t n[4] = {x * c.f16, x, y * c.f16, y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t e;
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(e) : "r"(n[i]), "r"(c.mask), "r"(c.top));       // (n & mask) | top
+        const __half2 h = __hfma2(*reinterpret_cast<const __half2*>(&e), s, o);
+        v[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
 }
-// value / 8 of nibble i of both halves of x: 16 + n by the mantissa's top bits of an fp16 in [16, 32), then (16 + n) s - 23.5 s
-template <int I>
-__device__ __forceinline__ uint32_t pair4(uint32_t x, __half2 s, __half2 o) {
-    const uint32_t y = I == 0 ? x << 4 : I == 1 ? x : I == 2 ? x >> 4 : __byte_perm(x, 0, 0x2301);
-    const uint32_t e = (y & 0x03c003c0u) | 0x4c004c00u;
-    const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&e), s, o);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-
 
 // The same as bf16 pairs of the value itself, for tiles in shared memory: 16 + n in [16, 32), - 23.5, times S / 8; each exact.
 __device__ __forceinline__ uint32_t scale_bf16_4(unsigned byte) {    // S / 8 twice

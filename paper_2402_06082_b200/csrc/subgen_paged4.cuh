@@ -53,12 +53,14 @@ __global__ void __launch_bounds__(kLoadThreads) paged4_load_kernel(Load4 a) {
         code[u] = __ldcs(reinterpret_cast<const uint32_t*>(cell + (row & 15) * Cell4<D>::kCodes) + l);
         scale[u] = *reinterpret_cast<const unsigned char*>(cell + Cell4<D>::kScaleAt + (row & 15) * Cell4<D>::kScales + l / 2);
     }
+    const Consts4 consts;
 #pragma unroll
     for (int u = 0; u < kLoadAhead; ++u) {
         if (!to[u]) continue;
         __half2 s, o;
-        scale_pair4(scale[u], 0, &s, &o);
-        const uint32_t x[4] = {pair4<0>(code[u], s, o), pair4<1>(code[u], s, o), pair4<2>(code[u], s, o), pair4<3>(code[u], s, o)};
+        scale_pair4(scale[u] * 0x00010001u, consts, &s, &o);
+        uint32_t x[4];
+        pairs4(code[u], s, o, consts, x);
         float f[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

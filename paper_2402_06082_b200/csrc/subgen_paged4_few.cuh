@@ -16,8 +16,8 @@
 // Weights are 2^(score - reference + 6), the reference a maximum that is replaced (and the sums rescaled) only when a score is
 // 2^8 above it: at most 2^14, and what fp16 loses at the other end is below 2^-31 of the largest.
 //
-// A block: 8 warps, a cell each of every tile of 128 tokens, and one that walks the block's share of the plan and brings tiles by
-// bulk copies (a page's cells lie on end) and the runs' queries. At the end of a run the 8 results are joined through shared
+// A block: 4 warps, two cells each of every tile of 128 tokens (two chains of products at a time), and one that walks the block's share of the plan and brings tiles by
+// bulk copies (a page's cells lie on end) and the runs' queries. At the end of a run the 4 results are joined through shared
 // memory. Every wait is bounded: when one gives up, the block sets SUBGEN_ST_TIMEOUT, waits for its copies (bounded) and returns.
 #pragma once
 #include <type_traits>
@@ -26,21 +26,21 @@
 
 namespace sgk {
 
-constexpr int kP4Warps = 8, kP4Threads = 32 * (kP4Warps + 1), kP4KT = 16 * kP4Warps, kP4Lead = 2, kP4Runs = 3;
+constexpr int kP4Warps = 4, kP4Cells = 2, kP4Threads = 32 * (kP4Warps + 1), kP4KT = 16 * kP4Warps * kP4Cells, kP4Lead = 2, kP4Runs = 2;
 constexpr float kP4Shift = 6.f, kP4Margin = 8.f;
 
 template <typename T, int D, int NT>
 struct P4Smem {
-    static constexpr int RU = 8 * NT, kTile = kP4Warps * Cell4<D>::kBytes, kTiles = 3, kQRow = D * (int)sizeof(T) + 16, kJoin = D + 4;
+    static constexpr int RU = 8 * NT, kTile = kP4Warps * kP4Cells * Cell4<D>::kBytes, kTiles = 3, kQRow = D * (int)sizeof(T) + 16, kJoin = D + 4;
     unsigned char tile[kTiles][kTile];
-    unsigned char q[kP4Runs][RU][kQRow];
+    unsigned char q[RU][kQRow];                       // of one run: free again as soon as it is in registers
     float join[kP4Warps][RU][kJoin];
     float2 stat[kP4Warps][RU];                        // reference * factor, sum
     SegRec run[kP4Runs];
-    unsigned long long full[kTiles], empty[kTiles], run_full[kP4Runs], run_empty[kP4Runs], joined, read;
+    unsigned long long full[kTiles], empty[kTiles], run_full[kP4Runs], run_empty[kP4Runs], q_full, q_empty, joined, read;
     int failed, flag;
 };
-template <int NT> constexpr int kP4Blocks = NT == 1 ? 2 : 1;
+template <int NT> constexpr int kP4Blocks = NT == 1 ? 3 : 2;
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, unsigned bytes, unsigned long long* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -69,7 +69,7 @@ template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_kernel(PagedView P, Attend a) {
     typedef P4Smem<T, D, NT> S;
     typedef Cell4<D> C;
-    constexpr int RU = S::RU, NW = kP4Warps, PIECES = sizeof(T) == 4 ? 2 : 1, KS = D / 16, MT = D / 16;
+    constexpr int RU = S::RU, NW = kP4Warps, U = kP4Cells, PIECES = sizeof(T) == 4 ? 2 : 1, KS = D / 16, MT = D / 16;
     extern __shared__ __align__(128) unsigned char dyn4[];
     S& sm = *reinterpret_cast<S*>(dyn4);
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
@@ -77,6 +77,8 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
     if (tid == 0) {
         for (int i = 0; i < S::kTiles; ++i) { bar_init(&sm.full[i], 1); bar_init(&sm.empty[i], NW); }
         for (int i = 0; i < kP4Runs; ++i) { bar_init(&sm.run_full[i], 1); bar_init(&sm.run_empty[i], NW); }
+        bar_init(&sm.q_full, 1);
+        bar_init(&sm.q_empty, NW);
         bar_init(&sm.joined, NW);
         bar_init(&sm.read, NW);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -107,13 +109,16 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
             const bool last = r.tile1 < 0;
             if (lane == 0) {
                 sm.run[slot] = r;
-                bar_expect(&sm.run_full[slot], last ? 0u : (unsigned)r.rows * (unsigned)(D * sizeof(T)));
+                bar_arrive(&sm.run_full[slot]);
             }
             __syncwarp();
-            if (last) { ++ns; break; }
+            if (last) break;
+            if (ns && !(ok = bar_wait(&sm.q_empty, (ns - 1) & 1, &sm.failed))) break;
+            if (lane == 0) bar_expect(&sm.q_full, (unsigned)r.rows * (unsigned)(D * sizeof(T)));
+            __syncwarp();
             if (lane < r.rows) {                                     // RU <= 32
                 const int gr = r.ru * RU + lane, tok = r.tok0 + (gr >> a.g_shift), head = (r.head << a.g_shift) + (gr & ((1 << a.g_shift) - 1));
-                bulk_load(sm.q[slot][lane], (const T*)a.q.p + tok * a.q.ts + head * a.q.hs, D * sizeof(T), &sm.run_full[slot]);
+                bulk_load(sm.q[lane], (const T*)a.q.p + tok * a.q.ts + head * a.q.hs, D * sizeof(T), &sm.q_full);
             }
             ++ns;
             // this lane's copy of tile t: tokens [pos, pos + 16 * cells) of a page; -1 a page outside the pool, cells 0: nothing
@@ -150,12 +155,13 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
         // copies in flight write shared memory: they have to be done before the block ends
         for (unsigned i = nt > (unsigned)S::kTiles ? nt - S::kTiles : 0; i < nt; ++i)
             for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.full[i % S::kTiles], (i / S::kTiles) & 1); ++j) {}
-        for (unsigned i = ns > (unsigned)kP4Runs ? ns - kP4Runs : 0; i < ns; ++i)
-            for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.run_full[i % kP4Runs], (i / kP4Runs) & 1); ++j) {}
+        if (ns)
+            for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.q_full, (ns - 1) & 1); ++j) {}
     } else {
         // ---- products ----
         const int g = lane >> 2, t = lane & 3;
         const int tk0 = g ^ (g >> 1 & 1), tv0 = 2 * t ^ (t & 1), tv1 = (2 * t + 1) ^ (t & 1);        // tokens of rows g, 2t, 2t + 1
+        const Consts4 consts;
         unsigned ns = 0, nt = 0;
         bool ok = true;
         while (ok) {
@@ -165,6 +171,7 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
             const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, rows = r.rows;
             if (tile1 < 0) break;
             // queries: row g of column block n, coordinates t * D / 4 ...
+            if (!(ok = bar_wait(&sm.q_full, ns & 1, &sm.failed))) break;
             uint32_t q[NT][PIECES][KS * 2];
             float c[NT][2];                                          // exponent per unit of a score, of columns 2t and 2t + 1
             int own[NT][2];
@@ -174,7 +181,7 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
             for (int n = 0; n < NT; ++n) {
                 float f[D / 4];
                 const bool live = n * 8 + g < rows;
-                const T* y = reinterpret_cast<const T*>(sm.q[slot][n * 8 + g]) + t * (D / 4);
+                const T* y = reinterpret_cast<const T*>(sm.q[n * 8 + g]) + t * (D / 4);
                 constexpr int VE = 16 / sizeof(T);
 #pragma unroll
                 for (int i = 0; i < D / 4; i += VE) {
@@ -205,8 +212,10 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
                     own[n][j] = plan.own_limit(e, r.ru * RU + n * 8 + 2 * t + j);
                 }
             }
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sm.q_empty);
             const int own_least = plan.own_limit(e, r.ru * RU);
-            float acc[NT][MT][4], m[NT][2], edge[NT][2], l[NT][2];
+            float acc[NT][MT][4], m[NT][2], ref[NT][2], edge[NT][2], l[NT][2];      // ref: m, or 0 where there is none
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -214,22 +223,25 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[n][i][j] = 0.f;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) { m[n][j] = edge[n][j] = -INFINITY; l[n][j] = 0.f; }
+                for (int j = 0; j < 2; ++j) { m[n][j] = edge[n][j] = -INFINITY; ref[n][j] = l[n][j] = 0.f; }
             }
             for (int ti = tile0; ti < tile1; ++ti, ++nt) {
                 const int s = nt % S::kTiles;
                 const bool pre = ti < kp;
-                const int base = (pre ? ti : ti - kp) * kP4KT + warp * 16, have = (pre ? r.P : r.S) - base;      // tokens of the cell
+                // cells u * NW + warp of the tile; all of them even if the last ones hold no tokens: their scores are masked, their values 0
+                const int base = (pre ? ti : ti - kp) * kP4KT + warp * 16, have = (pre ? r.P : r.S) - base;      // tokens from this warp's first cell on
                 if (!(ok = bar_wait(&sm.full[s], (nt / S::kTiles) & 1, &sm.failed))) break;
                 if (have > 0) {
-                    const unsigned char* cell = sm.tile[s] + warp * C::kBytes;
-                    // scores
-                    float sc[NT][4];
+                    const unsigned char* const tile = sm.tile[s] + warp * C::kBytes;
+                    const bool tail = have < 16 * NW * (U - 1) + 16;
+                    float sc[U][NT][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                    for (int u = 0; u < U; ++u) {
+                        const unsigned char* cell = tile + u * NW * C::kBytes;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) sc[n][j] = 0.f;
-                    {
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) sc[u][n][j] = 0.f;
                         constexpr int W = D / 32;                    // words of 8 codes
                         uint32_t k0[W], k1[W], s0, s1;
                         const unsigned char *y0 = cell + tk0 * C::kCodes + t * (W * 4), *y1 = y0 + 8 * C::kCodes;
@@ -245,49 +257,61 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
                             s0 = *z0;
                             s1 = *z1;
                         }
+                        __half2 f0[W / 2], o0[W / 2], f1[W / 2], o1[W / 2];
+#pragma unroll
+                        for (int w = 0; w < W / 2; ++w) {
+                            scale_pair4(__byte_perm(s0, 0, 0x4040 + w * 0x0101), consts, &f0[w], &o0[w]);
+                            scale_pair4(__byte_perm(s1, 0, 0x4040 + w * 0x0101), consts, &f1[w], &o1[w]);
+                        }
 #pragma unroll
                         for (int w = 0; w < W; ++w) {
-                            __half2 f0, o0, f1, o1;
-                            scale_pair4(s0, w / 2, &f0, &o0);
-                            scale_pair4(s1, w / 2, &f1, &o1);
-                            const uint32_t x0[4] = {pair4<0>(k0[w], f0, o0), pair4<1>(k0[w], f0, o0), pair4<2>(k0[w], f0, o0), pair4<3>(k0[w], f0, o0)};
-                            const uint32_t x1[4] = {pair4<0>(k1[w], f1, o1), pair4<1>(k1[w], f1, o1), pair4<2>(k1[w], f1, o1), pair4<3>(k1[w], f1, o1)};
+                            uint32_t x0[4], x1[4];
+                            pairs4(k0[w], f0[w / 2], o0[w / 2], consts, x0);
+                            pairs4(k1[w], f1[w / 2], o1[w / 2], consts, x1);
 #pragma unroll
                             for (int n = 0; n < NT; ++n)
 #pragma unroll
                                 for (int p = PIECES - 1; p >= 0; --p) {
-                                    mma_f16(sc[n], x0[0], x1[0], x0[1], x1[1], q[n][p][4 * w], q[n][p][4 * w + 1]);
-                                    mma_f16(sc[n], x0[2], x1[2], x0[3], x1[3], q[n][p][4 * w + 2], q[n][p][4 * w + 3]);
+                                    mma_f16(sc[u][n], x0[0], x1[0], x0[1], x1[1], q[n][p][4 * w], q[n][p][4 * w + 1]);
+                                    mma_f16(sc[u][n], x0[2], x1[2], x0[3], x1[3], q[n][p][4 * w + 2], q[n][p][4 * w + 3]);
                                 }
                         }
                     }
                     // limits: what a row does not see is -infinity
-                    if (have < 16 || (!pre && own_least - base < 16)) {
+                    if (tail || (!pre && own_least - base < 16 * NW * (U - 1) + 16)) {
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int u = 0; u < U; ++u)
 #pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                const int lim = pre ? have : own[n][j] - base;
-                                if (tk0 >= lim) sc[n][j] = -INFINITY;
-                                if (tk0 + 8 >= lim) sc[n][j + 2] = -INFINITY;
-                            }
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const int lim = (pre ? have : own[n][j] - base) - 16 * NW * u;
+                                    if (tk0 >= lim) sc[u][n][j] = -INFINITY;
+                                    if (tk0 + 8 >= lim) sc[u][n][j + 2] = -INFINITY;
+                                }
                     }
+                    float high[NT][2];
                     bool rise = false;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) rise |= !(sc[n][j] <= edge[n][j]) || !(sc[n][j + 2] <= edge[n][j]);      // a NaN too
+                        for (int j = 0; j < 2; ++j) {
+                            high[n][j] = m[n][j];
+#pragma unroll
+                            for (int u = 0; u < U; ++u) high[n][j] = max3(high[n][j], sc[u][n][j], sc[u][n][j + 2]);
+                            rise |= !(high[n][j] <= edge[n][j]);     // a NaN too
+                        }
                     if (__any_sync(0xffffffffu, rise)) {
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
-                                float top = max3(m[n][j], sc[n][j], sc[n][j + 2]);
+                                float top = high[n][j];
 #pragma unroll
                                 for (int off = 4; off < 32; off <<= 1) top = max3(top, top, __shfl_xor_sync(0xffffffffu, top, off));
                                 if (!(top <= edge[n][j])) {          // the same for the column's 8 lanes
                                     const float f = ex2_approx((m[n][j] - top) * c[n][j]);       // 0 where there was none yet
-                                    m[n][j] = top;
+                                    m[n][j] = ref[n][j] = top;
                                     edge[n][j] = top + kP4Margin / c[n][j];
                                     l[n][j] *= f;
 #pragma unroll
@@ -295,56 +319,59 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
                                 }
                             }
                     }
-                    uint32_t p[NT][PIECES][2];
+                    uint32_t p[U][NT][PIECES][2];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        float w[4];
+                    for (int u = 0; u < U; ++u)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float ref = m[n][j] == -INFINITY ? 0.f : m[n][j];
-                            w[j] = ex2_approx(fmaf(sc[n][j] - ref, c[n][j], kP4Shift));
-                            w[j + 2] = ex2_approx(fmaf(sc[n][j + 2] - ref, c[n][j], kP4Shift));
-                            l[n][j] += w[j] + w[j + 2];
+                        for (int n = 0; n < NT; ++n) {
+                            float w[4];
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                w[j] = ex2_approx(fmaf(sc[u][n][j] - ref[n][j], c[n][j], kP4Shift));
+                                w[j + 2] = ex2_approx(fmaf(sc[u][n][j + 2] - ref[n][j], c[n][j], kP4Shift));
+                                l[n][j] += w[j] + w[j + 2];
+                            }
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const uint32_t h = halves(w[2 * k], w[2 * k + 1]);
+                                p[u][n][0][k] = transposed(h);
+                                if constexpr (PIECES == 2) p[u][n][1][k] = transposed(rest(w[2 * k], w[2 * k + 1], h));
+                            }
                         }
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint32_t h = halves(w[2 * k], w[2 * k + 1]);
-                            p[n][0][k] = transposed(h);
-                            if constexpr (PIECES == 2) p[n][1][k] = transposed(rest(w[2 * k], w[2 * k + 1], h));
-                        }
-                    }
-                    // values
-                    {
+                    for (int u = 0; u < U; ++u) {
+                        const unsigned char* cell = tile + u * NW * C::kBytes + C::kHalf;
                         constexpr int W = D / 64;                    // words of 8 codes a token
                         uint32_t v[4][W], sv[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int tok = (i & 1 ? tv1 : tv0) + (i >> 1) * 8;
-                            const unsigned char* y = cell + C::kHalf + tok * C::kCodes + g * (W * 4);
+                            const unsigned char* y = cell + tok * C::kCodes + g * (W * 4);
                             if constexpr (W == 2) *reinterpret_cast<uint2*>(v[i]) = *reinterpret_cast<const uint2*>(y);
                             else v[i][0] = *reinterpret_cast<const uint32_t*>(y);
-                            sv[i] = *(cell + C::kHalf + C::kScaleAt + tok * C::kScales + (g * W >> 1));
-                            if (have < 16 && tok >= have) sv[i] = 0; // whatever lies there: 0 times it would be NaN where it is NaN
+                            sv[i] = *(cell + C::kScaleAt + tok * C::kScales + (g * W >> 1));
+                        }
+                        if (tail) {                                  // whatever lies there: 0 times it would be NaN where it is NaN
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if ((i & 1 ? tv1 : tv0) + (i >> 1) * 8 + 16 * NW * u >= have) sv[i] = 0;
                         }
                         __half2 f0, o0, f1, o1;
-                        scale_two4(sv[0], sv[1], &f0, &o0);
-                        scale_two4(sv[2], sv[3], &f1, &o1);
+                        scale_pair4(sv[1] * consts.f64k + sv[0], consts, &f0, &o0);
+                        scale_pair4(sv[3] * consts.f64k + sv[2], consts, &f1, &o1);
 #pragma unroll
                         for (int w = 0; w < W; ++w) {
-                            const uint32_t lo0 = __byte_perm(v[0][w], v[1][w], 0x5410), hi0 = __byte_perm(v[0][w], v[1][w], 0x7632);
-                            const uint32_t lo1 = __byte_perm(v[2][w], v[3][w], 0x5410), hi1 = __byte_perm(v[2][w], v[3][w], 0x7632);
-                            auto product = [&](auto i_) {
-                                constexpr int I = decltype(i_)::value;
-                                const uint32_t a0 = pair4<I>(lo0, f0, o0), a1 = pair4<I>(hi0, f0, o0), a2 = pair4<I>(lo1, f1, o1), a3 = pair4<I>(hi1, f1, o1);
+                            uint32_t a0[4], a1[4], a2[4], a3[4];
+                            pairs4(__byte_perm(v[0][w], v[1][w], 0x5410), f0, o0, consts, a0);
+                            pairs4(__byte_perm(v[0][w], v[1][w], 0x7632), f0, o0, consts, a1);
+                            pairs4(__byte_perm(v[2][w], v[3][w], 0x5410), f1, o1, consts, a2);
+                            pairs4(__byte_perm(v[2][w], v[3][w], 0x7632), f1, o1, consts, a3);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                                    for (int k = PIECES - 1; k >= 0; --k) mma_f16(acc[n][w * 4 + I], a0, a1, a2, a3, p[n][k][0], p[n][k][1]);
-                            };
-                            product(std::integral_constant<int, 0>());
-                            product(std::integral_constant<int, 1>());
-                            product(std::integral_constant<int, 2>());
-                            product(std::integral_constant<int, 3>());
+                                    for (int k = PIECES - 1; k >= 0; --k) mma_f16(acc[n][w * 4 + i], a0[i], a1[i], a2[i], a3[i], p[u][n][k][0], p[u][n][k][1]);
                         }
                     }
                 }
@@ -377,11 +404,11 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
                 for (int i = 0; i < D / 32; ++i) z[i] = 0.f;
 #pragma unroll
                 for (int k = 0; k < NW; ++k) { const float y = sm.stat[k][row].x; M = max3(M, y, y); }
-                const float ref = M == -INFINITY ? 0.f : M;
+                const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
                 for (int k = 0; k < NW; ++k) {
                     const float2 st = sm.stat[k][row];
-                    const float f = ex2_approx(st.x - ref);
+                    const float f = ex2_approx(st.x - base);
                     L = fmaf(st.y, f, L);
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) z[i] = fmaf(sm.join[k][row][lane * (D / 32) + i], f, z[i]);
