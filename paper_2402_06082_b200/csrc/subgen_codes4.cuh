@@ -94,18 +94,27 @@ __device__ __forceinline__ void pairs4(uint32_t x, __half2 s, __half2 o, const C
     }
 }
 
-// The same as bf16 pairs of the value itself, for tiles in shared memory: 16 + n in [16, 32), - 23.5, times S / 8; each exact.
-__device__ __forceinline__ uint32_t scale_bf16_4(unsigned byte) {    // S / 8 twice
-    const float s = byte == 255u ? __uint_as_float(0x7fc00000u) : byte >= 8 ? __uint_as_float((byte + (109u << 3)) << 20) : (float)byte * 9.5367431640625e-07f;
-    return __byte_perm(__float_as_uint(s), 0, 0x3232);
+// The same as bf16 pairs of the value itself: 16 + n in [16, 32), - 23.5, times S / 8; each exact.
+struct Consts4Bf16 {
+    uint32_t f2, mask, top;
+    __device__ __forceinline__ Consts4Bf16() : f2(opaque(2u)), mask(opaque(0x00780078u)), top(opaque(0x41804180u)) {}
+};
+// S / 8 twice, of bytes k and k + 1 of `bytes`
+__device__ __forceinline__ void scale_bf16_4(uint32_t bytes, unsigned k, uint32_t* s) {
+    const uint32_t u = __byte_perm(bytes, 0, 0x0404u + (k << 4) + ((k + 1) << 12)) >> 1;
+    const float2 f = __half22float2(__hmul2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x3000))));      // 2^-3
+    s[0] = __byte_perm(__float_as_uint(f.x), 0, 0x3232);
+    s[1] = __byte_perm(__float_as_uint(f.y), 0, 0x3232);
 }
-template <int I>
-__device__ __forceinline__ uint32_t pair4_bf16(uint32_t x, uint32_t s) {
-    const uint32_t y = I == 0 ? x << 1 : I == 1 ? x >> 3 : I == 2 ? x >> 7 : __byte_perm(x, 0, 0x2301) >> 3;
-    const uint32_t e = (y & 0x00780078u) | 0x41804180u;
-    uint32_t v;
-    asm("{\n\t.reg .b32 z;\n\tadd.rn.bf16x2 z, %1, %2;\n\tmul.rn.bf16x2 %0, z, %3;\n\t}\n" : "=r"(v) : "r"(e), "r"(0xc1bcc1bcu), "r"(s));
-    return v;
+__device__ __forceinline__ void pairs4_bf16(uint32_t x, uint32_t s, const Consts4Bf16& c, uint32_t* v) {
+    const uint32_t y = __byte_perm(x, 0, 0x2301);
+    const uint32_t n[4] = {x * c.f2, x >> 3, y * c.f2, y >> 3};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t e;
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(e) : "r"(n[i]), "r"(c.mask), "r"(c.top));
+        asm("{\n\t.reg .b32 z;\n\tadd.rn.bf16x2 z, %1, %2;\n\tmul.rn.bf16x2 %0, z, %3;\n\t}\n" : "=r"(v[i]) : "r"(e), "r"(0xc1bcc1bcu), "r"(s));
+    }
 }
 
 }  // namespace sgk

@@ -36,6 +36,7 @@ namespace sgk {
 constexpr int kPtThreads = 384, kPtThreads4 = 512, kPtRU = 256, kPtKT = 128, kPtRing = 8, kPtLead = 2;
 constexpr int kPtPoly = 2;                            // of 8 pairs of weights, those exponentiated on the fp32 pipe
 constexpr unsigned kPtSpins = 1u << 20;
+constexpr float kPtShift4 = 6.f;                      // CODES: weights are 2^(score - reference + 6), see there
 
 struct SegRec {
     const int *ptab, *stab;
@@ -218,12 +219,15 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // copies arrive later).
 __host__ __device__ __forceinline__ bool paired(const PagedView& P, int d) { return d == 128 && P.page_shift == 4; }
 
-// Warps 12 to 15 of a CODES block: every tile of the block's runs from the pool's cells into the ring, K and V in turn.
+// Warps 12 to 15 of a CODES block: every tile of the block's runs from the pool's cells into the ring, K and V in turn, a thread a
+// token. While one half is expanded the other's codes are on their way, and the page of the tile after is known.
 template <int D>
 __device__ __forceinline__ void expand_tiles(PtSmem<D>& sm, const PagedView& P) {
     typedef Cell4<D> C;
     constexpr int NS = PtSmem<D>::kSlots, PIECES = D / 32;           // of 32 codes, 16 bytes, two scales
     const int lane = threadIdx.x & 31, row = threadIdx.x - 384;
+    const Consts4 consts;
+    const Consts4Bf16 bconsts;
     unsigned ns = 0, nk = 0;
     struct Raw { uint4 code[PIECES]; uint32_t scale[D / 64]; };      // of this thread's token: K or V
     bool ok = true;
@@ -231,47 +235,55 @@ __device__ __forceinline__ void expand_tiles(PtSmem<D>& sm, const PagedView& P) 
         const int slot = ns % kPtRing;
         if (!(ok = bar_wait(&sm.seg_full[slot], (ns / kPtRing) & 1, &sm.failed))) break;
         SegRec& r = sm.seg[slot];
-        const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, P_ = r.P, S_ = r.S;
-        const int *ptab = r.ptab, *stab = r.stab;
-        const long long head = r.head * P.hs;
+        const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp;
         if (tile1 < 0) break;
-        // the token's cell in tile t: NULL nothing to bring
-        auto cell_of = [&](int t) -> const char* {
+        // the page of this token in tile t: -1 nothing to bring
+        auto page_of = [&](int t) {
             const bool pre = t < kp;
             const int pos = (pre ? t : t - kp) * kPtKT + row;
-            if (t >= tile1 || pos >= (pre ? P_ : S_)) return nullptr;
-            const int id = __ldg((pre ? ptab : stab) + (pos >> P.page_shift));
-            if (id < 0 || id >= P.pages) {
-                *reinterpret_cast<volatile int*>(&r.bad) = 1;
-                paged_status(P, kStPage);
-                return nullptr;
-            }
-            return P.K + id * P.ps + head + ((pos & ((1 << P.page_shift) - 1)) >> 4) * C::kBytes;
+            if (t >= tile1 || pos >= (pre ? r.P : r.S)) return -1;
+            const int id = __ldg((pre ? r.ptab : r.stab) + (pos >> P.page_shift));
+            return id < 0 || id >= P.pages ? -2 : id;
         };
-        auto fetch = [&](const char* cell, int kv, Raw& x) {
+        auto fetch = [&](int t, int id, int kv, Raw& x) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) x.code[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) x.scale[i] = 0;         // and scales of 0 make zeros
-            if (!cell) return;
-            const char* y = cell + kv * C::kHalf;
+            for (int i = 0; i < D / 64; ++i) x.scale[i] = 0;         // scales of 0 make zeros
+            if (id == -2) {
+                *reinterpret_cast<volatile int*>(&r.bad) = 1;
+                paged_status(P, kStPage);
+            }
+            if (id < 0) return;
+            const int pos = (t < kp ? t : t - kp) * kPtKT + row;
+            const char* y = P.K + id * P.ps + r.head * P.hs + ((pos & ((1 << P.page_shift) - 1)) >> 4) * C::kBytes + kv * C::kHalf;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) x.code[i] = __ldg(reinterpret_cast<const uint4*>(y + (row & 15) * C::kCodes) + i);
             const uint32_t* z = reinterpret_cast<const uint32_t*>(y + C::kScaleAt + (row & 15) * C::kScales);
 #pragma unroll
             for (int i = 0; i < D / 64; ++i) x.scale[i] = __ldg(z + i);
         };
-        auto store = [&](const Raw& x) {
+        auto store = [&](const Raw& x, auto kv_) {
+            constexpr int KV = decltype(kv_)::value;
             const int s = nk % NS;
             if (nk >= NS && !(ok = bar_wait(&sm.kv_empty[s], (nk / NS - 1) & 1, &sm.failed))) return;
+            unsigned char* const to = sm.KV[s] + row * 128;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const uint32_t w[4] = {x.code[i].x, x.code[i].y, x.code[i].z, x.code[i].w};
+                uint32_t sb[2];
+                if constexpr (KV == 0) scale_bf16_4(x.scale[i / 2], (i & 1) * 2, sb);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t sc = scale_bf16_4((x.scale[i / 2] >> ((i & 1) * 16 + (j >> 1) * 8)) & 255u);
-                    *reinterpret_cast<uint4*>(sm.KV[s] + (i >> 1) * 16384 + row * 128 + ((((i & 1) * 4 + j) ^ (row & 7)) << 4)) =
-                        make_uint4(pair4_bf16<0>(w[j], sc), pair4_bf16<1>(w[j], sc), pair4_bf16<2>(w[j], sc), pair4_bf16<3>(w[j], sc));
+                for (int h = 0; h < 2; ++h) {
+                    __half2 f, o;
+                    if constexpr (KV == 1) scale_pair4(__byte_perm(x.scale[i / 2], 0, 0x4040 + ((i & 1) * 2 + h) * 0x0101), consts, &f, &o);
+#pragma unroll
+                    for (int j = 2 * h; j < 2 * h + 2; ++j) {
+                        uint32_t y[4];
+                        if constexpr (KV == 0) pairs4_bf16(w[j], sb[h], bconsts, y);
+                        else pairs4(w[j], f, o, consts, y);
+                        *reinterpret_cast<uint4*>(to + (i >> 1) * 16384 + ((((i & 1) * 4 + j) ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                    }
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -280,15 +292,17 @@ __device__ __forceinline__ void expand_tiles(PtSmem<D>& sm, const PagedView& P) 
             ++nk;
         };
         Raw k, v;
-        const char* cell = cell_of(tile0);
-        fetch(cell, 0, k);
-        for (int t = tile0; t < tile1 && ok; ++t) {
-            fetch(cell, 1, v);
-            store(k);
+        int id = page_of(tile0), following = page_of(tile0 + 1);
+        fetch(tile0, id, 0, k);
+        for (int t = tile0; t < tile1; ++t) {
+            fetch(t, id, 1, v);
+            store(k, std::integral_constant<int, 0>());
             if (!ok) break;
-            cell = cell_of(t + 1);
-            fetch(cell, 0, k);
-            store(v);
+            id = following;
+            fetch(t + 1, id, 0, k);
+            following = page_of(t + 2);
+            store(v, std::integral_constant<int, 1>());
+            if (!ok) break;
         }
         __syncwarp();
         if (lane == 0) bar_arrive(&sm.seg_empty[slot]);
@@ -296,17 +310,20 @@ __device__ __forceinline__ void expand_tiles(PtSmem<D>& sm, const PagedView& P) 
     }
 }
 
-// CODES: a cache in 4-bit cells (P.K: the pool, strides in bytes). Four more warps take the producer's part for K and V: a thread
-// a token, the next tile's codes asked for while this one's become bf16 values (exact) in the same swizzled layout, zeros behind
-// the sequence's end. mk and mv are not used.
+// CODES: a cache in 4-bit cells (P.K: the pool, strides in bytes). Four more warps take the producer's part for K and V; they write
+// the same swizzled layouts, zeros behind the sequence's end. K is bf16 as Q is, V and the weights fp16, since an fp16 is expanded
+// by 11 instructions for 8 codes and a bf16 by 17 (each exact), and the weights are rounded 8 times finer. Weights are
+// 2^(score - reference + 6): the largest is at most 2^14 then, and what ends below fp16's 2^-25 is 2^-31 of it. mk and mv are not
+// used.
 template <int D, bool HAND, bool CODES = false>
 __global__ void __launch_bounds__(CODES ? kPtThreads4 : kPtThreads, 1)
 paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                        const __grid_constant__ CUtensorMap mv) {
     typedef PtSmem<D> Smem;
     constexpr int NS = Smem::kSlots, HALVES = D / 64;
+    constexpr float kOut = CODES ? 8.f : 1.f;         // V is value / 8
     constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
-    constexpr uint32_t kIdescO = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((128u >> 4) << 24);
+    constexpr uint32_t kIdescO = (1u << 4) | (CODES ? 0u : (1u << 7) | (1u << 10)) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((128u >> 4) << 24);
     extern __shared__ unsigned char dyn_raw[];
     unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~(uintptr_t)1023);
     Smem& sm = *reinterpret_cast<Smem*>(base);
@@ -600,7 +617,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     // are joined by c as ever.
                     const int e = max((__float_as_int(top * a.c) >> 23) & 255, 127 + 20);
                     cr = a.c * __int_as_float((127 + 127 + 20 - e) << 23);
-                    off = -top * cr;
+                    off = CODES ? fmaf(-top, cr, kPtShift4) : -top * cr;
                 }
                 l *= f;
                 if (begun) {
@@ -628,8 +645,13 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 if (i % 8 < kPtPoly) x = exp2_poly(x);
                 else x = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                 sum[i & 1] = add2(sum[i & 1], x);
-                const __nv_bfloat162 b = __float22bfloat162_rn(x);
-                p[i] = *reinterpret_cast<const uint32_t*>(&b);
+                if constexpr (CODES) {
+                    const __half2 h = __float22half2_rn(x);
+                    p[i] = *reinterpret_cast<const uint32_t*>(&h);
+                } else {
+                    const __nv_bfloat162 b = __float22bfloat162_rn(x);
+                    p[i] = *reinterpret_cast<const uint32_t*>(&b);
+                }
             }
             sum[0] = add2(sum[0], sum[1]);
             l += sum[0].x + sum[0].y;
@@ -791,14 +813,14 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                             }
                             const int gr = r.ru * kPtRU + rr, tok = r.tok0 + (gr >> gs), head = (r.head << gs) + (gr & ((1 << gs) - 1));
                             if (direct) {
-                                const float f = L == 0.f ? rr_none : 1.f / L;
+                                const float f = L == 0.f ? rr_none : kOut / L;
                                 __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
 #pragma unroll
                                 for (int j = 0; j < D / 32; ++j) y[j * 32 + lane] = __float2bfloat16_rn(z[j] * f);
                             } else {
                                 float* y = a.part + (long long)(slot0 + rr) * D;
 #pragma unroll
-                                for (int j = 0; j < D / 32; ++j) y[j * 32 + lane] = z[j];
+                                for (int j = 0; j < D / 32; ++j) y[j * 32 + lane] = z[j] * kOut;
                                 if (lane == 0) a.stat[slot0 + rr] = make_float2(M * a.c, L);
                             }
                         }
@@ -807,7 +829,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     tc_fence_after();
                     if (bad) l = NAN;
                     const int tok = r.tok0 + (urow >> gs), head = (r.head << gs) + (urow & ((1 << gs) - 1));
-                    const float f = direct ? (l == 0.f ? none : 1.f / l) : 1.f;
+                    const float f = direct ? (l == 0.f ? none : kOut / l) : kOut;
                     __nv_bfloat16* y = (__nv_bfloat16*)a.o.p + tok * a.o.ts + head * a.o.hs;
                     if (live && !direct) a.stat[slot0 + row] = make_float2(m * a.c, l);
                     __syncwarp();
@@ -833,7 +855,13 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     } else if (live) {
                         uint4* z = reinterpret_cast<uint4*>(a.part + (long long)(slot0 + row) * D);
 #pragma unroll
-                        for (int j = 0; j < D / 4; ++j) z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                        for (int j = 0; j < D / 4; ++j) {
+                            if constexpr (CODES) {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) o[4 * j + k] = __float_as_uint(__uint_as_float(o[4 * j + k]) * f);
+                            }
+                            z[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                        }
                     }
                 } else {
                     __syncwarp();
