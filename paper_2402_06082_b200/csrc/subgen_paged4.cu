@@ -87,7 +87,7 @@ template <int D>
 int attend4_bf16(const PagedView& P, const Attend& a, cudaStream_t st) {
     typedef __nv_bfloat16 T;
     static bool done[kMaxDevices];
-    constexpr size_t fixed = 1024 + ((sizeof(PtSmem<D>) + 15) & ~(size_t)15);
+    constexpr size_t fixed = 1024 + ((sizeof(PtSmem<D, true>) + 15) & ~(size_t)15);
     int dev, rc = this_device(&dev);
     if (!rc && !done[dev]) {                          // all kinds, whichever this call takes
         rc = opt_in_few<T, D, 1>();

@@ -43,18 +43,19 @@ struct SegRec {
     int slot, tile0, tile1, kp, rows, head, ru, tok0, nq, S, P, direct, bad;   // tile1 < 0: no more
 };
 
-template <int D>
+template <int D, bool CODES = false>
 struct PtSmem {                                       // after a 1024-byte aligned base
-    static constexpr int kTile = 128 * D * 2, kSlots = 131072 / kTile;
+    static constexpr int kTile = 128 * D * 2, kSlots = (CODES ? 98304 : 131072) / kTile, kStage = 8 * Cell4<D>::kBytes, kStages = 2;
     unsigned char Q[2][kTile];                        // [64-column half][row][128 B swizzled]
     unsigned char KV[kSlots][kTile];                  // K, V, K, V, ...; K: [half][token][128 B swizzled], V: also by pages
     float join[2][4][4][D];                           // [group][warp][row][column]: numerators of four rows to be added
     float2 join_stat[2][4][32];                       // maximum in use, sum
-    float hand[4][2][D];                              // [warp][which][column]: a row's numerator from the second group to the first
+    unsigned char stage[CODES ? kStages : 1][CODES ? kStage : 16];      // cells of a tile
+    float hand[CODES ? 1 : 4][2][D];                  // [warp][which][column]: a row's numerator from the second group to the first
     float2 hand_stat[4][2];
     SegRec seg[kPtRing];
     unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots], s_full[2], p_full[2], o_full[2], o_empty[2], join_bar[2], hand_full[4][2], hand_empty[4][2],
-        seg_full[kPtRing], seg_empty[kPtRing], drain;
+        seg_full[kPtRing], seg_empty[kPtRing], drain, stage_full[kStages], stage_empty[kStages];
     unsigned tmem;
     int failed, flag, turns[2];                       // turns: tiles shared by both groups that a group's issuer has done with
 };
@@ -219,64 +220,51 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // copies arrive later).
 __host__ __device__ __forceinline__ bool paired(const PagedView& P, int d) { return d == 128 && P.page_shift == 4; }
 
-// Warps 12 to 15 of a CODES block: every tile of the block's runs from the pool's cells into the ring, K and V in turn, a thread a
-// token. While one half is expanded the other's codes are on their way, and the page of the tile after is known.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, unsigned bytes, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
+// Warps 12 to 15 of a CODES block: every tile of the block's runs from its staged cells into the ring, K and V in turn, a thread a
+// token. A token's pieces of 16 bytes are taken in an order that goes by its row, so that neither the loads (rows of D / 2 bytes)
+// nor the stores (128 bytes, swizzled) of 8 neighbours meet the same banks.
 template <int D>
-__device__ __forceinline__ void expand_tiles(PtSmem<D>& sm, const PagedView& P) {
+__device__ __forceinline__ void expand_tiles(PtSmem<D, true>& sm) {
     typedef Cell4<D> C;
-    constexpr int NS = PtSmem<D>::kSlots, PIECES = D / 32;           // of 32 codes, 16 bytes, two scales
+    typedef PtSmem<D, true> Smem;
+    constexpr int NS = Smem::kSlots, PIECES = D / 32;                // of 32 codes, 16 bytes, two scales
     const int lane = threadIdx.x & 31, row = threadIdx.x - 384;
     const Consts4 consts;
     const Consts4Bf16 bconsts;
-    unsigned ns = 0, nk = 0;
-    struct Raw { uint4 code[PIECES]; uint32_t scale[D / 64]; };      // of this thread's token: K or V
+    const int turn = (row >> (D == 128 ? 1 : 2)) & (PIECES - 1);
+    const unsigned char* const from = sm.stage[0] + (row >> 4) * C::kBytes + (row & 15) * C::kCodes;
+    const unsigned char* const scales = sm.stage[0] + (row >> 4) * C::kBytes + C::kScaleAt + (row & 15) * C::kScales;
+    unsigned ns = 0, nk = 0, nt = 0;
     bool ok = true;
     while (ok) {
         const int slot = ns % kPtRing;
         if (!(ok = bar_wait(&sm.seg_full[slot], (ns / kPtRing) & 1, &sm.failed))) break;
-        SegRec& r = sm.seg[slot];
-        const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp;
+        const SegRec& r = sm.seg[slot];
+        const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, P_ = r.P, S_ = r.S;
         if (tile1 < 0) break;
-        // the page of this token in tile t: -1 nothing to bring
-        auto page_of = [&](int t) {
-            const bool pre = t < kp;
-            const int pos = (pre ? t : t - kp) * kPtKT + row;
-            if (t >= tile1 || pos >= (pre ? r.P : r.S)) return -1;
-            const int id = __ldg((pre ? r.ptab : r.stab) + (pos >> P.page_shift));
-            return id < 0 || id >= P.pages ? -2 : id;
-        };
-        auto fetch = [&](int t, int id, int kv, Raw& x) {
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) x.code[i] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) x.scale[i] = 0;         // scales of 0 make zeros
-            if (id == -2) {
-                *reinterpret_cast<volatile int*>(&r.bad) = 1;
-                paged_status(P, kStPage);
-            }
-            if (id < 0) return;
-            const int pos = (t < kp ? t : t - kp) * kPtKT + row;
-            const char* y = P.K + id * P.ps + r.head * P.hs + ((pos & ((1 << P.page_shift) - 1)) >> 4) * C::kBytes + kv * C::kHalf;
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) x.code[i] = __ldg(reinterpret_cast<const uint4*>(y + (row & 15) * C::kCodes) + i);
-            const uint32_t* z = reinterpret_cast<const uint32_t*>(y + C::kScaleAt + (row & 15) * C::kScales);
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) x.scale[i] = __ldg(z + i);
-        };
-        auto store = [&](const Raw& x, auto kv_) {
+        auto half = [&](auto kv_, int at, bool there) {
             constexpr int KV = decltype(kv_)::value;
             const int s = nk % NS;
             if (nk >= NS && !(ok = bar_wait(&sm.kv_empty[s], (nk / NS - 1) & 1, &sm.failed))) return;
             unsigned char* const to = sm.KV[s] + row * 128;
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                const uint32_t w[4] = {x.code[i].x, x.code[i].y, x.code[i].z, x.code[i].w};
+#pragma unroll 2
+            for (int k = 0; k < PIECES; ++k) {
+                const int i = k ^ turn;
+                const uint4 c = *reinterpret_cast<const uint4*>(from + at + KV * C::kHalf + i * 16);
+                uint32_t sc = *reinterpret_cast<const unsigned short*>(scales + at + KV * C::kHalf + i * 2);
+                if (!there) sc = 0;                                  // behind the sequence's end: zeros
+                const uint32_t w[4] = {c.x, c.y, c.z, c.w};
                 uint32_t sb[2];
-                if constexpr (KV == 0) scale_bf16_4(x.scale[i / 2], (i & 1) * 2, sb);
+                if constexpr (KV == 0) scale_bf16_4(sc, 0, sb);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     __half2 f, o;
-                    if constexpr (KV == 1) scale_pair4(__byte_perm(x.scale[i / 2], 0, 0x4040 + ((i & 1) * 2 + h) * 0x0101), consts, &f, &o);
+                    if constexpr (KV == 1) scale_pair4(__byte_perm(sc, 0, 0x4040 + h * 0x0101), consts, &f, &o);
 #pragma unroll
                     for (int j = 2 * h; j < 2 * h + 2; ++j) {
                         uint32_t y[4];
@@ -291,27 +279,26 @@ __device__ __forceinline__ void expand_tiles(PtSmem<D>& sm, const PagedView& P) 
             if (lane == 0) bar_arrive(&sm.kv_full[s]);
             ++nk;
         };
-        Raw k, v;
-        int id = page_of(tile0), following = page_of(tile0 + 1);
-        fetch(tile0, id, 0, k);
-        for (int t = tile0; t < tile1; ++t) {
-            fetch(t, id, 1, v);
-            store(k, std::integral_constant<int, 0>());
+        for (int t = tile0; t < tile1; ++t, ++nt) {
+            const int st = nt % Smem::kStages, at = st * Smem::kStage;
+            const bool pre = t < kp, there = (pre ? t : t - kp) * kPtKT + row < (pre ? P_ : S_);
+            if (!(ok = bar_wait(&sm.stage_full[st], (nt / Smem::kStages) & 1, &sm.failed))) break;
+            half(std::integral_constant<int, 0>(), at, there);
             if (!ok) break;
-            id = following;
-            fetch(t + 1, id, 0, k);
-            following = page_of(t + 2);
-            store(v, std::integral_constant<int, 1>());
+            half(std::integral_constant<int, 1>(), at, there);
             if (!ok) break;
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sm.stage_empty[st]);
         }
+        if (!ok) break;
         __syncwarp();
         if (lane == 0) bar_arrive(&sm.seg_empty[slot]);
         ++ns;
     }
 }
 
-// CODES: a cache in 4-bit cells (P.K: the pool, strides in bytes). Four more warps take the producer's part for K and V; they write
-// the same swizzled layouts, zeros behind the sequence's end. K is bf16 as Q is, V and the weights fp16, since an fp16 is expanded
+// CODES: a cache in 4-bit cells (P.K: the pool, strides in bytes). The producer brings cells by bulk copies, a tile at a time, and
+// four more warps write K and V of them in the same swizzled layouts, zeros behind the sequence's end. K is bf16 as Q is, V and the weights fp16, since an fp16 is expanded
 // by 11 instructions for 8 codes and a bf16 by 17 (each exact), and the weights are rounded 8 times finer. Weights are
 // 2^(score - reference + 6): the largest is at most 2^14 then, and what ends below fp16's 2^-25 is 2^-31 of it. mk and mv are not
 // used.
@@ -319,7 +306,7 @@ template <int D, bool HAND, bool CODES = false>
 __global__ void __launch_bounds__(CODES ? kPtThreads4 : kPtThreads, 1)
 paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                        const __grid_constant__ CUtensorMap mv) {
-    typedef PtSmem<D> Smem;
+    typedef PtSmem<D, CODES> Smem;
     constexpr int NS = Smem::kSlots, HALVES = D / 64;
     constexpr float kOut = CODES ? 8.f : 1.f;         // V is value / 8
     constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
@@ -346,6 +333,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
         for (int i = 0; i < NS; ++i) { bar_init(&sm.kv_full[i], CODES ? 4 : 1); bar_init(&sm.kv_empty[i], 2); }
         for (int i = 0; i < kPtRing; ++i) { bar_init(&sm.seg_full[i], 1); bar_init(&sm.seg_empty[i], CODES ? 15 : 11); }
         bar_init(&sm.drain, 2);
+        if (CODES)
+            for (int i = 0; i < Smem::kStages; ++i) { bar_init(&sm.stage_full[i], 1); bar_init(&sm.stage_empty[i], 4); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sm.failed = 0;
     }
@@ -362,12 +351,14 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
     const uint32_t tmem = (uint32_t)uniform((int)sm.tmem);
 
     // registers: three groups of four warps were launched with 168 a thread; 2 x 208 + 88 = 3 x 168. CODES: four groups with 128;
-    // 2 x 192 + 2 x 64 = 4 x 128
+    // 2 x 200 + 48 + 64 = 4 x 128
     if (x >= x1) {
         // nothing of the line is left for this block
     } else if (warp >= 8) {
-        if constexpr (CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if constexpr (CODES) {
+            if (warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+            else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        } else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == 11) {
             // ---- planner ----
             unsigned ns = 0;
@@ -391,7 +382,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                 if (r.tile1 < 0) break;
             }
         } else if (CODES && warp >= 12) {
-            expand_tiles<D>(sm, P);
+            if constexpr (CODES) expand_tiles<D>(sm);
         } else if (warp == 8) {
             // ---- producer ----
             unsigned ns = 0, nq = 0, nk = 0;          // runs, query tiles and ring tiles so far
@@ -446,13 +437,48 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                     }
                     id = following;
                 }
+                if constexpr (CODES) {
+                    // this lane's copy of tile t: `cells` of page id; -2 nothing to bring, -1 outside the pool
+                    auto cells_of = [&](int t, int* cells) {
+                        const bool pre = t < kp;
+                        const int pos = (pre ? t : t - kp) * kPtKT + lane * pb, len = pre ? P_ : S_;
+                        if (t >= tile1 || lane >= chunks || pos >= len) return -2;
+                        *cells = min(pb, len - pos + 15) >> 4;
+                        const int page = __ldg((pre ? ptab : stab) + (pos >> P.page_shift));
+                        return page < 0 || page >= P.pages ? -1 : page;
+                    };
+                    int cells = 0, cells2 = 0;
+                    id = cells_of(tile0, &cells);
+                    for (int t = tile0; t < tile1 && ok; ++t, ++nk) {
+                        const int following = cells_of(t + 1, &cells2);      // asked for a tile early
+                        const int row = ((t < kp ? t : t - kp) * kPtKT) & ((1 << P.page_shift) - 1), s = nk % Smem::kStages;
+                        if (nk >= Smem::kStages && !(ok = bar_wait(&sm.stage_empty[s], (nk / Smem::kStages - 1) & 1, &sm.failed))) break;
+                        if (__any_sync(0xffffffffu, id == -1) && lane == 0) {
+                            *reinterpret_cast<volatile int*>(&r.bad) = 1;
+                            paged_status(P, kStPage);
+                        }
+                        const unsigned bytes = id >= 0 ? cells * Cell4<D>::kBytes : 0u, all = __reduce_add_sync(0xffffffffu, bytes);
+                        if (lane == 0) bar_expect(&sm.stage_full[s], all);
+                        __syncwarp();
+                        if (bytes)
+                            bulk_load(sm.stage[s] + (lane * pb >> 4) * Cell4<D>::kBytes, P.K + id * P.ps + head * P.hs + (row >> 4) * Cell4<D>::kBytes, bytes,
+                                      &sm.stage_full[s]);
+                        id = following;
+                        cells = cells2;
+                    }
+                }
                 __syncwarp();
                 if (lane == 0) bar_arrive(&sm.seg_empty[slot]);
                 ++ns;
             }
             // copies in flight write shared memory: they have to be done before the block ends
-            for (unsigned i = nk > (unsigned)NS ? nk - NS : 0; i < nk; ++i)
-                for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.kv_full[i % NS], (i / NS) & 1); ++j) {}
+            if constexpr (CODES) {
+                for (unsigned i = nk > (unsigned)Smem::kStages ? nk - Smem::kStages : 0; i < nk; ++i)
+                    for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.stage_full[i % Smem::kStages], (i / Smem::kStages) & 1); ++j) {}
+            } else {
+                for (unsigned i = nk > (unsigned)NS ? nk - NS : 0; i < nk; ++i)
+                    for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.kv_full[i % NS], (i / NS) & 1); ++j) {}
+            }
             for (unsigned i = nq > 2 ? nq - 2 : 0; i < nq; ++i)
                 for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.q_full[i & 1], (i / 2) & 1); ++j) {}
         } else {
@@ -585,7 +611,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             for (unsigned j = 0; j < kPtSpins && !bar_try(&sm.drain, 0); ++j) {}
         }
     } else {
-        if constexpr (CODES) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        if constexpr (CODES) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ---- softmax ----
         const int w = warp >> 2, quarter = warp & 3;
