@@ -252,8 +252,8 @@ __device__ __forceinline__ void expand_tiles(PtSmem<D, true>& sm) {
             const int s = nk % NS;
             if (nk >= NS && !(ok = bar_wait(&sm.kv_empty[s], (nk / NS - 1) & 1, &sm.failed))) return;
             unsigned char* const to = sm.KV[s] + row * 128;
-#pragma unroll 2
-            for (int k = 0; k < PIECES; ++k) {
+#pragma unroll 1                                                     // code that stays in the caches beside the softmax's: unrolled by
+            for (int k = 0; k < PIECES; ++k) {                       // 4, prompt chunks take 1158 us, by 2 980, like this 957
                 const int i = k ^ turn;
                 const uint4 c = *reinterpret_cast<const uint4*>(from + at + KV * C::kHalf + i * 16);
                 uint32_t sc = *reinterpret_cast<const unsigned short*>(scales + at + KV * C::kHalf + i * 2);
@@ -308,6 +308,7 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
                        const __grid_constant__ CUtensorMap mv) {
     typedef PtSmem<D, CODES> Smem;
     constexpr int NS = Smem::kSlots, HALVES = D / 64;
+    constexpr int POLY = CODES ? 0 : kPtPoly;         // CODES: code is short of room (957 -> 940 us)
     constexpr float kOut = CODES ? 8.f : 1.f;         // V is value / 8
     constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
     constexpr uint32_t kIdescO = (1u << 4) | (CODES ? 0u : (1u << 7) | (1u << 10)) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((128u >> 4) << 24);
@@ -667,8 +668,8 @@ paged_attend_tc_kernel(PagedView P, Attend a, const __grid_constant__ CUtensorMa
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
-                float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), cc, i % 8 < kPtPoly ? oh : oo);
-                if (i % 8 < kPtPoly) x = exp2_poly(x);
+                float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), cc, i % 8 < POLY ? oh : oo);
+                if (i % 8 < POLY) x = exp2_poly(x);
                 else x = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                 sum[i & 1] = add2(sum[i & 1], x);
                 if constexpr (CODES) {
