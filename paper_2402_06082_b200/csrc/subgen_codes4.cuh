@@ -24,7 +24,7 @@ struct Cell4 {
 
 constexpr unsigned kMaxMagnitude4 = 0x47700000u;                     // 61440.f
 
-// ---- rounding: once a token, so exactness comes before speed ----
+// ---- rounding ----
 
 // The scale byte of a group whose largest magnitude has the bits `top` (without sign; NaN counts as the largest).
 __device__ __forceinline__ unsigned scale4(unsigned top) {
@@ -32,25 +32,33 @@ __device__ __forceinline__ unsigned scale4(unsigned top) {
     if (top >= 0x38800000u) return ((top + 0xfffffu) >> 20) - (112u << 3);                  // 2^-14 and more
     return (unsigned)__float2int_ru(__uint_as_float(top) * 131072.f);                       // 2^17
 }
-// S / 8 of a scale byte; 1 where there is none (the codes do not matter there)
-__device__ __forceinline__ float step4(unsigned byte) {
-    const float s = byte >= 8 ? __uint_as_float((byte + (112u << 3)) << 20) : (float)byte * 7.62939453125e-06f;
-    return byte == 0 || byte == 255 ? 1.f : s * 0.125f;
-}
-// min(15, floor(x / step) + 8) exactly: the quotient by a reciprocal is off by less than 1, and the signs of x - f step and
-// x - (f + 1) step, each one rounding of the exact difference, tell the floor.
-__device__ __forceinline__ unsigned code4(float x, float step, float rcp) {
-    const float big = 12582912.f;                                    // 1.5 * 2^23
-    float f = __fadd_rd(x * rcp, big) - big;
-    if (fmaf(-f, step, x) < 0.f) f -= 1.f;
-    else if (fmaf(-(f + 1.f), step, x) >= 0.f) f += 1.f;
-    return (unsigned)min((int)f + 8, 15) & 15u;
-}
+// How a group is rounded: S / 8 = s4 2^-k with a whole s4 below 16, and floor(8 x / S) = floor(floor(2^k x) / s4), where 2^k x is exact, its
+// floor comes with an fma that rounds down (to whole numbers, at 1.5 * 2^23) and a whole u = floor + 8 s4 <= 16 s4 is divided by s4
+// by a product with m, up to 2 more than 2^16 / s4, and a shift: exact, since u * 2 / 2^16 < 1 / s4. The fma's result is taken as a
+// whole number as it lies; `add` takes off what its exponent adds to the product.
+struct Rounder4 {
+    float factor, bias;
+    uint32_t m, add;
+    __device__ __forceinline__ explicit Rounder4(unsigned byte) {
+        const unsigned e = byte >> 3, s4 = e ? 8 + (byte & 7) : byte ? byte : 1;             // a group of zeros: any s4
+        factor = __uint_as_float((148u - (e ? e : 1)) << 23);
+        bias = 12582912.f + 8.f * (float)s4;
+        m = __float2uint_rz(__fdividef(65536.f, (float)s4)) + 1;
+        add = 0u - 0x4b400000u * m;
+    }
+    __device__ __forceinline__ uint32_t operator()(float x) const {   // the code, 16 bits up
+        return min(__float_as_uint(__fmaf_rd(x, factor, bias)) * m + add, 0xfffffu);
+    }
+};
 // eight coordinates
-__device__ __forceinline__ uint32_t word4(const float* x, float step, float rcp) {
+__device__ __forceinline__ uint32_t word4(const float* x, const Rounder4& r) {
     uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w |= code4(x[i], step, rcp) << ((i & 1) * 16 + (i >> 1) * 4);
+    for (int i = 0; i < 8; ++i) {
+        const int to = (i & 1) * 16 + (i >> 1) * 4;                  // its nibble before the rotation
+        const uint32_t c = r(x[i]);
+        w |= (to >= 16 ? c << (to - 16) : c >> (16 - to)) & (15u << to);
+    }
     return ((w << 2) & 0xfffcfffcu) | ((w >> 14) & 0x00030003u);
 }
 

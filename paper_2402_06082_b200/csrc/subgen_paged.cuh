@@ -193,10 +193,11 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
             wa = __ldg(reinterpret_cast<const uint4*>(wt + ca * VE));
             wb = __ldg(reinterpret_cast<const uint4*>(wt + cb * VE));
         }
-        for (int g = lo; g < hi; g += U) {
-            uint4 ra[U], rb[U];
+        constexpr int UU = kCodes && U > 2 ? 2 : U;                  // (less code)
+        for (int g = lo; g < hi; g += UU) {
+            uint4 ra[UU], rb[UU];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {                            // all loads first
+            for (int u = 0; u < UU; ++u) {                           // all loads first
                 const int h = (g + u) * RPW + sub;
                 ra[u] = rb[u] = make_uint4(0, 0, 0, 0);
                 if (g + u < hi && h < heads) {
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
                 }
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < UU; ++u) {
                 const int h = (g + u) * RPW + sub;
                 if (kCodes || (KIND < 2 && (wt || turn))) {          // else the bits go through as they are
                     float x2[2 * VE], *const xa = x2, *const xb = x2 + VE;
@@ -258,10 +259,10 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
                         for (int e = 0; e < 2 * VE; ++e) top = max(top, __float_as_uint(x2[e]) & 0x7fffffffu);
                         if constexpr (VE == 4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         const unsigned byte = scale4(top);
-                        const float step = step4(byte), rcp = 1.f / step;
-                        const uint32_t w0 = word4(x2, step, rcp);
+                        const Rounder4 round(byte);
+                        const uint32_t w0 = word4(x2, round);
                         [[maybe_unused]] uint32_t w1 = 0;
-                        if constexpr (VE == 8) w1 = word4(x2 + 8, step, rcp);
+                        if constexpr (VE == 8) w1 = word4(x2 + 8, round);
                         if (g + u < hi && h < heads) {
                             unsigned char* at = (unsigned char*)dst + h * dst_hs;
                             if constexpr (VE == 8) *reinterpret_cast<uint2*>(at + cell_row * (D / 2) + l * 8) = make_uint2(w0, w1);

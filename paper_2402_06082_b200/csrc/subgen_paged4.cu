@@ -48,10 +48,14 @@ int check_cache4(const char* fn, const subgen_pages4* c, const subgen_batch* b, 
 }
 
 template <typename T, int D>
-int launch_load(const Load4& a, cudaStream_t st) {
-    constexpr int rows = kLoadThreads / (D / 8) * kLoadAhead;
-    const long long blocks = ((long long)a.n * a.Hkv * 2 + rows - 1) / rows;
-    paged4_load_kernel<T, D><<<(unsigned)blocks, kLoadThreads, 0, st>>>(a);
+int launch_load(Load4 a, cudaStream_t st) {
+    constexpr int RPB = kLoadThreads / (D / 8);
+    const int rows = 2 * a.Hkv;
+    a.at_once = rows < RPB ? RPB / rows : 1;
+    const long long groups = (rows + RPB - 1) / RPB, tokens = ((long long)a.n + a.at_once - 1) / a.at_once;
+    if (groups > 65535) return fail(SUBGEN_EINVAL, "subgen_paged4_load: too many heads");
+    const long long once = (kSMs * kLoadBlocks + groups - 1) / groups, blocks = tokens < once ? tokens : once;       // all blocks at once
+    paged4_load_kernel<T, D><<<dim3((unsigned)blocks, (unsigned)groups), kLoadThreads, 0, st>>>(a);
     CUDA_TRY(cudaGetLastError());
     return SUBGEN_OK;
 }
