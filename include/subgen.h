@@ -516,12 +516,12 @@ int subgen_paged4_attend(const subgen_pages4* cache, const subgen_batch* batch, 
  * place. No other two arrays may overlap.
  * A length outside its row, a negative number of tokens (served as 0), a count outside [0, pages], more pages given back than the
  * stack has room for (they are dropped) or a table entry outside the pool (slot -1) set SUBGEN_ST_PAGE; a row with such a length
- * gets and gives nothing. Asynchronous on `stream`, one kernel. */
+ * gets and gives nothing. Asynchronous on `stream`, one kernel, or two where n is large. */
 typedef struct subgen_page_step_args {
     int B, n;               /* rows: 1 to 1024; new tokens that slots and positions hold */
     int pages, page;        /* in the pool; tokens per page: 16, 32, 64, ... 1024 (a power of two) */
     int* table;             /* device [B, table_stride] */
-    int table_stride;       /* pages a row of the table holds; fewer than 2^31 - 1024 tokens */
+    int table_stride;       /* pages a row of the table holds; fewer than 2^31 - 1024 tokens, in all rows fewer than 2^31 - 1 pages */
     int* free_pages;        /* device [pages] */
     const int* free_count;  /* device [1] */
     const int* lengths;     /* device [B] */

@@ -202,6 +202,7 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
         return fail(SUBGEN_EINVAL, "%s: only ended, first and status may be NULL", fn);
     if (x->table_stride <= 0 || (long long)x->table_stride * x->page > 0x7fffffffLL - 1024)
         return fail(SUBGEN_EINVAL, "%s: table_stride must be positive, a row of fewer than 2^31 - 1024 tokens", fn);
+    if ((long long)x->B * x->table_stride >= 0x7fffffffLL) return fail(SUBGEN_EINVAL, "%s: a table must hold fewer than 2^31 - 1 pages", fn);
     if ((uintptr_t)x->slots & 7) return fail(SUBGEN_EINVAL, "%s: slots must be 8-byte aligned", fn);
     PageStep a;
     a.B = x->B; a.n = x->n; a.pages = x->pages; a.page_shift = shift_of(x->page); a.stride = x->table_stride;
@@ -210,6 +211,7 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     a.free_count_out = x->free_count_out; a.lengths_out = x->lengths_out; a.cu_q = x->cu_q; a.positions = x->positions;
     a.slots = (long long*)x->slots;
     a.status = x->status;
+    a.split = x->n > 4 * kStepThreads;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     const int blocks = x->n > kStepThreads || x->B > 128 ? kStepCluster : 1;     // something to share out
@@ -223,6 +225,13 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     cfg.attrs = at;
     cfg.numAttrs = 1;
     CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel, a));
+    if (!a.split) return SUBGEN_OK;
+    const int parts = (x->n + kSlotThreads / 32 * kStepAhead * 32 - 1) / (kSlotThreads / 32 * kStepAhead * 32);        // a turn each
+    cfg.gridDim = dim3((unsigned)(parts < 4 * kSMs ? parts : 4 * kSMs));
+    cfg.blockDim = dim3(kSlotThreads);
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, page_slots_kernel, a));
     return SUBGEN_OK;
 }
 

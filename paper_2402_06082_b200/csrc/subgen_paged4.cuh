@@ -72,10 +72,10 @@ __global__ void __launch_bounds__(kLoadThreads, kLoadBlocks) paged4_load_kernel(
             scale_bf16_4(scale[b][u], 0, s);
             pairs4_bf16(code[b][u], s[0], consts, x);
             if constexpr (sizeof(T) == 4) {
-                *reinterpret_cast<uint4*>(z) = make_uint4(x[0] << 16, x[0] & 0xffff0000u, x[1] << 16, x[1] & 0xffff0000u);
-                *reinterpret_cast<uint4*>(z + 4) = make_uint4(x[2] << 16, x[2] & 0xffff0000u, x[3] << 16, x[3] & 0xffff0000u);
+                __stcs(reinterpret_cast<uint4*>(z), make_uint4(x[0] << 16, x[0] & 0xffff0000u, x[1] << 16, x[1] & 0xffff0000u));
+                __stcs(reinterpret_cast<uint4*>(z + 4), make_uint4(x[2] << 16, x[2] & 0xffff0000u, x[3] << 16, x[3] & 0xffff0000u));
             } else {
-                *reinterpret_cast<uint4*>(z) = make_uint4(x[0], x[1], x[2], x[3]);
+                __stcs(reinterpret_cast<uint4*>(z), make_uint4(x[0], x[1], x[2], x[3]));
             }
             tok += step;
             z += z_step;
@@ -105,7 +105,8 @@ __global__ void __launch_bounds__(kLoadThreads, kLoadBlocks) paged4_load_kernel(
 // Latency bound (some KB of lengths, sums over 1024 rows, one dependent read of the stack): one cluster. Each of its blocks
 // makes the sums over all rows for itself (a thread a row), and they share out pages and tokens; between giving back and
 // taking lies the one barrier of the cluster, and whatever a block changes in place it changes behind it. One block where
-// there is little to share.
+// there is little to share. Slots and positions of many tokens are left to a second kernel, since a cluster has 8 SMs only: with
+// 118000 new tokens in 1024 rows it took 29 us for both, bound by their instructions.
 struct PageStep {
     int B, n, pages, page_shift, stride;
     int *table, *free;
@@ -113,44 +114,83 @@ struct PageStep {
     int *free_count_out, *lengths_out, *cu_q, *positions;
     long long* slots;
     int* status;
+    int split;                                        // slots and positions are the second kernel's
 };
 
-constexpr int kStepThreads = 1024, kStepCluster = 8;
+constexpr int kStepThreads = 1024, kStepCluster = 8, kStepAhead = 4, kSlotThreads = 256;
 
-// exclusive sums of x over the block; *all: the total
-__device__ __forceinline__ long long block_scan(long long x, long long* sums, long long* all) {
+// Inclusive sums of K numbers over the block, and their totals. Sums stay at kStepMost once they reach it.
+constexpr unsigned kStepMost = 0x7fffffffu;
+template <int K>
+__device__ __forceinline__ void block_scan(unsigned* x, unsigned (*sums)[32], unsigned* all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long s = x;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, s, off);
-        if (lane >= off) s += y;
-    }
+    for (int off = 1; off < 32; off <<= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const unsigned y = __shfl_up_sync(0xffffffffu, x[k], off);
+            if (lane >= off) x[k] = min(x[k] + y, kStepMost);
+        }
     __syncthreads();                                                 // what was there has been read
-    if (lane == 31) sums[warp] = s;
-    __syncthreads();
-    long long w = sums[lane];                                        // 32 warps
+    if (lane == 31)
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, w, off);
-        if (lane >= off) w += y;
+        for (int k = 0; k < K; ++k) sums[k][warp] = x[k];
+    __syncthreads();
+    unsigned w[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) w[k] = sums[k][lane];                // 32 warps
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const unsigned y = __shfl_up_sync(0xffffffffu, w[k], off);
+            if (lane >= off) w[k] = min(w[k] + y, kStepMost);
+        }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const unsigned before = __shfl_sync(0xffffffffu, w[k], warp ? warp - 1 : 0);
+        all[k] = __shfl_sync(0xffffffffu, w[k], 31);
+        if (warp) x[k] = min(x[k] + before, kStepMost);
     }
-    *all = __shfl_sync(0xffffffffu, w, 31);
-    const long long before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
-    return s - x + (warp ? before : 0);
 }
-// the last row whose sum is at most i
-__device__ __forceinline__ int row_of(const int* scan, int B, int i) {
-    int lo = 0, hi = B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (scan[mid] <= i) lo = mid; else hi = mid - 1;
+// The last row whose sum is at most i, for the warp's 32 numbers that follow each other; r: such a row of an earlier number, the
+// same in all lanes. Long rows need one look; else each lane searches.
+__device__ __forceinline__ int row_from(const int* scan, int B, int i, int r) {
+    if (__all_sync(0xffffffffu, r + 1 >= B || scan[r + 1] > i)) return r;
+    int hi = B - 1;
+    while (r < hi) {
+        const int mid = (r + hi + 1) >> 1;
+        if (scan[mid] <= i) r = mid; else hi = mid - 1;
     }
-    return lo;
+    return r;
+}
+// f(k, i, row) for k < N and the warp's share of the numbers below `count`, N times 32 of them at a time, then g(k, i) for the same:
+// what f asks for is on its way for all of them before g uses it. i may be `count` or more.
+template <int N, typename F, typename G>
+__device__ __forceinline__ void share_out(const int* scan, int B, int count, F f, G g) {
+    const int warps = gridDim.x * (blockDim.x / 32), per = ((count + warps - 1) / warps + 31) & ~31;
+    const long long from = (long long)(blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5)) * per;
+    const int end = (int)min((long long)count, from + per);
+    int r = 0;
+    for (int i0 = (int)min((long long)count, from); i0 < end; i0 += N * 32) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int i = i0 + k * 32 + (threadIdx.x & 31);
+            const int mine = row_from(scan, B, i, r);
+            f(k, i, mine);
+            r = __shfl_sync(0xffffffffu, mine, 0);                   // numbers grow, rows do
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int i = i0 + k * 32 + (threadIdx.x & 31);
+            if (i < end) g(k, i);
+        }
+    }
 }
 
 __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
-    __shared__ long long sums[32];
+    pdl_trigger();
+    __shared__ unsigned sums[3][32];
     __shared__ int back[kPlanMax], cu[kPlanMax], take[kPlanMax], kept[kPlanMax], held[kPlanMax], lead[kPlanMax];
     const int b = threadIdx.x, page = 1 << a.page_shift, me = blockIdx.x, blocks = gridDim.x;
     const bool mine = b < a.B;
@@ -167,34 +207,35 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
     }
     int count = *a.free_count;
     if (count < 0 || count > a.pages) { wrong |= kStPage; count = 0; }
-    long long all;
     const int mine_back = end ? (int)(((long long)len + page - 1) >> a.page_shift) : 0;
-    const long long before = block_scan(mine_back, sums, &all);
-    int returned = (int)min(all, (long long)(a.pages - count));
-    if (returned < all) wrong |= kStPage;                            // more pages than there are
-    const int top = count + returned;
     const int stay = end ? 0 : len, has = sound ? (int)(((long long)stay + page - 1) >> a.page_shift) : 0;
-    const long long want = sound ? (((long long)stay + add + page - 1) >> a.page_shift) - has : 0;
-    long long none;
-    const long long pages_before = block_scan(want, sums, &none), tokens_before = block_scan(add, sums, &none);
-    const bool fits = (want == 0 || pages_before + want <= top) && (add == 0 || tokens_before + add <= a.n) && has + want <= a.stride;
+    const int want = sound ? (int)((((long long)stay + add + page - 1) >> a.page_shift) - has) : 0;
+    unsigned asked[3] = {(unsigned)mine_back, (unsigned)want, (unsigned)add}, all[3];
+    block_scan<3>(asked, sums, all);
+    const int returned = min((int)all[0], a.pages - count);
+    if ((int)all[0] > returned) wrong |= kStPage;                    // more pages than there are
+    const int top = count + returned;
+    const bool fits = (want == 0 || (asked[1] <= (unsigned)top && asked[1] < kStepMost)) && (add == 0 || (asked[2] <= (unsigned)a.n && asked[2] < kStepMost)) &&
+                      (long long)has + want <= a.stride;
     if (mine && !fits) wrong |= kStCapacity;
-    const int given = fits ? add : 0, got = fits ? (int)want : 0;
-    long long tokens, taken;
-    const int at = (int)block_scan(given, sums, &tokens), from = (int)block_scan(got, sums, &taken);
+    const int given = fits ? add : 0, got = fits ? want : 0;
+    unsigned served[2] = {(unsigned)given, (unsigned)got}, totals[2];
+    block_scan<2>(served, sums, totals);
+    const int tokens = (int)totals[0], taken = (int)totals[1], at = (int)served[0] - given, from = (int)served[1] - got;
     if (mine) {
-        back[b] = (int)min(before, (long long)INT32_MAX);
+        back[b] = (int)asked[0] - mine_back;                        // (a whole table has fewer than kStepMost)
         cu[b] = at;
         take[b] = from;
         kept[b] = stay;
         held[b] = has;
     }
     __syncthreads();
-    const int stride = blocks * kStepThreads, i0 = me * kStepThreads + threadIdx.x;
-    for (int i = i0; i < returned; i += stride) {
-        const int r = row_of(back, a.B, i);
-        a.free[count + i] = __ldcg(a.table + (long long)r * a.stride + i - back[r]);
-    }
+    // a warp's pages and tokens follow each other (searched for one by one, all threads apart, 1024 rows with 118000 new tokens took
+    // 31 us: 8 SMs' instructions)
+    constexpr int N = kStepAhead;
+    int id[N];
+    share_out<N>(back, a.B, returned, [&](int k, int i, int r) { id[k] = i < returned ? __ldcg(a.table + (long long)r * a.stride + i - back[r]) : 0; },
+                 [&](int k, int i) { a.free[count + i] = id[k]; });
     __syncwarp();
     if (blocks > 1) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -207,28 +248,62 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
             a.cu_q[b] = at;
         }
         if (threadIdx.x == 0) {
-            a.cu_q[a.B] = (int)tokens;
-            *a.free_count_out = top - (int)taken;
+            a.cu_q[a.B] = tokens;
+            *a.free_count_out = top - taken;
         }
         if (wrong && a.status) atomicOr(a.status, wrong);
     }
-    for (int i = i0; i < taken; i += stride) {
-        const int r = row_of(take, a.B, i);
-        a.table[(long long)r * a.stride + held[r] + i - take[r]] = __ldcg(a.free + top - 1 - i);
-    }
-    for (int i = i0; i < a.n; i += stride) {
-        long long slot = -1;
-        int position = 0;
-        if (i < tokens) {
-            const int r = row_of(cu, a.B, i), place = kept[r] + i - cu[r], p = place >> a.page_shift;
-            const int id = p < held[r] ? __ldcg(a.table + (long long)r * a.stride + p) : __ldcg(a.free + top - 1 - (take[r] + p - held[r]));
-            if (id >= 0 && id < a.pages) slot = ((long long)id << a.page_shift) + (place & (page - 1));
-            else if (a.status) atomicOr(a.status, kStPage);
-            position = place + lead[r];
-        }
-        a.slots[i] = slot;
-        a.positions[i] = position;
-    }
+    long long at_table[N];
+    share_out<N>(take, a.B, taken,
+                 [&](int k, int i, int r) {
+                     id[k] = i < taken ? __ldcg(a.free + top - 1 - i) : 0;
+                     at_table[k] = (long long)r * a.stride + held[r] + i - take[r];
+                 },
+                 [&](int k, int i) { a.table[at_table[k]] = id[k]; });
+    if (a.split) return;
+    int place[N], before_own[N];
+    share_out<N>(cu, a.B, a.n,
+                 [&](int k, int i, int r) {
+                     id[k] = -1;
+                     place[k] = before_own[k] = 0;
+                     if (i >= tokens) return;
+                     place[k] = kept[r] + i - cu[r];
+                     before_own[k] = lead[r];
+                     const int p = place[k] >> a.page_shift;
+                     id[k] = p < held[r] ? __ldcg(a.table + (long long)r * a.stride + p) : __ldcg(a.free + top - 1 - (take[r] + p - held[r]));
+                 },
+                 [&](int k, int i) {
+                     const bool there = i < tokens, sound_page = id[k] >= 0 && id[k] < a.pages;
+                     if (there && !sound_page && a.status) atomicOr(a.status, kStPage);
+                     a.slots[i] = there && sound_page ? ((long long)id[k] << a.page_shift) + (place[k] & (page - 1)) : -1;
+                     a.positions[i] = place[k] + before_own[k];
+                 });
+}
+
+// Slots and positions from the step's results: offsets, lengths and tables, the new tokens among them.
+__global__ void __launch_bounds__(kSlotThreads) page_slots_kernel(PageStep a) {
+    __shared__ int cu[kPlanMax + 1];
+    pdl_wait();
+    for (int b = threadIdx.x; b <= a.B; b += kSlotThreads) cu[b] = __ldcg(a.cu_q + b);
+    __syncthreads();
+    constexpr int N = kStepAhead;
+    const int tokens = cu[a.B], page = 1 << a.page_shift;
+    int id[N], place[N], before_own[N];
+    share_out<N>(cu, a.B, a.n,
+                 [&](int k, int i, int r) {
+                     id[k] = -1;
+                     place[k] = before_own[k] = 0;
+                     if (i >= tokens) return;
+                     place[k] = __ldcg(a.lengths_out + r) - cu[r + 1] + i;
+                     before_own[k] = a.first ? __ldg(a.first + r) : 0;
+                     id[k] = __ldcg(a.table + (long long)r * a.stride + (place[k] >> a.page_shift));
+                 },
+                 [&](int k, int i) {
+                     const bool there = i < tokens, sound_page = id[k] >= 0 && id[k] < a.pages;
+                     if (there && !sound_page && a.status) atomicOr(a.status, kStPage);
+                     a.slots[i] = there && sound_page ? ((long long)id[k] << a.page_shift) + (place[k] & (page - 1)) : -1;
+                     a.positions[i] = place[k] + before_own[k];
+                 });
 }
 
 }  // namespace sgk

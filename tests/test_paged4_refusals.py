@@ -121,7 +121,7 @@ def _step(**kw):
 
 @pytest.mark.parametrize("kw, word", [
     (dict(B=0), "B must be"), (dict(B=1025), "B must be"), (dict(n=-1), "n >= 0"), (dict(pages=0), "pages"), (dict(page=12), "page"),
-    (dict(page=2048), "page"), (dict(table_stride=0), "table_stride"), (dict(table_stride=1 << 27), "2^31"), (dict(slots=P + 4), "8-byte")]
+    (dict(page=2048), "page"), (dict(table_stride=0), "table_stride"), (dict(table_stride=1 << 27), "2^31"), (dict(slots=P + 4), "8-byte"), (dict(B=1024, table_stride=1 << 21), "2^31 - 1 pages")]
     + [({k: None}, "NULL") for k in ("table", "free_pages", "free_count", "lengths", "added", "free_count_out", "lengths_out", "cu_q", "slots", "positions")])
 def test_step(kw, word):
     assert _step(**kw) == -1 and word in _said()
