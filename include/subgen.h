@@ -490,8 +490,8 @@ int subgen_paged4_append(const subgen_pages4* cache, const subgen_batch* batch, 
 int subgen_paged4_load(const subgen_pages4* cache, const int64_t* slots, int n, const subgen_heads* K, const subgen_heads* V, int dtype, void* stream);
 
 /* As subgen_paged_attend, over the values of the cells; dtype: of q and out. What that says of units of rows, with these numbers:
- * bf16 queries in units of 8 rows (new tokens x H / Hkv) in calls of at most 8 rows a sequence on average (a group, where there
- * are any), 16 up to 16 rows, else 256; fp32 queries in units of 8. Key tiles have 128 tokens.
+ * bf16 queries in units of 8 rows (new tokens x H / Hkv) in calls of at most 8 rows a sequence on average, of 16 up to 32 rows
+ * (where several sequences share a prefix: up to 32 rows a group), else of 256; fp32 queries in units of 8. Key tiles have 128 tokens.
  * Units of 8 and 16 rows take queries and softmax weights in fp16 (fp32 queries: as two fp16 each, 22 bits), queries scaled by
  * a power of two first, so that what is below 2^-29 of a row's largest coordinate is rounded more coarsely; weights below 2^-31 of
  * the largest count for the sum alone. Units of 256 rows take them in bf16 as the bf16 cache does. */

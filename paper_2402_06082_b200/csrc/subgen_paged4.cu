@@ -61,19 +61,28 @@ int launch_load(Load4 a, cudaStream_t st) {
 }
 
 // ---- attention ----
+template <typename T, int D, int NT, int TILES>
+constexpr size_t few_smem() { return (sizeof(P4Smem<T, D, NT, TILES>) + 15) & ~(size_t)15; }
+
 template <typename T, int D, int NT>
 int opt_in_few() {
-    typedef P4Smem<T, D, NT> S;
-    return opt_in(paged4_attend_few_kernel<T, D, NT>, paged_merge_kernel<T, D, S::RU, kP4KT, 0, kP4Lead>, ((sizeof(S) + 15) & ~(size_t)15) + plan_bytes(kPlanMax));
+    int rc = opt_in(paged4_attend_few_kernel<T, D, NT, 3>, paged_merge_kernel<T, D, 8 * NT, kP4KT, 0, kP4Lead>, few_smem<T, D, NT, 3>() + plan_bytes(kPlanMax));
+    if (!rc) rc = opt_in(paged4_attend_few_kernel<T, D, NT, 2>, paged_merge_kernel<T, D, 8 * NT, kP4KT, 0, kP4Lead>, few_smem<T, D, NT, 2>() + plan_bytes(kPlanMax));
+    return rc;
 }
 template <typename T, int D, int NT>
 int attend_few(const PagedView& P, const Attend& a, cudaStream_t st) {
-    typedef P4Smem<T, D, NT> S;
-    const int blocks = kSMs * kP4Blocks<NT>;
-    static_assert(S::RU * kP4Blocks<NT> <= 256, "slot_count");
-    paged4_attend_few_kernel<T, D, NT><<<blocks, kP4Threads, ((sizeof(S) + 15) & ~(size_t)15) + plan_bytes(P.B + P.groups), st>>>(P, a);
+    constexpr int blocks = kSMs * kP4Blocks<NT>;
+    constexpr size_t room = 233472 / kP4Blocks<NT> - 1024;           // shared memory of a block, so that all of them are there at once
+    static_assert(8 * NT * kP4Blocks<NT> <= 256, "slot_count");
+    static_assert(few_smem<T, D, NT, 2>() + ((size_t)8 * (kPlanMax + 1) + 15) <= room, "two tiles always fit");
+    const size_t plan = plan_bytes(P.B + P.groups);
+    // A third tile in flight where the plan (8 bytes a sequence) leaves room for it: 64 sequences 89 -> 86 us. Without room (256 sequences of
+    // 1024 tokens) a third of the blocks would run after the others.
+    if (few_smem<T, D, NT, 3>() + plan <= room) paged4_attend_few_kernel<T, D, NT, 3><<<blocks, kP4Threads, few_smem<T, D, NT, 3>() + plan, st>>>(P, a);
+    else paged4_attend_few_kernel<T, D, NT, 2><<<blocks, kP4Threads, few_smem<T, D, NT, 2>() + plan, st>>>(P, a);
     CUDA_TRY(cudaGetLastError());
-    return launch_merge<T, D, S::RU, kP4KT, 0, kP4Lead>(P, a, blocks, st);
+    return launch_merge<T, D, 8 * NT, kP4KT, 0, kP4Lead>(P, a, blocks, st);
 }
 
 template <int D>
@@ -100,9 +109,14 @@ int attend4_bf16(const PagedView& P, const Attend& a, cudaStream_t st) {
         done[dev] = !rc;
     }
     if (rc) return rc;
-    const long long rows = (long long)a.n << a.g_shift, of = P.groups ? P.groups : P.B;
-    if (rows <= 8 * of) return attend_few<T, D, 1>(P, a, st);
-    if (rows <= 16 * of) return attend_few<T, D, 2>(P, a, st);
+    // By the mean of rows a sequence, or a group where several sequences share a prefix. 16 sequences of 8192 tokens, 8 KV heads, in
+    // units of 8 rows / units of 16 / units of 256 on the other tensor cores: 4 rows 46 / 56 / 101 us, 8 rows 45 / 56 / 102, 12 rows
+    // 73 / 58 / 105, 24 rows 101 / 97 / 113, 32 rows 131 / 99 / 121. A prefix of 32768 tokens before single tokens (4 rows each): 2
+    // sequences 31 / 27 / 43, 4 45 / 29 / 48, 8 75 / 41 / 58.
+    const long long rows = (long long)a.n << a.g_shift;
+    const bool shared = P.groups && P.groups < P.B;
+    if (!shared && rows <= 8LL * P.B) return attend_few<T, D, 1>(P, a, st);
+    if (rows <= 32LL * (shared ? P.groups : P.B)) return attend_few<T, D, 2>(P, a, st);
     CUtensorMap mq;
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.H, (cuuint64_t)a.n};
     const cuuint64_t strides[2] = {(cuuint64_t)a.q.hs * 2, (cuuint64_t)a.q.ts * 2};

@@ -29,9 +29,9 @@ namespace sgk {
 constexpr int kP4Warps = 4, kP4Cells = 2, kP4Threads = 32 * (kP4Warps + 1), kP4KT = 16 * kP4Warps * kP4Cells, kP4Lead = 2, kP4Runs = 2;
 constexpr float kP4Shift = 6.f, kP4Margin = 8.f;
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, int TILES>
 struct P4Smem {
-    static constexpr int RU = 8 * NT, kTile = kP4Warps * kP4Cells * Cell4<D>::kBytes, kTiles = 3, kQRow = D * (int)sizeof(T) + 16, kJoin = D + 4;
+    static constexpr int RU = 8 * NT, kTile = kP4Warps * kP4Cells * Cell4<D>::kBytes, kTiles = TILES, kQRow = D * (int)sizeof(T) + 16, kJoin = D + 4;
     unsigned char tile[kTiles][kTile];
     unsigned char q[RU][kQRow];                       // of one run: free again as soon as it is in registers
     float join[kP4Warps][RU][kJoin];
@@ -61,9 +61,9 @@ __device__ __forceinline__ uint32_t rest(float x, float y, uint32_t h) {
     return halves(x - f.x, y - f.y);
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, int TILES>
 __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_kernel(PagedView P, Attend a) {
-    typedef P4Smem<T, D, NT> S;
+    typedef P4Smem<T, D, NT, TILES> S;
     typedef Cell4<D> C;
     constexpr int RU = S::RU, NW = kP4Warps, U = kP4Cells, PIECES = sizeof(T) == 4 ? 2 : 1, KS = D / 16, MT = D / 16;
     extern __shared__ __align__(128) unsigned char dyn4[];

@@ -181,8 +181,8 @@ class Setting4:
 
     def few(self):
         """Which kernel a call takes."""
-        rows = self.n * self.H // self.Hkv
-        return self.dtype == torch.float32 or rows <= 16 * (len(self.prefix) or len(self.own))
+        rows, groups, B = self.n * self.H // self.Hkv, len(self.prefix), len(self.own)
+        return self.dtype == torch.float32 or rows <= 32 * (groups if 0 < groups < B else B)
 
     def want(self, scale, causal=True, few=None):
         K, V = decoded(self.pool, self.page, self.d)

@@ -546,7 +546,7 @@ def test_serving(dtype):
                     p[i, :, : len(y)] = torch.stack(y, 1)
         table = torch.arange(B)[:, None]
         rows = n * H // Hkv
-        want, bound = p4.attend(turned[:total], pools[0], pools[1], cu, [len(x[0]) for x in kept], table, 0.125, few=dtype == F32 or rows <= 16 * B)
+        want, bound = p4.attend(turned[:total], pools[0], pools[1], cu, [len(x[0]) for x in kept], table, 0.125, few=dtype == F32 or rows <= 32 * B)
         assert_within(out[:total], want, bound, "turn %d" % turn)
     assert cache.status() == 0
 
