@@ -674,8 +674,8 @@ def page_step(lengths: torch.Tensor, table: torch.Tensor, free: torch.Tensor, fr
     """
     if _calls is None:
         _bind_calls()
-    return PageStep._make(_calls.page_step(lengths, table, free, free_count, added, page, n, ended, first, lengths if in_place else None,
-                                           free_count if in_place else None, cu_q, slots, positions, status))
+    return PageStep(*_calls.page_step(lengths, table, free, free_count, added, page, n, ended, first, lengths if in_place else None,
+                                      free_count if in_place else None, cu_q, slots, positions, status))
 
 
 class PageTables:

@@ -10,6 +10,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <utility>
 #include <stdexcept>
 #include <string>
 
@@ -85,6 +86,20 @@ subgen_heads output(PyObject*& o, const char* name, const at::Tensor& from, cons
     o = THPVariable_Wrap(std::move(y));
     if (!o) throw std::bad_alloc();
     return h;
+}
+// A tensor of its own in a part of another's memory, from byte `at` on: several outputs of one allocation, each of which (with the
+// checks and bookkeeping that torch's dispatcher does for a view) would cost a microsecond on the host.
+at::Tensor part_of(const at::Tensor& all, at::ScalarType type, at::IntArrayRef sizes, int64_t at) {
+    const c10::Storage storage = all.storage();
+    at::Tensor x = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(storage), all.key_set(), c10::scalarTypeToTypeMeta(type));
+    x.unsafeGetTensorImpl()->set_storage_offset(at / (int64_t)c10::elementSize(type));
+    x.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    return x;
+}
+PyObject* wrapped(at::Tensor x) {
+    PyObject* o = THPVariable_Wrap(std::move(x));
+    if (!o) throw std::bad_alloc();
+    return o;
 }
 int dtype_of(const Like& w) { return w.type == at::kFloat ? SUBGEN_DTYPE_FP32 : SUBGEN_DTYPE_BF16; }
 int integer(PyObject* o) {
@@ -301,11 +316,22 @@ PyObject* load4(PyObject*, PyObject* const* a, Py_ssize_t got) {
         if (n > INT_MAX) refuse("slots: too many rows");
         const c10::cuda::CUDAGuard on((c10::DeviceIndex)w.device);
         const void* at_slots = whole(a[2], "slots", at::kLong, w.device, n);
-        const at::Tensor none = at::empty({0}, slots->options().dtype(w.type));
-        Held k(a[4]), v(a[5]);
-        const subgen_heads hk = output(k.o, "K", none, w, n, c->Hkv, c->d);
+        const bool new_k = a[4] == Py_None, new_v = a[5] == Py_None;
+        const int64_t bytes = n * c->Hkv * c->d * (int64_t)c10::elementSize(w.type);        // (a multiple of 64)
+        at::Tensor both_new;
+        if (new_k || new_v) both_new = at::empty({bytes * (new_k + new_v)}, slots->options().dtype(at::kByte));
+        auto out = [&](PyObject* o, const char* name, int64_t at) {
+            Held h(o);
+            if (o == Py_None) h.o = wrapped(part_of(both_new, w.type, {n, c->Hkv, c->d}, at));
+            else Py_INCREF(o);
+            h.mine = true;
+            return std::make_pair(rows(*tensor(h.o, name), name, w, n, c->Hkv, c->d), h.release());
+        };
+        const auto [hk, ko] = out(a[4], "K", 0);
+        Held k(ko);
         k.mine = true;
-        const subgen_heads hv = output(v.o, "V", none, w, n, c->Hkv, c->d);
+        const auto [hv, vo] = out(a[5], "V", new_k ? bytes : 0);
+        Held v(vo);
         v.mine = true;
         check(f_load4(c, (const int64_t*)at_slots, (int)n, &hk, &hv, dtype_of(w), c10::cuda::getCurrentCUDAStream(w.device).stream()));
         PyObject* both = PyTuple_New(2);
@@ -344,20 +370,23 @@ PyObject* page_step(PyObject*, PyObject* const* a, Py_ssize_t got) {
         if (!five) throw std::bad_alloc();
         Held held(five);
         held.mine = true;
+        at::Tensor all;                               // slots first: 8-byte aligned
+        int64_t at_byte = 0;
         auto out = [&](int i, PyObject* o, const char* name, at::ScalarType type, int64_t count) {
             if (o == Py_None) {
-                o = THPVariable_Wrap(at::empty({count}, lengths->options().dtype(type)));
-                if (!o) throw std::bad_alloc();
+                if (!all.defined()) all = at::empty({8 * n + 4 * (n + 2 * B + 2)}, lengths->options().dtype(at::kByte));
+                o = wrapped(part_of(all, type, {count}, at_byte));
+                at_byte += count * (int64_t)c10::elementSize(type);
             } else {
                 Py_INCREF(o);
             }
             PyTuple_SET_ITEM(five, i, o);
             return const_cast<void*>(whole(o, name, type, dev, count));
         };
+        p.slots = (int64_t*)out(3, a[12], "slots", at::kLong, n);
         p.cu_q = (int*)out(0, a[11], "cu_q", at::kInt, B + 1);
         p.lengths_out = (int*)out(1, a[9], "lengths_out", at::kInt, B);
         p.free_count_out = (int*)out(2, a[10], "free_count_out", at::kInt, 1);
-        p.slots = (int64_t*)out(3, a[12], "slots", at::kLong, n);
         p.positions = (int*)out(4, a[13], "positions", at::kInt, n);
         check(f_step(&p, c10::cuda::getCurrentCUDAStream(dev).stream()));
         return held.release();

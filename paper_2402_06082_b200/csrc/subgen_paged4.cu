@@ -238,7 +238,8 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel, a));
+    if (blocks == 1) CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel<1>, a));
+    else CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel<kStepAhead>, a));
     if (!a.split) return SUBGEN_OK;
     const int parts = (x->n + kSlotThreads / 32 * kStepAhead * 32 - 1) / (kSlotThreads / 32 * kStepAhead * 32);        // a turn each
     cfg.gridDim = dim3((unsigned)(parts < 4 * kSMs ? parts : 4 * kSMs));

@@ -124,7 +124,7 @@ constexpr unsigned kStepMost = 0x7fffffffu;
 template <int K>
 __device__ __forceinline__ void block_scan(unsigned* x, unsigned (*sums)[32], unsigned* all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
+#pragma unroll 1
     for (int off = 1; off < 32; off <<= 1)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -139,7 +139,7 @@ __device__ __forceinline__ void block_scan(unsigned* x, unsigned (*sums)[32], un
     unsigned w[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) w[k] = sums[k][lane];                // 32 warps
-#pragma unroll
+#pragma unroll 1
     for (int off = 1; off < 32; off <<= 1)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -188,6 +188,9 @@ __device__ __forceinline__ void share_out(const int* scan, int B, int count, F f
     }
 }
 
+// N: how many turns of a warp are under way at once; 1 in a lone block, which has a turn or two in all and runs through its code once:
+// each new 128 bytes of that cost more than a turn does (4: 64 rows with a token each 10.2 us).
+template <int N>
 __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
     pdl_trigger();
     __shared__ unsigned sums[3][32];
@@ -232,7 +235,6 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
     __syncthreads();
     // a warp's pages and tokens follow each other (searched for one by one, all threads apart, 1024 rows with 118000 new tokens took
     // 31 us: 8 SMs' instructions)
-    constexpr int N = kStepAhead;
     int id[N];
     share_out<N>(back, a.B, returned, [&](int k, int i, int r) { id[k] = i < returned ? __ldcg(a.table + (long long)r * a.stride + i - back[r]) : 0; },
                  [&](int k, int i) { a.free[count + i] = id[k]; });
