@@ -469,7 +469,8 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
  * [16][d / 16], their values' codes and scales: 2304 bytes at d = 128, 1152 at d = 64. A page has page / 16 of them on end in
  * each head. Eight codes are a 32-bit word, least byte first: codes 0, 2, 4, 6 (least first) in the low half, 1, 3, 5, 7 in the high
  * half, each half rotated left by 2. A scale is the upper byte of the 15 bits that an fp16 has below its sign; 255 is NaN.
- * All 8-bit contents are valid, so a pool needs no initial values. */
+ * All 8-bit contents are valid, so a pool needs no initial values. As above, the first call of an operator (of subgen_page_step, too) with
+ * a dtype and d on a device loads its kernels: make it before starting any stream capture. */
 typedef struct subgen_pages4 {
     void* pool;             /* device; cell (page, head, i) at pool + page * page_stride + head * head_stride + i * cell bytes */
     int64_t page_stride, head_stride;   /* bytes, multiples of 16; at least page / 16 cells (not looked at for one page, one head) */

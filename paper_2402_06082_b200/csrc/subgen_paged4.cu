@@ -226,6 +226,16 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     a.slots = (long long*)x->slots;
     a.status = x->status;
     a.split = x->n > 4 * kStepThreads;
+    static bool done[kMaxDevices];
+    int dev;
+    rc = this_device(&dev);
+    if (rc) return rc;
+    if (!done[dev]) {                                 // loads both, so that a call of any size may be captured later
+        cudaFuncAttributes at;
+        CUDA_TRY(cudaFuncGetAttributes(&at, page_step_kernel));
+        CUDA_TRY(cudaFuncGetAttributes(&at, page_slots_kernel));
+        done[dev] = true;
+    }
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     const int blocks = x->n > kStepThreads || x->B > 128 ? kStepCluster : 1;     // something to share out
@@ -238,10 +248,9 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (blocks == 1) CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel<1>, a));
-    else CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel<kStepAhead>, a));
+    CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel, a));
     if (!a.split) return SUBGEN_OK;
-    const int parts = (x->n + kSlotThreads / 32 * kStepAhead * 32 - 1) / (kSlotThreads / 32 * kStepAhead * 32);        // a turn each
+    const int parts = (x->n + kSlotThreads - 1) / kSlotThreads;      // a turn a warp
     cfg.gridDim = dim3((unsigned)(parts < 4 * kSMs ? parts : 4 * kSMs));
     cfg.blockDim = dim3(kSlotThreads);
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

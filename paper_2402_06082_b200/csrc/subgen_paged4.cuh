@@ -117,7 +117,7 @@ struct PageStep {
     int split;                                        // slots and positions are the second kernel's
 };
 
-constexpr int kStepThreads = 1024, kStepCluster = 8, kStepAhead = 4, kSlotThreads = 256;
+constexpr int kStepThreads = 1024, kStepCluster = 8, kSlotThreads = 256;
 
 // Inclusive sums of K numbers over the block, and their totals. Sums stay at kStepMost once they reach it.
 constexpr unsigned kStepMost = 0x7fffffffu;
@@ -164,33 +164,30 @@ __device__ __forceinline__ int row_from(const int* scan, int B, int i, int r) {
     }
     return r;
 }
-// f(k, i, row) for k < N and the warp's share of the numbers below `count`, N times 32 of them at a time, then g(k, i) for the same:
-// what f asks for is on its way for all of them before g uses it. i may be `count` or more.
-template <int N, typename F, typename G>
-__device__ __forceinline__ void share_out(const int* scan, int B, int count, F f, G g) {
+// f(i, row) for the warp's share of the numbers below `count`, 32 of them at a time. (Several turns under way at once hide the loads of
+// one another, but take more code, and a launch runs through it cold, each 128 bytes some 300 cycles: 64 rows with a token each
+// 8.2 us like this, 10.2 with four turns; 1024 rows with 118000 tokens 16.4, 17.2 with two and 20.5 with four.)
+template <typename F>
+__device__ __forceinline__ void share_out(const int* scan, int B, int count, F f) {
     const int warps = gridDim.x * (blockDim.x / 32), per = ((count + warps - 1) / warps + 31) & ~31;
     const long long from = (long long)(blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5)) * per;
     const int end = (int)min((long long)count, from + per);
     int r = 0;
-    for (int i0 = (int)min((long long)count, from); i0 < end; i0 += N * 32) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int i = i0 + k * 32 + (threadIdx.x & 31);
-            const int mine = row_from(scan, B, i, r);
-            f(k, i, mine);
-            r = __shfl_sync(0xffffffffu, mine, 0);                   // numbers grow, rows do
-        }
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int i = i0 + k * 32 + (threadIdx.x & 31);
-            if (i < end) g(k, i);
-        }
+#pragma unroll 1
+    for (int i0 = (int)min((long long)count, from); i0 < end; i0 += 32) {
+        const int i = i0 + (threadIdx.x & 31), mine = row_from(scan, B, i, r);
+        r = __shfl_sync(0xffffffffu, mine, 0);                       // numbers grow, rows do
+        if (i < end) f(i, mine);
     }
 }
 
-// N: how many turns of a warp are under way at once; 1 in a lone block, which has a turn or two in all and runs through its code once:
-// each new 128 bytes of that cost more than a turn does (4: 64 rows with a token each 10.2 us).
-template <int N>
+__device__ __forceinline__ void put_slot(const PageStep& a, int i, bool there, int id, int place, int lead) {
+    const bool sound = id >= 0 && id < a.pages;
+    if (there && !sound && a.status) atomicOr(a.status, kStPage);
+    a.slots[i] = there && sound ? ((long long)id << a.page_shift) + (place & ((1 << a.page_shift) - 1)) : -1;
+    a.positions[i] = there ? place + lead : 0;
+}
+
 __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
     pdl_trigger();
     __shared__ unsigned sums[3][32];
@@ -235,9 +232,7 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
     __syncthreads();
     // a warp's pages and tokens follow each other (searched for one by one, all threads apart, 1024 rows with 118000 new tokens took
     // 31 us: 8 SMs' instructions)
-    int id[N];
-    share_out<N>(back, a.B, returned, [&](int k, int i, int r) { id[k] = i < returned ? __ldcg(a.table + (long long)r * a.stride + i - back[r]) : 0; },
-                 [&](int k, int i) { a.free[count + i] = id[k]; });
+    share_out(back, a.B, returned, [&](int i, int r) { a.free[count + i] = __ldcg(a.table + (long long)r * a.stride + i - back[r]); });
     __syncwarp();
     if (blocks > 1) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -255,31 +250,14 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
         }
         if (wrong && a.status) atomicOr(a.status, wrong);
     }
-    long long at_table[N];
-    share_out<N>(take, a.B, taken,
-                 [&](int k, int i, int r) {
-                     id[k] = i < taken ? __ldcg(a.free + top - 1 - i) : 0;
-                     at_table[k] = (long long)r * a.stride + held[r] + i - take[r];
-                 },
-                 [&](int k, int i) { a.table[at_table[k]] = id[k]; });
+    share_out(take, a.B, taken, [&](int i, int r) { a.table[(long long)r * a.stride + held[r] + i - take[r]] = __ldcg(a.free + top - 1 - i); });
     if (a.split) return;
-    int place[N], before_own[N];
-    share_out<N>(cu, a.B, a.n,
-                 [&](int k, int i, int r) {
-                     id[k] = -1;
-                     place[k] = before_own[k] = 0;
-                     if (i >= tokens) return;
-                     place[k] = kept[r] + i - cu[r];
-                     before_own[k] = lead[r];
-                     const int p = place[k] >> a.page_shift;
-                     id[k] = p < held[r] ? __ldcg(a.table + (long long)r * a.stride + p) : __ldcg(a.free + top - 1 - (take[r] + p - held[r]));
-                 },
-                 [&](int k, int i) {
-                     const bool there = i < tokens, sound_page = id[k] >= 0 && id[k] < a.pages;
-                     if (there && !sound_page && a.status) atomicOr(a.status, kStPage);
-                     a.slots[i] = there && sound_page ? ((long long)id[k] << a.page_shift) + (place[k] & (page - 1)) : -1;
-                     a.positions[i] = place[k] + before_own[k];
-                 });
+    share_out(cu, a.B, a.n, [&](int i, int r) {
+        const int place = kept[r] + i - cu[r], p = place >> a.page_shift;
+        int id = -1;
+        if (i < tokens) id = p < held[r] ? __ldcg(a.table + (long long)r * a.stride + p) : __ldcg(a.free + top - 1 - (take[r] + p - held[r]));
+        put_slot(a, i, i < tokens, id, place, lead[r]);
+    });
 }
 
 // Slots and positions from the step's results: offsets, lengths and tables, the new tokens among them.
@@ -288,24 +266,16 @@ __global__ void __launch_bounds__(kSlotThreads) page_slots_kernel(PageStep a) {
     pdl_wait();
     for (int b = threadIdx.x; b <= a.B; b += kSlotThreads) cu[b] = __ldcg(a.cu_q + b);
     __syncthreads();
-    constexpr int N = kStepAhead;
-    const int tokens = cu[a.B], page = 1 << a.page_shift;
-    int id[N], place[N], before_own[N];
-    share_out<N>(cu, a.B, a.n,
-                 [&](int k, int i, int r) {
-                     id[k] = -1;
-                     place[k] = before_own[k] = 0;
-                     if (i >= tokens) return;
-                     place[k] = __ldcg(a.lengths_out + r) - cu[r + 1] + i;
-                     before_own[k] = a.first ? __ldg(a.first + r) : 0;
-                     id[k] = __ldcg(a.table + (long long)r * a.stride + (place[k] >> a.page_shift));
-                 },
-                 [&](int k, int i) {
-                     const bool there = i < tokens, sound_page = id[k] >= 0 && id[k] < a.pages;
-                     if (there && !sound_page && a.status) atomicOr(a.status, kStPage);
-                     a.slots[i] = there && sound_page ? ((long long)id[k] << a.page_shift) + (place[k] & (page - 1)) : -1;
-                     a.positions[i] = place[k] + before_own[k];
-                 });
+    const int tokens = cu[a.B];
+    share_out(cu, a.B, a.n, [&](int i, int r) {
+        int id = -1, place = 0, lead = 0;
+        if (i < tokens) {
+            place = __ldcg(a.lengths_out + r) - cu[r + 1] + i;
+            lead = a.first ? __ldg(a.first + r) : 0;
+            id = __ldcg(a.table + (long long)r * a.stride + (place >> a.page_shift));
+        }
+        put_slot(a, i, i < tokens, id, place, lead);
+    });
 }
 
 }  // namespace sgk

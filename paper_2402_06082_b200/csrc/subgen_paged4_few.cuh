@@ -36,8 +36,9 @@ struct P4Smem {
     unsigned char q[RU][kQRow];                       // of one run: free again as soon as it is in registers
     float join[kP4Warps][RU][kJoin];
     float2 stat[kP4Warps][RU];                        // reference * factor, sum
+    float factor[RU];                                 // of a row's scores
     SegRec run[kP4Runs];
-    unsigned long long full[kTiles], empty[kTiles], run_full[kP4Runs], run_empty[kP4Runs], q_full, q_empty, joined, read;
+    unsigned long long full[kTiles], empty[kTiles], run_full[kP4Runs], run_empty[kP4Runs], q_full, q_ready, q_empty, joined, read;
     int failed, flag;
 };
 template <int NT> constexpr int kP4Blocks = NT == 1 ? 3 : 2;
@@ -51,6 +52,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {         // 8 x 8 pa
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ uint32_t halves(float x, float y) {
     const __half2 h = __floats2half2_rn(x, y);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -74,6 +77,7 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
         for (int i = 0; i < S::kTiles; ++i) { bar_init(&sm.full[i], 1); bar_init(&sm.empty[i], NW); }
         for (int i = 0; i < kP4Runs; ++i) { bar_init(&sm.run_full[i], 1); bar_init(&sm.run_empty[i], NW); }
         bar_init(&sm.q_full, 1);
+        bar_init(&sm.q_ready, NW);
         bar_init(&sm.q_empty, NW);
         bar_init(&sm.joined, NW);
         bar_init(&sm.read, NW);
@@ -166,8 +170,40 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
             const SegRec& r = sm.run[slot];
             const int tile0 = r.tile0, tile1 = r.tile1, kp = r.kp, rows = r.rows;
             if (tile1 < 0) break;
-            // queries: row g of column block n, coordinates t * D / 4 ...
+            // queries, to fp16 where they lie, a warp a row (fp32: the rest behind), and from there every warp's fragments: row g of column
+            // block n, coordinates t * D / 4 ... (Each warp on its own, all in registers, was four times the work in straight code, which
+            // short calls spend their time on fetching.)
             if (!(ok = bar_wait(&sm.q_full, ns & 1, &sm.failed))) break;
+#pragma unroll 1
+            for (int row = warp; row < RU; row += NW) {
+                constexpr int VL = D / 32;
+                float f[VL];
+                unsigned top = 0;
+#pragma unroll
+                for (int i = 0; i < VL; ++i) {
+                    f[i] = row < rows ? to_float(reinterpret_cast<const T*>(sm.q[row])[lane * VL + i]) : 0.f;
+                    top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+                }
+                top = __reduce_max_sync(0xffffffffu, top);
+                // 2^(14 - e) and its reciprocal, both normal numbers; a row that is not finite becomes NaN
+                const int ex = min(max((int)(top >> 23), 15), 254);
+                const float up = top >= 0x7f800000u ? NAN : __uint_as_float((unsigned)(268 - ex) << 23);
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < VL; i += 2) {
+                    const float u0 = f[i] * up, u1 = f[i + 1] * up;
+                    const uint32_t h = halves(u0, u1);
+                    uint32_t* to = reinterpret_cast<uint32_t*>(sm.q[row]) + (lane * VL + i) / 2;
+                    to[0] = h;
+                    if constexpr (PIECES == 2) to[D / 2] = rest(u0, u1, h);
+                }
+                const float cc = a.c * 8.f * __uint_as_float((unsigned)(ex - 14) << 23);
+                if (lane == 0) sm.factor[row] = cc < 1.1754944e-38f ? 1.1754944e-38f : cc;       // not 0: times -infinity it would be NaN
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the next run's queries come by a copy
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sm.q_ready);
+            if (!(ok = bar_wait(&sm.q_ready, ns & 1, &sm.failed))) break;
             uint32_t q[NT][PIECES][KS * 2];
             float c[NT][2];                                          // exponent per unit of a score, of columns 2t and 2t + 1
             int own[NT][2];
@@ -175,36 +211,14 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
             e.S = r.S; e.nq = r.nq;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                float f[D / 4];
-                const bool live = n * 8 + g < rows;
-                const T* y = reinterpret_cast<const T*>(sm.q[n * 8 + g]) + t * (D / 4);
-                constexpr int VE = 16 / sizeof(T);
 #pragma unroll
-                for (int i = 0; i < D / 4; i += VE) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (live) v = *reinterpret_cast<const uint4*>(y + i);
-                    Elem<T>::unpack(v, f + i);
-                }
-                unsigned top = 0;
+                for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-                for (int i = 0; i < D / 4; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                // 2^(14 - e) and its reciprocal, both normal numbers; a row that is not finite becomes NaN
-                const int ex = min(max((int)(top >> 23), 15), 254);
-                const float up = top >= 0x7f800000u ? NAN : __uint_as_float((unsigned)(268 - ex) << 23);
-                const float down = __uint_as_float((unsigned)(ex - 14) << 23);
-#pragma unroll
-                for (int i = 0; i < D / 4; i += 2) {
-                    const float u0 = f[i] * up, u1 = f[i + 1] * up;
-                    q[n][0][i / 2] = halves(u0, u1);
-                    if constexpr (PIECES == 2) q[n][1][i / 2] = rest(u0, u1, q[n][0][i / 2]);
-                }
-                float cc = a.c * 8.f * down;
-                if (cc < 1.1754944e-38f) cc = 1.1754944e-38f;        // not 0: times -infinity it would be NaN
+                    for (int i = 0; i < KS * 2; i += 4)
+                        *reinterpret_cast<uint4*>(&q[n][p][i]) = *reinterpret_cast<const uint4*>(sm.q[n * 8 + g] + p * 2 * D + t * (D / 2) + i * 4);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    c[n][j] = __shfl_sync(0xffffffffu, cc, (2 * t + j) * 4);
+                    c[n][j] = sm.factor[n * 8 + 2 * t + j];
                     own[n][j] = plan.own_limit(e, r.ru * RU + n * 8 + 2 * t + j);
                 }
             }
