@@ -113,9 +113,30 @@ __device__ __forceinline__ uint4 pack_row(const float* f) {
     return r;
 }
 
+// Sine and cosine of turns * 2^-64 turns, to 2^-40 before the rounding to fp32: Taylor's series in 64 bits on an eighth of a turn to
+// either side of the nearest quarter.
+__device__ __forceinline__ void sincos_turns(unsigned long long turns, float* si, float* co) {
+    const double t = (double)(long long)turns * 5.421010862427522e-20;                       // 2^-64
+    const int quarter = __double2int_rn(4.0 * t);
+    const double y = (t - 0.25 * quarter) * 6.283185307179586, z = y * y;
+    double s = 1.0 / 6227020800.0, c = 1.0 / 479001600.0;                                    // 1 / 13!, 1 / 12!
+    s = fma(s, z, -1.0 / 39916800.0); c = fma(c, z, -1.0 / 3628800.0);
+    s = fma(s, z, 1.0 / 362880.0);    c = fma(c, z, 1.0 / 40320.0);
+    s = fma(s, z, -1.0 / 5040.0);     c = fma(c, z, -1.0 / 720.0);
+    s = fma(s, z, 1.0 / 120.0);       c = fma(c, z, 1.0 / 24.0);
+    s = fma(s, z, -1.0 / 6.0);        c = fma(c, z, -1.0 / 2.0);
+    const float fs = (float)fma(s * z, y, y), fc = (float)fma(c, z, 1.0);
+    const float u = quarter & 1 ? fc : fs, v = quarter & 1 ? fs : fc;
+    *si = quarter & 2 ? -u : u;
+    *co = (quarter + 1) & 2 ? -v : v;
+}
+
 // PAGED: 0 keys to an output, 1 keys and values into exact pages, 2 into 4-bit cells (P.K: the pool, strides in bytes). There a
 // lane rounds the two pieces that follow each other (16 coordinates in bf16; 8 in fp32, whose scale two lanes share); keys that
-// were rotated in halves lie apart and change lanes through shared memory first.
+// were rotated in halves lie apart and change lanes through shared memory first. What is rounded to 4 bits falls on either side of a
+// border by its last fp32 bits, so there every step is one plain fp32 operation on correctly rounded sines and cosines, and the
+// squares are added pair by pair (a value then differs from the same formula in plain fp32 operations by rare last bits alone,
+// and a code hardly ever).
 template <typename T, int D, int PAGED, int U>
 __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(NormRope a, PagedView P) {
     constexpr int VE = 16 / sizeof(T), LPR = D / VE / 2, RPW = 32 / LPR;
@@ -172,7 +193,8 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
             const unsigned long long turns = (unsigned long long)pos * __ldg(a.words + l * VE + e);
-            sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &si[e], &co[e]);   // 2^-31: half turns
+            if constexpr (PAGED == 2) sincos_turns(turns, &si[e], &co[e]);
+            else sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &si[e], &co[e]);   // 2^-31: half turns
         }
     }
 
@@ -214,19 +236,61 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
                     Elem<T>::unpack(rb[u], xb);
                     if (KIND < 2 && wt) {
                         float ss = 0.f;
+                        if constexpr (PAGED == 2) {
+                            // d = 128: four neighbours in turn, then halves on halves; d = 64: halves on halves all the way
+                            constexpr int N = D == 128 ? VE / 4 : VE, E = VE / N;
+                            float t[N];
 #pragma unroll
-                        for (int e = 0; e < VE; ++e) ss = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], ss));
+                            for (int i = 0; i < N; ++i) {
+                                float u = __fmul_rn(xa[i * E], xa[i * E]), v = __fmul_rn(xb[i * E], xb[i * E]);
 #pragma unroll
-                        for (int off = LPR / 2; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                                for (int e = 1; e < E; ++e) {
+                                    u = __fadd_rn(u, __fmul_rn(xa[i * E + e], xa[i * E + e]));
+                                    v = __fadd_rn(v, __fmul_rn(xb[i * E + e], xb[i * E + e]));
+                                }
+                                t[i] = __fadd_rn(u, v);
+                            }
+#pragma unroll
+                            for (int off = LPR / 2; off > 0; off >>= 1)
+#pragma unroll
+                                for (int i = 0; i < N; ++i) t[i] = __fadd_rn(t[i], __shfl_xor_sync(0xffffffffu, t[i], off));
+#pragma unroll
+                            for (int off = N / 2; off > 0; off >>= 1)
+#pragma unroll
+                                for (int i = 0; i < off; ++i) t[i] = __fadd_rn(t[i], t[i + off]);
+                            ss = t[0];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) ss = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], ss));
+#pragma unroll
+                            for (int off = LPR / 2; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                        }
                         const float r = rsqrtf(ss * (1.f / D) + a.eps);
                         float fa[VE], fb[VE];
                         Elem<T>::unpack(wa, fa);
                         Elem<T>::unpack(wb, fb);
 #pragma unroll
-                        for (int e = 0; e < VE; ++e) { xa[e] *= r * fa[e]; xb[e] *= r * fb[e]; }
+                        for (int e = 0; e < VE; ++e) {
+                            if constexpr (PAGED == 2) {
+                                xa[e] = __fmul_rn(__fmul_rn(xa[e], r), fa[e]);
+                                xb[e] = __fmul_rn(__fmul_rn(xb[e], r), fb[e]);
+                            } else {
+                                xa[e] *= r * fa[e];
+                                xb[e] *= r * fb[e];
+                            }
+                        }
                     }
                     if (KIND < 2 && turn) {
-                        if (a.interleaved) {
+                        if constexpr (PAGED == 2) {
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) {
+                                // pair e, and its cosine and sine, lie by the layout
+                                float &p = !a.interleaved ? xa[e] : x2[2 * e], &q = !a.interleaved ? xb[e] : x2[2 * e + 1];
+                                const float p0 = p, q0 = q;
+                                p = __fsub_rn(__fmul_rn(p0, co[e]), __fmul_rn(q0, si[e]));
+                                q = __fadd_rn(__fmul_rn(q0, co[e]), __fmul_rn(p0, si[e]));
+                            }
+                        } else if (a.interleaved) {
 #pragma unroll
                             for (int e = 0; e < VE / 2; ++e) {
                                 const float p0 = xa[2 * e], p1 = xa[2 * e + 1], r0 = xb[2 * e], r1 = xb[2 * e + 1];
