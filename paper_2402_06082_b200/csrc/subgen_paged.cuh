@@ -136,7 +136,7 @@ __device__ __forceinline__ void sincos_turns(unsigned long long turns, float* si
 // were rotated in halves lie apart and change lanes through shared memory first. What is rounded to 4 bits falls on either side of a
 // border by its last fp32 bits, so there every step is one plain fp32 operation on correctly rounded sines and cosines, and the
 // squares are added pair by pair (a value then differs from the same formula in plain fp32 operations by rare last bits alone,
-// and a code hardly ever).
+// and a code hardly ever). 19.7 K tokens x (32 + 8 + 8) heads x 128: 94 us, floor 65.
 template <typename T, int D, int PAGED, int U>
 __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(NormRope a, PagedView P) {
     constexpr int VE = 16 / sizeof(T), LPR = D / VE / 2, RPW = 32 / LPR;

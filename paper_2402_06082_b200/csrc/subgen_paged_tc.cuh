@@ -227,7 +227,10 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, unsigned b
 
 // Warps 12 to 15 of a CODES block: every tile of the block's runs from its staged cells into the ring, K and V in turn, a thread a
 // token. A token's pieces of 16 bytes are taken in an order that goes by its row, so that neither the loads (rows of D / 2 bytes)
-// nor the stores (128 bytes, swizzled) of 8 neighbours meet the same banks.
+// nor the stores (128 bytes, swizzled) of 8 neighbours meet the same banks. Prompt chunks behind 8192 shared tokens: codes loaded by
+// these warps themselves, a half tile ahead, 1180 us (890 without the loads); staged by bulk copies a tile ahead, for which the
+// ring of K and V has 3 places instead of 4, 981; code that fits the instruction caches 937 (857 on the bf16 cache; 851 with the
+// stores left out).
 template <int D>
 __device__ __forceinline__ void expand_tiles(PtSmem<D, true>& sm) {
     typedef Cell4<D> C;
