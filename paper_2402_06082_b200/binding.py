@@ -693,7 +693,8 @@ class PageTables:
         self.free_count = torch.full((1,), pages, dtype=torch.int32, device=device)
         self.slots, self.positions = torch.full((self.n,), -1, dtype=torch.int64, device=device), ints(self.n)
         self.batch = PagedBatch(self.cu_q, self.lengths, self.table)
-        torch.cuda.current_stream(self.lengths.device).synchronize()                       # before a call on any stream
+        if not torch.cuda.is_current_stream_capturing():   # as they are before a call on any stream reads them
+            torch.cuda.current_stream(self.lengths.device).synchronize()
 
     def step(self, added: torch.Tensor, ended: Optional[torch.Tensor] = None) -> PageStep:
         """added [B]: the tokens that each request gets now; ended [B]: nonzero where a request is over (both int32). What is given back is

@@ -105,6 +105,7 @@ int dtype_of(const Like& w) { return w.type == at::kFloat ? SUBGEN_DTYPE_FP32 : 
 int integer(PyObject* o) {
     const long x = PyLong_AsLong(o);
     if (x == -1 && PyErr_Occurred()) { PyErr_Clear(); refuse("a whole number is wanted"); }
+    if (x < INT_MIN || x > INT_MAX) refuse("a whole number below 2^31 is wanted");
     return (int)x;
 }
 float real(PyObject* o) {

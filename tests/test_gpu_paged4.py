@@ -584,6 +584,9 @@ def test_other_refusals():
                  lambda: b.page_step(_ints([1]), _ints([1]), _ints([1]), _ints([1]), _ints([1]), 16, 4)):
         with pytest.raises(ValueError):
             call()
+    for n in (-1, 2 ** 31, 2 ** 32 + 4, 2 ** 70, None):
+        with pytest.raises(ValueError):
+            b.page_step(_ints([1]), _ints([[1]]), _ints([1]), _ints([1]), _ints([1]), 16, n)
     with pytest.raises(b.SubgenError):
         cache.attend(batch, s.q, scale=0.0)
     with pytest.raises(b.SubgenError):
