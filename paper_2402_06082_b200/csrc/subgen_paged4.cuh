@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kLoadThreads, kLoadBlocks) paged4_load_kernel(
             const long long page = slot[u] >> a.page_shift;
             if (page >= a.pages) {
                 scale[b][u] = 255u;
-                if (i == 0 && l == 0 && a.status) atomicOr(a.status, kStPage);
+                if (h == 0 && l == 0 && (!kv || !a.k.p) && a.status) atomicOr(a.status, kStPage);        // once a token, K wanted or not
             } else if (page >= 0) {
                 const int id = (int)page, at = (int)slot[u] & ((1 << a.page_shift) - 1);
                 const char* cell = from + id * a.ps + (at >> 4) * Cell4<D>::kBytes;

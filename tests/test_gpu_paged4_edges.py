@@ -1,0 +1,58 @@
+"""The 4-bit paged cache and the tables of a step where the calls of test_gpu_paged4.py do not go."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paged4_helpers as p4
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _binding():
+    from paper_2402_06082_b200 import binding
+    return binding
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+# ---- load ----
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d, Hkv", [(64, 1), (64, 9), (128, 3)])
+@pytest.mark.parametrize("side", [0, 1])
+def test_load_of_one_side(dtype, d, Hkv, side):
+    """The library's call with K or V alone: values, padding, and the status of a slot behind the pool."""
+    b = _binding()
+    page, pages, n = 32, 5, 70
+    g = torch.Generator(device="cuda").manual_seed(d + Hkv)
+    pool = torch.randint(0, 248, (pages, Hkv, b.PagedCache4.bytes(page, d)), generator=g, device="cuda").to(torch.uint8)
+    slots = torch.randint(0, pages * page, (n,), generator=g, device="cuda")
+    slots[2] = -1
+    status = _ints([0])
+    desc = b.Pages4Desc(pool.data_ptr(), pool.stride(0), pool.stride(1), pages, page, Hkv, d, status.data_ptr())
+    want = p4.decoded(pool, page, d)[side][slots.clamp(min=0) // page, :, slots.clamp(min=0) % page]
+    want[2] = 0
+    for behind in (None, 0, n - 1):
+        if behind is not None:
+            slots[behind] = pages * page + 3
+        out = torch.full((n, Hkv, d), 7.0, device="cuda").to(dtype)
+        heads = [b.Heads(None, 0, 0), b.Heads(None, 0, 0)]
+        heads[side] = b.Heads(out.data_ptr(), Hkv * d, d)
+        assert b.load().subgen_paged4_load(desc, slots.data_ptr(), n, C.byref(heads[0]), C.byref(heads[1]), 0 if dtype is F32 else 1, _stream()) == 0
+        kept = torch.ones(n, dtype=torch.bool, device="cuda")
+        if behind is not None:
+            kept[behind] = False
+            if behind:
+                kept[0] = False
+            assert out[~kept].isnan().all()
+        assert torch.equal(out[kept].double(), want[kept])
+        assert int(status) == (0 if behind is None else b.ST_PAGE)
+        status.zero_()
