@@ -326,7 +326,8 @@ PyObject* load4(PyObject*, PyObject* const* a, Py_ssize_t got) {
             if (o == Py_None) h.o = wrapped(part_of(both_new, w.type, {n, c->Hkv, c->d}, at));
             else Py_INCREF(o);
             h.mine = true;
-            return std::make_pair(rows(*tensor(h.o, name), name, w, n, c->Hkv, c->d), h.release());
+            const subgen_heads lies = rows(*tensor(h.o, name), name, w, n, c->Hkv, c->d);           // before the release: it may refuse
+            return std::make_pair(lies, h.release());
         };
         const auto [hk, ko] = out(a[4], "K", 0);
         Held k(ko);

@@ -1,5 +1,6 @@
 """The 4-bit paged cache and the tables of a step where the calls of test_gpu_paged4.py do not go."""
 import ctypes as C
+import sys
 
 import pytest
 import torch
@@ -56,3 +57,19 @@ def test_load_of_one_side(dtype, d, Hkv, side):
         assert torch.equal(out[kept].double(), want[kept])
         assert int(status) == (0 if behind is None else b.ST_PAGE)
         status.zero_()
+
+
+def test_load_refuses_outputs_without_keeping_them():
+    b = _binding()
+    cache = b.PagedCache4(torch.zeros(2, 2, b.PagedCache4.bytes(16, 64), dtype=torch.uint8, device="cuda"), 16, 64)
+    slots = torch.zeros(3, dtype=torch.int64, device="cuda")
+    good = torch.empty(3, 2, 64, dtype=BF, device="cuda")
+    for bad in (torch.empty(3, 2, 128, dtype=BF, device="cuda"), torch.empty(3, 2, 64, device="cuda"), torch.empty(3, 2, 64, dtype=BF)):
+        counts = [sys.getrefcount(x) for x in (good, bad)]
+        for K, V in ((bad, None), (None, bad), (good, bad), (bad, good)):
+            with pytest.raises(ValueError, match="must be a"):
+                cache.load(slots, BF, K=K, V=V)
+        with pytest.raises(b.SubgenError):                   # refused by the library
+            cache.load(slots, BF, K=good, V=good)
+        del K, V
+        assert [sys.getrefcount(x) for x in (good, bad)] == counts
