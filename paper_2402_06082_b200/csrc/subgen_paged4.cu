@@ -250,7 +250,7 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     cfg.numAttrs = 1;
     CUDA_TRY(cudaLaunchKernelEx(&cfg, page_step_kernel, a));
     if (!a.split) return SUBGEN_OK;
-    const int parts = (x->n + kSlotThreads - 1) / kSlotThreads;      // a turn a warp
+    const int parts = (x->n - 1) / kSlotThreads + 1;      // a turn a warp
     cfg.gridDim = dim3((unsigned)(parts < 4 * kSMs ? parts : 4 * kSMs));
     cfg.blockDim = dim3(kSlotThreads);
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -170,15 +170,16 @@ __device__ __forceinline__ int row_from(const int* scan, int B, int i, int r) {
 // 8.2 us like this, 10.2 with four turns; 1024 rows with 118000 tokens 16.4, 17.2 with two and 20.5 with four.)
 template <typename F>
 __device__ __forceinline__ void share_out(const int* scan, int B, int count, F f) {
-    const int warps = gridDim.x * (blockDim.x / 32), per = ((count + warps - 1) / warps + 31) & ~31;
-    const long long from = (long long)(blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5)) * per;
-    const int end = (int)min((long long)count, from + per);
+    const unsigned warps = gridDim.x * (blockDim.x / 32), per = (((unsigned)count + warps - 1) / warps + 31) & ~31u;     // a count may be 2^31 - 1
+    const unsigned long long from = (unsigned long long)(blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5)) * per;
+    const unsigned end = (unsigned)min((unsigned long long)count, from + per);
     int r = 0;
 #pragma unroll 1
-    for (int i0 = (int)min((long long)count, from); i0 < end; i0 += 32) {
-        const int i = i0 + (threadIdx.x & 31), mine = row_from(scan, B, i, r);
+    for (unsigned i0 = (unsigned)min((unsigned long long)count, from); i0 < end; i0 += 32) {
+        const unsigned i = i0 + (threadIdx.x & 31);
+        const int mine = row_from(scan, B, (int)min(i, end - 1), r);
         r = __shfl_sync(0xffffffffu, mine, 0);                       // numbers grow, rows do
-        if (i < end) f(i, mine);
+        if (i < end) f((int)i, mine);
     }
 }
 

@@ -73,3 +73,34 @@ def test_load_refuses_outputs_without_keeping_them():
             cache.load(slots, BF, K=good, V=good)
         del K, V
         assert [sys.getrefcount(x) for x in (good, bad)] == counts
+
+
+# ---- the tables of a step ----
+
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 4000])
+def test_page_step_for_the_most_tokens(n):
+    """Slots and positions of 2^31 - 1 tokens: all of them are written, the last row's too."""
+    b = _binding()
+    slots, positions = torch.full((n,), 5, dtype=torch.int64, device="cuda"), torch.full((n,), 5, dtype=torch.int32, device="cuda")
+    wide = (2 ** 31 - 1024) // 1024 - 1
+    added = [3, 0, wide * 1024]                              # the last row takes all but what is behind
+    table = torch.zeros(3, wide, dtype=torch.int32, device="cuda")
+    free = torch.arange(wide + 1, dtype=torch.int32, device="cuda")
+    status = _ints([0])
+    x = b.page_step(_ints([0, 0, 0]), table, free, _ints([wide + 1]), _ints(added), 1024, n, slots=slots, positions=positions, status=status)
+    total = 3 + wide * 1024
+    if total > n:
+        assert int(status) == b.ST_CAPACITY and x.cu_q.tolist() == [0, 3, 3, 3]
+        total = 3
+    else:
+        assert int(status) == 0 and x.cu_q.tolist() == [0, 3, 3, total]
+        assert positions[:5].tolist() == [0, 1, 2, 0, 1] and slots[:5].tolist() == [wide * 1024, wide * 1024 + 1, wide * 1024 + 2, (wide - 1) * 1024, (wide - 1) * 1024 + 1]
+        for at in (3 + 1024 * 1000, total - 1024):
+            page = (at - 3) // 1024
+            assert (slots[at:at + 1024] == (wide - 1 - page) * 1024 + torch.arange(1024, device="cuda")).all()
+            assert (positions[at:at + 1024] == page * 1024 + torch.arange(1024, device="cuda")).all()
+    step = 1 << 28
+    for i in range(total, n, step):
+        assert (slots[i:i + step] == -1).all() and (positions[i:i + step] == 0).all()
+    for i in range(3, total, step):
+        assert int(slots[i:min(i + step, total)].min()) >= 0
