@@ -395,8 +395,34 @@ struct Attend {
     int fresh;                                        // o holds nothing yet: NaN where nothing can be computed
 };
 
+// The weight of an entry's first `units` row units of 2^ru_shift rows, each LEAD + its tiles of 2^kt_shift tokens, 0 where it has none;
+// `prefix` tiles before its own, tokens of 2^g_shift rows, which see their own tokens as Plan::own_limit says. Unit k's last row sees
+// b + (k + 1) t of them, b = S - nq, t = 2^(ru_shift - g_shift) (clipped to [0, S]), so the sum of ceil((b + j t) / KT) is one of floor(i / c),
+// c = KT / t. Out of line: short calls should not have to pass through its code.
+__host__ __device__ __noinline__ inline long long first_units_weight(int units, int S, int nq, int prefix, int causal, int ru_shift, int g_shift, int kt_shift, int lead) {
+    const long long KT = 1LL << kt_shift, whole = prefix + (S + KT - 1) / KT;
+    if (!causal) return whole ? units * (lead + whole) : 0;
+    const int t_shift = ru_shift - g_shift, c_shift = kt_shift - t_shift;        // both >= 0
+    const long long b = (long long)S - nq, all = ((long long)nq + (1LL << t_shift) - 1) >> t_shift;
+    long long blind = b < 0 ? (-b) >> t_shift : 0;                   // units that see nothing of their own
+    if (blind > units) blind = units;
+    long long n = units, w = prefix ? blind * (lead + prefix) : 0;
+    if (n == all && n > blind) { --n; w += whole ? lead + whole : 0; }           // the last unit sees all, whole or not
+    if (n <= blind) return w;
+    auto floors = [&](long long i) {                                 // of j / c for j < i
+        const long long q = i >> c_shift, r = i - (q << c_shift);
+        return (q * (q - 1) / 2 << c_shift) + q * r;
+    };
+    const long long at = (b + KT - 1) >> t_shift;
+    return w + (n - blind) * (lead + prefix) + floors(at + n + 1) - floors(at + blind + 1);
+}
+
 template <int RU, int KT, int DUAL, int LEAD>
 struct Plan {
+    // Small units: there may be any number of them, and what comes before one is summed up instead of walked through (a launch with 524288
+    // units of 8 rows walked for seconds). Larger ones, and small ones in calls that have few rows a sequence, are walked faster.
+    static constexpr bool kSum = RU <= 16 && KT == 128 && !DUAL;
+    static constexpr int kWalk = 16;                                 // units that are walked through
     const PagedView& P;
     const Attend& a;
     const int* tscan;                                 // [E+1] weights before each entry, per head
@@ -482,6 +508,10 @@ struct Plan {
     }
     __device__ static __forceinline__ int shift(int rows) { return RU >= 128 && rows > RU / 2 ? 1 : 0; }     // a tile weighs 1 << shift
     __device__ __forceinline__ int unit_weight(int tiles, int rows) const { return tiles ? LEAD + (tiles << shift(rows)) : 0; }
+    __device__ __forceinline__ long long units_before(const Entry& e, int ru) const {
+        constexpr int RUS = RU == 8 ? 3 : 4;
+        return first_units_weight(ru, e.S, e.nq, prefix_tiles(e), a.causal, RUS, a.g_shift, 7, LEAD);
+    }
     // tiles of a unit before position p of its weight
     __device__ static __forceinline__ int tile_at(int p, int sh) { return p <= LEAD ? 0 : (p - LEAD + sh) >> sh; }
 
@@ -510,7 +540,10 @@ struct Plan {
             long long w = 0;
             int sl = 0;
             if (bad) *flag = 1;
-            else {
+            else if (kSum && e.rows > kWalk * RU) {
+                w = units_before(e, (e.rows + RU - 1) / RU);
+                sl = e.rows;
+            } else {
 #pragma unroll 1
                 for (int ru = 0; ru * RU < e.rows; ++ru) {
                     const int rows = unit_rows(e, ru);
@@ -584,6 +617,15 @@ struct Plan {
         g.e = entry(lo);
         g.kp = prefix_tiles(g.e);
         int ru = 0, w;
+        if (kSum && g.e.rows > kWalk * RU) {                         // the last unit that starts at r or before
+            int last = (g.e.rows - 1) / RU;
+#pragma unroll 1
+            while (ru < last) {
+                const int mid = (ru + last + 1) >> 1;
+                if (units_before(g.e, mid) <= r) ru = mid; else last = mid - 1;
+            }
+            r -= (int)units_before(g.e, ru);
+        }
 #pragma unroll 1
         while (true) {
             g.rows = unit_rows(g.e, ru);
@@ -671,6 +713,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
     // first position of the line that belongs to row unit ru of a sequence's entry
     auto unit_start = [&](const Entry& e, int ei, int h, int ru) {
         int u0 = h * plan.head_w + plan.tscan[ei];
+        if (PlanT::kSum && ru > PlanT::kWalk) return u0 + (int)plan.units_before(e, ru);
 #pragma unroll 1
         for (int k = 0; k < ru; ++k) u0 += plan.unit_weight(plan.unit_tiles(e, k), RU);
         return u0;

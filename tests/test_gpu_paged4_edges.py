@@ -6,6 +6,8 @@ import pytest
 import torch
 
 import paged4_helpers as p4
+from paged4_helpers import Setting4
+from paged_helpers import assert_within
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -73,6 +75,38 @@ def test_load_refuses_outputs_without_keeping_them():
             cache.load(slots, BF, K=good, V=good)
         del K, V
         assert [sys.getrefcount(x) for x in (good, bad)] == counts
+
+
+# ---- attend ----
+
+def test_half_a_million_row_units():
+    """fp32 rows by the million against a short memory: units of 8 rows, whose place in the division of the work is not walked to."""
+    b = _binding()
+    n, H, d, own = 1 << 19, 8, 64, 200
+    s = Setting4([n], [own], H, 1, d, F32, page=64, seed=21)
+    cache = s.cache()
+    got = cache.attend(s.batch(), s.q, scale=0.125, causal=False)
+    assert cache.status() == 0
+    some = torch.cat([torch.arange(40), torch.randint(0, n, (200,), generator=torch.Generator().manual_seed(0)), torch.arange(n - 40, n)]).cuda()
+    K, V = p4.decoded(s.pool, 64, d)
+    want, bound = p4.attend(s.q[some], K, V, [0, len(some)], [own], s.table, 0.125, False)
+    assert_within(got[some], want, bound)
+    k, v = (x[s.table[0].long(), 0].flatten(0, 1)[:own].float() for x in (K, V))
+    for i in range(0, n, 1 << 16):                           # every row: none is left out
+        y = torch.softmax(s.q[i:i + (1 << 16)] @ k.T * 0.125, -1) @ v
+        assert (got[i:i + (1 << 16)] - y).abs().max() < 1e-2
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("causal", [True, False])
+def test_one_prompt_among_single_tokens(dtype, causal):
+    """Hundreds of small row units of one sequence (fp32, and bf16 without a prefix), behind a prefix or not, some of them blind."""
+    for new, own, edges, prefix in (([1] * 150 + [1000] + [1] * 150, [50] * 150 + [1030] + [9] * 150, [], []),
+                                    ([1] * 140 + [999], [3] * 140 + [400], [0, 140, 141], [100, 130]), ([1] * 140 + [999], [3] * 140 + [400], [0, 141], [300])):
+        s = Setting4(new, own, 4, 1, 64, dtype, seed=len(new), edges=edges, prefix=prefix)
+        cache = s.cache()
+        assert_within(cache.attend(s.batch(), s.q, scale=0.125, causal=causal), *s.want(0.125, causal))
+        assert cache.status() == 0
 
 
 # ---- the tables of a step ----
