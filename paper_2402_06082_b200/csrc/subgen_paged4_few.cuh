@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(kP4Threads, kP4Blocks<NT>) paged4_attend_few_k
                     if constexpr (PIECES == 2) to[D / 2] = rest(u0, u1, h);
                 }
                 const float cc = a.c * 8.f * __uint_as_float((unsigned)(ex - 14) << 23);
-                if (lane == 0) sm.factor[row] = cc < 1.1754944e-38f ? 1.1754944e-38f : cc;       // not 0: times -infinity it would be NaN
+                // not 0, which times -infinity would be NaN, nor infinite, which times 0 would be
+                if (lane == 0) sm.factor[row] = fminf(fmaxf(cc, 1.1754944e-38f), 3.4028235e38f);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the next run's queries come by a copy
             __syncwarp();

@@ -109,6 +109,23 @@ def test_one_prompt_among_single_tokens(dtype, causal):
         assert cache.status() == 0
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new, own", [([1], [300]), ([5, 2], [5, 900]), ([80], [200])])
+def test_scores_of_zero_whatever_the_scale(dtype, new, own):
+    """Keys of zeros: every token weighs the same, also where queries times the scale leave fp32."""
+    s = Setting4(new, own, 4, 1, 64, dtype, seed=31)
+    for row, length in zip(s.table, own):
+        tok = torch.arange(length, device="cuda")
+        none = torch.zeros(length, 1, 64, device="cuda")
+        p4.put(s.pool, 16, 64, 0, row[tok // 16].long(), tok % 16, *p4.rounded(none)[:2])
+    cache = s.cache()
+    plain = cache.attend(s.batch(), s.q, scale=1.0)
+    assert not plain.isnan().any()
+    s.q.fill_(2.0 ** 127)
+    for scale in (1.0, 2.0 ** 14, 2.0 ** 100):
+        assert torch.equal(cache.attend(s.batch(), s.q, scale=scale), plain)
+
+
 # ---- the tables of a step ----
 
 @pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 4000])
