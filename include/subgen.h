@@ -512,6 +512,9 @@ int subgen_paged4_attend(const subgen_pages4* cache, const subgen_batch* batch, 
  *    new tokens, and SUBGEN_ST_CAPACITY is set.
  * 3. cu_q[b] .. cu_q[b + 1] - 1 are the new tokens of row b; slots[i] = table entry * page + row in it of new token i, positions[i] = its
  *    index in its sequence, plus first[b] where given (the length of a prefix). From cu_q[B] on up to n: -1 and 0.
+ *    A row that is not served has none, so the new tokens of the rows behind it are cu_q's, not where `added` alone would put them: inputs
+ *    that lie by `added` (row b's tokens from added[0] + ... + added[b - 1] on, at most n in all) have to be taken to cu_q's places before a
+ *    call on the cache. sources[i], where given, is the place among them of new token i; from cu_q[B] on 0 (always below n).
  * cu_q, lengths_out and table are what a subgen_batch takes, slots what subgen_paged4_load takes, positions what
  * subgen_qk_norm_rope takes. lengths_out may be lengths, free_count_out may be free_count; the table and the stack change in
  * place. No other two arrays may overlap.
@@ -535,6 +538,7 @@ typedef struct subgen_page_step_args {
     int64_t* slots;         /* device [n] */
     int* positions;         /* device [n] */
     int* status;            /* sticky SUBGEN_ST_* bits, or NULL */
+    int* sources;           /* device [n], or NULL */
 } subgen_page_step_args;
 int subgen_page_step(const subgen_page_step_args* args, void* stream);
 

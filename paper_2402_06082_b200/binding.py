@@ -94,7 +94,7 @@ class AttendArgs(C.Structure):
 class PageStepArgs(C.Structure):
     _fields_ = [("B", C.c_int), ("n", C.c_int), ("pages", C.c_int), ("page", C.c_int), ("table", C.c_void_p), ("table_stride", C.c_int)] + [
         (k, C.c_void_p) for k in ("free_pages", "free_count", "lengths", "added", "ended", "first", "free_count_out", "lengths_out", "cu_q",
-                                  "slots", "positions", "status")]
+                                  "slots", "positions", "status", "sources")]
 
 
 class SubgenError(RuntimeError):
@@ -665,24 +665,28 @@ class PageStep(NamedTuple):
 
 def page_step(lengths: torch.Tensor, table: torch.Tensor, free: torch.Tensor, free_count: torch.Tensor, added: torch.Tensor, page: int, n: int,
               *, ended: Optional[torch.Tensor] = None, first: Optional[torch.Tensor] = None, in_place: bool = True, cu_q: Optional[torch.Tensor] = None,
-              slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> PageStep:
+              slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+              sources: Optional[torch.Tensor] = None) -> PageStep:
     """The tables of a step, on the device (see subgen_page_step): rows that ended give their pages back, rows with new tokens get pages.
 
     lengths, added, ended, first [B], table [B, m], free [pages], free_count, status [1]: int32. The table and the stack of free pages change
     in place; lengths and free_count too, or (in_place=False) into new tensors. n: rows of the step's tensors, which slots and positions are
-    made for. added may ask for more than there is: rows that are not served get no new tokens.
+    made for. added may ask for more than there is: rows that are not served get no new tokens, and those of the rows behind them move up. sources
+    (int32 [n], an output) then tells which of the tokens that were asked for each one is: inputs that lie by `added` are taken by it.
     """
     if _calls is None:
         _bind_calls()
     return PageStep(*_calls.page_step(lengths, table, free, free_count, added, page, n, ended, first, lengths if in_place else None,
-                                      free_count if in_place else None, cu_q, slots, positions, status))
+                                      free_count if in_place else None, cu_q, slots, positions, status, sources))
 
 
 class PageTables:
     """Lengths, page tables and free pages of B requests over a pool, kept on the device, and the batch that a paged cache's calls take.
 
-    step() serves a step's new tokens and moves on; a captured graph may hold it and the calls behind it, since batch, slots and positions
-    stay where they are. A row's request is over when `ended` says so, and the row is free for the next one, in the same step if it has to be.
+    step() serves a step's new tokens and moves on; a captured graph may hold it and the calls behind it, since batch, slots, positions and
+    sources stay where they are. A row that is not served (status()) gets nothing, and what is behind it moves up: q[tables.sources] are the
+    rows of a q that holds all tokens that were asked for, [n, ...] (its row 0 behind the last).
+    A row's request is over when `ended` says so, and the row is free for the next one, in the same step if it has to be.
     """
 
     def __init__(self, B: int, pages_per_row: int, pages: int, page: int, n: int, device="cuda"):
@@ -691,7 +695,7 @@ class PageTables:
         self.lengths, self.table, self.cu_q, self._status = ints(B), ints(B, pages_per_row), ints(B + 1), ints(1)
         self.free = torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device)      # page 0 is on top
         self.free_count = torch.full((1,), pages, dtype=torch.int32, device=device)
-        self.slots, self.positions = torch.full((self.n,), -1, dtype=torch.int64, device=device), ints(self.n)
+        self.slots, self.positions, self.sources = torch.full((self.n,), -1, dtype=torch.int64, device=device), ints(self.n), ints(self.n)
         self.batch = PagedBatch(self.cu_q, self.lengths, self.table)
         if not torch.cuda.is_current_stream_capturing():   # as they are before a call on any stream reads them
             torch.cuda.current_stream(self.lengths.device).synchronize()
@@ -700,7 +704,7 @@ class PageTables:
         """added [B]: the tokens that each request gets now; ended [B]: nonzero where a request is over (both int32). What is given back is
         what the object holds: the next step changes it."""
         return page_step(self.lengths, self.table, self.free, self.free_count, added, self.page, self.n, ended=ended, cu_q=self.cu_q,
-                         slots=self.slots, positions=self.positions, status=self._status)
+                         slots=self.slots, positions=self.positions, status=self._status, sources=self.sources)
 
     def status(self) -> int:
         """Waits for the device's work, returns the status bits that steps have set: ST_CAPACITY where a row was not served (0: none)."""

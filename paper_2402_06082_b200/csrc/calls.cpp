@@ -344,10 +344,10 @@ PyObject* load4(PyObject*, PyObject* const* a, Py_ssize_t got) {
     });
 }
 
-// (lengths, table, free, free_count, added, page, n, ended, first, lengths_out, free_count_out, cu_q, slots, positions, status)
-// -> (cu_q, lengths_out, free_count_out, slots, positions); outputs that are None are made
+// (lengths, table, free, free_count, added, page, n, ended, first, lengths_out, free_count_out, cu_q, slots, positions, status,
+// sources) -> (cu_q, lengths_out, free_count_out, slots, positions); outputs among these that are None are made
 PyObject* page_step(PyObject*, PyObject* const* a, Py_ssize_t got) {
-    if (!count(got, 15)) return nullptr;
+    if (!count(got, 16)) return nullptr;
     return guarded([&]() -> PyObject* {
         const at::Tensor *lengths = tensor(a[0], "lengths"), *table = tensor(a[1], "table"), *free = tensor(a[2], "free");
         if (!lengths || !table || !free || lengths->dim() != 1 || table->dim() != 2 || free->dim() != 1) refuse("lengths, table and free must be tensors of one, two and one axes");
@@ -368,6 +368,7 @@ PyObject* page_step(PyObject*, PyObject* const* a, Py_ssize_t got) {
         p.ended = (const int*)whole(a[7], "ended", at::kInt, dev, B);
         p.first = (const int*)whole(a[8], "first", at::kInt, dev, B);
         p.status = (int*)whole(a[14], "status", at::kInt, dev, 1);
+        p.sources = (int*)whole(a[15], "sources", at::kInt, dev, n);
         PyObject* five = PyTuple_New(5);
         if (!five) throw std::bad_alloc();
         Held held(five);

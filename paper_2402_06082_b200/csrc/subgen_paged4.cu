@@ -213,7 +213,7 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     if (x->B < 1 || x->B > kPlanMax || x->n < 0) return fail(SUBGEN_EINVAL, "%s: B must be 1 to %d, n >= 0", fn, kPlanMax);
     if (!x->table || !x->free_pages || !x->free_count || !x->lengths || !x->added || !x->free_count_out || !x->lengths_out || !x->cu_q ||
         (x->n && (!x->slots || !x->positions)))
-        return fail(SUBGEN_EINVAL, "%s: only ended, first and status may be NULL", fn);
+        return fail(SUBGEN_EINVAL, "%s: only ended, first, status and sources may be NULL", fn);
     if (x->table_stride <= 0 || (long long)x->table_stride * x->page > 0x7fffffffLL - 1024)
         return fail(SUBGEN_EINVAL, "%s: table_stride must be positive, a row of fewer than 2^31 - 1024 tokens", fn);
     if ((long long)x->B * x->table_stride >= 0x7fffffffLL) return fail(SUBGEN_EINVAL, "%s: a table must hold fewer than 2^31 - 1 pages", fn);
@@ -222,7 +222,7 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     a.B = x->B; a.n = x->n; a.pages = x->pages; a.page_shift = shift_of(x->page); a.stride = x->table_stride;
     a.table = x->table; a.free = x->free_pages;
     a.free_count = x->free_count; a.lengths = x->lengths; a.added = x->added; a.ended = x->ended; a.first = x->first;
-    a.free_count_out = x->free_count_out; a.lengths_out = x->lengths_out; a.cu_q = x->cu_q; a.positions = x->positions;
+    a.free_count_out = x->free_count_out; a.lengths_out = x->lengths_out; a.cu_q = x->cu_q; a.positions = x->positions; a.sources = x->sources;
     a.slots = (long long*)x->slots;
     a.status = x->status;
     a.split = x->n > 4 * kStepThreads;

@@ -112,7 +112,7 @@ struct PageStep {
     int B, n, pages, page_shift, stride;
     int *table, *free;
     const int *free_count, *lengths, *added, *ended, *first;
-    int *free_count_out, *lengths_out, *cu_q, *positions;
+    int *free_count_out, *lengths_out, *cu_q, *positions, *sources;       // sources may be NULL
     long long* slots;
     int* status;
     int split;                                        // slots and positions are the second kernel's
@@ -183,24 +183,27 @@ __device__ __forceinline__ void share_out(const int* scan, int B, int count, F f
     }
 }
 
-__device__ __forceinline__ void put_slot(const PageStep& a, int i, bool there, int id, int place, int lead) {
+// source: of token i among those asked for
+__device__ __forceinline__ void put_slot(const PageStep& a, int i, bool there, int id, int place, int lead, int source) {
     const bool sound = id >= 0 && id < a.pages;
     if (there && !sound && a.status) atomicOr(a.status, kStPage);
     a.slots[i] = there && sound ? ((long long)id << a.page_shift) + (place & ((1 << a.page_shift) - 1)) : -1;
     a.positions[i] = there ? place + lead : 0;
+    if (a.sources) a.sources[i] = there ? (int)min((unsigned)source, (unsigned)a.n - 1) : 0;
 }
 
 __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
     pdl_trigger();
     __shared__ unsigned sums[3][32];
-    __shared__ int back[kPlanMax], cu[kPlanMax], take[kPlanMax], kept[kPlanMax], held[kPlanMax], lead[kPlanMax];
+    __shared__ int back[kPlanMax], cu[kPlanMax], take[kPlanMax], kept[kPlanMax], held[kPlanMax], lead[kPlanMax], ask[kPlanMax];
     const int b = threadIdx.x, page = 1 << a.page_shift, me = blockIdx.x, blocks = gridDim.x;
     const bool mine = b < a.B;
-    int len = 0, add = 0, wrong = 0;
+    int len = 0, add = 0, raw = 0, wrong = 0;
     bool end = false, sound = true;
     if (mine) {
         len = __ldg(a.lengths + b);
         add = __ldg(a.added + b);
+        raw = max(add, 0);
         end = a.ended && __ldg(a.ended + b) != 0;
         lead[b] = a.first ? __ldg(a.first + b) : 0;
         sound = len >= 0 && len <= (long long)a.stride << a.page_shift;
@@ -231,6 +234,11 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
         kept[b] = stay;
         held[b] = has;
     }
+    if (a.sources && !a.split) {                                     // tokens asked for before each row, whatever its length says
+        unsigned before[1] = {(unsigned)raw}, sum[1];
+        block_scan<1>(before, sums, sum);
+        ask[b] = (int)before[0] - raw;
+    }
     __syncthreads();
     // a warp's pages and tokens follow each other (searched for one by one, all threads apart, 1024 rows with 118000 new tokens took
     // 31 us: 8 SMs' instructions)
@@ -258,25 +266,50 @@ __global__ void __launch_bounds__(kStepThreads) page_step_kernel(PageStep a) {
         const int place = kept[r] + i - cu[r], p = place >> a.page_shift;
         int id = -1;
         if (i < tokens) id = p < held[r] ? __ldcg(a.table + (long long)r * a.stride + p) : __ldcg(a.free + top - 1 - (take[r] + p - held[r]));
-        put_slot(a, i, i < tokens, id, place, lead[r]);
+        put_slot(a, i, i < tokens, id, place, lead[r], a.sources ? ask[r] + i - cu[r] : 0);
     });
 }
 
 // Slots and positions from the step's results: offsets, lengths and tables, the new tokens among them.
 __global__ void __launch_bounds__(kSlotThreads) page_slots_kernel(PageStep a) {
-    __shared__ int cu[kPlanMax + 1];
+    __shared__ int cu[kPlanMax + 1], ask[kPlanMax];
+    __shared__ unsigned sums[kSlotThreads / 32];
     pdl_wait();
     for (int b = threadIdx.x; b <= a.B; b += kSlotThreads) cu[b] = __ldcg(a.cu_q + b);
+    if (a.sources) {                                                 // tokens asked for before each row, a thread a few rows
+        constexpr int R = kPlanMax / kSlotThreads;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        unsigned add[R], sum = 0;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const int b = threadIdx.x * R + k;
+            add[k] = b < a.B ? max(__ldg(a.added + b), 0) : 0;
+            sum += add[k];                                           // (may pass 31 bits behind the last token that an input of n rows has)
+        }
+        unsigned at = sum;
+#pragma unroll 1
+        for (int off = 1; off < 32; off <<= 1) {
+            const unsigned y = __shfl_up_sync(0xffffffffu, at, off);
+            if (lane >= off) at += y;
+        }
+        if (lane == 31) sums[warp] = at;
+        __syncthreads();
+        for (int k = 0; k < warp; ++k) at += sums[k];
+        at -= sum;
+#pragma unroll
+        for (int k = 0; k < R; ++k) { ask[threadIdx.x * R + k] = (int)at; at += add[k]; }
+    }
     __syncthreads();
     const int tokens = cu[a.B];
     share_out(cu, a.B, a.n, [&](int i, int r) {
-        int id = -1, place = 0, lead = 0;
+        int id = -1, place = 0, lead = 0, source = 0;
         if (i < tokens) {
             place = __ldcg(a.lengths_out + r) - cu[r + 1] + i;
             lead = a.first ? __ldg(a.first + r) : 0;
             id = __ldcg(a.table + (long long)r * a.stride + (place >> a.page_shift));
+            if (a.sources) source = ask[r] + i - cu[r];
         }
-        put_slot(a, i, i < tokens, id, place, lead);
+        put_slot(a, i, i < tokens, id, place, lead, source);
     });
 }
 

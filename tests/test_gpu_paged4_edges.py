@@ -1,5 +1,6 @@
 """The 4-bit paged cache and the tables of a step where the calls of test_gpu_paged4.py do not go."""
 import ctypes as C
+import random
 import sys
 
 import pytest
@@ -155,3 +156,92 @@ def test_page_step_for_the_most_tokens(n):
         assert (slots[i:i + step] == -1).all() and (positions[i:i + step] == 0).all()
     for i in range(3, total, step):
         assert int(slots[i:min(i + step, total)].min()) >= 0
+
+
+def _sources(cu, added, n):
+    """By the definition: token i of a step is that row's token, counted from where `added` alone puts the row; below n, which no input passes."""
+    out, at = [], 0
+    for b, k in enumerate(added):
+        out += [min(at + i, n - 1) for i in range(cu[b + 1] - cu[b])]
+        at += max(k, 0)
+    return out + [0] * (n - len(out))
+
+
+@pytest.mark.parametrize("B, most, n", [(1, 5, 9), (40, 3, 70), (1024, 2, 900), (129, 60, 3000), (300, 60, 7000), (1000, 30, 14000)])
+def test_sources(B, most, n):
+    """Where a step's tokens lie in inputs that hold what was asked for, with rows that are not served; one kernel and two."""
+    b = _binding()
+    r = random.Random(B)
+    for turn in range(3):
+        added = [r.randint(0, most) for _ in range(B)]
+        if turn == 2:
+            added[B // 2] = 2 ** 31 - 1                      # nobody behind it is served
+        lengths = [r.randint(0, 40) for _ in range(B)]
+        if turn:
+            lengths[B // 3] = -1                             # gets nothing, and its tokens are in the input
+        pages = 5 * B + 200
+        ids = list(range(pages))
+        table = [[ids.pop() if k < -(-max(x, 0) // 16) else -1 for k in range(10)] for x in lengths]
+        count = len(ids) if not turn else B // 2
+        ids += [0] * (pages - len(ids))                      # the stack has room for all of the pool's pages
+        sources, status = torch.full((n,), 9, dtype=torch.int32, device="cuda"), _ints([0])
+        x = b.page_step(_ints(lengths), _ints(table), _ints(ids), _ints([count]), _ints(added), 16, n, sources=sources, status=status)
+        cu = x.cu_q.tolist()
+        if not turn:                                         # pages and places for all whose tokens come before the n-th
+            total = 0
+            for k, y, z in zip(added, cu, cu[1:]):
+                total += k
+                assert z - y == (k if total <= n else 0)
+        assert sources.tolist() == _sources(cu, added, n)
+        assert (x.slots[: cu[-1]] >= 0).all()
+
+
+def test_page_tables_that_run_out():
+    """Requests in a captured graph on a pool that is too small: tables, stack, lengths and inputs of every step as a host program has
+    them, the values that are read back those of each request's own inputs."""
+    b = _binding()
+    B, Hkv, d, page, n, pages, wide = 6, 2, 64, 16, 64, 9, 5
+    tables = b.PageTables(B, wide, pages, page, n)
+    cache = b.PagedCache4(torch.zeros(pages, Hkv, b.PagedCache4.bytes(page, d), dtype=torch.uint8, device="cuda"), page, d)
+    k, v = (torch.zeros(n, Hkv, d, device="cuda") for _ in "kv")
+    added, ended = _ints([0] * B), _ints([0] * B)
+
+    def once():
+        tables.step(added, ended)
+        i = tables.sources
+        cache.append(tables.batch, k[i], v[i])
+        return cache.load(tables.slots, F32)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        once()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        K, V = once()
+    r = random.Random(5)
+    lengths, table, free, count = [0] * B, [[0] * wide for _ in range(B)], list(range(pages - 1, -1, -1)), pages
+    short = []
+    for turn in range(25):
+        over = [int(r.random() < 0.15) for _ in range(B)]
+        new = [r.choice([0, 1, 5, 20]) for _ in range(B)]
+        while sum(new) > n:
+            new = [x // 2 for x in new]
+        added.copy_(_ints(new))
+        ended.copy_(_ints(over))
+        for x in (k, v):
+            x.copy_(torch.randn(x.shape, device="cuda"))
+        tables._status.zero_()
+        graph.replay()
+        cu, lengths, count, slots, positions, served = p4.step(lengths, table, free, count, new, page, n, over)
+        assert tables.status() == (0 if served else b.ST_CAPACITY)
+        short.append(not served)
+        assert tables.cu_q.tolist() == cu and tables.lengths.tolist() == lengths and tables.free_count.tolist() == [count]
+        assert tables.table.tolist() == table and tables.free.tolist() == free
+        assert tables.slots.tolist() == slots and tables.positions.tolist() == positions
+        at, where = [sum(new[:i]) for i in range(B)], []
+        for i in range(B):
+            where += [at[i] + j for j in range(cu[i + 1] - cu[i])]
+        for got, x in ((K, k), (V, v)):
+            assert torch.equal(got[: cu[-1]].double(), p4.rounded(x[where])[2])
+    assert any(short) and not all(short) and cache.status() == 0
