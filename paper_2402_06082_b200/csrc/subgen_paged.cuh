@@ -282,13 +282,18 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
                     }
                     if (KIND < 2 && turn) {
                         if constexpr (PAGED == 2) {
-#pragma unroll
-                            for (int e = 0; e < VE; ++e) {
-                                // pair e, and its cosine and sine, lie by the layout
-                                float &p = !a.interleaved ? xa[e] : x2[2 * e], &q = !a.interleaved ? xb[e] : x2[2 * e + 1];
+                            auto pair = [](float& p, float& q, float c, float s) {
                                 const float p0 = p, q0 = q;
-                                p = __fsub_rn(__fmul_rn(p0, co[e]), __fmul_rn(q0, si[e]));
-                                q = __fadd_rn(__fmul_rn(q0, co[e]), __fmul_rn(p0, si[e]));
+                                p = __fsub_rn(__fmul_rn(p0, c), __fmul_rn(q0, s));
+                                q = __fadd_rn(__fmul_rn(q0, c), __fmul_rn(p0, s));
+                            };
+                            // two loops: a choice of pairs inside one would put x2 into local memory (prompt chunks 159 us instead of 94)
+                            if (a.interleaved) {
+#pragma unroll
+                                for (int e = 0; e < VE; ++e) pair(x2[2 * e], x2[2 * e + 1], co[e], si[e]);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < VE; ++e) pair(xa[e], xb[e], co[e], si[e]);
                             }
                         } else if (a.interleaved) {
 #pragma unroll
