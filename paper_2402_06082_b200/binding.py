@@ -605,7 +605,7 @@ class PagedCache:
 class PagedCache4:
     """A cache in pages that holds keys and values in 4 bits, 4.5 with their scales (see subgen_pages4): pool [pages, Hkv, bytes] uint8
     with bytes(page, d) on end for each head, owned by the caller (any strides of pages and heads, multiples of 16). Takes fp32 and bf16
-    queries, keys and values, call by call."""
+    queries, keys and values, call by call. (Made while a stream captures, every replay begins with a status of 0.)"""
 
     def __init__(self, pool: torch.Tensor, page: int, d: int):
         dev = self.device = _cuda(pool, "pool")
@@ -687,6 +687,8 @@ class PageTables:
     sources stay where they are. A row that is not served (status()) gets nothing, and what is behind it moves up: q[tables.sources] are the
     rows of a q that holds all tokens that were asked for, [n, ...] (its row 0 behind the last).
     A row's request is over when `ended` says so, and the row is free for the next one, in the same step if it has to be.
+    Make it before a capture. Made while a stream captures, its empty tables are a part of the graph: it holds nothing before the first replay, and
+    every replay begins with no tokens and all pages free.
     """
 
     def __init__(self, B: int, pages_per_row: int, pages: int, page: int, n: int, device="cuda"):

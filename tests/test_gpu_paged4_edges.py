@@ -245,3 +245,24 @@ def test_page_tables_that_run_out():
         for got, x in ((K, k), (V, v)):
             assert torch.equal(got[: cu[-1]].double(), p4.rounded(x[where])[2])
     assert any(short) and not all(short) and cache.status() == 0
+
+
+def test_tables_made_in_a_capture_begin_anew():
+    b = _binding()
+    added = _ints([3, 20, 0])
+    b.PageTables(3, 4, 10, 16, 32).step(added)               # the kernels, before the capture
+    pool = torch.zeros(10, 1, b.PagedCache4.bytes(16, 64), dtype=torch.uint8, device="cuda")
+    k = torch.full((32, 1, 64), 70000.0, device="cuda")      # beyond what has a scale
+    b.PagedCache4(pool, 16, 64).append(b.PageTables(3, 4, 10, 16, 32).batch, k, k)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tables, cache = b.PageTables(3, 4, 10, 16, 32), b.PagedCache4(pool, 16, 64)
+        tables.step(added)
+        tables.step(added)
+        cache.append(tables.batch, k, k)
+    for _ in range(3):
+        cache._status.fill_(b.ST_PAGE)
+        graph.replay()
+        assert tables.lengths.tolist() == [6, 40, 0] and tables.free_count.tolist() == [6] and tables.cu_q.tolist() == [0, 3, 23, 23]
+        assert tables.table.tolist() == [[0, 0, 0, 0], [1, 2, 3, 0], [0, 0, 0, 0]] and tables.status() == 0
+        assert cache.status() == b.ST_RANGE
