@@ -64,23 +64,37 @@ int launch_load(Load4 a, cudaStream_t st) {
 template <typename T, int D, int NT, int TILES>
 constexpr size_t few_smem() { return (sizeof(P4Smem<T, D, NT, TILES>) + 15) & ~(size_t)15; }
 
+// Tiles in flight. A third one where the plan (8 bytes a sequence) leaves room for it with all blocks there at once: 64 sequences 89 -> 86 us.
+// Without room (256 sequences of 1024 tokens) a third of the blocks would run after the others. By size of the rest it fits never, always
+// or with small plans (bf16, D = 128, units of 8 rows: up to 233 sequences and prefixes).
+template <typename T, int D, int NT>
+struct Few {
+    static constexpr size_t kRoom = 233472 / kP4Blocks<NT> - 1024;   // shared memory of a block
+    static constexpr bool kThree = few_smem<T, D, NT, 3>() + plan_bytes(1) <= kRoom, kTwo = few_smem<T, D, NT, 3>() + plan_bytes(kPlanMax) > kRoom;
+    static_assert(few_smem<T, D, NT, 2>() + plan_bytes(kPlanMax) <= kRoom, "two tiles always fit");
+};
+
 template <typename T, int D, int NT>
 int opt_in_few() {
-    int rc = opt_in(paged4_attend_few_kernel<T, D, NT, 3>, paged_merge_kernel<T, D, 8 * NT, kP4KT, 0, kP4Lead>, few_smem<T, D, NT, 3>() + plan_bytes(kPlanMax));
-    if (!rc) rc = opt_in(paged4_attend_few_kernel<T, D, NT, 2>, paged_merge_kernel<T, D, 8 * NT, kP4KT, 0, kP4Lead>, few_smem<T, D, NT, 2>() + plan_bytes(kPlanMax));
+    int rc = SUBGEN_OK;
+    if constexpr (Few<T, D, NT>::kThree)
+        rc = opt_in(paged4_attend_few_kernel<T, D, NT, 3>, paged_merge_kernel<T, D, 8 * NT, kP4KT, 0, kP4Lead>, few_smem<T, D, NT, 3>() + plan_bytes(kPlanMax));
+    if constexpr (Few<T, D, NT>::kTwo)
+        if (!rc) rc = opt_in(paged4_attend_few_kernel<T, D, NT, 2>, paged_merge_kernel<T, D, 8 * NT, kP4KT, 0, kP4Lead>, few_smem<T, D, NT, 2>() + plan_bytes(kPlanMax));
     return rc;
 }
 template <typename T, int D, int NT>
 int attend_few(const PagedView& P, const Attend& a, cudaStream_t st) {
+    typedef Few<T, D, NT> F;
     constexpr int blocks = kSMs * kP4Blocks<NT>;
-    constexpr size_t room = 233472 / kP4Blocks<NT> - 1024;           // shared memory of a block, so that all of them are there at once
     static_assert(8 * NT * kP4Blocks<NT> <= 256, "slot_count");
-    static_assert(few_smem<T, D, NT, 2>() + ((size_t)8 * (kPlanMax + 1) + 15) <= room, "two tiles always fit");
     const size_t plan = plan_bytes(P.B + P.groups);
-    // A third tile in flight where the plan (8 bytes a sequence) leaves room for it: 64 sequences 89 -> 86 us. Without room (256 sequences of
-    // 1024 tokens) a third of the blocks would run after the others.
-    if (few_smem<T, D, NT, 3>() + plan <= room) paged4_attend_few_kernel<T, D, NT, 3><<<blocks, kP4Threads, few_smem<T, D, NT, 3>() + plan, st>>>(P, a);
-    else paged4_attend_few_kernel<T, D, NT, 2><<<blocks, kP4Threads, few_smem<T, D, NT, 2>() + plan, st>>>(P, a);
+    bool three = F::kThree;
+    if (F::kTwo) three = three && few_smem<T, D, NT, 3>() + plan <= F::kRoom;
+    if constexpr (F::kThree)
+        if (three) paged4_attend_few_kernel<T, D, NT, 3><<<blocks, kP4Threads, few_smem<T, D, NT, 3>() + plan, st>>>(P, a);
+    if constexpr (F::kTwo)
+        if (!three) paged4_attend_few_kernel<T, D, NT, 2><<<blocks, kP4Threads, few_smem<T, D, NT, 2>() + plan, st>>>(P, a);
     CUDA_TRY(cudaGetLastError());
     return launch_merge<T, D, 8 * NT, kP4KT, 0, kP4Lead>(P, a, blocks, st);
 }

@@ -171,7 +171,7 @@ void fill_norm_rope(NormRope* a, const subgen_qk_args* x, int H, int Hkv) {
 }
 
 // ---- attention ----
-size_t plan_bytes(int E) { return ((size_t)8 * (E + 1) + 15) & ~(size_t)15; }
+constexpr size_t plan_bytes(int E) { return ((size_t)8 * (E + 1) + 15) & ~(size_t)15; }
 
 long long slot_count(const PagedView& P, int n, int H) {
     // every row once per entry it belongs to; up to 128 rows of an entry's last unit twice, where the two groups of a block
