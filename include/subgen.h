@@ -493,9 +493,11 @@ int subgen_paged4_load(const subgen_pages4* cache, const int64_t* slots, int n, 
 /* As subgen_paged_attend, over the values of the cells; dtype: of q and out. What that says of units of rows, with these numbers:
  * bf16 queries in units of 8 rows (new tokens x H / Hkv) in calls of at most 8 rows a sequence on average, of 16 up to 32 rows
  * (where several sequences share a prefix: up to 32 rows a group), else of 256; fp32 queries in units of 8. Key tiles have 128 tokens.
- * Units of 8 and 16 rows take queries and softmax weights in fp16 (fp32 queries: as two fp16 each, 22 bits), queries scaled by
- * a power of two first, so that what is below 2^-29 of a row's largest coordinate is rounded more coarsely; weights below 2^-31 of
- * the largest count for the sum alone. Units of 256 rows take them in bf16 as the bf16 cache does. */
+ * Softmax weights are rounded to fp16 for the product with V; those below 2^-31 of the largest count for the sum alone. Units of 8 and
+ * 16 rows take queries in fp16 as well, scaled by a power of two first, so that what is below 2^-29 of a row's largest coordinate is rounded
+ * more coarsely. fp32 queries and their weights are two fp16 each, together off by at most 2^-23, twice what fp32 rounds by (a query's
+ * coordinates below 2^-16 of the row's largest, weights below 2^-8 of the largest: by 2^-39 and 2^-31 of that). Units of 256 rows take bf16
+ * queries as they are. No part of the result depends on how blocks are scheduled. */
 size_t subgen_paged4_workspace_bytes(const subgen_pages4* cache, const subgen_batch* batch, int n, int H);
 int subgen_paged4_attend(const subgen_pages4* cache, const subgen_batch* batch, const subgen_attend_args* args, int dtype, void* stream);
 

@@ -127,6 +127,45 @@ def test_scores_of_zero_whatever_the_scale(dtype, new, own):
         assert torch.equal(cache.attend(s.batch(), s.q, scale=scale), plain)
 
 
+@pytest.mark.parametrize("d, H, Hkv", [(64, 8, 1), (128, 8, 2), (128, 4, 4), (64, 2, 1)])
+@pytest.mark.parametrize("new, own, edges, prefix, causal", [
+    ([300], [300], [], [], True), ([129, 64], [1025, 200], [], [], True), ([70, 90], [500, 300], [], [], False), ([60, 70, 90], [60, 100, 400], [0, 2, 3], [333, 128], True),
+    ([40] * 6, [40, 60, 80, 100, 500, 900], [0, 6], [1000], True), ([33, 40], [2000, 3000], [], [], True)])
+def test_weights_of_units_of_256_rows(d, H, Hkv, new, own, edges, prefix, causal):
+    """bf16 rows in units of 256: weights are off by fp16's rounding, an eighth of bf16's."""
+    s = Setting4(new, own, H, Hkv, d, BF, page=32, seed=d + H, edges=edges, prefix=prefix)
+    assert not s.few()
+    got = s.cache().attend(s.batch(), s.q, scale=d ** -0.5, causal=causal)
+    want, bound = s.want(d ** -0.5, causal, few=True)        # the bound of fp16 weights
+    assert_within(got, want, bound)
+
+
+@pytest.mark.parametrize("n", [1, 8, 100])
+def test_weights_that_nearly_cancel(n):
+    """Two tokens whose values cancel in some coordinate of some rows: there the weights' rounding shows, and bf16's would not do."""
+    d, H = 64, 4
+    s = Setting4([n], [2], H, 1, d, BF, seed=n)
+    tok = torch.arange(2, device="cuda")
+    steps = torch.zeros(2, 1, d, dtype=torch.int64, device="cuda")           # codes; scale 1: (code - 7.5) / 8
+    steps[0] = 15
+    steps[1, 0] = torch.arange(d, device="cuda") % 8                         # -0.9375 to -0.0625
+    one = torch.full((2, 1, d // 16), 15 << 3, dtype=torch.uint8, device="cuda")
+    p4.put(s.pool, 16, d, 1, s.table[0, tok // 16].long(), tok % 16, one, steps)
+    steps[1] = 0
+    one[1] = 0                                                               # a key of zeros
+    p4.put(s.pool, 16, d, 0, s.table[0, tok // 16].long(), tok % 16, one, steps)
+    score = torch.linspace(-2.8, 0.0, n * H, device="cuda").view(n, H, 1)
+    s.q = (score / (0.9375 * d)).expand(n, H, d).to(BF).contiguous()
+    want, bound = s.want(1.0, False, few=True)
+    assert_within(s.cache().attend(s.batch(), s.q, scale=1.0, causal=False), want, bound)
+    if n == 100:                                                             # what bf16 weights would give is beyond it
+        x = s.q[..., :1].double().cpu() * 0.9375 * d
+        V = p4.decoded(s.pool, 16, d)[1][s.table[0, 0].long(), 0, :2].cpu()
+        w = torch.exp(x).to(BF).double()
+        off = ((w * V[0] + V[1]) / (1 + torch.exp(x)) - want).abs() - bound
+        assert float(off.max()) > 0
+
+
 # ---- the tables of a step ----
 
 @pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 4000])
