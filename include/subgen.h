@@ -463,8 +463,9 @@ int subgen_paged_attend(const subgen_pages* cache, const subgen_batch* batch, co
 /* Pages as above, at 4.5 bits a value. 16 consecutive coordinates of a head are a group with a scale S: the group's largest
  * magnitude, rounded up to 4 significant bits (below 2^-14: to a multiple of 2^-17). A coordinate x has the code
  * n = min(15, floor(8 x / S) + 8), which stands for (n - 7.5) S / 8: |x| is off by S / 16 at most, and every value is exact in
- * fp32, bf16 and fp16. A group whose largest magnitude is above 61440 or that holds anything that is not finite reads as NaN (in
- * any row that attends to tokens of its page tile) and sets SUBGEN_ST_RANGE. A group of zeros reads as zeros.
+ * fp32, bf16 and fp16. A group whose largest magnitude is above 61440 or that holds anything that is not finite reads as NaN and sets
+ * SUBGEN_ST_RANGE: a row that attends to it becomes NaN, all of it for a key's group, the group's coordinates for a value's; the latter also
+ * in rows of the same unit (see subgen_paged4_attend) that do not see the token themselves. A group of zeros reads as zeros.
  * 16 tokens of a page (rows 16 i .. 16 i + 15) have a cell in each head: their keys' codes [16][d / 2], their keys' scales
  * [16][d / 16], their values' codes and scales: 2304 bytes at d = 128, 1152 at d = 64. A page has page / 16 of them on end in
  * each head. Eight codes are a 32-bit word, least byte first: codes 0, 2, 4, 6 (least first) in the low half, 1, 3, 5, 7 in the high

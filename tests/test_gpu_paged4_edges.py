@@ -166,6 +166,33 @@ def test_weights_that_nearly_cancel(n):
         assert float(off.max()) > 0
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new, own, edges, prefix", [([1, 2], [200, 90], [], []), ([6, 1], [140, 30], [], []), ([300, 5], [300, 70], [], []), ([1, 3, 1], [5, 20, 9], [0, 2, 3], [50, 60])])
+def test_groups_that_read_as_nan(dtype, new, own, edges, prefix):
+    """A key's group makes the rows that see it NaN and no other; a value's group its 16 coordinates, in no row of another unit."""
+    s = Setting4(new, own, 4, 1, 64, dtype, seed=17, edges=edges, prefix=prefix)
+    clean = s.cache().attend(s.batch(), s.q, scale=0.125)
+    assert not clean.isnan().any()
+    for at in (own[0] - 1, max(0, own[0] - 3), 0):                           # own token `at` of sequence 0
+        first = max(0, at - (own[0] - new[0]))                               # the first of its rows that sees it
+        sees = torch.zeros(s.n, dtype=torch.bool, device="cuda")
+        sees[first:new[0]] = True
+        x = s.pool.unflatten(-1, (1, 2, 16 * (32 + 4)))
+        page, row = int(s.table[0, at // 16]), at % 16
+        for kv in range(2):
+            was = x[page, 0, 0, kv, 16 * 32 + row * 4 + 2].clone()
+            x[page, 0, 0, kv, 16 * 32 + row * 4 + 2] = 255                   # coordinates 32 to 47
+            got = s.cache().attend(s.batch(), s.q, scale=0.125)
+            x[page, 0, 0, kv, 16 * 32 + row * 4 + 2] = was
+            if kv == 0:
+                assert got[sees].isnan().all() and torch.equal(got[~sees], clean[~sees])
+            else:
+                assert got[sees][:, :, 32:48].isnan().all()
+                rest = torch.cat((got[:, :, :32], got[:, :, 48:]), -1)
+                assert torch.equal(rest, torch.cat((clean[:, :, :32], clean[:, :, 48:]), -1))
+                assert torch.equal(got[new[0]:], clean[new[0]:])             # other sequences
+
+
 # ---- the tables of a step ----
 
 @pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 4000])
