@@ -545,7 +545,7 @@ struct Plan {
             long long w = 0;
             int sl = 0;
             if (bad) *flag = 1;
-            else if (kSum && e.rows > kWalk * RU) {
+            else if (kSum && __builtin_expect(e.rows > kWalk * RU, 0)) {
                 w = units_before(e, (e.rows + RU - 1) / RU);
                 sl = e.rows;
             } else {
@@ -622,7 +622,7 @@ struct Plan {
         g.e = entry(lo);
         g.kp = prefix_tiles(g.e);
         int ru = 0, w;
-        if (kSum && g.e.rows > kWalk * RU) {                         // the last unit that starts at r or before
+        if (kSum && __builtin_expect(g.e.rows > kWalk * RU, 0)) {                         // the last unit that starts at r or before
             int last = (g.e.rows - 1) / RU;
 #pragma unroll 1
             while (ru < last) {
@@ -718,7 +718,7 @@ __global__ void __launch_bounds__(kMergeThreads, kMergeBlocks) paged_merge_kerne
     // first position of the line that belongs to row unit ru of a sequence's entry
     auto unit_start = [&](const Entry& e, int ei, int h, int ru) {
         int u0 = h * plan.head_w + plan.tscan[ei];
-        if (PlanT::kSum && ru > PlanT::kWalk) return u0 + (int)plan.units_before(e, ru);
+        if (PlanT::kSum && __builtin_expect(ru > PlanT::kWalk, 0)) return u0 + (int)plan.units_before(e, ru);
 #pragma unroll 1
         for (int k = 0; k < ru; ++k) u0 += plan.unit_weight(plan.unit_tiles(e, k), RU);
         return u0;
