@@ -134,9 +134,11 @@ __device__ __forceinline__ void sincos_turns(unsigned long long turns, float* si
 // PAGED: 0 keys to an output, 1 keys and values into exact pages, 2 into 4-bit cells (P.K: the pool, strides in bytes). There a
 // lane rounds the two pieces that follow each other (16 coordinates in bf16; 8 in fp32, whose scale two lanes share); keys that
 // were rotated in halves lie apart and change lanes through shared memory first. What is rounded to 4 bits falls on either side of a
-// border by its last fp32 bits, so there every step is one plain fp32 operation on correctly rounded sines and cosines, and the
-// squares are added pair by pair (a value then differs from the same formula in plain fp32 operations by rare last bits alone,
-// and a code hardly ever). 19.7 K tokens x (32 + 8 + 8) heads x 128: 94 us, floor 65.
+// border by its last fp32 bits, so there every step is one plain fp32 operation, on sines and cosines rounded once from 2^-40. The
+// squares' sum has to have some order as well. It is the one in which a sum over a row of elementary torch operations was found, by its
+// results on this GPU, to come out, so that a cache filled by those holds the same codes: another one for each d, 8 additions deep at
+// d = 128 and 6 at d = 64, where pair by pair would be 7 and 6. 19.7 K tokens x (32 + 8 + 8) heads x 128: 103 us, with norms 119, floor 65
+// (fp32 140 and 146, floor 126).
 template <typename T, int D, int PAGED, int U>
 __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(NormRope a, PagedView P) {
     constexpr int VE = 16 / sizeof(T), LPR = D / VE / 2, RPW = 32 / LPR;
@@ -287,7 +289,7 @@ __global__ void __launch_bounds__(kNrThreads, U > 1 ? 5 : 1) norm_rope_kernel(No
                                 p = __fsub_rn(__fmul_rn(p0, c), __fmul_rn(q0, s));
                                 q = __fadd_rn(__fmul_rn(q0, c), __fmul_rn(p0, s));
                             };
-                            // two loops: a choice of pairs inside one would put x2 into local memory (prompt chunks 159 us instead of 94)
+                            // two loops: a choice of pairs inside one would put x2 into local memory (prompt chunks 169 us instead of 103)
                             if (a.interleaved) {
 #pragma unroll
                                 for (int e = 0; e < VE; ++e) pair(x2[2 * e], x2[2 * e + 1], co[e], si[e]);

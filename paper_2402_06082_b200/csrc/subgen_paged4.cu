@@ -99,6 +99,9 @@ int attend_few(const PagedView& P, const Attend& a, cudaStream_t st) {
     return launch_merge<T, D, 8 * NT, kP4KT, 0, kP4Lead>(P, a, blocks, st);
 }
 
+// fp32 queries: units of 8 rows whatever the call. With more rows a sequence every unit reads and expands the cache for itself: 32 heads of
+// 128 on 8 KV heads, 2047 prompt tokens 999 us (bytes and products 62), 4 x 512 behind 4096 shared ones 1350 (88); one token behind
+// 131072 54 (bf16 45).
 template <int D>
 int attend4_fp32(const PagedView& P, const Attend& a, cudaStream_t st) {
     static bool done[kMaxDevices];
@@ -127,6 +130,8 @@ int attend4_bf16(const PagedView& P, const Attend& a, cudaStream_t st) {
     // units of 8 rows / units of 16 / units of 256 on the other tensor cores: 4 rows 46 / 56 / 101 us, 8 rows 45 / 56 / 102, 12 rows
     // 73 / 58 / 105, 24 rows 101 / 97 / 113, 32 rows 131 / 99 / 121. A prefix of 32768 tokens before single tokens (4 rows each): 2
     // sequences 31 / 27 / 43, 4 45 / 29 / 48, 8 75 / 41 / 58.
+    // The mean is all that the host knows, so a prompt among many single tokens takes the units of the others: 255 tokens behind 1000 each
+    // with a prompt of 1500 319 us (in units of 16), with one of 2000 320 (in units of 256); the tokens alone 88, the prompt of 1500 alone 84.
     const long long rows = (long long)a.n << a.g_shift;
     const bool shared = P.groups && P.groups < P.B;
     if (!shared && rows <= 8LL * P.B) return attend_few<T, D, 1>(P, a, st);
@@ -239,6 +244,8 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     a.free_count_out = x->free_count_out; a.lengths_out = x->lengths_out; a.cu_q = x->cu_q; a.positions = x->positions; a.sources = x->sources;
     a.slots = (long long*)x->slots;
     a.status = x->status;
+    // Slots and positions: in the one kernel / by the second (us a call, in a graph): 64 rows with 64 tokens 5.2 / 6.4, 4096 6.3 / 6.9; 128 rows with
+    // 8192 6.5 / 7.0; 1024 rows with 8192 7.2 / 8.4, 16384 8.3 / 8.4, 112640 19.1 / 8.1.
     a.split = x->n > 4 * kStepThreads;
     static bool done[kMaxDevices];
     int dev;
@@ -252,7 +259,9 @@ int subgen_page_step(const subgen_page_step_args* x, void* stream) {
     }
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
-    const int blocks = x->n > kStepThreads || x->B > 128 ? kStepCluster : 1;     // something to share out
+    // Something to share out. One block / the cluster: 64 rows with a token each 5.2 / 5.7, 256 5.5 / 6.0; 64 rows with 2048 tokens 6.7 / 6.3,
+    // 4096 7.9 / 6.3. Pages that rows give back are not known here: 4 x 512 of them 6.5 / 6.7, 8 x 1024 8.5 / 6.9, 65536 25.8 / 7.9.
+    const int blocks = x->n > kStepThreads || x->B > 128 ? kStepCluster : 1;
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kStepThreads);
     cfg.stream = (cudaStream_t)stream;
